@@ -51,6 +51,25 @@ class LAWeights(ctypes.Structure):
                 ("dt_bias", ctypes.c_void_p), ("norm_w", ctypes.c_void_p), ("w_out", ctypes.c_void_p)]
 
 
+class ConvShape(ctypes.Structure):
+    _fields_ = [("num_seqs", ctypes.c_int32), ("channels", ctypes.c_int32), ("taps", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("activation", ctypes.c_int32), ("ld_x", ctypes.c_int64),
+                ("ld_y", ctypes.c_int64)]
+
+
+class SSMShape(ctypes.Structure):
+    _fields_ = [("num_seqs", ctypes.c_int32), ("num_heads", ctypes.c_int32), ("num_groups", ctypes.c_int32),
+                ("d_state", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("dt_dtype", ctypes.c_int32), ("ld_x", ctypes.c_int64), ("ld_dt", ctypes.c_int64),
+                ("ld_b", ctypes.c_int64), ("ld_c", ctypes.c_int64), ("ld_y", ctypes.c_int64)]
+
+
+class LoraShape(ctypes.Structure):
+    _fields_ = [("num_seqs", ctypes.c_int32), ("num_adapters", ctypes.c_int32), ("hidden", ctypes.c_int32),
+                ("width", ctypes.c_int32), ("rank", ctypes.c_int32), ("out_dtype", ctypes.c_int32),
+                ("ld_x", ctypes.c_int64), ("ld_base", ctypes.c_int64), ("ld_out", ctypes.c_int64)]
+
+
 _lib = None
 
 
@@ -108,6 +127,22 @@ def load_library():
     lib.gdn_la_block_num_stages.restype = ctypes.c_int32
     lib.gdn_la_block_stage_name.argtypes = [ctypes.c_int32, ctypes.c_int32]
     lib.gdn_la_block_stage_name.restype = ctypes.c_char_p
+    ZP = ctypes.POINTER(ctypes.c_size_t)
+    CP, MP, AP = ctypes.POINTER(ConvShape), ctypes.POINTER(SSMShape), ctypes.POINTER(LoraShape)
+    lib.gdn_causal_conv.argtypes = [CP, P, P, P, P, P, P, P, P, P]
+    lib.gdn_causal_conv.restype = ctypes.c_int
+    lib.gdn_causal_conv_step.argtypes = [CP, P, P, P, P, P, P, P]
+    lib.gdn_causal_conv_step.restype = ctypes.c_int
+    lib.gdn_ssm_workspace_size.argtypes = [MP, P, ZP]
+    lib.gdn_ssm_workspace_size.restype = ctypes.c_int
+    lib.gdn_ssm_scan.argtypes = [MP, P, P, P, P, P, P, P, P, P, P, P, P, P, ctypes.c_size_t, P]
+    lib.gdn_ssm_scan.restype = ctypes.c_int
+    lib.gdn_ssm_step.argtypes = [MP, P, P, P, P, P, P, P, P, P, P, P]
+    lib.gdn_ssm_step.restype = ctypes.c_int
+    lib.gdn_lora_workspace_size.argtypes = [AP, P, ZP]
+    lib.gdn_lora_workspace_size.restype = ctypes.c_int
+    lib.gdn_lora_add.argtypes = [AP, P, P, P, P, P, P, P, P, P, P, P, ctypes.c_size_t, P]
+    lib.gdn_lora_add.restype = ctypes.c_int
     lib.gdn_replay_len.argtypes = [ctypes.c_int64, ctypes.c_int64, ctypes.c_int64]
     lib.gdn_replay_len.restype = ctypes.c_int64
     lib.gdn_status_string.argtypes = [ctypes.c_int]

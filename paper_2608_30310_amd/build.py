@@ -15,7 +15,8 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB_NAME = "libgdn_tailreplay.so"
 LIB_PATH = os.path.join(HERE, LIB_NAME)
-SOURCES = ["gdn_plan.cpp", "gdn_gemm.cpp", "gdn_api.hip", "gdn_block.hip"]
+SOURCES = ["gdn_plan.cpp", "gdn_layer_plan.cpp", "gdn_gemm.cpp", "gdn_api.hip", "gdn_block.hip", "gdn_conv.hip",
+           "gdn_ssm.hip", "gdn_lora.hip"]
 ROCM_LIB = "/opt/rocm/lib"
 ARCH = "gfx950"
 

@@ -1,0 +1,160 @@
+// The short causal convolution (gdn_ssm.h), for packed sequences and for one
+// token per sequence.  W multiply-adds per element read and written: HBM bound.
+// fp32 arithmetic whatever the element type, one rounding at the store.
+#pragma once
+
+#include "gdn_varlen.h"
+
+namespace gdn {
+
+constexpr int kConvThreads = 256;
+constexpr int kConvLanes = 32;                          // channel groups of a workgroup
+constexpr int kConvRows = kConvThreads / kConvLanes;    // token rows of a workgroup
+// channels of a thread: 16 bytes of them, or one where rows are not aligned
+template <typename T, bool ALIGNED>
+constexpr int conv_vec() { return ALIGNED ? 16 / static_cast<int>(sizeof(T)) : 1; }
+// tokens of a workgroup's tile when each thread takes tpt of them
+constexpr int conv_tile(int tpt) { return kConvRows * tpt; }
+
+template <int VEC, int W>
+__device__ __forceinline__ void load_taps(const float* __restrict__ w, const float* __restrict__ bias, int c0, bool any,
+                                          float (&tap)[W][VEC], float (&b)[VEC]) {
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) {
+#pragma unroll
+    for (int j = 0; j < W; ++j) tap[j][e] = any ? w[static_cast<int64_t>(c0 + e) * W + j] : 0.0f;
+    b[e] = any && bias ? bias[c0 + e] : 0.0f;
+  }
+}
+
+template <int VEC, bool SILU>
+__device__ __forceinline__ void activate(float (&acc)[VEC]) {
+  if constexpr (SILU) {
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) acc[e] = silu_f(acc[e]);
+  }
+}
+
+// Workgroup: 32 channel groups x 8 rows of TPT consecutive tokens; a thread
+// loads the TPT + W - 1 rows that its tokens need once.  blockIdx.x %
+// slabs is its channel slab for good (the taps stay in registers), its tiles
+// are the slots from blockIdx.x / slabs in steps of gridDim.x / slabs.
+// The rows before a sequence and the history after it belong to the sequence's
+// first tile, so history_out may be history_in: that workgroup alone touches
+// them, and it reads before it writes.
+template <typename T, int VEC, int W, int TPT, bool SILU>
+__global__ __launch_bounds__(kConvThreads)
+void k_causal_conv(int32_t slots, int32_t slabs, int32_t n_seqs, const int32_t* __restrict__ cu, int32_t C,
+                   const T* __restrict__ x, int64_t ldx, const float* __restrict__ w, const float* __restrict__ bias,
+                   const T* hist_in, T* __restrict__ y, int64_t ldy, T* hist_out) {
+  constexpr int H = W - 1;
+  constexpr int TILE = conv_tile(TPT);
+  const int tid = threadIdx.x;
+  const int row = tid / kConvLanes;
+  const int slab = blockIdx.x % slabs;
+  const int c0 = (slab * kConvLanes + tid % kConvLanes) * VEC;
+  const bool any = c0 < C;
+  float tap[W][VEC], b[VEC];
+  load_taps<VEC, W>(w, bias, c0, any, tap, b);
+  const int step = gridDim.x / slabs;
+  for (int slot = blockIdx.x / slabs; slot < slots; slot += step) {   // uniform per workgroup
+    const int n = slot_seq(cu, n_seqs, slot, TILE);
+    const int start = cu[n], len = cu[n + 1] - start;
+    const int j = slot - (start / TILE + n);
+    if (j > 0 && j * TILE >= len) continue;   // an unused slot
+    const int t0 = j * TILE + row * TPT;
+    const T* xs = x + static_cast<int64_t>(start) * ldx + c0;
+    const int64_t hbase = static_cast<int64_t>(n) * H * C + c0;
+    float u[TPT + H][VEC];
+#pragma unroll
+    for (int r = 0; r < TPT + H; ++r) {
+      const int t = t0 - H + r;
+      if (any && t >= 0 && t < len) {
+        load_run<T, VEC>(xs + static_cast<int64_t>(t) * ldx, u[r]);
+      } else if (any && t < 0 && hist_in) {
+        load_run<T, VEC>(hist_in + hbase + static_cast<int64_t>(H + t) * C, u[r]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) u[r][e] = 0.0f;
+      }
+    }
+    if (j == 0 && hist_out) {
+      // rows len .. len + H - 1 of (history | sequence); bf16 -> fp32 -> bf16 is exact
+      float h[H][VEC];
+      if (any && row == 0) {
+#pragma unroll
+        for (int r = 0; r < H; ++r) {
+          const int t = len - H + r;
+          if (t >= 0) {
+            load_run<T, VEC>(xs + static_cast<int64_t>(t) * ldx, h[r]);
+          } else if (hist_in) {
+            load_run<T, VEC>(hist_in + hbase + static_cast<int64_t>(H + t) * C, h[r]);
+          } else {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) h[r][e] = 0.0f;
+          }
+        }
+      }
+      __syncthreads();   // every row's history_in is in registers
+      if (any && row == 0) {
+#pragma unroll
+        for (int r = 0; r < H; ++r) store_run<T, VEC>(hist_out + hbase + static_cast<int64_t>(r) * C, h[r]);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < TPT; ++i) {
+      if (!any || t0 + i >= len) continue;
+      float acc[VEC];
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        acc[e] = b[e];
+#pragma unroll
+        for (int k = 0; k < W; ++k) acc[e] = fmaf(tap[k][e], u[i + k][e], acc[e]);
+      }
+      activate<VEC, SILU>(acc);
+      store_run<T, VEC>(y + static_cast<int64_t>(start + t0 + i) * ldy + c0, acc);
+    }
+  }
+}
+
+// One token per sequence: a thread takes VEC channels of the sequences from
+// blockIdx.y in steps of gridDim.y, its taps in registers.  It reads its
+// history before it writes it, so the two may be one.
+template <typename T, int VEC, int W, bool SILU>
+__global__ __launch_bounds__(kConvThreads)
+void k_causal_conv_step(int32_t n_seqs, int32_t C, const T* __restrict__ x, int64_t ldx, const float* __restrict__ w,
+                        const float* __restrict__ bias, const T* hist_in, T* __restrict__ y, int64_t ldy,
+                        T* hist_out) {
+  constexpr int H = W - 1;
+  const int c0 = (blockIdx.x * blockDim.x + threadIdx.x) * VEC;
+  if (c0 >= C) return;
+  float tap[W][VEC], b[VEC];
+  load_taps<VEC, W>(w, bias, c0, true, tap, b);
+  for (int n = blockIdx.y; n < n_seqs; n += gridDim.y) {
+    const int64_t hbase = static_cast<int64_t>(n) * H * C + c0;
+    float u[W][VEC];
+#pragma unroll
+    for (int r = 0; r < H; ++r) {
+      if (hist_in) {
+        load_run<T, VEC>(hist_in + hbase + static_cast<int64_t>(r) * C, u[r]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) u[r][e] = 0.0f;
+      }
+    }
+    load_run<T, VEC>(x + static_cast<int64_t>(n) * ldx + c0, u[H]);
+    float acc[VEC];
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+      acc[e] = b[e];
+#pragma unroll
+      for (int k = 0; k < W; ++k) acc[e] = fmaf(tap[k][e], u[k][e], acc[e]);
+    }
+    activate<VEC, SILU>(acc);
+#pragma unroll
+    for (int r = 0; r < H; ++r) store_run<T, VEC>(hist_out + hbase + static_cast<int64_t>(r) * C, u[r + 1]);
+    store_run<T, VEC>(y + static_cast<int64_t>(n) * ldy + c0, acc);
+  }
+}
+
+}  // namespace gdn

@@ -1,0 +1,128 @@
+// Host-side validation and planning (see gdn_layer_plan.h).
+#include "gdn_layer_plan.h"
+
+#include <algorithm>
+#include <limits>
+
+namespace gdn {
+namespace {
+
+constexpr int64_t kMaxGrid = std::numeric_limits<int32_t>::max();
+// strides and row counts stay far inside 64-bit element offsets
+constexpr int64_t kMaxStride = int64_t{1} << 40;
+
+bool known_dtype(int32_t d) { return d == GDN_F32 || d == GDN_BF16; }
+
+gdn_status bad_stride(const char* name, int64_t least, std::string* err) {
+  *err = std::string(name) + " must be between " + std::to_string(least) + " and 2^40";
+  return GDN_ERR_BAD_SHAPE;
+}
+
+}  // namespace
+
+gdn_status check_seqlens(int32_t n, const int32_t* cu, int64_t* tokens, int64_t* longest, std::string* err) {
+  if (!cu) { *err = "cu_seqlens_host is NULL"; return GDN_ERR_NULL_ARG; }
+  if (cu[0] != 0) { *err = "cu_seqlens_host[0] must be 0"; return GDN_ERR_BAD_SEQLENS; }
+  int64_t top = 0;
+  for (int32_t i = 0; i < n; ++i) {
+    const int64_t len = static_cast<int64_t>(cu[i + 1]) - cu[i];
+    if (len < 0) { *err = "cu_seqlens_host must be non-decreasing"; return GDN_ERR_BAD_SEQLENS; }
+    top = std::max(top, len);
+  }
+  *tokens = cu[n];
+  *longest = top;
+  return GDN_OK;
+}
+
+gdn_status check_conv(const gdn_conv_shape* s, std::string* err) {
+  if (!s) { *err = "shape is NULL"; return GDN_ERR_NULL_ARG; }
+  if (s->num_seqs < 0) { *err = "num_seqs must be >= 0"; return GDN_ERR_BAD_SHAPE; }
+  if (s->channels < 1) { *err = "channels must be >= 1"; return GDN_ERR_BAD_SHAPE; }
+  if (s->taps < 2 || s->taps > 4) { *err = "taps must be 2, 3 or 4"; return GDN_ERR_UNSUPPORTED; }
+  if (!known_dtype(s->dtype)) { *err = "dtype must be GDN_F32 or GDN_BF16"; return GDN_ERR_UNSUPPORTED; }
+  if (s->activation != GDN_ACT_NONE && s->activation != GDN_ACT_SILU) {
+    *err = "activation must be GDN_ACT_NONE or GDN_ACT_SILU";
+    return GDN_ERR_UNSUPPORTED;
+  }
+  if (s->ld_x < s->channels || s->ld_x > kMaxStride) return bad_stride("ld_x", s->channels, err);
+  if (s->ld_y < s->channels || s->ld_y > kMaxStride) return bad_stride("ld_y", s->channels, err);
+  return GDN_OK;
+}
+
+gdn_status check_ssm(const gdn_ssm_shape* s, std::string* err) {
+  if (!s) { *err = "shape is NULL"; return GDN_ERR_NULL_ARG; }
+  if (s->num_seqs < 0) { *err = "num_seqs must be >= 0"; return GDN_ERR_BAD_SHAPE; }
+  if (s->num_heads < 1 || s->num_groups < 1) { *err = "head counts must be >= 1"; return GDN_ERR_BAD_SHAPE; }
+  if (s->num_heads % s->num_groups != 0) {
+    *err = "num_heads must be a multiple of num_groups";
+    return GDN_ERR_BAD_SHAPE;
+  }
+  if (s->num_heads > 65535) { *err = "num_heads must be <= 65535"; return GDN_ERR_UNSUPPORTED; }
+  const auto dim = [](int32_t d) { return d == 64 || d == 128; };
+  if (!dim(s->d_state) || !dim(s->head_dim)) {
+    *err = "d_state and head_dim must each be 64 or 128";
+    return GDN_ERR_UNSUPPORTED;
+  }
+  if (!known_dtype(s->dtype)) { *err = "dtype must be GDN_F32 or GDN_BF16"; return GDN_ERR_UNSUPPORTED; }
+  if (s->dt_dtype != GDN_F32 && s->dt_dtype != s->dtype) {
+    *err = "dt_dtype must be GDN_F32 or the same as dtype";
+    return GDN_ERR_UNSUPPORTED;
+  }
+  const int64_t H = s->num_heads, G = s->num_groups, vec = s->dtype == GDN_BF16 ? 8 : 4;
+  struct { const char* name; int64_t ld, least; bool aligned; } rows[] = {
+      {"ld_x", s->ld_x, H * s->head_dim, true}, {"ld_dt", s->ld_dt, H, false}, {"ld_b", s->ld_b, G * s->d_state, true},
+      {"ld_c", s->ld_c, G * s->d_state, true},  {"ld_y", s->ld_y, H * s->head_dim, true}};
+  for (const auto& r : rows)
+    if (r.ld < r.least || r.ld > kMaxStride) return bad_stride(r.name, r.least, err);
+  for (const auto& r : rows)
+    if (r.aligned && r.ld % vec != 0) {
+      *err = std::string(r.name) + " must be a multiple of 16 bytes";
+      return GDN_ERR_UNSUPPORTED;
+    }
+  if (static_cast<int64_t>(s->num_seqs) * H > kMaxGrid / 256) {
+    *err = "num_seqs * num_heads too large";
+    return GDN_ERR_UNSUPPORTED;
+  }
+  return GDN_OK;
+}
+
+gdn_status check_lora(const gdn_lora_shape* s, std::string* err) {
+  if (!s) { *err = "shape is NULL"; return GDN_ERR_NULL_ARG; }
+  if (s->num_seqs < 0 || s->num_adapters < 0) {
+    *err = "num_seqs and num_adapters must be >= 0";
+    return GDN_ERR_BAD_SHAPE;
+  }
+  if (s->hidden < 1 || s->width < 1 || s->rank < 1) {
+    *err = "hidden, width and rank must be >= 1";
+    return GDN_ERR_BAD_SHAPE;
+  }
+  if (s->hidden % 8 != 0) { *err = "hidden must be a multiple of 8"; return GDN_ERR_UNSUPPORTED; }
+  if (s->rank % 8 != 0 || s->rank > 128) {
+    *err = "rank must be a multiple of 8, at most 128";
+    return GDN_ERR_UNSUPPORTED;
+  }
+  if (!known_dtype(s->out_dtype)) { *err = "out_dtype must be GDN_F32 or GDN_BF16"; return GDN_ERR_UNSUPPORTED; }
+  if (s->ld_x < s->hidden || s->ld_x > kMaxStride) return bad_stride("ld_x", s->hidden, err);
+  if (s->ld_base < s->width || s->ld_base > kMaxStride) return bad_stride("ld_base", s->width, err);
+  if (s->ld_out < s->width || s->ld_out > kMaxStride) return bad_stride("ld_out", s->width, err);
+  if (s->ld_x % 8 != 0) { *err = "ld_x must be a multiple of 8"; return GDN_ERR_UNSUPPORTED; }
+  return GDN_OK;
+}
+
+bool overlap(const void* pa, size_t na, const void* pb, size_t nb) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(pa), b = reinterpret_cast<uintptr_t>(pb);
+  return na > 0 && nb > 0 && a < b + nb && b < a + na;
+}
+
+bool rows_overlap(const void* pa, int64_t wa, int64_t lda, const void* pb, int64_t wb, int64_t ldb, int64_t rows) {
+  if (rows < 1) return false;
+  const size_t na = static_cast<size_t>((rows - 1) * lda + wa), nb = static_cast<size_t>((rows - 1) * ldb + wb);
+  if (!overlap(pa, na, pb, nb)) return false;
+  if (lda != ldb) return true;
+  // windows [0, wa) and [d, d + wb) of a circle of lda bytes
+  const int64_t gap = static_cast<int64_t>(reinterpret_cast<uintptr_t>(pb) - reinterpret_cast<uintptr_t>(pa));
+  const int64_t d = ((gap % lda) + lda) % lda;
+  return d < wa || d + wb > lda;
+}
+
+}  // namespace gdn

@@ -1,0 +1,35 @@
+// Host-side validation and planning of the recurrent layer's other operators
+// (gdn_ssm.h, gdn_lora.h).  Pure C++ (no HIP), like gdn_plan.h.
+#pragma once
+
+#include <cstddef>
+#include <cstdint>
+#include <string>
+
+#include "gdn_lora.h"
+#include "gdn_ssm.h"
+
+namespace gdn {
+
+// Packed sequences cut into tiles of `tile` tokens, each sequence from its own
+// start: tile j of sequence n is slot cu[n] / tile + n + j.  The map is
+// injective and every sequence has a slot of its own, the empty ones too; at
+// most N slots stay unused.  The kernels find a slot's sequence from cu alone.
+inline int64_t tile_slots(int64_t tokens, int64_t seqs, int64_t tile) { return seqs > 0 ? tokens / tile + seqs : 0; }
+
+// Validates the host copy of the offsets; *tokens = cu[N], *longest = the
+// longest sequence.
+gdn_status check_seqlens(int32_t n, const int32_t* cu, int64_t* tokens, int64_t* longest, std::string* err);
+
+gdn_status check_conv(const gdn_conv_shape* s, std::string* err);
+gdn_status check_ssm(const gdn_ssm_shape* s, std::string* err);
+gdn_status check_lora(const gdn_lora_shape* s, std::string* err);
+
+// Two row-strided regions of `rows` rows: a starts at pa, has wa bytes in each
+// row and lda bytes between rows.  False only where no byte is in both: their
+// extents do not meet, or the strides are equal and the rows' windows never meet.
+bool rows_overlap(const void* pa, int64_t wa, int64_t lda, const void* pb, int64_t wb, int64_t ldb, int64_t rows);
+// Two flat regions.
+bool overlap(const void* pa, size_t na, const void* pb, size_t nb);
+
+}  // namespace gdn

@@ -1,0 +1,109 @@
+// Low-rank adapters beside a shared projection: validation and launches (C ABI
+// in gdn_lora.h).
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <string>
+
+#include "gdn_layer_plan.h"
+#include "gdn_lora_kernels.h"
+#include "gdn_plan.h"
+
+namespace gdn {
+namespace {
+
+gdn_status lfail(gdn_status st, const std::string& msg) {
+  set_last_error(msg);
+  return st;
+}
+
+gdn_status llaunched(const char* what) {
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return lfail(GDN_ERR_HIP, std::string(what) + ": " + hipGetErrorString(e));
+  return GDN_OK;
+}
+
+template <typename T>
+gdn_status launch_lora(const gdn_lora_shape& s, int64_t tokens, const int32_t* cu, const int32_t* adapters,
+                       const void* base, const void* x, const void* A, const void* B, const float* scales, void* out,
+                       float* u, hipStream_t stream) {
+  hipLaunchKernelGGL(k_lora_down, dim3(2048), dim3(kLoraThreads), 0, stream, static_cast<int32_t>(tokens), s.num_seqs,
+                     cu, adapters, s.num_adapters, s.hidden, s.rank, static_cast<const uint16_t*>(x), s.ld_x,
+                     static_cast<const uint16_t*>(A), scales, u);
+  hipLaunchKernelGGL((k_lora_up<T>), dim3(2048), dim3(kLoraThreads), 0, stream, static_cast<int32_t>(tokens),
+                     s.num_seqs, cu, adapters, s.num_adapters, s.width, s.rank, u, static_cast<const uint16_t*>(B),
+                     static_cast<const T*>(base), s.ld_base, static_cast<T*>(out), s.ld_out);
+  return llaunched("adapter launch");
+}
+
+gdn_status lora_plan(const gdn_lora_shape* s, const int32_t* cu_host, int64_t* tokens, size_t* bytes, std::string* err) {
+  gdn_status st = check_lora(s, err);
+  int64_t longest = 0;
+  if (st == GDN_OK) st = check_seqlens(s->num_seqs, cu_host, tokens, &longest, err);
+  if (st != GDN_OK) return st;
+  *bytes = (static_cast<size_t>(*tokens) * s->rank * sizeof(float) + kAlign - 1) / kAlign * kAlign;
+  return GDN_OK;
+}
+
+gdn_status lora_impl(const gdn_lora_shape* s, const int32_t* cu_host, const int32_t* cu, const int32_t* adapters_host,
+                     const int32_t* adapters, const void* base, const void* x, const void* A, const void* B,
+                     const float* scales, void* out, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  std::string err;
+  int64_t tokens = 0;
+  size_t bytes = 0;
+  const gdn_status st = lora_plan(s, cu_host, &tokens, &bytes, &err);
+  if (st != GDN_OK) return lfail(st, err);
+  if (s->num_seqs == 0) return GDN_OK;
+  if (!adapters_host) return lfail(GDN_ERR_NULL_ARG, "adapters_host is NULL");
+  bool any = false;
+  for (int32_t n = 0; n < s->num_seqs; ++n) {
+    if (adapters_host[n] < -1 || adapters_host[n] >= s->num_adapters)
+      return lfail(GDN_ERR_BAD_SHAPE, "adapters_host must hold -1 or an adapter's index");
+    any = any || (adapters_host[n] >= 0 && cu_host[n + 1] > cu_host[n]);
+  }
+  if (tokens == 0) return GDN_OK;
+  if (!cu || !adapters) return lfail(GDN_ERR_NULL_ARG, "cu_seqlens and adapters (device) must be non-NULL");
+  if (!base || !out) return lfail(GDN_ERR_NULL_ARG, "base and out must be non-NULL");
+  if (any && (!x || !A || !B)) return lfail(GDN_ERR_NULL_ARG, "x, lora_a and lora_b must be non-NULL");
+  const auto off = [](const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a != 0; };
+  if (off(x, 16) || off(A, 16) || off(B, 16)) return lfail(GDN_ERR_UNSUPPORTED, "x, lora_a and lora_b must be 16-byte aligned");
+  const int64_t e = s->out_dtype == GDN_BF16 ? 2 : 4, row = s->width * e;
+  if (off(base, e) || off(out, e)) return lfail(GDN_ERR_UNSUPPORTED, "base and out must be aligned to their elements");
+  if (base == out ? s->ld_base != s->ld_out : rows_overlap(base, row, s->ld_base * e, out, row, s->ld_out * e, tokens))
+    return lfail(GDN_ERR_BAD_SHAPE, "out overlaps base without being equal");
+  if (x && rows_overlap(x, s->hidden * 2, s->ld_x * 2, out, row, s->ld_out * e, tokens))
+    return lfail(GDN_ERR_BAD_SHAPE, "out overlaps x");
+  if (!workspace) return lfail(GDN_ERR_WORKSPACE, "workspace is NULL");
+  if (workspace_bytes < bytes)
+    return lfail(GDN_ERR_WORKSPACE, "workspace too small: need " + std::to_string(bytes) + " bytes, got " +
+                                        std::to_string(workspace_bytes));
+  if (off(workspace, kAlign)) return lfail(GDN_ERR_WORKSPACE, "workspace must be 256-byte aligned");
+  if (!any && base == out) return GDN_OK;
+  float* u = static_cast<float*>(workspace);
+  return s->out_dtype == GDN_BF16
+             ? launch_lora<uint16_t>(*s, tokens, cu, adapters, base, x, A, B, scales, out, u, stream)
+             : launch_lora<float>(*s, tokens, cu, adapters, base, x, A, B, scales, out, u, stream);
+}
+
+}  // namespace
+}  // namespace gdn
+
+extern "C" {
+
+gdn_status gdn_lora_workspace_size(const gdn_lora_shape* shape, const int32_t* cu_seqlens_host, size_t* bytes) {
+  if (!bytes) return gdn::lfail(GDN_ERR_NULL_ARG, "bytes is NULL");
+  std::string err;
+  int64_t tokens = 0;
+  const gdn_status st = gdn::lora_plan(shape, cu_seqlens_host, &tokens, bytes, &err);
+  return st == GDN_OK ? st : gdn::lfail(st, err);
+}
+
+gdn_status gdn_lora_add(const gdn_lora_shape* shape, const int32_t* cu_seqlens_host, const int32_t* cu_seqlens,
+                        const int32_t* adapters_host, const int32_t* adapters, const void* base, const void* x,
+                        const void* lora_a, const void* lora_b, const float* scales, void* out, void* workspace,
+                        size_t workspace_bytes, void* stream) {
+  return gdn::lora_impl(shape, cu_seqlens_host, cu_seqlens, adapters_host, adapters, base, x, lora_a, lora_b, scales,
+                        out, workspace, workspace_bytes, static_cast<hipStream_t>(stream));
+}
+
+}  // extern "C"

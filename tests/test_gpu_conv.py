@@ -1,0 +1,159 @@
+"""The short causal convolution against its fp64 form.
+
+Bounds.  W products and the bias are summed in fp32: within (W + 1) 2^-24 of
+the sum over magnitudes; SiLU passes an error on by at most 1.1 times and adds
+that of its exponential (its argument's 2^-24 relative, so |x| 2^-23 of the
+value with the scaling by log2 e) and a few roundings.  bf16 outputs are
+rounded by 2^-8 of themselves.  Histories are copies: equal bits.
+"""
+import pytest
+import torch
+
+import paper_2608_30310_amd as gdn
+from oracle import layer_ops as ref
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU visible")
+    gdn.load_library()
+
+
+def inputs(lens, C, W=4, dtype="bf16", ld=None, seed=0, history=True, bias=True, spare=0, shift=0):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    rn = lambda *s: torch.randn(*s, device=DEV, generator=g)
+    T = sum(lens) + spare
+    x = rn(T, shift + (ld or C)).to(DT[dtype])[:, shift:shift + C]
+    cu = torch.tensor([0] + list(torch.tensor(lens).cumsum(0)), dtype=torch.int32)
+    return dict(x=x, w=rn(C, W), bias=rn(C) if bias else None, cu=cu.to(DEV), cu_host=cu,
+                history=rn(len(lens), W - 1, C).to(DT[dtype]) if history else None)
+
+
+def close(got, i, e, mag, silu=True):
+    W = i["w"].shape[1]
+    bound = 1.1 * (W + 2) * 2.0 ** -24 * mag
+    if silu:
+        bound = bound + (mag + 8) * 2.0 ** -23 * e.abs()
+    if got.dtype == torch.bfloat16:
+        bound = bound + 2.0 ** -8 * e.abs() * (1 + 2.0 ** -7)
+    off = (got.double() - e).abs()
+    worst = float((off / (bound + 1e-37)).max()) if off.numel() else 0.0
+    print(f"[conv] worst {worst:.3f} of the bound", flush=True)
+    assert worst <= 1.0
+
+
+def check(i, y, h, silu=True):
+    T = int(i["cu_host"][-1])
+    e, after, mag = ref.causal_conv(i["x"], i["w"], i["cu_host"].tolist(), i["bias"], i["history"], silu)
+    close(y[:T], i, e[:T], mag[:T], silu)
+    if h is not None:
+        assert torch.equal(h.double(), after)
+
+
+def conv(i, **kw):
+    kw = dict(dict(bias=i["bias"], history_in=i["history"]), **kw)
+    return gdn.causal_conv(i["x"], i["w"], i["cu"], i["cu_host"], **kw)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("W", [2, 3, 4])
+@pytest.mark.parametrize("C,ld,shift", [(8, None, 0), (1, None, 0), (255, None, 0), (256, 264, 0), (264, 301, 0),
+                                        (520, 528, 8), (64, 80, 3)])
+def test_channels_and_strides(dtype, W, C, ld, shift):
+    i = inputs([5, 0, 1, 70, 2, 3], C, W, dtype, ld, seed=C + W, shift=shift)
+    check(i, *conv(i))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("history", [False, True])
+@pytest.mark.parametrize("lens", [[1], [2], [3], [4], [7, 8, 9], [64, 63, 65, 0, 1], [0, 0], [2500], [1] * 70])
+def test_lengths(dtype, history, lens):
+    i = inputs(lens, 72, 4, dtype, seed=len(lens), history=history, bias=history)
+    y, h = conv(i)
+    check(i, y, h)
+    y2, none = conv(i, write_history=False)
+    assert none is None and torch.equal(y, y2)
+    check(i, *conv(i, activation="none"), silu=False)
+
+
+def test_many_channels_and_tokens():
+    """Enough work for the form with eight tokens to a thread."""
+    i = inputs([700, 0, 3, 1900, 1], 4096, seed=2, ld=4104)
+    check(i, *conv(i))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lens", [[1, 0, 2, 3, 100], [300, 2, 0]])
+def test_history_in_place(dtype, lens):
+    i = inputs(lens, 136, 4, dtype, seed=3)
+    y, h = conv(i)
+    buf = i["history"].clone()
+    y2, h2 = conv(i, history_in=buf, history_out=buf)
+    assert h2 is buf and torch.equal(y, y2) and torch.equal(h, h2)
+
+
+def test_continues_and_steps():
+    """A prompt cut in two, then tokens one by one, is the whole."""
+    i = inputs([40], 72, seed=4)
+    y, h = gdn.causal_conv(i["x"][:7], i["w"], [0, 7], bias=i["bias"], history_in=i["history"])
+    y2, h = gdn.causal_conv(i["x"][7:30], i["w"], [0, 23], bias=i["bias"], history_in=h, history_out=h)
+    ys = [y, y2]
+    for t in range(30, 40):
+        yt, h = gdn.causal_conv_step(i["x"][t:t + 1], i["w"], h, bias=i["bias"], history_out=h)
+        ys.append(yt)
+    whole, hw = conv(i)
+    assert torch.equal(torch.cat(ys), whole) and torch.equal(h, hw)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("W", [2, 3, 4])
+@pytest.mark.parametrize("n,C,ld", [(1, 8, None), (3, 257, 260), (300, 64, None), (5, 4096, 4104)])
+def test_step(dtype, W, n, C, ld):
+    i = inputs([1] * n, C, W, dtype, ld, seed=n)
+    y, h = gdn.causal_conv_step(i["x"], i["w"], i["history"], bias=i["bias"])
+    check(i, y, h)
+    buf = i["history"].clone()
+    y2, h2 = gdn.causal_conv_step(i["x"], i["w"], buf, bias=i["bias"], history_out=buf)
+    assert h2 is buf and torch.equal(y, y2) and torch.equal(h, h2)
+    i["history"] = None
+    check(i, *gdn.causal_conv_step(i["x"], i["w"], bias=i["bias"], activation="none"), silu=False)
+
+
+def test_rows_behind_and_neighbours():
+    i = inputs([30, 50, 20], 72, seed=5, spare=12, ld=80)
+    i["x"][100:] = float("nan")
+    rows = torch.full((112, 100), 3.0, dtype=torch.bfloat16, device=DEV)
+    y, h = conv(i, out=rows[:, 4:76])
+    check(i, y, h)
+    assert (rows[100:] == 3.0).all() and (rows[:, :4] == 3.0).all() and (rows[:, 76:] == 3.0).all()
+    bad = dict(i, x=i["x"].clone(), history=i["history"].clone())
+    bad["x"][30:80] = float("nan")
+    bad["history"][1] = float("inf")
+    y2, h2 = conv(bad)
+    for k in (slice(0, 30), slice(80, 100)):
+        assert torch.equal(y[k], y2[k])
+    assert torch.equal(h[0], h2[0]) and torch.equal(h[2], h2[2])
+
+
+def test_graph_replays():
+    i = inputs([30, 0, 300], 264, seed=6)
+    one = inputs([1] * 4, 264, seed=7)
+    y0, h0 = conv(i)
+    s0, g0 = gdn.causal_conv_step(one["x"], one["w"], one["history"])
+    y, h, s, g = (torch.empty_like(t) for t in (y0, h0, s0, g0))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        conv(i, out=y, history_out=h)
+        gdn.causal_conv_step(one["x"], one["w"], one["history"], out=s, history_out=g)
+    for _ in range(3):
+        for t in (y, h, s, g):
+            t.zero_()
+        graph.replay()
+        conv(inputs([500], 264, seed=8))
+        torch.cuda.synchronize()
+        assert torch.equal(y, y0) and torch.equal(h, h0) and torch.equal(s, s0) and torch.equal(g, g0)

@@ -1,0 +1,133 @@
+"""Low-rank adapters beside a shared projection against their fp64 form.
+
+Bounds.  x A^T is summed over K and its product with B^T over R products in
+fp32, the first factor through the matrix cores in two bf16 parts (2^-16): the
+result is within (K + R + 8) 2^-24 + 2^-16 of the sum over magnitudes; a bf16
+output is rounded by 2^-8 of itself.
+"""
+import pytest
+import torch
+
+import paper_2608_30310_amd as gdn
+from oracle import layer_ops as ref
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU visible")
+    gdn.load_library()
+
+
+def inputs(lens, ids, K=64, M=96, R=16, n=3, dtype="bf16", seed=0, scales=True, spare=0, pads=(0, 0)):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    rn = lambda *s: torch.randn(*s, device=DEV, generator=g)
+    T = sum(lens) + spare
+    cu = torch.tensor([0] + list(torch.tensor(lens).cumsum(0)), dtype=torch.int32)
+    return dict(x=rn(T, K + pads[0]).bfloat16()[:, :K], base=rn(T, M + pads[1]).to(DT[dtype])[:, :M],
+                a=(rn(n, R, K) / K ** 0.5).bfloat16(), b=(rn(n, M, R) / R ** 0.5).bfloat16(), ids=ids,
+                scales=rn(n) if scales else None, cu=cu.to(DEV), cu_host=cu)
+
+
+def lora(i, **kw):
+    return gdn.lora_add(i["base"], i["x"], i["a"], i["b"], i["ids"], i["cu"], i["cu_host"], scales=i["scales"], **kw)
+
+
+def check(i, out):
+    T = int(i["cu_host"][-1])
+    e, mag = ref.lora(i["base"], i["x"], i["a"], i["b"], i["ids"], i["cu_host"].tolist(), i["scales"])
+    K, R = i["x"].shape[1], i["a"].shape[1]
+    bound = ((K + R + 8) * 2.0 ** -24 + 2.0 ** -16) * mag
+    if out.dtype == torch.bfloat16:
+        bound = bound + 2.0 ** -8 * e.abs() * (1 + 2.0 ** -7)
+    off = (out.double() - e).abs()[:T]
+    worst = float((off / (bound[:T] + 1e-37)).max()) if off.numel() else 0.0
+    print(f"[lora] worst {worst:.3f} of the bound", flush=True)
+    assert worst <= 1.0
+    # rows without an adapter are copies
+    for s, a in enumerate(i["ids"]):
+        if a < 0:
+            r = slice(int(i["cu_host"][s]), int(i["cu_host"][s + 1]))
+            assert torch.equal(out[r], i["base"][r])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("R", [8, 16, 24, 32, 40, 64, 128])
+@pytest.mark.parametrize("K,M", [(8, 1), (64, 96), (200, 257), (1024, 520)])
+def test_sizes(dtype, R, K, M):
+    i = inputs([5, 0, 1, 70, 130], [0, 1, 2, -1, 0], K, M, R, dtype=dtype, seed=R + K)
+    check(i, lora(i))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lens,ids", [([1], [0]), ([1] * 40, [k % 4 - 1 for k in range(40)]), ([63, 64, 65], [2, 2, 1]),
+                                      ([0, 0, 3], [-1, 2, 1]), ([1000], [1]), ([4, 4], [-1, -1])])
+def test_lengths(dtype, lens, ids):
+    i = inputs(lens, ids, 264, 328, 16, dtype=dtype, seed=len(lens))
+    check(i, lora(i))
+
+
+def test_wide_projection():
+    """Many column tiles and a deep contraction, for single tokens and for prompts."""
+    for lens in ([1] * 9, [300, 90]):
+        i = inputs(lens, [k % 3 for k in range(len(lens))], 2048, 4104, 32, seed=3)
+        check(i, lora(i))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("pads", [(0, 0), (8, 8), (16, 3)])
+def test_strides_in_place_and_rows_behind(dtype, pads):
+    i = inputs([40, 3, 7], [1, -1, 0], 72, 136, 16, dtype=dtype, seed=4, spare=9, pads=pads, scales=False)
+    i["x"][50:] = float("nan")
+    out = lora(i)
+    check(i, out)
+    rows = torch.full((59, 136 + pads[1]), 3.0, dtype=DT[dtype], device=DEV)
+    buf = rows[:, :136]
+    buf.copy_(i["base"])
+    assert lora(dict(i, base=buf), out=buf) is buf
+    assert torch.equal(buf[:50], out[:50]) and torch.equal(buf[50:], i["base"][50:]) and (rows[:, 136:] == 3.0).all()
+
+
+def test_neighbours_and_unused_adapters():
+    """What is not finite in one request, or in an adapter nobody uses, reaches no other request."""
+    i = inputs([30, 20, 40], [0, 1, 0], 72, 136, 16, n=4, seed=5)
+    out = lora(i)
+    bad = dict(i, x=i["x"].clone(), a=i["a"].clone(), b=i["b"].clone())
+    bad["x"][30:50] = float("nan")
+    bad["a"][2:] = float("inf")
+    bad["b"][1:] = float("nan")
+    out2 = lora(bad)
+    assert torch.equal(out[:30], out2[:30]) and torch.equal(out[50:], out2[50:])
+    assert torch.isnan(out2[30:50].float()).all()
+    assert torch.equal(out, lora(i))
+
+
+def test_graph_replays():
+    i = inputs([200, 0, 5], [0, 1, 2], 264, 520, 16, seed=6)
+    i["ids"] = torch.tensor(i["ids"], dtype=torch.int32)
+    ids = i["ids"].to(DEV)
+    call = lambda **kw: gdn.lora_add(i["base"], i["x"], i["a"], i["b"], ids, i["cu"], i["cu_host"],
+                                     adapters_host=i["ids"], scales=i["scales"], **kw)
+    o0 = call()
+    o = torch.empty_like(o0)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(out=o)
+    for k in range(3):
+        o.zero_()
+        graph.replay()
+        lora(inputs([900 + k], [0], 264, 520, 64, seed=7))
+        torch.cuda.synchronize()
+        assert torch.equal(o, o0)
+
+
+def test_no_tokens_and_no_adapters():
+    i = inputs([0, 0], [0, -1], seed=8)
+    assert lora(i).shape == (0, 96)
+    i = inputs([4], [-1], seed=8)
+    i.update(a=i["a"][:0], b=i["b"][:0], scales=None)
+    assert torch.equal(lora(i), i["base"])
