@@ -1,6 +1,8 @@
 // Host-side validation and planning (see gdn_layer_plan.h).
 #include "gdn_layer_plan.h"
 
+#include "gdn_plan.h"
+
 #include <algorithm>
 #include <limits>
 
@@ -10,6 +12,11 @@ namespace {
 constexpr int64_t kMaxGrid = std::numeric_limits<int32_t>::max();
 // strides and row counts stay far inside 64-bit element offsets
 constexpr int64_t kMaxStride = int64_t{1} << 40;
+
+// Segments of the state space scan
+constexpr int64_t kSsmPlaces = 512;       // workgroups that the chip holds at once
+constexpr int64_t kSsmSplitChunks = 8;    // the longest sequence from which it pays
+constexpr int64_t kSsmSegChunks = 4;      // the shortest segment
 
 bool known_dtype(int32_t d) { return d == GDN_F32 || d == GDN_BF16; }
 
@@ -83,6 +90,37 @@ gdn_status check_ssm(const gdn_ssm_shape* s, std::string* err) {
     *err = "num_seqs * num_heads too large";
     return GDN_ERR_UNSUPPORTED;
   }
+  return GDN_OK;
+}
+
+gdn_status make_ssm_plan(const gdn_ssm_shape* s, const int32_t* cu, SsmPlan* plan, std::string* err) {
+  gdn_status st = check_ssm(s, err);
+  SsmPlan p;
+  if (st == GDN_OK) st = check_seqlens(s->num_seqs, cu, &p.tokens, &p.longest, err);
+  if (st != GDN_OK) return st;
+  const int64_t H = s->num_heads, N = s->num_seqs;
+  const int32_t share = (s->dtype == GDN_BF16 ? kSsmCols : kSsmColsF32) / s->head_dim;
+  p.heads_per_group = H / s->num_groups % share == 0 ? share : 1;
+  p.slots = N;
+  const int64_t groups = H / p.heads_per_group;   // workgroups of a sequence
+  const int64_t longest = (p.longest + 63) / 64;
+  if (longest >= kSsmSplitChunks && N * groups < kSsmPlaces) {
+    int64_t chunks = 0;
+    for (int64_t n = 0; n < N; ++n) chunks += (static_cast<int64_t>(cu[n + 1]) - cu[n] + 63) / 64;
+    const int64_t seg = std::max<int64_t>(kSsmSegChunks, (chunks * groups + kSsmPlaces - 1) / kSsmPlaces);
+    if (seg * 2 <= longest) {
+      p.seg_tokens = static_cast<int32_t>(64 * seg);
+      p.slots = tile_slots(p.tokens, N, p.seg_tokens);
+      const size_t state = static_cast<size_t>(H) * s->d_state * s->head_dim * sizeof(float);
+      p.off_decay = static_cast<size_t>(p.slots) * state;   // a multiple of 256
+      p.bytes = (p.off_decay + static_cast<size_t>(p.slots) * H * sizeof(float) + kAlign - 1) / kAlign * kAlign;
+    }
+  }
+  if (p.slots * groups > kMaxGrid / 1024) {
+    *err = "too many segments";
+    return GDN_ERR_UNSUPPORTED;
+  }
+  *plan = p;
   return GDN_OK;
 }
 

@@ -11,6 +11,10 @@
 
 namespace gdn {
 
+// State columns of a workgroup of the state space scan, where a B/C group has
+// that many heads to share them (bf16, fp32); one head's otherwise.
+constexpr int32_t kSsmCols = 128, kSsmColsF32 = 128;
+
 // Packed sequences cut into tiles of `tile` tokens, each sequence from its own
 // start: tile j of sequence n is slot cu[n] / tile + n + j.  The map is
 // injective and every sequence has a slot of its own, the empty ones too; at
@@ -23,6 +27,19 @@ gdn_status check_seqlens(int32_t n, const int32_t* cu, int64_t* tokens, int64_t*
 
 gdn_status check_conv(const gdn_conv_shape* s, std::string* err);
 gdn_status check_ssm(const gdn_ssm_shape* s, std::string* err);
+
+// How gdn_ssm_scan runs: which heads share a workgroup and whether sequences
+// are worked on in segments.
+struct SsmPlan {
+  int64_t tokens = 0, longest = 0;
+  int32_t heads_per_group = 1;   // heads of a workgroup
+  int32_t seg_tokens = 0;        // 0: whole sequences
+  int64_t slots = 0;             // segment slots (tile_slots), or sequences
+  size_t off_decay = 0;          // workspace: states [slots, H, d_state, head_dim], then decays [slots, H]
+  size_t bytes = 0;
+};
+gdn_status make_ssm_plan(const gdn_ssm_shape* s, const int32_t* cu, SsmPlan* p, std::string* err);
+
 gdn_status check_lora(const gdn_lora_shape* s, std::string* err);
 
 // Two row-strided regions of `rows` rows: a starts at pa, has wa bytes in each

@@ -6,7 +6,8 @@
 
 #include "gdn_layer_plan.h"
 #include "gdn_plan.h"
-#include "gdn_ssm_kernels.h"
+#include "gdn_ssm_scan.h"
+#include "gdn_ssm_step.h"
 
 namespace gdn {
 namespace {
@@ -24,7 +25,8 @@ gdn_status slaunched(const char* what) {
 
 struct SsmArgs {
   const gdn_ssm_shape* s;
-  const int32_t* cu;   // NULL: one token per sequence
+  const SsmPlan* p;   // NULL: one token per sequence
+  const int32_t* cu;
   int64_t tokens;
   const void* x;
   const void* dt;
@@ -36,26 +38,56 @@ struct SsmArgs {
   const float* state_in;
   void* y;
   float* state_out;
+  char* ws;
   hipStream_t stream;
 };
 
 template <typename T, int DK, int DV>
-gdn_status launch_ssm(const SsmArgs& a) {
+gdn_status launch_step(const SsmArgs& a) {
   const gdn_ssm_shape& s = *a.s;
-  const bool dt_bf16 = s.dt_dtype == GDN_BF16;
-  const uint32_t blocks = static_cast<uint32_t>(s.num_seqs) * s.num_heads;
-  if (!a.cu) {
-    hipLaunchKernelGGL((k_ssm_step<T, DK, DV>), dim3(blocks), dim3(kSsmThreads), 0, a.stream, s.num_heads,
-                       s.num_groups, static_cast<const T*>(a.x), s.ld_x, a.dt, dt_bf16, s.ld_dt, a.a_log,
-                       static_cast<const T*>(a.B), s.ld_b, static_cast<const T*>(a.C), s.ld_c, a.d_skip, a.dt_bias,
-                       a.state_in, static_cast<T*>(a.y), s.ld_y, a.state_out);
-    return slaunched("state space step launch");
+  hipLaunchKernelGGL((k_ssm_step<T, DK, DV>), dim3(static_cast<uint32_t>(s.num_seqs) * s.num_heads), dim3(kSsmThreads),
+                     0, a.stream, s.num_heads, s.num_groups, static_cast<const T*>(a.x), s.ld_x, a.dt,
+                     s.dt_dtype == GDN_BF16, s.ld_dt, a.a_log, static_cast<const T*>(a.B), s.ld_b,
+                     static_cast<const T*>(a.C), s.ld_c, a.d_skip, a.dt_bias, a.state_in, static_cast<T*>(a.y), s.ld_y,
+                     a.state_out);
+  return slaunched("state space step launch");
+}
+
+template <typename T, int DK, int DV, int CT, int NW>
+gdn_status launch_scan(const SsmArgs& a) {
+  const gdn_ssm_shape& s = *a.s;
+  const SsmPlan& p = *a.p;
+  SsmScanArgs k{s.num_seqs, s.num_heads, s.num_groups, p.seg_tokens, a.cu, a.x, a.dt, a.B, a.C,
+                s.ld_x, s.ld_dt, s.ld_b, s.ld_c, s.ld_y, s.dt_dtype == GDN_BF16, a.a_log, a.d_skip, a.dt_bias,
+                a.state_in, a.y, a.state_out, reinterpret_cast<f32x4*>(a.ws),
+                reinterpret_cast<float*>(a.ws + p.off_decay)};
+  const dim3 grid(static_cast<uint32_t>(p.slots * (s.num_heads / p.heads_per_group))), block(NW * kWave);
+  const auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, a.stream, k); };
+  if (p.seg_tokens == 0) {
+    if (a.y) run(k_ssm_scan<T, DK, DV, CT, NW, SsmMode::kWhole, true>);
+    else run(k_ssm_scan<T, DK, DV, CT, NW, SsmMode::kWhole, false>);
+    return slaunched("state space scan launch");
   }
-  hipLaunchKernelGGL((k_ssm_walk<T, DK, DV>), dim3(blocks), dim3(kSsmThreads), 0, a.stream, s.num_heads, s.num_groups,
-                     a.cu, static_cast<const T*>(a.x), s.ld_x, a.dt, dt_bf16, s.ld_dt, a.a_log,
-                     static_cast<const T*>(a.B), s.ld_b, static_cast<const T*>(a.C), s.ld_c, a.d_skip, a.dt_bias,
-                     a.state_in, static_cast<T*>(a.y), s.ld_y, a.state_out);
+  run(k_ssm_scan<T, DK, DV, CT, NW, SsmMode::kLocal, false>);
+  const int64_t vecs = static_cast<int64_t>(s.num_seqs) * s.num_heads * DK * DV / 4;
+  const dim3 jgrid(static_cast<uint32_t>((vecs + 255) / 256));
+  if (a.y) {
+    hipLaunchKernelGGL((k_ssm_join<DK, DV, CT, NW, true>), jgrid, dim3(256), 0, a.stream, k);
+    run(k_ssm_scan<T, DK, DV, CT, NW, SsmMode::kJoined, true>);
+  } else {
+    hipLaunchKernelGGL((k_ssm_join<DK, DV, CT, NW, false>), jgrid, dim3(256), 0, a.stream, k);
+  }
   return slaunched("state space scan launch");
+}
+
+template <typename T, int DK, int DV>
+gdn_status launch_ssm(const SsmArgs& a) {
+  if (!a.p) return launch_step<T, DK, DV>(a);
+  constexpr int CT = 2;
+  constexpr int cols = sizeof(T) == 2 ? kSsmCols : kSsmColsF32;
+  if constexpr (cols > DV)
+    if (a.p->heads_per_group > 1) return launch_scan<T, DK, DV, CT, cols / (16 * CT)>(a);
+  return launch_scan<T, DK, DV, CT, DV / (16 * CT)>(a);
 }
 
 template <typename T>
@@ -97,11 +129,10 @@ extern "C" {
 gdn_status gdn_ssm_workspace_size(const gdn_ssm_shape* shape, const int32_t* cu_seqlens_host, size_t* bytes) {
   if (!bytes) return gdn::sfail(GDN_ERR_NULL_ARG, "bytes is NULL");
   std::string err;
-  gdn_status st = gdn::check_ssm(shape, &err);
-  int64_t tokens = 0, longest = 0;
-  if (st == GDN_OK) st = gdn::check_seqlens(shape->num_seqs, cu_seqlens_host, &tokens, &longest, &err);
+  gdn::SsmPlan p;
+  const gdn_status st = gdn::make_ssm_plan(shape, cu_seqlens_host, &p, &err);
   if (st != GDN_OK) return gdn::sfail(st, err);
-  *bytes = 0;
+  *bytes = p.bytes;
   return GDN_OK;
 }
 
@@ -110,15 +141,20 @@ gdn_status gdn_ssm_scan(const gdn_ssm_shape* shape, const int32_t* cu_seqlens_ho
                         const float* d_skip, const float* dt_bias, const float* state_in, void* y, float* state_out,
                         void* workspace, size_t workspace_bytes, void* stream) {
   std::string err;
-  gdn_status st = gdn::check_ssm(shape, &err);
-  int64_t tokens = 0, longest = 0;
-  if (st == GDN_OK) st = gdn::check_seqlens(shape->num_seqs, cu_seqlens_host, &tokens, &longest, &err);
+  gdn::SsmPlan p;
+  const gdn_status st = gdn::make_ssm_plan(shape, cu_seqlens_host, &p, &err);
   if (st != GDN_OK) return gdn::sfail(st, err);
   if (shape->num_seqs == 0) return GDN_OK;
   if (!cu_seqlens) return gdn::sfail(GDN_ERR_NULL_ARG, "cu_seqlens (device) is NULL");
   if (!y && !state_out) return gdn::sfail(GDN_ERR_NULL_ARG, "y and state_out are both NULL");
-  return gdn::ssm_impl({shape, cu_seqlens, tokens, x, dt, a_log, B, C, d_skip, dt_bias, state_in, y, state_out,
-                        static_cast<hipStream_t>(stream)});
+  if (p.bytes > 0 && !workspace) return gdn::sfail(GDN_ERR_WORKSPACE, "workspace is NULL");
+  if (workspace_bytes < p.bytes)
+    return gdn::sfail(GDN_ERR_WORKSPACE, "workspace too small: need " + std::to_string(p.bytes) + " bytes, got " +
+                                             std::to_string(workspace_bytes));
+  if (p.bytes > 0 && reinterpret_cast<uintptr_t>(workspace) % gdn::kAlign != 0)
+    return gdn::sfail(GDN_ERR_WORKSPACE, "workspace must be 256-byte aligned");
+  return gdn::ssm_impl({shape, &p, cu_seqlens, p.tokens, x, dt, a_log, B, C, d_skip, dt_bias, state_in, y, state_out,
+                        static_cast<char*>(workspace), static_cast<hipStream_t>(stream)});
 }
 
 gdn_status gdn_ssm_step(const gdn_ssm_shape* shape, const void* x, const void* dt, const float* a_log, const void* B,
@@ -129,8 +165,8 @@ gdn_status gdn_ssm_step(const gdn_ssm_shape* shape, const void* x, const void* d
   if (st != GDN_OK) return gdn::sfail(st, err);
   if (shape->num_seqs == 0) return GDN_OK;
   if (!y || !state_out) return gdn::sfail(GDN_ERR_NULL_ARG, "y and state_out must be non-NULL");
-  return gdn::ssm_impl({shape, nullptr, shape->num_seqs, x, dt, a_log, B, C, d_skip, dt_bias, state_in, y, state_out,
-                        static_cast<hipStream_t>(stream)});
+  return gdn::ssm_impl({shape, nullptr, nullptr, shape->num_seqs, x, dt, a_log, B, C, d_skip, dt_bias, state_in, y,
+                        state_out, nullptr, static_cast<hipStream_t>(stream)});
 }
 
 }  // extern "C"

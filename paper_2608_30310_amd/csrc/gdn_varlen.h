@@ -43,4 +43,9 @@ __device__ __forceinline__ void store_run(T* __restrict__ p, const float (&x)[N]
 // log(1 + e^x); from 20 on x itself is within 2e-9 of it
 __device__ __forceinline__ float softplus_f(float x) { return x > 20.0f ? x : log1pf(expf(x)); }
 
+// dt is fp32 or has the element type
+__device__ __forceinline__ float load_dt(const void* __restrict__ dt, bool bf16, int64_t i) {
+  return bf16 ? bf2f(static_cast<const uint16_t*>(dt)[i]) : static_cast<const float*>(dt)[i];
+}
+
 }  // namespace gdn
