@@ -18,7 +18,7 @@
  * everything on `stream`, capturable, no allocation), and:
  *   - Rows.  Token rows may be strided: ld_* is the distance of two tokens'
  *     rows in elements, so that a call reads its columns out of a projection's
- *     rows.  Inside a row the elements are dense.
+ *     rows; at most 2^23.  Inside a row the elements are dense.
  *   - Rows at or behind cu_seqlens[N] are neither read nor written.
  *   - An input that is not finite reaches outputs of its own sequence only.
  *     In gdn_ssm_scan it may reach every output of its 64-token chunk

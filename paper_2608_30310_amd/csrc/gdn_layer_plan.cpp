@@ -10,8 +10,8 @@ namespace gdn {
 namespace {
 
 constexpr int64_t kMaxGrid = std::numeric_limits<int32_t>::max();
-// strides and row counts stay far inside 64-bit element offsets
-constexpr int64_t kMaxStride = int64_t{1} << 40;
+// a tile's rows are addressed with 32-bit byte offsets: 64 rows of 2^23 fp32 elements
+constexpr int64_t kMaxStride = int64_t{1} << 23;
 
 // Segments of the state space scan
 constexpr int64_t kSsmPlaces = 512;       // workgroups that the chip holds at once
@@ -20,9 +20,10 @@ constexpr int64_t kSsmSegChunks = 4;      // the shortest segment
 
 bool known_dtype(int32_t d) { return d == GDN_F32 || d == GDN_BF16; }
 
-gdn_status bad_stride(const char* name, int64_t least, std::string* err) {
-  *err = std::string(name) + " must be between " + std::to_string(least) + " and 2^40";
-  return GDN_ERR_BAD_SHAPE;
+gdn_status check_stride(const char* name, int64_t ld, int64_t least, std::string* err) {
+  if (ld < least) { *err = std::string(name) + " must be at least " + std::to_string(least); return GDN_ERR_BAD_SHAPE; }
+  if (ld > kMaxStride) { *err = std::string(name) + " must be at most 2^23"; return GDN_ERR_UNSUPPORTED; }
+  return GDN_OK;
 }
 
 }  // namespace
@@ -51,9 +52,8 @@ gdn_status check_conv(const gdn_conv_shape* s, std::string* err) {
     *err = "activation must be GDN_ACT_NONE or GDN_ACT_SILU";
     return GDN_ERR_UNSUPPORTED;
   }
-  if (s->ld_x < s->channels || s->ld_x > kMaxStride) return bad_stride("ld_x", s->channels, err);
-  if (s->ld_y < s->channels || s->ld_y > kMaxStride) return bad_stride("ld_y", s->channels, err);
-  return GDN_OK;
+  const gdn_status st = check_stride("ld_x", s->ld_x, s->channels, err);
+  return st != GDN_OK ? st : check_stride("ld_y", s->ld_y, s->channels, err);
 }
 
 gdn_status check_ssm(const gdn_ssm_shape* s, std::string* err) {
@@ -80,7 +80,7 @@ gdn_status check_ssm(const gdn_ssm_shape* s, std::string* err) {
       {"ld_x", s->ld_x, H * s->head_dim, true}, {"ld_dt", s->ld_dt, H, false}, {"ld_b", s->ld_b, G * s->d_state, true},
       {"ld_c", s->ld_c, G * s->d_state, true},  {"ld_y", s->ld_y, H * s->head_dim, true}};
   for (const auto& r : rows)
-    if (r.ld < r.least || r.ld > kMaxStride) return bad_stride(r.name, r.least, err);
+    if (const gdn_status st = check_stride(r.name, r.ld, r.least, err); st != GDN_OK) return st;
   for (const auto& r : rows)
     if (r.aligned && r.ld % vec != 0) {
       *err = std::string(r.name) + " must be a multiple of 16 bytes";
@@ -140,9 +140,10 @@ gdn_status check_lora(const gdn_lora_shape* s, std::string* err) {
     return GDN_ERR_UNSUPPORTED;
   }
   if (!known_dtype(s->out_dtype)) { *err = "out_dtype must be GDN_F32 or GDN_BF16"; return GDN_ERR_UNSUPPORTED; }
-  if (s->ld_x < s->hidden || s->ld_x > kMaxStride) return bad_stride("ld_x", s->hidden, err);
-  if (s->ld_base < s->width || s->ld_base > kMaxStride) return bad_stride("ld_base", s->width, err);
-  if (s->ld_out < s->width || s->ld_out > kMaxStride) return bad_stride("ld_out", s->width, err);
+  gdn_status st = check_stride("ld_x", s->ld_x, s->hidden, err);
+  if (st == GDN_OK) st = check_stride("ld_base", s->ld_base, s->width, err);
+  if (st == GDN_OK) st = check_stride("ld_out", s->ld_out, s->width, err);
+  if (st != GDN_OK) return st;
   if (s->ld_x % 8 != 0) { *err = "ld_x must be a multiple of 8"; return GDN_ERR_UNSUPPORTED; }
   return GDN_OK;
 }

@@ -6,9 +6,9 @@
 //   y  = diag(e^G) C M0 + ((C B^T) o L o delta_j) x + d_skip x,
 //   M <- e^{G_last} M0 + B^T diag(e^{G_last - G_j} delta_j) x,
 //   L_ij = e^{G_i - G_j} for j <= i.
-// C B^T is computed once per chunk for all of the workgroup's heads (they share
-// a B/C group), everything else per wave: a wave owns 16 CT state columns of
-// one head.
+// A wave owns 16 CT state columns of one head; the waves of a head share the
+// decayed products P = (C B^T) o L o delta_j through LDS, and the heads of a
+// workgroup, which are of one B/C group, share the B and C rows.
 #pragma once
 
 #include "gdn_varlen.h"
@@ -52,6 +52,27 @@ struct Mx<uint16_t> {
     f.lo = __builtin_bit_cast(bf16x8, lo);
     return f;
   }
+  // an F2 operand in LDS: 64 lanes x 16 bytes of high parts, then of low parts
+  static constexpr int kF2Bytes = 2048;
+  static __device__ __forceinline__ void put4(char* frag, int slot, int half, const float (&v)[4]) {
+    u32x2 hi, lo;
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      const f32x2 x = {v[2 * p], v[2 * p + 1]};
+      const uint32_t h = __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
+      const f32x2 d = {x[0] - __uint_as_float(h << 16), x[1] - __uint_as_float(h & 0xFFFF0000u)};
+      hi[p] = h;
+      lo[p] = __builtin_bit_cast(uint32_t, __builtin_convertvector(d, bf16x2));
+    }
+    *reinterpret_cast<u32x2*>(frag + 16 * slot + 8 * half) = hi;
+    *reinterpret_cast<u32x2*>(frag + 1024 + 16 * slot + 8 * half) = lo;
+  }
+  static __device__ __forceinline__ F2 get(const char* frag, int lane) {
+    F2 f;
+    f.hi = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(frag + 16 * lane));
+    f.lo = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(frag + 1024 + 16 * lane));
+    return f;
+  }
   static __device__ __forceinline__ float elt(const R& r, int j) {
     const u32x4 w = __builtin_bit_cast(u32x4, r);
     return __uint_as_float((j & 1) ? (w[j / 2] & 0xFFFF0000u) : (w[j / 2] << 16));
@@ -73,6 +94,15 @@ struct Mx<float> {
     return f32x8{v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]};
   }
   static __device__ __forceinline__ f32x8 f3(const float (&v)[8]) { return f2(v); }
+  static constexpr int kF2Bytes = 2048;   // 64 lanes x 32 bytes
+  static __device__ __forceinline__ void put4(char* frag, int slot, int half, const float (&v)[4]) {
+    *reinterpret_cast<f32x4*>(frag + 32 * slot + 16 * half) = f32x4{v[0], v[1], v[2], v[3]};
+  }
+  static __device__ __forceinline__ f32x8 get(const char* frag, int lane) {
+    const f32x4 a = *reinterpret_cast<const f32x4*>(frag + 32 * lane);
+    const f32x4 b = *reinterpret_cast<const f32x4*>(frag + 32 * lane + 16);
+    return f32x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+  }
   static __device__ __forceinline__ float elt(const R& r, int j) { return r[j]; }
   static __device__ __forceinline__ f32x4 rr(const R& a, const R& b, f32x4 c) {
 #pragma unroll
@@ -93,12 +123,15 @@ struct RowsLds {
   static constexpr int kPieces = D * static_cast<int>(sizeof(T)) / 16;   // of a row
   static constexpr int kPitch = sizeof(T) == 2 ? 2 * D : 4 * D + 16;
   static constexpr int kBytes = kSsmChunk * kPitch;
+  // The swizzle repeats every 16 rows, so a row's address may be taken from any
+  // row a multiple of 16 above it.
   static __device__ __forceinline__ int at(int row, int piece) {
     if constexpr (sizeof(T) == 2) return row * kPitch + ((piece ^ row_swz<kPitch>(row)) << 4);
     else return row * kPitch + (piece << 4);
   }
-  // elements 8 e8 .. + 7 of a row
-  static __device__ __forceinline__ typename Mx<T>::R row_frag(const char* base, int row, int e8) {
+  // elements 8 e8 .. + 7 of row `up` + row, up a multiple of 16
+  static __device__ __forceinline__ typename Mx<T>::R row_frag(const char* base, int up, int row, int e8) {
+    base += up * kPitch;
     if constexpr (sizeof(T) == 2) {
       return __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(base + at(row, e8)));
     } else {
@@ -107,25 +140,52 @@ struct RowsLds {
       return f32x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
     }
   }
-  // rows row0 + 8 g + j (j = 0..7) of column col32 + 8 (c / 4) + 4 half + c % 4, for lane (g, c)
-  static __device__ __forceinline__ typename Mx<T>::R col_frag(const char* base, int row0, int col32, int half, int g,
+  // rows up + 8 g + j (j = 0..7; up a multiple of 32) of column col32 + 8 (c / 4) + 4 half + c % 4, for lane (g, c)
+  static __device__ __forceinline__ typename Mx<T>::R col_frag(const char* base, int up, int col32, int half, int g,
                                                                int c) {
+    base += up * kPitch;
     if constexpr (sizeof(T) == 2) {
       // lane 4 t + q of a group of 16 supplies four elements of row t, columns 8 q ..; lane i receives
       // column 8 (i / 4) + i % 4 of rows 0..3
-      const int row = row0 + 8 * g + c / 4, piece = col32 / 8 + c % 4;
+      const int row = 8 * g + c / 4, piece = col32 / 8 + c % 4;
       const u32x2 a = lds_read_tr16(base + at(row, piece) + 8 * half);
       const u32x2 b = lds_read_tr16(base + at(row + 4, piece) + 8 * half);
       return join_halves(a, b);
     } else {
-      const float* p = reinterpret_cast<const float*>(base + (row0 + 8 * g) * kPitch) + col32 + 8 * (c / 4) + 4 * half + c % 4;
+      const float* p = reinterpret_cast<const float*>(base + 8 * g * kPitch) + col32 + 8 * (c / 4) + 4 * half + c % 4;
       f32x8 r;
 #pragma unroll
       for (int j = 0; j < 8; ++j) r[j] = p[j * (kPitch / 4)];
       return r;
     }
   }
+  // address of row + k STEP
+  template <int STEP>
+  static __device__ __forceinline__ int at_step(int row, int k, int piece) {
+    if constexpr (STEP % 16 == 0) return at(row, piece) + k * STEP * kPitch;
+    else return at(row + k * STEP, piece);
+  }
 };
+
+// Eight elements to a buffer at byte offset `off`; a row behind the buffer's end is dropped.
+__device__ __forceinline__ void buffer_store8(__amdgpu_buffer_rsrc_t r, uint32_t off, const float (&x)[8], uint16_t*) {
+  u32x4 w;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const f32x2 pair = {x[2 * j], x[2 * j + 1]};
+    w[j] = __builtin_bit_cast(uint32_t, __builtin_convertvector(pair, bf16x2));
+  }
+  __builtin_amdgcn_raw_buffer_store_b128(w, r, off, 0, 0);
+}
+__device__ __forceinline__ void buffer_store8(__amdgpu_buffer_rsrc_t r, uint32_t off, const float (&x)[8], float*) {
+  const f32x4 a = {x[0], x[1], x[2], x[3]}, b = {x[4], x[5], x[6], x[7]};
+  __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, a), r, off, 0, 0);
+  __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, b), r, off + 16, 0, 0);
+}
+// Raw buffer of `bytes` bytes: a load behind its end gives zero.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_buffer(const void* base, uint32_t bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, bytes, 0x00020000);
+}
 
 // Per head and chunk, base-2 logarithms: with l the inclusive cumulative log
 // alpha inside a token's 16-token tile and s what is left of the tile after it,
@@ -139,9 +199,26 @@ struct HeadScalars {
   float suf[kSsmChunk];    // e^{G_last - G} delta
   float tile[4];           // log2 alpha summed over each tile
   float total;             // e^{G_last}
-  float log_total;         // G_last, base 2
-  float pad[2];
+  float pad[3];
 };
+
+// Lane exchanges inside a DPP row of 16 lanes; a lane without a source gets 0.
+template <int CTRL>
+__device__ __forceinline__ float dpp(float x) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, true));
+}
+// Inclusive sums along the row: SHIFT 0x110 (row_shr) from its start, 0x100 (row_shl) from its end.
+template <int SHIFT>
+__device__ __forceinline__ float row_scan(float x) {
+  x += dpp<SHIFT + 1>(x);
+  x += dpp<SHIFT + 2>(x);
+  x += dpp<SHIFT + 4>(x);
+  x += dpp<SHIFT + 8>(x);
+  return x;
+}
+__device__ __forceinline__ float read_lane(float x, int lane) {
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), lane));
+}
 
 struct SsmScanArgs {
   int32_t n_seqs, heads, groups, seg_tokens;
@@ -176,12 +253,13 @@ struct SsmLayout {
   static constexpr int kTiles = DK / 16 * CT;         // accumulator tiles of a wave's state
   typedef RowsLds<T, DK> KRows;
   typedef RowsLds<T, DV> XRows;
-  static constexpr int kCbPitch = kSsmChunk + 4;
+  static constexpr int kPFrags = 6;                   // (row tile ti, k step kk <= ti / 2)
+  static constexpr int kPBytes = kPFrags * Mx<T>::kF2Bytes;
   static constexpr int kOffB = 0;
   static constexpr int kOffC = kOffB + KRows::kBytes;
   static constexpr int kOffX = kOffC + (OUT ? KRows::kBytes : 0);
-  static constexpr int kOffCb = kOffX + kHeads * XRows::kBytes;
-  static constexpr int kOffS = kOffCb + (OUT ? kSsmChunk * kCbPitch * 4 : 0);
+  static constexpr int kOffP = kOffX + kHeads * XRows::kBytes;
+  static constexpr int kOffS = kOffP + (OUT ? kHeads * kPBytes : 0);
   static constexpr int kBytes = kOffS + kHeads * static_cast<int>(sizeof(HeadScalars));
   static_assert(NW % kWavesPerHead == 0 && kHeads <= NW, "whole heads");
   static_assert(kSsmChunk * KRows::kPieces % kThreads == 0 && kSsmChunk * XRows::kPieces * kHeads % kThreads == 0,
@@ -192,7 +270,7 @@ struct SsmLayout {
 __device__ __forceinline__ int ssm_col(int ct, int c) { return 32 * (ct >> 1) + 8 * (c / 4) + 4 * (ct & 1) + c % 4; }
 
 template <typename T, int DK, int DV, int CT, int NW, SsmMode MODE, bool OUT>
-__global__ __launch_bounds__(NW * kWave)
+__global__ __launch_bounds__(NW * kWave, 2)
 void k_ssm_scan(SsmScanArgs a) {
   typedef SsmLayout<T, DK, DV, CT, NW, OUT> L;
   typedef typename L::KRows KRows;
@@ -212,7 +290,8 @@ void k_ssm_scan(SsmScanArgs a) {
   const int hg = unit % hgs, slot = unit / hgs;
   int n = slot, first = 0;
   if constexpr (MODE != SsmMode::kWhole) n = slot_seq(a.cu, a.n_seqs, slot, a.seg_tokens);
-  const int start = a.cu[n], seq_len = a.cu[n + 1] - start;
+  const int start = __builtin_amdgcn_readfirstlane(a.cu[n]);
+  const int seq_len = __builtin_amdgcn_readfirstlane(a.cu[n + 1]) - start;
   if constexpr (MODE != SsmMode::kWhole) {
     const int64_t at = static_cast<int64_t>(slot - (start / a.seg_tokens + n)) * a.seg_tokens;
     if (at > 0 && at >= seq_len) return;   // an unused slot
@@ -230,7 +309,6 @@ void k_ssm_scan(SsmScanArgs a) {
   const T* bb = static_cast<const T*>(a.B) + t0 * a.ldb + static_cast<int64_t>(gh) * DK;
   const T* cb = OUT ? static_cast<const T*>(a.C) + t0 * a.ldc + static_cast<int64_t>(gh) * DK : nullptr;
   HeadScalars* sc = reinterpret_cast<HeadScalars*>(lds + L::kOffS);
-  float* cbm = reinterpret_cast<float*>(lds + L::kOffCb);
 
   // the state
   f32x4 m[DK / 16][CT];
@@ -255,100 +333,132 @@ void k_ssm_scan(SsmScanArgs a) {
   const float skip = OUT && a.d_skip ? a.d_skip[head] : 0.0f;
   float log_total = 0.0f;   // of the whole segment (kLocal)
 
+  // A thread's pieces of a chunk: rows tid / pieces + k (threads / pieces).  A
+  // chunk is a buffer from its first row: its offsets fit 32 bits (row strides
+  // are below 2^24 elements), rows behind the sequence's last one read as zero.
+  constexpr uint32_t E = sizeof(T);
   u32x4 pb[KB], pc[OUT ? KB : 1], px[KX];
-  float pdt = 0.0f;
-  // Rows behind the last token repeat it: their steps are zero, so what is
-  // multiplied with it vanishes, and their outputs are not written.
-  auto fetch = [&](int at) {
-    const int rows = min(kSsmChunk, len - at);
+  uint32_t pdt = 0;   // dt as loaded
+  const uint32_t ldb = static_cast<uint32_t>(a.ldb) * E, ldc = static_cast<uint32_t>(a.ldc) * E,
+                 ldx = static_cast<uint32_t>(a.ldx) * E, ldy = static_cast<uint32_t>(a.ldy) * E;
+  const uint32_t rowk = tid / KRows::kPieces, colk = tid % KRows::kPieces, rowx = tid / XP, colx = tid % XP;
+  constexpr uint32_t KSTEP = L::kThreads / KRows::kPieces, XSTEP = L::kThreads / XP;   // rows from k to k + 1
+  static_assert(KSTEP * KRows::kPieces == L::kThreads && XSTEP * XP == L::kThreads, "whole rows per step");
+  const auto fetch = [&](int at) {
+    const uint32_t rows = min(kSsmChunk, len - at);
+    uint32_t vb = rowk * ldb + colk * 16, vc = rowk * ldc + colk * 16, vx = rowx * ldx + colx * 16;
+    asm volatile("" : "+v"(vb), "+v"(vc), "+v"(vx));   // added to here, not kept in a register per piece
+    const __amdgpu_buffer_rsrc_t rb = rows_buffer(bb + at * a.ldb, (rows - 1) * ldb + DK * E);
 #pragma unroll
-    for (int k = 0; k < KB; ++k) {
-      const int i = tid + k * L::kThreads, row = min(i / KRows::kPieces, rows - 1), piece = i % KRows::kPieces;
-      pb[k] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(bb + (at + row) * a.ldb) + piece * 16);
-      if constexpr (OUT)
-        pc[k] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(cb + (at + row) * a.ldc) + piece * 16);
-    }
+    for (int k = 0; k < KB; ++k) pb[k] = __builtin_amdgcn_raw_buffer_load_b128(rb, vb + k * KSTEP * ldb, 0, 0);
+    if constexpr (OUT) {
+      const __amdgpu_buffer_rsrc_t rc = rows_buffer(cb + at * a.ldc, (rows - 1) * ldc + DK * E);
 #pragma unroll
-    for (int k = 0; k < KX; ++k) {
-      const int i = tid + k * L::kThreads, row = min(i / XP, rows - 1), piece = i % XP;
-      px[k] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(xb + (at + row) * a.ldx) + piece * 16);
+      for (int k = 0; k < KB; ++k) pc[k] = __builtin_amdgcn_raw_buffer_load_b128(rc, vc + k * KSTEP * ldc, 0, 0);
     }
-    if (wave < L::kHeads) pdt = load_dt(a.dt, a.dt_bf16, (t0 + at + min(lane, rows - 1)) * a.ld_dt + h0 + wave);
+    const __amdgpu_buffer_rsrc_t rx = rows_buffer(xb + at * a.ldx, (rows - 1) * ldx + L::kHeads * DV * E);
+#pragma unroll
+    for (int k = 0; k < KX; ++k) px[k] = __builtin_amdgcn_raw_buffer_load_b128(rx, vx + k * XSTEP * ldx, 0, 0);
+    if (wave < L::kHeads) {
+      const int64_t base = (t0 + at) * a.ld_dt + h0 + wave;
+      const uint32_t off = min(static_cast<uint32_t>(lane), rows - 1) * static_cast<uint32_t>(a.ld_dt);
+      if (a.dt_bf16) pdt = (static_cast<const uint16_t*>(a.dt) + base)[off];
+      else pdt = (static_cast<const uint32_t*>(a.dt) + base)[off];
+    }
   };
 
+  if constexpr (OUT) {
+    // the halves of P's diagonal operands that lie above the diagonal
+    if (wave % L::kWavesPerHead == 0) {
+      char* pf = lds + L::kOffP + hl * L::kPBytes;
+      const float zero[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+      X::put4(pf, 32 + lane % 32, lane / 32, zero);
+      X::put4(pf + 3 * X::kF2Bytes, 32 + lane % 32, lane / 32, zero);
+    }
+  }
   if (len > 0) fetch(0);
   for (int at = 0; at < len; at += kSsmChunk) {
     const int rows = min(kSsmChunk, len - at);
     // registers -> LDS
 #pragma unroll
     for (int k = 0; k < KB; ++k) {
-      const int i = tid + k * L::kThreads, row = i / KRows::kPieces, piece = i % KRows::kPieces;
-      *reinterpret_cast<u32x4*>(lds + L::kOffB + KRows::at(row, piece)) = pb[k];
-      if constexpr (OUT) *reinterpret_cast<u32x4*>(lds + L::kOffC + KRows::at(row, piece)) = pc[k];
+      *reinterpret_cast<u32x4*>(lds + L::kOffB + KRows::template at_step<KSTEP>(rowk, k, colk)) = pb[k];
+      if constexpr (OUT) *reinterpret_cast<u32x4*>(lds + L::kOffC + KRows::template at_step<KSTEP>(rowk, k, colk)) = pc[k];
     }
 #pragma unroll
-    for (int k = 0; k < KX; ++k) {
-      const int i = tid + k * L::kThreads, row = i / XP, piece = i % XP;
-      *reinterpret_cast<u32x4*>(lds + L::kOffX + (piece / XRows::kPieces) * XRows::kBytes +
-                                XRows::at(row, piece % XRows::kPieces)) = px[k];
-    }
+    for (int k = 0; k < KX; ++k)
+      *reinterpret_cast<u32x4*>(lds + L::kOffX + (colx / XRows::kPieces) * XRows::kBytes +
+                                XRows::template at_step<XSTEP>(rowx, k, colx % XRows::kPieces)) = px[k];
     if (wave < L::kHeads) {
       // this head's steps, a token per lane
       float delta = 0.0f, la = 0.0f;
       if (lane < rows) {
-        delta = softplus_f(pdt + dt_bias);
+        delta = softplus_f(__uint_as_float(a.dt_bf16 ? pdt << 16 : pdt) + dt_bias);
         la = fmaxf(neg_a2 * delta, -150.0f);   // 2^-150 rounds to zero
       }
-      float l = la, s = la;
-#pragma unroll
-      for (int off = 1; off < 16; off <<= 1) {
-        const float up = __shfl_up(l, off, 16), down = __shfl_down(s, off, 16);
-        l += c >= off ? up : 0.0f;
-        s += c + off < 16 ? down : 0.0f;
-      }
-      s = __shfl_down(s, 1, 16);
-      if (c == 15) s = 0.0f;
-      const float q0 = __shfl(l, 15, kWave), q1 = __shfl(l, 31, kWave), q2 = __shfl(l, 47, kWave), q3 = __shfl(l, 63, kWave);
+      // sums over the 16-token tiles (a tile is a DPP row): up to the token, and behind it
+      const float l = row_scan<0x110>(la), s = row_scan<0x100>(dpp<0x101>(la));
+      const float q0 = read_lane(l, 15), q1 = read_lane(l, 31), q2 = read_lane(l, 47), q3 = read_lane(l, 63);
       const float before = g == 0 ? 0.0f : g == 1 ? q0 : g == 2 ? q0 + q1 : q0 + q1 + q2;
       const float after = g == 3 ? 0.0f : g == 2 ? q3 : g == 1 ? q2 + q3 : q1 + (q2 + q3);
-      const float ld = __log2f(delta);
       HeadScalars& o = sc[wave];
-      o.l[lane] = l;
-      o.same[lane] = ld - l;
-      o.past[lane] = ld + s;
-      o.pre[lane] = __builtin_amdgcn_exp2f(before + l);
+      if constexpr (OUT) {
+        const float ld = __log2f(delta);
+        o.l[lane] = l;
+        o.same[lane] = ld - l;
+        o.past[lane] = ld + s;
+        o.pre[lane] = __builtin_amdgcn_exp2f(before + l);
+        if (c == 15) o.tile[g] = l;
+      }
       o.suf[lane] = __builtin_amdgcn_exp2f(s + after) * delta;
-      if (c == 15) o.tile[g] = l;
       const float sum = (q0 + q1) + (q2 + q3);
       log_total += sum;
       if (lane == 0) o.total = __builtin_amdgcn_exp2f(sum);
     }
-    __syncthreads();
+    lds_barrier();
     if (at + kSsmChunk < len) fetch(at + kSsmChunk);
     const HeadScalars& hs = sc[hl];
     const char* xt = lds + L::kOffX + hl * XRows::kBytes;
+    char* pt = lds + L::kOffP + hl * L::kPBytes;
 
     if constexpr (OUT) {
-      // C B^T, lower triangle of 16 x 16 tiles, transposed through the
-      // accumulators: a lane holds four columns j of row i
-      for (int t = wave; t < 10; t += NW) {
+      // P^T = (C B^T o L o delta)^T by 16 x 16 tiles of the lower triangle, shared
+      // by the head's waves: a lane's accumulator is four columns j of row i, which
+      // are half of one lane's operand for x^T P^T
+#pragma unroll
+      for (int k = 0; k < (10 + L::kWavesPerHead - 1) / L::kWavesPerHead; ++k) {
+        const int t = wave % L::kWavesPerHead + k * L::kWavesPerHead;
+        if (t >= 10) break;
         const int ti = t < 1 ? 0 : t < 3 ? 1 : t < 6 ? 2 : 3, tj = t - ti * (ti + 1) / 2;
         f32x4 acc = zero4();
 #pragma unroll
         for (int kk = 0; kk < DK / 32; ++kk)
-          acc = X::rr(KRows::row_frag(lds + L::kOffB, 16 * tj + c, 4 * kk + g),
-                      KRows::row_frag(lds + L::kOffC, 16 * ti + c, 4 * kk + g), acc);
-        *reinterpret_cast<f32x4*>(cbm + (16 * ti + c) * L::kCbPitch + 16 * tj + 4 * g) = acc;
+          acc = X::rr(KRows::row_frag(lds + L::kOffB, 16 * tj, c, 4 * kk + g),
+                      KRows::row_frag(lds + L::kOffC, 16 * ti, c, 4 * kk + g), acc);
+        float e = hs.l[16 * ti + c];
+        if (tj + 1 < ti) e += hs.tile[ti - 1];
+        if (tj + 2 < ti) e += hs.tile[ti - 2];
+        const f32x4 b = *reinterpret_cast<const f32x4*>((tj < ti ? hs.past : hs.same) + 16 * tj + 4 * g);
+        float v[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float p = acc[r] * __builtin_amdgcn_exp2f(e + b[r]);
+          v[r] = tj < ti || 4 * g + r <= c ? p : 0.0f;
+        }
+        X::put4(pt + (ti < 2 ? ti : ti == 2 ? 2 + tj / 2 : 4 + tj / 2) * X::kF2Bytes, 16 * (2 * (tj & 1) + g / 2) + c,
+                g & 1, v);
       }
-      __syncthreads();
     }
 
-    // x as an operand: tokens 32 kk + 8 g + j of column ct
     R xf[2][CT];
-#pragma unroll
-    for (int kk = 0; kk < 2; ++kk)
-#pragma unroll
-      for (int ct = 0; ct < CT; ++ct) xf[kk][ct] = XRows::col_frag(xt, 32 * kk, p0 + 32 * (ct >> 1), ct & 1, g, c);
+    const auto load_x = [&] {
+      // x as an operand: tokens 32 kk + 8 g + j of column ct
+  #pragma unroll
+      for (int kk = 0; kk < 2; ++kk)
+  #pragma unroll
+        for (int ct = 0; ct < CT; ++ct) xf[kk][ct] = XRows::col_frag(xt, 32 * kk, p0 + 32 * (ct >> 1), ct & 1, g, c);
+    };
+    if constexpr (!OUT) load_x();
 
     if constexpr (OUT) {
       // y^T tiles: rows are state columns, columns are tokens
@@ -372,10 +482,11 @@ void k_ssm_scan(SsmScanArgs a) {
         }
 #pragma unroll
         for (int ti = 0; ti < 4; ++ti) {
-          const R cf = KRows::row_frag(lds + L::kOffC, 16 * ti + c, 4 * kk + g);
+          const R cf = KRows::row_frag(lds + L::kOffC, 16 * ti, c, 4 * kk + g);
 #pragma unroll
           for (int ct = 0; ct < CT; ++ct) yt[ti][ct] = X::fr(mf[ct], cf, yt[ti][ct]);
         }
+        __builtin_amdgcn_sched_barrier(0);   // keeps the next step's operands out of registers
       }
 #pragma unroll
       for (int ti = 0; ti < 4; ++ti) {
@@ -385,47 +496,32 @@ void k_ssm_scan(SsmScanArgs a) {
 #pragma unroll
           for (int i = 0; i < 4; ++i) yt[ti][ct][i] *= e;
       }
+      load_x();
+      lds_barrier();   // P is whole
       // + x^T P^T
 #pragma unroll
-      for (int ti = 0; ti < 4; ++ti) {
-        const float li = hs.l[16 * ti + c];
+      for (int ti = 0; ti < 4; ++ti)
 #pragma unroll
         for (int kk = 0; kk <= ti / 2; ++kk) {
-          const int tj = 2 * kk + (g >> 1);
-          const int j0 = 32 * kk + 8 * g;
-          float between = 0.0f;
-          if (tj + 1 < ti) between += hs.tile[ti - 1];
-          if (tj + 2 < ti) between += hs.tile[ti - 2];
-          const float* src = tj < ti ? hs.past : hs.same;
-          const f32x4 b0 = *reinterpret_cast<const f32x4*>(src + j0), b1 = *reinterpret_cast<const f32x4*>(src + j0 + 4);
-          const float* row = cbm + (16 * ti + c) * L::kCbPitch + j0;
-          const f32x4 s0 = *reinterpret_cast<const f32x4*>(row), s1 = *reinterpret_cast<const f32x4*>(row + 4);
-          const float e = li + between;
-          float v[8];
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const float p = (j < 4 ? s0[j & 3] : s1[j & 3]) * __builtin_amdgcn_exp2f(e + (j < 4 ? b0[j & 3] : b1[j & 3]));
-            v[j] = j0 + j <= 16 * ti + c ? p : 0.0f;
-          }
-          const typename X::F2 pf = X::f2(v);
+          const typename X::F2 pf = X::get(pt + (ti < 2 ? ti : 2 * ti - 2 + kk) * X::kF2Bytes, lane);
 #pragma unroll
           for (int ct = 0; ct < CT; ++ct) yt[ti][ct] = X::rf(xf[kk][ct], pf, yt[ti][ct]);
         }
-      }
       // + d_skip x, and out
-      T* yb = static_cast<T*>(a.y) + (t0 + at) * a.ldy + static_cast<int64_t>(head) * DV + p0;
+      const __amdgpu_buffer_rsrc_t ry = rows_buffer(static_cast<T*>(a.y) + (t0 + at) * a.ldy + static_cast<int64_t>(head) * DV + p0,
+                                                    (rows - 1) * ldy + L::kCols * E);
+      uint32_t vy = c * ldy + 8 * g * E;
+      asm volatile("" : "+v"(vy));
 #pragma unroll
-      for (int ti = 0; ti < 4; ++ti) {
-        const int i = 16 * ti + c;
+      for (int ti = 0; ti < 4; ++ti)
 #pragma unroll
         for (int b = 0; b < CT / 2; ++b) {
-          const R xr = XRows::row_frag(xt, i, (p0 + 32 * b) / 8 + g);
+          const R xr = XRows::row_frag(xt, 16 * ti, c, (p0 + 32 * b) / 8 + g);
           float o[8];
 #pragma unroll
           for (int j = 0; j < 8; ++j) o[j] = fmaf(skip, X::elt(xr, j), yt[ti][2 * b + j / 4][j & 3]);
-          if (i < rows) store8(yb + i * a.ldy + 32 * b + 8 * g, o);
+          buffer_store8(ry, vy + 16 * ti * ldy + 32 * b * E, o, static_cast<T*>(nullptr));
         }
-      }
     }
 
     // M <- e^{G_last} M + B^T (diag(suf) x)
@@ -455,7 +551,7 @@ void k_ssm_scan(SsmScanArgs a) {
         for (int ct = 0; ct < CT; ++ct) m[td][ct] = X::rf3(bt, wx[ct], m[td][ct]);
       }
     }
-    __syncthreads();   // the chunk's LDS has been read
+    lds_barrier();   // the chunk's LDS has been read
   }
 
   if constexpr (MODE == SsmMode::kLocal) {
