@@ -11,6 +11,8 @@
 // workgroup, which are of one B/C group, share the B and C rows.
 #pragma once
 
+#include <type_traits>
+
 #include "gdn_varlen.h"
 
 namespace gdn {
@@ -27,30 +29,40 @@ constexpr int kSsmChunk = 64;
 template <typename T>
 struct Mx;
 
+// x rounded to a bf16 pair, and what the rounding left of it: exact, one
+// instruction per value (a dot product of the pair with (-1, 0) or (0, -1) added
+// to the value; the multiplier stays out of the instruction's inline constants,
+// whose packed form the compiler takes in the wrong half).
+__device__ __forceinline__ uint32_t round_pair(f32x2& x) {
+  uint32_t first, second;
+  asm("s_mov_b32 %0, 0xbf80" : "=s"(first));
+  asm("s_mov_b32 %0, 0xbf800000" : "=s"(second));
+  const bf16x2 h = __builtin_convertvector(x, bf16x2);
+  x[0] = __builtin_amdgcn_fdot2_f32_bf16(h, __builtin_bit_cast(bf16x2, first), x[0], false);
+  x[1] = __builtin_amdgcn_fdot2_f32_bf16(h, __builtin_bit_cast(bf16x2, second), x[1], false);
+  return __builtin_bit_cast(uint32_t, h);
+}
+__device__ __forceinline__ uint32_t last_pair(const f32x2& x) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
+}
+
 template <>
 struct Mx<uint16_t> {
   typedef bf16x8 R;
-  typedef Frag F2;
-  struct F3 { bf16x8 hi, mid, lo; };
-  static __device__ __forceinline__ F2 f2(const float (&v)[8]) { return split8(v); }
-  static __device__ __forceinline__ F3 f3(const float (&v)[8]) {
-    F3 f;
-    u32x4 hi, mid, lo;
+  struct F2 { R part[2]; };
+  struct F3 { R part[3]; };
+  template <int N>
+  static __device__ __forceinline__ void split(const float (&v)[8], R (&part)[N]) {
+    u32x4 w[N];
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
-      const f32x2 x = {v[2 * p], v[2 * p + 1]};
-      const uint32_t h = __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
-      const f32x2 d = {x[0] - __uint_as_float(h << 16), x[1] - __uint_as_float(h & 0xFFFF0000u)};
-      const uint32_t m = __builtin_bit_cast(uint32_t, __builtin_convertvector(d, bf16x2));
-      const f32x2 e = {d[0] - __uint_as_float(m << 16), d[1] - __uint_as_float(m & 0xFFFF0000u)};
-      hi[p] = h;
-      mid[p] = m;
-      lo[p] = __builtin_bit_cast(uint32_t, __builtin_convertvector(e, bf16x2));
+      f32x2 x = {v[2 * p], v[2 * p + 1]};
+#pragma unroll
+      for (int k = 0; k < N - 1; ++k) w[k][p] = round_pair(x);
+      w[N - 1][p] = last_pair(x);
     }
-    f.hi = __builtin_bit_cast(bf16x8, hi);
-    f.mid = __builtin_bit_cast(bf16x8, mid);
-    f.lo = __builtin_bit_cast(bf16x8, lo);
-    return f;
+#pragma unroll
+    for (int k = 0; k < N; ++k) part[k] = __builtin_bit_cast(R, w[k]);
   }
   // an F2 operand in LDS: 64 lanes x 16 bytes of high parts, then of low parts
   static constexpr int kF2Bytes = 2048;
@@ -58,61 +70,53 @@ struct Mx<uint16_t> {
     u32x2 hi, lo;
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
-      const f32x2 x = {v[2 * p], v[2 * p + 1]};
-      const uint32_t h = __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
-      const f32x2 d = {x[0] - __uint_as_float(h << 16), x[1] - __uint_as_float(h & 0xFFFF0000u)};
-      hi[p] = h;
-      lo[p] = __builtin_bit_cast(uint32_t, __builtin_convertvector(d, bf16x2));
+      f32x2 x = {v[2 * p], v[2 * p + 1]};
+      hi[p] = round_pair(x);
+      lo[p] = last_pair(x);
     }
     *reinterpret_cast<u32x2*>(frag + 16 * slot + 8 * half) = hi;
     *reinterpret_cast<u32x2*>(frag + 1024 + 16 * slot + 8 * half) = lo;
   }
   static __device__ __forceinline__ F2 get(const char* frag, int lane) {
     F2 f;
-    f.hi = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(frag + 16 * lane));
-    f.lo = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(frag + 1024 + 16 * lane));
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+      f.part[k] = __builtin_bit_cast(R, *reinterpret_cast<const u32x4*>(frag + 1024 * k + 16 * lane));
     return f;
   }
   static __device__ __forceinline__ float elt(const R& r, int j) {
     const u32x4 w = __builtin_bit_cast(u32x4, r);
     return __uint_as_float((j & 1) ? (w[j / 2] & 0xFFFF0000u) : (w[j / 2] << 16));
   }
-  static __device__ __forceinline__ f32x4 rr(const R& a, const R& b, f32x4 c) { return mma(a, b, c); }
-  static __device__ __forceinline__ f32x4 fr(const F2& a, const R& b, f32x4 c) { return mma(a.lo, b, mma(a.hi, b, c)); }
-  static __device__ __forceinline__ f32x4 rf(const R& a, const F2& b, f32x4 c) { return mma(a, b.lo, mma(a, b.hi, c)); }
-  static __device__ __forceinline__ f32x4 rf3(const R& a, const F3& b, f32x4 c) {
-    return mma(a, b.lo, mma(a, b.mid, mma(a, b.hi, c)));
-  }
+  static __device__ __forceinline__ f32x4 mul(const R& a, const R& b, f32x4 c) { return mma(a, b, c); }
 };
 
 template <>
 struct Mx<float> {
   typedef f32x8 R;
-  typedef f32x8 F2;
-  typedef f32x8 F3;
-  static __device__ __forceinline__ f32x8 f2(const float (&v)[8]) {
-    return f32x8{v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]};
+  struct F2 { R part[1]; };
+  struct F3 { R part[1]; };
+  static __device__ __forceinline__ void split(const float (&v)[8], R (&part)[1]) {
+    part[0] = R{v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]};
   }
-  static __device__ __forceinline__ f32x8 f3(const float (&v)[8]) { return f2(v); }
   static constexpr int kF2Bytes = 2048;   // 64 lanes x 32 bytes
   static __device__ __forceinline__ void put4(char* frag, int slot, int half, const float (&v)[4]) {
     *reinterpret_cast<f32x4*>(frag + 32 * slot + 16 * half) = f32x4{v[0], v[1], v[2], v[3]};
   }
-  static __device__ __forceinline__ f32x8 get(const char* frag, int lane) {
+  static __device__ __forceinline__ F2 get(const char* frag, int lane) {
     const f32x4 a = *reinterpret_cast<const f32x4*>(frag + 32 * lane);
     const f32x4 b = *reinterpret_cast<const f32x4*>(frag + 32 * lane + 16);
-    return f32x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+    return {{R{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}}};
   }
   static __device__ __forceinline__ float elt(const R& r, int j) { return r[j]; }
-  static __device__ __forceinline__ f32x4 rr(const R& a, const R& b, f32x4 c) {
+  static __device__ __forceinline__ f32x4 mul(const R& a, const R& b, f32x4 c) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[j], b[j], c, 0, 0, 0);
     return c;
   }
-  static __device__ __forceinline__ f32x4 fr(const F2& a, const R& b, f32x4 c) { return rr(a, b, c); }
-  static __device__ __forceinline__ f32x4 rf(const R& a, const F2& b, f32x4 c) { return rr(a, b, c); }
-  static __device__ __forceinline__ f32x4 rf3(const R& a, const F3& b, f32x4 c) { return rr(a, b, c); }
 };
+template <typename F>
+constexpr int parts_of() { return sizeof(F::part) / sizeof(typename std::remove_extent<decltype(F::part)>::type); }
 
 // ---------------------------------------------------------------- token rows in LDS
 // 64 rows of D elements.  bf16: 16-byte pieces swizzled as key rows are
@@ -270,7 +274,7 @@ struct SsmLayout {
 __device__ __forceinline__ int ssm_col(int ct, int c) { return 32 * (ct >> 1) + 8 * (c / 4) + 4 * (ct & 1) + c % 4; }
 
 template <typename T, int DK, int DV, int CT, int NW, SsmMode MODE, bool OUT>
-__global__ __launch_bounds__(NW * kWave, 2)
+__global__ __launch_bounds__(NW * kWave, sizeof(T) == 2 ? 2 : 1)
 void k_ssm_scan(SsmScanArgs a) {
   typedef SsmLayout<T, DK, DV, CT, NW, OUT> L;
   typedef typename L::KRows KRows;
@@ -416,60 +420,87 @@ void k_ssm_scan(SsmScanArgs a) {
       if (lane == 0) o.total = __builtin_amdgcn_exp2f(sum);
     }
     lds_barrier();
-    if (at + kSsmChunk < len) fetch(at + kSsmChunk);
     const HeadScalars& hs = sc[hl];
     const char* xt = lds + L::kOffX + hl * XRows::kBytes;
     char* pt = lds + L::kOffP + hl * L::kPBytes;
 
+    constexpr int KK = DK / 32;
+    constexpr int N2 = parts_of<typename X::F2>(), N3 = parts_of<typename X::F3>();
+    R xf[2][CT];
+    const auto load_x = [&] {   // tokens 32 kk + 8 g + j of column ct
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) xf[kk][ct] = XRows::col_frag(xt, 32 * kk, p0 + 32 * (ct >> 1), ct & 1, g, c);
+    };
+
+    // Operands are read one step ahead of the products that take them: the
+    // scheduling barriers keep the reads in front (left to itself the compiler
+    // waits for every read right after it).
     if constexpr (OUT) {
+      R cf[2][4];
+      const auto load_c = [&](int kk) {
+#pragma unroll
+        for (int ti = 0; ti < 4; ++ti) cf[kk & 1][ti] = KRows::row_frag(lds + L::kOffC, 16 * ti, c, 4 * kk + g);
+      };
       // P^T = (C B^T o L o delta)^T by 16 x 16 tiles of the lower triangle, shared
       // by the head's waves: a lane's accumulator is four columns j of row i, which
       // are half of one lane's operand for x^T P^T
+      constexpr int PT = (10 + L::kWavesPerHead - 1) / L::kWavesPerHead;
+      R tb[2][KK], tc[2][KK];
+      f32x4 pe[2];
+      int first_tile = wave % L::kWavesPerHead;
+      asm volatile("" : "+s"(first_tile));   // tile addresses are made here, not kept in registers over the chunks
+      const auto tile_of = [&](int k, int& ti, int& tj) {
+        const int t = min(first_tile + k * L::kWavesPerHead, 9);
+        ti = t < 1 ? 0 : t < 3 ? 1 : t < 6 ? 2 : 3;
+        tj = t - ti * (ti + 1) / 2;
+      };
+      const auto load_tile = [&](int k) {
+        int ti, tj;
+        tile_of(k, ti, tj);
 #pragma unroll
-      for (int k = 0; k < (10 + L::kWavesPerHead - 1) / L::kWavesPerHead; ++k) {
-        const int t = wave % L::kWavesPerHead + k * L::kWavesPerHead;
-        if (t >= 10) break;
-        const int ti = t < 1 ? 0 : t < 3 ? 1 : t < 6 ? 2 : 3, tj = t - ti * (ti + 1) / 2;
-        f32x4 acc = zero4();
-#pragma unroll
-        for (int kk = 0; kk < DK / 32; ++kk)
-          acc = X::rr(KRows::row_frag(lds + L::kOffB, 16 * tj, c, 4 * kk + g),
-                      KRows::row_frag(lds + L::kOffC, 16 * ti, c, 4 * kk + g), acc);
+        for (int kk = 0; kk < KK; ++kk) {
+          tb[k & 1][kk] = KRows::row_frag(lds + L::kOffB, 16 * tj, c, 4 * kk + g);
+          tc[k & 1][kk] = KRows::row_frag(lds + L::kOffC, 16 * ti, c, 4 * kk + g);
+        }
         float e = hs.l[16 * ti + c];
         if (tj + 1 < ti) e += hs.tile[ti - 1];
         if (tj + 2 < ti) e += hs.tile[ti - 2];
-        const f32x4 b = *reinterpret_cast<const f32x4*>((tj < ti ? hs.past : hs.same) + 16 * tj + 4 * g);
+        pe[k & 1] = *reinterpret_cast<const f32x4*>((tj < ti ? hs.past : hs.same) + 16 * tj + 4 * g);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) pe[k & 1][r] += e;
+      };
+      load_tile(0);
+#pragma unroll
+      for (int k = 0; k < PT; ++k) {
+        if (k + 1 < PT) load_tile(k + 1);
+        else load_c(0);
+        __builtin_amdgcn_sched_barrier(0);
+        int ti, tj;
+        tile_of(k, ti, tj);
+        f32x4 acc = zero4();
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) acc = X::mul(tb[k & 1][kk], tc[k & 1][kk], acc);
         float v[4];
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const float p = acc[r] * __builtin_amdgcn_exp2f(e + b[r]);
-          v[r] = tj < ti || 4 * g + r <= c ? p : 0.0f;
+          const float p = acc[r] * __builtin_amdgcn_exp2f(pe[k & 1][r]);
+          v[r] = tj < ti || 4 * g + r < c ? p : 4 * g + r == c ? p + skip : 0.0f;   // d_skip x rides on the diagonal
         }
-        X::put4(pt + (ti < 2 ? ti : ti == 2 ? 2 + tj / 2 : 4 + tj / 2) * X::kF2Bytes, 16 * (2 * (tj & 1) + g / 2) + c,
-                g & 1, v);
+        if (10 % L::kWavesPerHead == 0 || first_tile + k * L::kWavesPerHead < 10)
+          X::put4(pt + (ti < 2 ? ti : ti == 2 ? 2 + tj / 2 : 4 + tj / 2) * X::kF2Bytes,
+                  16 * (2 * (tj & 1) + g / 2) + c, g & 1, v);
       }
-    }
 
-    R xf[2][CT];
-    const auto load_x = [&] {
-      // x as an operand: tokens 32 kk + 8 g + j of column ct
-  #pragma unroll
-      for (int kk = 0; kk < 2; ++kk)
-  #pragma unroll
-        for (int ct = 0; ct < CT; ++ct) xf[kk][ct] = XRows::col_frag(xt, 32 * kk, p0 + 32 * (ct >> 1), ct & 1, g, c);
-    };
-    if constexpr (!OUT) load_x();
-
-    if constexpr (OUT) {
       // y^T tiles: rows are state columns, columns are tokens
       f32x4 yt[4][CT];
 #pragma unroll
       for (int ti = 0; ti < 4; ++ti)
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) yt[ti][ct] = zero4();
-#pragma unroll
-      for (int kk = 0; kk < DK / 32; ++kk) {
-        typename X::F2 mf[CT];
+      typename X::F2 mf[2][CT];
+      const auto split_m = [&](int kk) {
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
           float v[8];
@@ -478,15 +509,23 @@ void k_ssm_scan(SsmScanArgs a) {
             v[j] = m[2 * kk][ct][j];
             v[4 + j] = m[2 * kk + 1][ct][j];
           }
-          mf[ct] = X::f2(v);
+          X::split(v, mf[kk & 1][ct].part);
         }
+      };
+      split_m(0);
 #pragma unroll
-        for (int ti = 0; ti < 4; ++ti) {
-          const R cf = KRows::row_frag(lds + L::kOffC, 16 * ti, c, 4 * kk + g);
+      for (int kk = 0; kk < KK; ++kk) {
+        if (kk + 1 < KK) load_c(kk + 1);
+        else load_x();
+        __builtin_amdgcn_sched_barrier(0);
+        if (kk + 1 < KK) split_m(kk + 1);   // beside the products
 #pragma unroll
-          for (int ct = 0; ct < CT; ++ct) yt[ti][ct] = X::fr(mf[ct], cf, yt[ti][ct]);
-        }
-        __builtin_amdgcn_sched_barrier(0);   // keeps the next step's operands out of registers
+        for (int k = 0; k < N2; ++k)
+#pragma unroll
+          for (int ti = 0; ti < 4; ++ti)
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) yt[ti][ct] = X::mul(mf[kk & 1][ct].part[k], cf[kk & 1][ti], yt[ti][ct]);
+        __builtin_amdgcn_sched_barrier(0);
       }
 #pragma unroll
       for (int ti = 0; ti < 4; ++ti) {
@@ -496,18 +535,24 @@ void k_ssm_scan(SsmScanArgs a) {
 #pragma unroll
           for (int i = 0; i < 4; ++i) yt[ti][ct][i] *= e;
       }
-      load_x();
       lds_barrier();   // P is whole
       // + x^T P^T
+      typename X::F2 pf[L::kPFrags];
 #pragma unroll
-      for (int ti = 0; ti < 4; ++ti)
+      for (int f = 0; f < L::kPFrags; ++f) pf[f] = X::get(pt + f * X::kF2Bytes, lane);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int kk = 0; kk <= ti / 2; ++kk) {
-          const typename X::F2 pf = X::get(pt + (ti < 2 ? ti : 2 * ti - 2 + kk) * X::kF2Bytes, lane);
+      for (int k = 0; k < N2; ++k)
 #pragma unroll
-          for (int ct = 0; ct < CT; ++ct) yt[ti][ct] = X::rf(xf[kk][ct], pf, yt[ti][ct]);
-        }
-      // + d_skip x, and out
+        for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+          for (int ti = 2 * kk; ti < 4; ++ti)
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct)
+              yt[ti][ct] = X::mul(xf[kk][ct], pf[ti < 2 ? ti : 2 * ti - 2 + kk].part[k], yt[ti][ct]);
+      // the next chunk's rows are on their way from here on (not earlier: the
+      // operands above need the registers)
+      if (at + kSsmChunk < len) fetch(at + kSsmChunk);
       const __amdgpu_buffer_rsrc_t ry = rows_buffer(static_cast<T*>(a.y) + (t0 + at) * a.ldy + static_cast<int64_t>(head) * DV + p0,
                                                     (rows - 1) * ldy + L::kCols * E);
       uint32_t vy = c * ldy + 8 * g * E;
@@ -516,16 +561,42 @@ void k_ssm_scan(SsmScanArgs a) {
       for (int ti = 0; ti < 4; ++ti)
 #pragma unroll
         for (int b = 0; b < CT / 2; ++b) {
-          const R xr = XRows::row_frag(xt, 16 * ti, c, (p0 + 32 * b) / 8 + g);
           float o[8];
 #pragma unroll
-          for (int j = 0; j < 8; ++j) o[j] = fmaf(skip, X::elt(xr, j), yt[ti][2 * b + j / 4][j & 3]);
+          for (int j = 0; j < 8; ++j) o[j] = yt[ti][2 * b + j / 4][j & 3];
           buffer_store8(ry, vy + 16 * ti * ldy + 32 * b * E, o, static_cast<T*>(nullptr));
         }
+    } else {
+      if (at + kSsmChunk < len) fetch(at + kSsmChunk);
+      load_x();
     }
 
     // M <- e^{G_last} M + B^T (diag(suf) x)
+    constexpr int TS = DK / 32;   // state row tiles of a step, two steps for each kk
+    R bt[2][TS];
+    typename X::F3 wx[CT];
+    const auto load_b = [&](int step) {
+#pragma unroll
+      for (int t = 0; t < TS; ++t) {
+        const int td = step % 2 * TS + t;
+        bt[step & 1][t] = KRows::col_frag(lds + L::kOffB, 32 * (step / 2), 32 * (td >> 1), td & 1, g, c);
+      }
+    };
+    const auto weigh_x = [&](int kk) {
+      const f32x4 w0 = *reinterpret_cast<const f32x4*>(hs.suf + 32 * kk + 8 * g);
+      const f32x4 w1 = *reinterpret_cast<const f32x4*>(hs.suf + 32 * kk + 8 * g + 4);
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) {
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = (j < 4 ? w0[j & 3] : w1[j & 3]) * X::elt(xf[kk][ct], j);
+        X::split(v, wx[ct].part);
+      }
+    };
     const float total = hs.total;
+    load_b(0);
+    __builtin_amdgcn_sched_barrier(0);
+    weigh_x(0);
 #pragma unroll
     for (int td = 0; td < DK / 16; ++td)
 #pragma unroll
@@ -533,23 +604,20 @@ void k_ssm_scan(SsmScanArgs a) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) m[td][ct][i] *= total;
 #pragma unroll
-    for (int kk = 0; kk < 2; ++kk) {
-      const f32x4 w0 = *reinterpret_cast<const f32x4*>(hs.suf + 32 * kk + 8 * g);
-      const f32x4 w1 = *reinterpret_cast<const f32x4*>(hs.suf + 32 * kk + 8 * g + 4);
-      typename X::F3 wx[CT];
+    for (int step = 0; step < 4; ++step) {
+      if (step < 3) load_b(step + 1);
+      __builtin_amdgcn_sched_barrier(0);
+      if (step == 2) weigh_x(1);
 #pragma unroll
-      for (int ct = 0; ct < CT; ++ct) {
-        float v[8];
+      for (int k = 0; k < N3; ++k)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = (j < 4 ? w0[j & 3] : w1[j & 3]) * X::elt(xf[kk][ct], j);
-        wx[ct] = X::f3(v);
-      }
+        for (int t = 0; t < TS; ++t)
 #pragma unroll
-      for (int td = 0; td < DK / 16; ++td) {
-        const R bt = KRows::col_frag(lds + L::kOffB, 32 * kk, 32 * (td >> 1), td & 1, g, c);
-#pragma unroll
-        for (int ct = 0; ct < CT; ++ct) m[td][ct] = X::rf3(bt, wx[ct], m[td][ct]);
-      }
+          for (int ct = 0; ct < CT; ++ct) {
+            f32x4& acc = m[step % 2 * TS + t][ct];
+            acc = X::mul(bt[step & 1][t], wx[ct].part[k], acc);
+          }
+      __builtin_amdgcn_sched_barrier(0);
     }
     lds_barrier();   // the chunk's LDS has been read
   }

@@ -40,8 +40,14 @@ __device__ __forceinline__ void store_run(T* __restrict__ p, const float (&x)[N]
   }
 }
 
-// log(1 + e^x); from 20 on x itself is within 2e-9 of it
-__device__ __forceinline__ float softplus_f(float x) { return x > 20.0f ? x : log1pf(expf(x)); }
+// log(1 + e^x) = max(x, 0) + log(1 + e), e = e^-|x| <= 1.  With u the rounded
+// 1 + e, log(1 + e) = log(u) e / (u - 1) to within the logarithm's own rounding.
+__device__ __forceinline__ float softplus_f(float x) {
+  const float e = __builtin_amdgcn_exp2f(-1.44269504088896f * fabsf(x));
+  const float u = 1.0f + e, d = u - 1.0f;
+  const float l = __builtin_amdgcn_logf(u) * 0.693147180559945f;   // v_log_f32 is base 2
+  return fmaxf(x, 0.0f) + (d == 0.0f ? e : l * (e * __builtin_amdgcn_rcpf(d)));
+}
 
 // dt is fp32 or has the element type
 __device__ __forceinline__ float load_dt(const void* __restrict__ dt, bool bf16, int64_t i) {
