@@ -14,7 +14,7 @@ constexpr int64_t kMaxGrid = std::numeric_limits<int32_t>::max();
 constexpr int64_t kMaxStride = int64_t{1} << 23;
 
 // Segments of the state space scan
-constexpr int64_t kSsmPlaces = 512;       // workgroups that the chip holds at once
+constexpr int64_t kSsmPlaces = 256;       // workgroups that the chip holds at once
 constexpr int64_t kSsmSplitChunks = 8;    // the longest sequence from which it pays
 constexpr int64_t kSsmSegChunks = 4;      // the shortest segment
 

@@ -13,7 +13,7 @@ namespace gdn {
 
 // State columns of a workgroup of the state space scan, where a B/C group has
 // that many heads to share them (bf16, fp32); one head's otherwise.
-constexpr int32_t kSsmCols = 128, kSsmColsF32 = 128;
+constexpr int32_t kSsmCols = 256, kSsmColsF32 = 128;
 
 // Packed sequences cut into tiles of `tile` tokens, each sequence from its own
 // start: tile j of sequence n is slot cu[n] / tile + n + j.  The map is

@@ -191,19 +191,21 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_buffer(const void* base, 
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, bytes, 0x00020000);
 }
 
-// Per head and chunk, base-2 logarithms: with l the inclusive cumulative log
-// alpha inside a token's 16-token tile and s what is left of the tile after it,
-// e^{G_i - G_j} = 2^(l_i - l_j) within a tile and 2^(l_i + between + s_j) across
-// tiles: sums of terms of one sign, never the difference of two long ones.
+// Per head and chunk, in base 2: with l the inclusive cumulative log alpha inside
+// a token's 16-token tile and s what is left of the tile after it, e^{G_i - G_j}
+// = 2^(l_i - l_j) within a tile and 2^l_i 2^between 2^s_j across tiles, three
+// factors of at most one: exponents are sums of terms of one sign, never the
+// difference of two long ones, and no factor overflows.
 struct HeadScalars {
   float l[kSsmChunk];      // l
   float same[kSsmChunk];   // log2 delta - l
-  float past[kSsmChunk];   // log2 delta + s
+  float row[kSsmChunk];    // 2^l
+  float past[kSsmChunk];   // 2^s delta
   float pre[kSsmChunk];    // e^G
   float suf[kSsmChunk];    // e^{G_last - G} delta
-  float tile[4];           // log2 alpha summed over each tile
+  float between[10];       // 2^(log2 alpha summed over the tiles between those of tile pair t), see tile_rows
   float total;             // e^{G_last}
-  float pad[3];
+  float pad[5];
 };
 
 // Lane exchanges inside a DPP row of 16 lanes; a lane without a source gets 0.
@@ -245,7 +247,7 @@ struct SsmScanArgs {
 
 // kWhole: a unit is a sequence, from state_in to y (where given) and state_out.
 // kLocal: a unit is a segment from the zero state to seg_state and seg_decay.
-// kJoined: a unit is a segment from seg_state to y and, the last one, state_out.
+// kJoined: a unit is a segment from seg_state to y.
 enum class SsmMode { kWhole, kLocal, kJoined };
 
 template <typename T, int DK, int DV, int CT, int NW, bool OUT>
@@ -263,7 +265,8 @@ struct SsmLayout {
   static constexpr int kOffC = kOffB + KRows::kBytes;
   static constexpr int kOffX = kOffC + (OUT ? KRows::kBytes : 0);
   static constexpr int kOffP = kOffX + kHeads * XRows::kBytes;
-  static constexpr int kOffS = kOffP + (OUT ? kHeads * kPBytes : 0);
+  static constexpr int kOffCb = kOffP + (OUT ? kHeads * kPBytes : 0);   // C B^T: 10 tiles, 16 bytes a lane
+  static constexpr int kOffS = kOffCb + (OUT ? 10 * 1024 : 0);
   static constexpr int kBytes = kOffS + kHeads * static_cast<int>(sizeof(HeadScalars));
   static_assert(NW % kWavesPerHead == 0 && kHeads <= NW, "whole heads");
   static_assert(kSsmChunk * KRows::kPieces % kThreads == 0 && kSsmChunk * XRows::kPieces * kHeads % kThreads == 0,
@@ -302,8 +305,6 @@ void k_ssm_scan(SsmScanArgs a) {
     first = static_cast<int>(at);
   }
   const int len = MODE == SsmMode::kWhole ? seq_len : min(a.seg_tokens, seq_len - first);
-  const bool last = first + len >= seq_len;
-  if (MODE == SsmMode::kLocal && OUT == false && last && a.y) return;   // the joined pass ends there by itself
   const int64_t t0 = static_cast<int64_t>(start) + first;
   const int h0 = hg * L::kHeads, gh = h0 / (a.heads / a.groups);
   const int hl = wave / L::kWavesPerHead, head = h0 + hl;
@@ -410,9 +411,10 @@ void k_ssm_scan(SsmScanArgs a) {
         const float ld = __log2f(delta);
         o.l[lane] = l;
         o.same[lane] = ld - l;
-        o.past[lane] = ld + s;
+        o.row[lane] = __builtin_amdgcn_exp2f(l);
+        o.past[lane] = __builtin_amdgcn_exp2f(s) * delta;
         o.pre[lane] = __builtin_amdgcn_exp2f(before + l);
-        if (c == 15) o.tile[g] = l;
+        if (lane < 10) o.between[lane] = __builtin_amdgcn_exp2f(lane == 3 ? q1 : lane == 6 ? q1 + q2 : lane == 7 ? q2 : 0.0f);
       }
       o.suf[lane] = __builtin_amdgcn_exp2f(s + after) * delta;
       const float sum = (q0 + q1) + (q2 + q3);
@@ -425,7 +427,10 @@ void k_ssm_scan(SsmScanArgs a) {
     char* pt = lds + L::kOffP + hl * L::kPBytes;
 
     constexpr int KK = DK / 32;
-    constexpr int N2 = parts_of<typename X::F2>(), N3 = parts_of<typename X::F3>();
+    constexpr int N2 = parts_of<typename X::F2>();
+    // the state that kJoined carries ends in outputs alone (the join has written the final one)
+    typedef typename std::conditional<MODE == SsmMode::kJoined, typename X::F2, typename X::F3>::type FS;
+    constexpr int NS = parts_of<FS>();
     R xf[2][CT];
     const auto load_x = [&] {   // tokens 32 kk + 8 g + j of column ct
 #pragma unroll
@@ -437,64 +442,40 @@ void k_ssm_scan(SsmScanArgs a) {
     // Operands are read one step ahead of the products that take them: the
     // scheduling barriers keep the reads in front (left to itself the compiler
     // waits for every read right after it).
+    const auto tile_rows = [](int t, int& ti, int& tj) {   // tile t of the lower triangle
+      ti = t < 1 ? 0 : t < 3 ? 1 : t < 6 ? 2 : 3;
+      tj = t - ti * (ti + 1) / 2;
+    };
+    f32x4 yt[4][OUT ? CT : 1];   // y^T tiles: rows are state columns, columns are tokens
     if constexpr (OUT) {
+      // C B^T by 16 x 16 tiles of the lower triangle, one after another over the
+      // workgroup's waves: a lane's accumulator is four columns j of row i
+      int first = wave;
+      asm volatile("" : "+s"(first));   // tile addresses are made here, not kept in registers over the chunks
+      constexpr int CB = (10 + NW - 1) / NW;
+#pragma unroll
+      for (int k = 0; k < CB; ++k) {
+        const int t = first + k * NW;
+        if (10 % NW != 0 && t >= 10) break;
+        int ti, tj;
+        tile_rows(t, ti, tj);
+        R tb[KK], tc[KK];
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) {
+          tb[kk] = KRows::row_frag(lds + L::kOffB, 16 * tj, c, 4 * kk + g);
+          tc[kk] = KRows::row_frag(lds + L::kOffC, 16 * ti, c, 4 * kk + g);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        f32x4 acc = zero4();
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) acc = X::mul(tb[kk], tc[kk], acc);
+        *reinterpret_cast<f32x4*>(lds + L::kOffCb + 1024 * t + 16 * lane) = acc;
+      }
       R cf[2][4];
       const auto load_c = [&](int kk) {
 #pragma unroll
         for (int ti = 0; ti < 4; ++ti) cf[kk & 1][ti] = KRows::row_frag(lds + L::kOffC, 16 * ti, c, 4 * kk + g);
       };
-      // P^T = (C B^T o L o delta)^T by 16 x 16 tiles of the lower triangle, shared
-      // by the head's waves: a lane's accumulator is four columns j of row i, which
-      // are half of one lane's operand for x^T P^T
-      constexpr int PT = (10 + L::kWavesPerHead - 1) / L::kWavesPerHead;
-      R tb[2][KK], tc[2][KK];
-      f32x4 pe[2];
-      int first_tile = wave % L::kWavesPerHead;
-      asm volatile("" : "+s"(first_tile));   // tile addresses are made here, not kept in registers over the chunks
-      const auto tile_of = [&](int k, int& ti, int& tj) {
-        const int t = min(first_tile + k * L::kWavesPerHead, 9);
-        ti = t < 1 ? 0 : t < 3 ? 1 : t < 6 ? 2 : 3;
-        tj = t - ti * (ti + 1) / 2;
-      };
-      const auto load_tile = [&](int k) {
-        int ti, tj;
-        tile_of(k, ti, tj);
-#pragma unroll
-        for (int kk = 0; kk < KK; ++kk) {
-          tb[k & 1][kk] = KRows::row_frag(lds + L::kOffB, 16 * tj, c, 4 * kk + g);
-          tc[k & 1][kk] = KRows::row_frag(lds + L::kOffC, 16 * ti, c, 4 * kk + g);
-        }
-        float e = hs.l[16 * ti + c];
-        if (tj + 1 < ti) e += hs.tile[ti - 1];
-        if (tj + 2 < ti) e += hs.tile[ti - 2];
-        pe[k & 1] = *reinterpret_cast<const f32x4*>((tj < ti ? hs.past : hs.same) + 16 * tj + 4 * g);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) pe[k & 1][r] += e;
-      };
-      load_tile(0);
-#pragma unroll
-      for (int k = 0; k < PT; ++k) {
-        if (k + 1 < PT) load_tile(k + 1);
-        else load_c(0);
-        __builtin_amdgcn_sched_barrier(0);
-        int ti, tj;
-        tile_of(k, ti, tj);
-        f32x4 acc = zero4();
-#pragma unroll
-        for (int kk = 0; kk < KK; ++kk) acc = X::mul(tb[k & 1][kk], tc[k & 1][kk], acc);
-        float v[4];
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const float p = acc[r] * __builtin_amdgcn_exp2f(pe[k & 1][r]);
-          v[r] = tj < ti || 4 * g + r < c ? p : 4 * g + r == c ? p + skip : 0.0f;   // d_skip x rides on the diagonal
-        }
-        if (10 % L::kWavesPerHead == 0 || first_tile + k * L::kWavesPerHead < 10)
-          X::put4(pt + (ti < 2 ? ti : ti == 2 ? 2 + tj / 2 : 4 + tj / 2) * X::kF2Bytes,
-                  16 * (2 * (tj & 1) + g / 2) + c, g & 1, v);
-      }
-
-      // y^T tiles: rows are state columns, columns are tokens
-      f32x4 yt[4][CT];
 #pragma unroll
       for (int ti = 0; ti < 4; ++ti)
 #pragma unroll
@@ -512,6 +493,7 @@ void k_ssm_scan(SsmScanArgs a) {
           X::split(v, mf[kk & 1][ct].part);
         }
       };
+      load_c(0);
       split_m(0);
 #pragma unroll
       for (int kk = 0; kk < KK; ++kk) {
@@ -535,52 +517,51 @@ void k_ssm_scan(SsmScanArgs a) {
 #pragma unroll
           for (int i = 0; i < 4; ++i) yt[ti][ct][i] *= e;
       }
-      lds_barrier();   // P is whole
-      // + x^T P^T
-      typename X::F2 pf[L::kPFrags];
+      lds_barrier();   // C B^T is whole
+      // P^T = (C B^T o L o delta)^T, the head's tiles shared by its waves: the four
+      // values of a lane are half of one lane's operand for x^T P^T
+      int own = wave % L::kWavesPerHead;
+      asm volatile("" : "+s"(own));
 #pragma unroll
-      for (int f = 0; f < L::kPFrags; ++f) pf[f] = X::get(pt + f * X::kF2Bytes, lane);
-      __builtin_amdgcn_sched_barrier(0);
+      for (int k = 0; k < (10 + L::kWavesPerHead - 1) / L::kWavesPerHead; ++k) {
+        const int t = own + k * L::kWavesPerHead;
+        if (10 % L::kWavesPerHead != 0 && t >= 10) break;
+        int ti, tj;
+        tile_rows(t, ti, tj);
+        const f32x4 cbt = *reinterpret_cast<const f32x4*>(lds + L::kOffCb + 1024 * t + 16 * lane);
+        float v[4];
+        if (tj < ti) {   // uniform
+          const f32x4 pj = *reinterpret_cast<const f32x4*>(hs.past + 16 * tj + 4 * g);
+          const float e = hs.row[16 * ti + c] * hs.between[t];
 #pragma unroll
-      for (int k = 0; k < N2; ++k)
+          for (int r = 0; r < 4; ++r) v[r] = cbt[r] * (e * pj[r]);
+        } else {
+          const f32x4 pj = *reinterpret_cast<const f32x4*>(hs.same + 16 * tj + 4 * g);
+          const float e = hs.l[16 * ti + c];
 #pragma unroll
-        for (int kk = 0; kk < 2; ++kk)
-#pragma unroll
-          for (int ti = 2 * kk; ti < 4; ++ti)
-#pragma unroll
-            for (int ct = 0; ct < CT; ++ct)
-              yt[ti][ct] = X::mul(xf[kk][ct], pf[ti < 2 ? ti : 2 * ti - 2 + kk].part[k], yt[ti][ct]);
-      // the next chunk's rows are on their way from here on (not earlier: the
-      // operands above need the registers)
-      if (at + kSsmChunk < len) fetch(at + kSsmChunk);
-      const __amdgpu_buffer_rsrc_t ry = rows_buffer(static_cast<T*>(a.y) + (t0 + at) * a.ldy + static_cast<int64_t>(head) * DV + p0,
-                                                    (rows - 1) * ldy + L::kCols * E);
-      uint32_t vy = c * ldy + 8 * g * E;
-      asm volatile("" : "+v"(vy));
-#pragma unroll
-      for (int ti = 0; ti < 4; ++ti)
-#pragma unroll
-        for (int b = 0; b < CT / 2; ++b) {
-          float o[8];
-#pragma unroll
-          for (int j = 0; j < 8; ++j) o[j] = yt[ti][2 * b + j / 4][j & 3];
-          buffer_store8(ry, vy + 16 * ti * ldy + 32 * b * E, o, static_cast<T*>(nullptr));
+          for (int r = 0; r < 4; ++r) {
+            const float p = cbt[r] * __builtin_amdgcn_exp2f(e + pj[r]);
+            v[r] = 4 * g + r < c ? p : 4 * g + r == c ? p + skip : 0.0f;   // d_skip x rides on the diagonal
+          }
         }
+        X::put4(pt + (ti < 2 ? ti : ti == 2 ? 2 + tj / 2 : 4 + tj / 2) * X::kF2Bytes, 16 * (2 * (tj & 1) + g / 2) + c,
+                g & 1, v);
+      }
     } else {
-      if (at + kSsmChunk < len) fetch(at + kSsmChunk);
       load_x();
     }
+    // the next chunk's rows are on their way from here on (not earlier: the
+    // operands above need the registers)
+    if (at + kSsmChunk < len) fetch(at + kSsmChunk);
 
     // M <- e^{G_last} M + B^T (diag(suf) x)
-    constexpr int TS = DK / 32;   // state row tiles of a step, two steps for each kk
+    constexpr int TS = 2, STEPS = DK / 16 / TS;   // state row tiles of a step, steps for each kk
     R bt[2][TS];
-    typename X::F3 wx[CT];
+    FS wx[CT];
     const auto load_b = [&](int step) {
 #pragma unroll
-      for (int t = 0; t < TS; ++t) {
-        const int td = step % 2 * TS + t;
-        bt[step & 1][t] = KRows::col_frag(lds + L::kOffB, 32 * (step / 2), 32 * (td >> 1), td & 1, g, c);
-      }
+      for (int t = 0; t < TS; ++t)
+        bt[step & 1][t] = KRows::col_frag(lds + L::kOffB, 32 * (step / STEPS), 32 * (step % STEPS), t, g, c);
     };
     const auto weigh_x = [&](int kk) {
       const f32x4 w0 = *reinterpret_cast<const f32x4*>(hs.suf + 32 * kk + 8 * g);
@@ -604,20 +585,50 @@ void k_ssm_scan(SsmScanArgs a) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) m[td][ct][i] *= total;
 #pragma unroll
-    for (int step = 0; step < 4; ++step) {
-      if (step < 3) load_b(step + 1);
+    for (int step = 0; step < 2 * STEPS; ++step) {
+      if (step + 1 < 2 * STEPS) load_b(step + 1);
       __builtin_amdgcn_sched_barrier(0);
-      if (step == 2) weigh_x(1);
+      if (step == STEPS) weigh_x(1);
 #pragma unroll
-      for (int k = 0; k < N3; ++k)
+      for (int k = 0; k < NS; ++k)
 #pragma unroll
         for (int t = 0; t < TS; ++t)
 #pragma unroll
           for (int ct = 0; ct < CT; ++ct) {
-            f32x4& acc = m[step % 2 * TS + t][ct];
+            f32x4& acc = m[step % STEPS * TS + t][ct];
             acc = X::mul(bt[step & 1][t], wx[ct].part[k], acc);
           }
       __builtin_amdgcn_sched_barrier(0);
+    }
+    if constexpr (OUT) {
+      lds_barrier();   // P is whole
+      // y^T += x^T P^T, and out
+      typename X::F2 pf[L::kPFrags];
+#pragma unroll
+      for (int f = 0; f < L::kPFrags; ++f) pf[f] = X::get(pt + f * X::kF2Bytes, lane);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int k = 0; k < N2; ++k)
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+          for (int ti = 2 * kk; ti < 4; ++ti)
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct)
+              yt[ti][ct] = X::mul(xf[kk][ct], pf[ti < 2 ? ti : 2 * ti - 2 + kk].part[k], yt[ti][ct]);
+      const __amdgpu_buffer_rsrc_t ry = rows_buffer(static_cast<T*>(a.y) + (t0 + at) * a.ldy + static_cast<int64_t>(head) * DV + p0,
+                                                    (rows - 1) * ldy + L::kCols * E);
+      uint32_t vy = c * ldy + 8 * g * E;
+      asm volatile("" : "+v"(vy));
+#pragma unroll
+      for (int ti = 0; ti < 4; ++ti)
+#pragma unroll
+        for (int b = 0; b < CT / 2; ++b) {
+          float o[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) o[j] = yt[ti][2 * b + j / 4][j & 3];
+          buffer_store8(ry, vy + 16 * ti * ldy + 32 * b * E, o, static_cast<T*>(nullptr));
+        }
     }
     lds_barrier();   // the chunk's LDS has been read
   }
@@ -628,7 +639,7 @@ void k_ssm_scan(SsmScanArgs a) {
 #pragma unroll
       for (int ct = 0; ct < CT; ++ct) seg[(td * CT + ct) * kWave] = m[td][ct];
     if (wave < L::kHeads && lane == 0) a.seg_decay[static_cast<int64_t>(slot) * a.heads + h0 + wave] = log_total;
-  } else if (last && a.state_out) {
+  } else if (MODE == SsmMode::kWhole && a.state_out) {
 #pragma unroll
     for (int td = 0; td < DK / 16; ++td)
 #pragma unroll
@@ -639,10 +650,10 @@ void k_ssm_scan(SsmScanArgs a) {
 }
 
 // The segments' states become their starts: per sequence and state element,
-//   start_0 = state_in,  start_{j+1} = decay_j start_j + local_j.
-// With JOIN the starts replace the local states (the last segment's is not
-// read); without, only the last state is wanted and goes to state_out.  A thread
-// takes one accumulator element (four rows of a column) of one sequence.
+//   start_0 = state_in,  start_{j+1} = decay_j start_j + local_j,
+// the last of them state_out (where wanted).  With JOIN the starts replace the
+// local states, for kJoined.  A thread takes one accumulator element (four rows
+// of a column) of one sequence.
 template <int DK, int DV, int CT, int NW, bool JOIN>
 __global__ __launch_bounds__(256)
 void k_ssm_join(SsmScanArgs a) {
@@ -666,19 +677,13 @@ void k_ssm_join(SsmScanArgs a) {
   const int segs = max(1, (len + a.seg_tokens - 1) / a.seg_tokens);
   for (int j = 0; j < segs; ++j) {
     f32x4* p = a.seg_state + (slot0 + j) * per_seq + e;
-    if (JOIN && j == segs - 1) {
-      *p = run;
-      return;
-    }
-    if (j * static_cast<int64_t>(a.seg_tokens) < len) {
-      const f32x4 local = *p;
-      const float decay = __builtin_amdgcn_exp2f(a.seg_decay[(slot0 + j) * a.heads + head]);
-      if (JOIN) *p = run;
+    const f32x4 local = *p;
+    const float decay = __builtin_amdgcn_exp2f(a.seg_decay[(slot0 + j) * a.heads + head]);
+    if (JOIN) *p = run;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) run[r] = fmaf(decay, run[r], local[r]);
-    }
+    for (int r = 0; r < 4; ++r) run[r] = fmaf(decay, run[r], local[r]);   // an empty segment: decay 1, local 0
   }
-  if (!JOIN) {
+  if (a.state_out) {
 #pragma unroll
     for (int r = 0; r < 4; ++r) a.state_out[sbase + strow(td, g, r) * DV] = run[r];
   }
