@@ -13,10 +13,7 @@ constexpr int64_t kMaxGrid = std::numeric_limits<int32_t>::max();
 // a tile's rows are addressed with 32-bit byte offsets: 64 rows of 2^23 fp32 elements
 constexpr int64_t kMaxStride = int64_t{1} << 23;
 
-// Segments of the state space scan
-constexpr int64_t kSsmPlaces = 256;       // workgroups that the chip holds at once
-constexpr int64_t kSsmSplitChunks = 8;    // the longest sequence from which it pays
-constexpr int64_t kSsmSegChunks = 4;      // the shortest segment
+constexpr int64_t kSsmPlaces = 256;   // workgroups of the state space scan that the chip holds at once, one per CU
 
 bool known_dtype(int32_t d) { return d == GDN_F32 || d == GDN_BF16; }
 
@@ -103,18 +100,26 @@ gdn_status make_ssm_plan(const gdn_ssm_shape* s, const int32_t* cu, SsmPlan* pla
   p.heads_per_group = H / s->num_groups % share == 0 ? share : 1;
   p.slots = N;
   const int64_t groups = H / p.heads_per_group;   // workgroups of a sequence
+  // Whole sequences end with the longest one, or with the work per place; in
+  // segments the work is even, but every chunk is walked twice (once for the
+  // states alone) and the states pass through memory.  In chunks of the whole
+  // walk (~8 us for bf16 inputs): a segment's chunk costs 1.5, the join and the
+  // two launches 1.5.
+  const auto chunks_of = [&](int64_t n) { return (static_cast<int64_t>(cu[n + 1]) - cu[n] + 63) / 64; };
+  int64_t chunks = 0;
+  for (int64_t n = 0; n < N; ++n) chunks += chunks_of(n);
   const int64_t longest = (p.longest + 63) / 64;
-  if (longest >= kSsmSplitChunks && N * groups < kSsmPlaces) {
-    int64_t chunks = 0;
-    for (int64_t n = 0; n < N; ++n) chunks += (static_cast<int64_t>(cu[n + 1]) - cu[n] + 63) / 64;
-    const int64_t seg = std::max<int64_t>(kSsmSegChunks, (chunks * groups + kSsmPlaces - 1) / kSsmPlaces);
-    if (seg * 2 <= longest) {
-      p.seg_tokens = static_cast<int32_t>(64 * seg);
-      p.slots = tile_slots(p.tokens, N, p.seg_tokens);
-      const size_t state = static_cast<size_t>(H) * s->d_state * s->head_dim * sizeof(float);
-      p.off_decay = static_cast<size_t>(p.slots) * state;   // a multiple of 256
-      p.bytes = (p.off_decay + static_cast<size_t>(p.slots) * H * sizeof(float) + kAlign - 1) / kAlign * kAlign;
-    }
+  const double whole = std::max(static_cast<double>(longest), static_cast<double>(chunks * groups) / kSsmPlaces);
+  const int64_t seg = std::max<int64_t>(1, (chunks * groups + kSsmPlaces - 1) / kSsmPlaces);
+  int64_t segs = 0;
+  for (int64_t n = 0; n < N; ++n) segs += std::max<int64_t>(1, (chunks_of(n) + seg - 1) / seg);
+  const int64_t rounds = (segs * groups + kSsmPlaces - 1) / kSsmPlaces;
+  if (1.5 * static_cast<double>(seg * rounds) + 1.5 < whole) {
+    p.seg_tokens = static_cast<int32_t>(64 * seg);
+    p.slots = tile_slots(p.tokens, N, p.seg_tokens);
+    const size_t state = static_cast<size_t>(H) * s->d_state * s->head_dim * sizeof(float);
+    p.off_decay = static_cast<size_t>(p.slots) * state;   // a multiple of 256
+    p.bytes = (p.off_decay + static_cast<size_t>(p.slots) * H * sizeof(float) + kAlign - 1) / kAlign * kAlign;
   }
   if (p.slots * groups > kMaxGrid / 1024) {
     *err = "too many segments";

@@ -675,13 +675,27 @@ void k_ssm_join(SsmScanArgs a) {
   const int start = a.cu[n], len = a.cu[n + 1] - start;
   const int64_t slot0 = start / a.seg_tokens + n;
   const int segs = max(1, (len + a.seg_tokens - 1) / a.seg_tokens);
-  for (int j = 0; j < segs; ++j) {
-    f32x4* p = a.seg_state + (slot0 + j) * per_seq + e;
-    const f32x4 local = *p;
-    const float decay = __builtin_amdgcn_exp2f(a.seg_decay[(slot0 + j) * a.heads + head]);
-    if (JOIN) *p = run;
+  // eight segments' loads are in flight at a time
+  constexpr int AHEAD = 8;
+  f32x4* p = a.seg_state + slot0 * per_seq + e;
+  const float* dec = a.seg_decay + slot0 * a.heads + head;
+  for (int j0 = 0; j0 < segs; j0 += AHEAD) {
+    f32x4 local[AHEAD];
+    float decay[AHEAD];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) run[r] = fmaf(decay, run[r], local[r]);   // an empty segment: decay 1, local 0
+    for (int k = 0; k < AHEAD; ++k) {
+      const int64_t j = min(j0 + k, segs - 1);
+      local[k] = p[j * per_seq];
+      decay[k] = dec[j * a.heads];
+    }
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+      if (j0 + k >= segs) break;
+      if (JOIN) p[(j0 + k) * static_cast<int64_t>(per_seq)] = run;
+      const float d = __builtin_amdgcn_exp2f(decay[k]);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) run[r] = fmaf(d, run[r], local[k][r]);   // an empty segment: decay 1, local 0
+    }
   }
   if (a.state_out) {
 #pragma unroll
