@@ -15,6 +15,8 @@ constexpr int64_t kMaxStride = int64_t{1} << 23;
 
 constexpr int64_t kSsmPlaces = 256;   // workgroups of the state space scan that the chip holds at once, one per CU
 
+constexpr int64_t kLoraGroups = 384;   // workgroups that the first product of the adapters aims at
+
 bool known_dtype(int32_t d) { return d == GDN_F32 || d == GDN_BF16; }
 
 gdn_status check_stride(const char* name, int64_t ld, int64_t least, std::string* err) {
@@ -150,6 +152,31 @@ gdn_status check_lora(const gdn_lora_shape* s, std::string* err) {
   if (st == GDN_OK) st = check_stride("ld_out", s->ld_out, s->width, err);
   if (st != GDN_OK) return st;
   if (s->ld_x % 8 != 0) { *err = "ld_x must be a multiple of 8"; return GDN_ERR_UNSUPPORTED; }
+  return GDN_OK;
+}
+
+gdn_status make_lora_plan(const gdn_lora_shape* s, const int32_t* cu, LoraPlan* plan, std::string* err) {
+  gdn_status st = check_lora(s, err);
+  LoraPlan p;
+  int64_t longest = 0;
+  if (st == GDN_OK) st = check_seqlens(s->num_seqs, cu, &p.tokens, &longest, err);
+  if (st != GDN_OK) return st;
+  const bool tokenwise = p.tokens <= 16 * static_cast<int64_t>(s->num_seqs);
+  p.down_tile = tokenwise ? 16 : 32;
+  p.up_tile = tokenwise ? 16 : 64;
+  p.down_slots = tile_slots(p.tokens, s->num_seqs, p.down_tile);
+  p.up_slots = tile_slots(p.tokens, s->num_seqs, p.up_tile);
+  // x A^T in enough workgroups for every CU, each with at least two 32-wide steps
+  // for each of its four waves; every part is read by all column tiles
+  const int64_t most = std::max<int64_t>(1, s->hidden / 256);
+  p.parts = static_cast<int32_t>(std::min(most, std::max<int64_t>(1, kLoraGroups / std::max<int64_t>(1, p.down_slots))));
+  const int64_t tiles = (static_cast<int64_t>(s->width) + 255) / 256;
+  if (p.down_slots * p.parts > kMaxGrid / 256 || p.up_slots * tiles > kMaxGrid / 256) {
+    *err = "too many tokens for one call";
+    return GDN_ERR_UNSUPPORTED;
+  }
+  p.bytes = (static_cast<size_t>(p.parts) * p.tokens * s->rank * sizeof(float) + kAlign - 1) / kAlign * kAlign;
+  *plan = p;
   return GDN_OK;
 }
 

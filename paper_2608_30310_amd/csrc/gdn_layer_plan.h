@@ -42,6 +42,17 @@ gdn_status make_ssm_plan(const gdn_ssm_shape* s, const int32_t* cu, SsmPlan* p, 
 
 gdn_status check_lora(const gdn_lora_shape* s, std::string* err);
 
+struct LoraPlan {
+  int64_t tokens = 0;
+  // tokens of a tile of the first and of the second product (32 and 64, or 16
+  // where sequences are short) and their slots
+  int32_t down_tile = 0, up_tile = 0;
+  int64_t down_slots = 0, up_slots = 0;
+  int32_t parts = 1;   // pieces of the first product's contraction over K
+  size_t bytes = 0;          // workspace: partial x A^T, fp32 [parts, tokens, rank]
+};
+gdn_status make_lora_plan(const gdn_lora_shape* s, const int32_t* cu, LoraPlan* p, std::string* err);
+
 // Two row-strided regions of `rows` rows: a starts at pa, has wa bytes in each
 // row and lda bytes between rows.  False only where no byte is in both: their
 // extents do not meet, or the strides are equal and the rows' windows never meet.

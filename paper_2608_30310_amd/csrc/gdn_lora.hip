@@ -23,36 +23,47 @@ gdn_status llaunched(const char* what) {
   return GDN_OK;
 }
 
-template <typename T>
-gdn_status launch_lora(const gdn_lora_shape& s, int64_t tokens, const int32_t* cu, const int32_t* adapters,
-                       const void* base, const void* x, const void* A, const void* B, const float* scales, void* out,
-                       float* u, hipStream_t stream) {
-  hipLaunchKernelGGL(k_lora_down, dim3(2048), dim3(kLoraThreads), 0, stream, static_cast<int32_t>(tokens), s.num_seqs,
-                     cu, adapters, s.num_adapters, s.hidden, s.rank, static_cast<const uint16_t*>(x), s.ld_x,
-                     static_cast<const uint16_t*>(A), scales, u);
-  hipLaunchKernelGGL((k_lora_up<T>), dim3(2048), dim3(kLoraThreads), 0, stream, static_cast<int32_t>(tokens),
-                     s.num_seqs, cu, adapters, s.num_adapters, s.width, s.rank, u, static_cast<const uint16_t*>(B),
-                     static_cast<const T*>(base), s.ld_base, static_cast<T*>(out), s.ld_out);
-  return llaunched("adapter launch");
+template <typename T, int TT, bool WIDE>
+void launch_up(const LoraArgs& k, int64_t slots, hipStream_t stream) {
+  const dim3 grid(static_cast<uint32_t>(slots * ((k.M + kLoraCols - 1) / kLoraCols)));
+  const auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kLoraThreads), 0, stream, k); };
+  if (k.R <= 32) run(k_lora_up<T, TT, 1, WIDE>);
+  else if (k.R <= 64) run(k_lora_up<T, TT, 2, WIDE>);
+  else run(k_lora_up<T, TT, 4, WIDE>);
 }
 
-gdn_status lora_plan(const gdn_lora_shape* s, const int32_t* cu_host, int64_t* tokens, size_t* bytes, std::string* err) {
-  gdn_status st = check_lora(s, err);
-  int64_t longest = 0;
-  if (st == GDN_OK) st = check_seqlens(s->num_seqs, cu_host, tokens, &longest, err);
-  if (st != GDN_OK) return st;
-  *bytes = (static_cast<size_t>(*tokens) * s->rank * sizeof(float) + kAlign - 1) / kAlign * kAlign;
-  return GDN_OK;
+template <int TT>
+void launch_down(const LoraArgs& k, int64_t slots, hipStream_t stream) {
+  const dim3 grid(static_cast<uint32_t>(slots * k.parts));
+  const auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kLoraThreads), 0, stream, k); };
+  if (k.R <= 16) run(k_lora_down<TT, 1>);
+  else if (k.R <= 32) run(k_lora_down<TT, 2>);
+  else if (k.R <= 64) run(k_lora_down<TT, 4>);
+  else run(k_lora_down<TT, 8>);
+}
+
+template <typename T>
+gdn_status launch_lora(const LoraArgs& k, const LoraPlan& p, bool any, bool wide, hipStream_t stream) {
+  if (p.up_tile == lora_tile(4)) {
+    if (any) launch_down<2>(k, p.down_slots, stream);
+    if (wide) launch_up<T, 4, true>(k, p.up_slots, stream);
+    else launch_up<T, 4, false>(k, p.up_slots, stream);
+  } else {
+    if (any) launch_down<1>(k, p.down_slots, stream);
+    if (wide) launch_up<T, 1, true>(k, p.up_slots, stream);
+    else launch_up<T, 1, false>(k, p.up_slots, stream);
+  }
+  return llaunched("adapter launch");
 }
 
 gdn_status lora_impl(const gdn_lora_shape* s, const int32_t* cu_host, const int32_t* cu, const int32_t* adapters_host,
                      const int32_t* adapters, const void* base, const void* x, const void* A, const void* B,
                      const float* scales, void* out, void* workspace, size_t workspace_bytes, hipStream_t stream) {
   std::string err;
-  int64_t tokens = 0;
-  size_t bytes = 0;
-  const gdn_status st = lora_plan(s, cu_host, &tokens, &bytes, &err);
+  LoraPlan p;
+  const gdn_status st = make_lora_plan(s, cu_host, &p, &err);
   if (st != GDN_OK) return lfail(st, err);
+  const int64_t tokens = p.tokens;
   if (s->num_seqs == 0) return GDN_OK;
   if (!adapters_host) return lfail(GDN_ERR_NULL_ARG, "adapters_host is NULL");
   bool any = false;
@@ -74,15 +85,20 @@ gdn_status lora_impl(const gdn_lora_shape* s, const int32_t* cu_host, const int3
   if (x && rows_overlap(x, s->hidden * 2, s->ld_x * 2, out, row, s->ld_out * e, tokens))
     return lfail(GDN_ERR_BAD_SHAPE, "out overlaps x");
   if (!workspace) return lfail(GDN_ERR_WORKSPACE, "workspace is NULL");
-  if (workspace_bytes < bytes)
-    return lfail(GDN_ERR_WORKSPACE, "workspace too small: need " + std::to_string(bytes) + " bytes, got " +
+  if (workspace_bytes < p.bytes)
+    return lfail(GDN_ERR_WORKSPACE, "workspace too small: need " + std::to_string(p.bytes) + " bytes, got " +
                                         std::to_string(workspace_bytes));
   if (off(workspace, kAlign)) return lfail(GDN_ERR_WORKSPACE, "workspace must be 256-byte aligned");
   if (!any && base == out) return GDN_OK;
-  float* u = static_cast<float*>(workspace);
-  return s->out_dtype == GDN_BF16
-             ? launch_lora<uint16_t>(*s, tokens, cu, adapters, base, x, A, B, scales, out, u, stream)
-             : launch_lora<float>(*s, tokens, cu, adapters, base, x, A, B, scales, out, u, stream);
+  const LoraArgs k{s->num_seqs, s->num_adapters, s->hidden, s->width, s->rank, p.parts,
+                   tokens, cu, adapters, static_cast<const uint16_t*>(x), s->ld_x, static_cast<const uint16_t*>(A),
+                   static_cast<const uint16_t*>(B), scales, base, s->ld_base, out, s->ld_out,
+                   static_cast<float*>(workspace)};
+  const int64_t vec = 16 / e;
+  const bool wide = s->width % vec == 0 && s->ld_base % vec == 0 && s->ld_out % vec == 0 && s->width % 8 == 0 &&
+                    !off(base, 16) && !off(out, 16);
+  return s->out_dtype == GDN_BF16 ? launch_lora<uint16_t>(k, p, any, wide, stream)
+                                  : launch_lora<float>(k, p, any, wide, stream);
 }
 
 }  // namespace
@@ -93,9 +109,11 @@ extern "C" {
 gdn_status gdn_lora_workspace_size(const gdn_lora_shape* shape, const int32_t* cu_seqlens_host, size_t* bytes) {
   if (!bytes) return gdn::lfail(GDN_ERR_NULL_ARG, "bytes is NULL");
   std::string err;
-  int64_t tokens = 0;
-  const gdn_status st = gdn::lora_plan(shape, cu_seqlens_host, &tokens, bytes, &err);
-  return st == GDN_OK ? st : gdn::lfail(st, err);
+  gdn::LoraPlan p;
+  const gdn_status st = gdn::make_lora_plan(shape, cu_seqlens_host, &p, &err);
+  if (st != GDN_OK) return gdn::lfail(st, err);
+  *bytes = p.bytes;
+  return GDN_OK;
 }
 
 gdn_status gdn_lora_add(const gdn_lora_shape* shape, const int32_t* cu_seqlens_host, const int32_t* cu_seqlens,
