@@ -3,6 +3,8 @@
 // fp32 arithmetic whatever the element type, one rounding at the store.
 #pragma once
 
+#include <type_traits>
+
 #include "gdn_varlen.h"
 
 namespace gdn {
@@ -16,14 +18,33 @@ constexpr int conv_vec() { return ALIGNED ? 16 / static_cast<int>(sizeof(T)) : 1
 // tokens of a workgroup's tile when each thread takes tpt of them
 constexpr int conv_tile(int tpt) { return kConvRows * tpt; }
 
+// A thread's channels of one row as they lie in memory: 16 bytes, or one element.
+template <typename T, int VEC>
+struct Chans {
+  typedef typename std::conditional<VEC == 1, T, u32x4>::type Raw;
+  Raw raw;
+  __device__ __forceinline__ void load(const T* p) { raw = *reinterpret_cast<const Raw*>(p); }
+  __device__ __forceinline__ void store(T* p) const { *reinterpret_cast<Raw*>(p) = raw; }
+  __device__ __forceinline__ void clear() {
+    if constexpr (VEC == 1) raw = T(0);
+    else raw = u32x4{0u, 0u, 0u, 0u};
+  }
+  __device__ __forceinline__ float get(int e) const {
+    if constexpr (VEC == 1) return load_elt(&raw, 0);
+    else return vec_elt<T>(raw, e);
+  }
+};
+
+// The taps and the bias of a thread's channels.  c0 + VEC <= C for every thread
+// that stores; the others take the last channels'.
 template <int VEC, int W>
-__device__ __forceinline__ void load_taps(const float* __restrict__ w, const float* __restrict__ bias, int c0, bool any,
+__device__ __forceinline__ void load_taps(const float* __restrict__ w, const float* __restrict__ bias, int c0,
                                           float (&tap)[W][VEC], float (&b)[VEC]) {
 #pragma unroll
   for (int e = 0; e < VEC; ++e) {
 #pragma unroll
-    for (int j = 0; j < W; ++j) tap[j][e] = any ? w[static_cast<int64_t>(c0 + e) * W + j] : 0.0f;
-    b[e] = any && bias ? bias[c0 + e] : 0.0f;
+    for (int j = 0; j < W; ++j) tap[j][e] = w[static_cast<int64_t>(c0 + e) * W + j];
+    b[e] = bias ? bias[c0 + e] : 0.0f;
   }
 }
 
@@ -36,9 +57,10 @@ __device__ __forceinline__ void activate(float (&acc)[VEC]) {
 }
 
 // Workgroup: 32 channel groups x 8 rows of TPT consecutive tokens; a thread
-// loads the TPT + W - 1 rows that its tokens need once.  blockIdx.x %
-// slabs is its channel slab for good (the taps stay in registers), its tiles
-// are the slots from blockIdx.x / slabs in steps of gridDim.x / slabs.
+// loads the TPT + W - 1 rows that its tokens need once, all of them before
+// anything waits.  blockIdx.x % slabs is its channel slab for good (the taps stay
+// in registers), its tiles are the slots from blockIdx.x / slabs in steps of
+// gridDim.x / slabs.
 // The rows before a sequence and the history after it belong to the sequence's
 // first tile, so history_out may be history_in: that workgroup alone touches
 // them, and it reads before it writes.
@@ -49,13 +71,15 @@ void k_causal_conv(int32_t slots, int32_t slabs, int32_t n_seqs, const int32_t* 
                    const T* hist_in, T* __restrict__ y, int64_t ldy, T* hist_out) {
   constexpr int H = W - 1;
   constexpr int TILE = conv_tile(TPT);
+  typedef Chans<T, VEC> Row;
   const int tid = threadIdx.x;
   const int row = tid / kConvLanes;
   const int slab = blockIdx.x % slabs;
-  const int c0 = (slab * kConvLanes + tid % kConvLanes) * VEC;
-  const bool any = c0 < C;
+  const int mine = (slab * kConvLanes + tid % kConvLanes) * VEC;
+  const bool any = mine < C;              // C is a multiple of VEC
+  const int c0 = any ? mine : C - VEC;    // the others load the last channels and store nothing
   float tap[W][VEC], b[VEC];
-  load_taps<VEC, W>(w, bias, c0, any, tap, b);
+  load_taps<VEC, W>(w, bias, c0, tap, b);
   const int step = gridDim.x / slabs;
   for (int slot = blockIdx.x / slabs; slot < slots; slot += step) {   // uniform per workgroup
     const int n = slot_seq(cu, n_seqs, slot, TILE);
@@ -65,40 +89,37 @@ void k_causal_conv(int32_t slots, int32_t slabs, int32_t n_seqs, const int32_t* 
     const int t0 = j * TILE + row * TPT;
     const T* xs = x + static_cast<int64_t>(start) * ldx + c0;
     const int64_t hbase = static_cast<int64_t>(n) * H * C + c0;
-    float u[TPT + H][VEC];
+    Row u[TPT + H];
+    if (len > 0) {
 #pragma unroll
-    for (int r = 0; r < TPT + H; ++r) {
-      const int t = t0 - H + r;
-      if (any && t >= 0 && t < len) {
-        load_run<T, VEC>(xs + static_cast<int64_t>(t) * ldx, u[r]);
-      } else if (any && t < 0 && hist_in) {
-        load_run<T, VEC>(hist_in + hbase + static_cast<int64_t>(H + t) * C, u[r]);
-      } else {
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) u[r][e] = 0.0f;
-      }
+      for (int r = 0; r < TPT + H; ++r) u[r].load(xs + static_cast<int64_t>(min(max(t0 - H + r, 0), len - 1)) * ldx);
     }
-    if (j == 0 && hist_out) {
-      // rows len .. len + H - 1 of (history | sequence); bf16 -> fp32 -> bf16 is exact
-      float h[H][VEC];
-      if (any && row == 0) {
+    if (j == 0) {   // uniform: rows before the sequence, and the history after it
 #pragma unroll
-        for (int r = 0; r < H; ++r) {
-          const int t = len - H + r;
-          if (t >= 0) {
-            load_run<T, VEC>(xs + static_cast<int64_t>(t) * ldx, h[r]);
-          } else if (hist_in) {
-            load_run<T, VEC>(hist_in + hbase + static_cast<int64_t>(H + t) * C, h[r]);
-          } else {
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) h[r][e] = 0.0f;
-          }
+      for (int r = 0; r < TPT + H; ++r) {
+        const int t = t0 - H + r;
+        if (t < 0) {
+          if (hist_in) u[r].load(hist_in + hbase + static_cast<int64_t>(H + t) * C);
+          else u[r].clear();
         }
       }
-      __syncthreads();   // every row's history_in is in registers
-      if (any && row == 0) {
+      if (hist_out) {
+        // rows len .. len + H - 1 of (history | sequence)
+        Row h[H];
+        if (any && row == 0) {
 #pragma unroll
-        for (int r = 0; r < H; ++r) store_run<T, VEC>(hist_out + hbase + static_cast<int64_t>(r) * C, h[r]);
+          for (int r = 0; r < H; ++r) {
+            const int t = len - H + r;
+            if (t >= 0) h[r].load(xs + static_cast<int64_t>(t) * ldx);
+            else if (hist_in) h[r].load(hist_in + hbase + static_cast<int64_t>(H + t) * C);
+            else h[r].clear();
+          }
+        }
+        __syncthreads();   // every row's history_in is in registers
+        if (any && row == 0) {
+#pragma unroll
+          for (int r = 0; r < H; ++r) h[r].store(hist_out + hbase + static_cast<int64_t>(r) * C);
+        }
       }
     }
 #pragma unroll
@@ -109,10 +130,10 @@ void k_causal_conv(int32_t slots, int32_t slabs, int32_t n_seqs, const int32_t* 
       for (int e = 0; e < VEC; ++e) {
         acc[e] = b[e];
 #pragma unroll
-        for (int k = 0; k < W; ++k) acc[e] = fmaf(tap[k][e], u[i + k][e], acc[e]);
+        for (int k = 0; k < W; ++k) acc[e] = fmaf(tap[k][e], u[i + k].get(e), acc[e]);
       }
       activate<VEC, SILU>(acc);
-      store_run<T, VEC>(y + static_cast<int64_t>(start + t0 + i) * ldy + c0, acc);
+      store_run<T, VEC>(y + static_cast<int64_t>(start + t0 + i) * ldy + mine, acc);
     }
   }
 }
@@ -126,33 +147,35 @@ void k_causal_conv_step(int32_t n_seqs, int32_t C, const T* __restrict__ x, int6
                         const float* __restrict__ bias, const T* hist_in, T* __restrict__ y, int64_t ldy,
                         T* hist_out) {
   constexpr int H = W - 1;
+  typedef Chans<T, VEC> Row;
   const int c0 = (blockIdx.x * blockDim.x + threadIdx.x) * VEC;
   if (c0 >= C) return;
   float tap[W][VEC], b[VEC];
-  load_taps<VEC, W>(w, bias, c0, true, tap, b);
-  for (int n = blockIdx.y; n < n_seqs; n += gridDim.y) {
+  Row u[W];
+  const auto fetch = [&](int n) {
     const int64_t hbase = static_cast<int64_t>(n) * H * C + c0;
-    float u[W][VEC];
 #pragma unroll
     for (int r = 0; r < H; ++r) {
-      if (hist_in) {
-        load_run<T, VEC>(hist_in + hbase + static_cast<int64_t>(r) * C, u[r]);
-      } else {
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) u[r][e] = 0.0f;
-      }
+      if (hist_in) u[r].load(hist_in + hbase + static_cast<int64_t>(r) * C);
+      else u[r].clear();
     }
-    load_run<T, VEC>(x + static_cast<int64_t>(n) * ldx + c0, u[H]);
+    u[H].load(x + static_cast<int64_t>(n) * ldx + c0);
+  };
+  fetch(blockIdx.y);   // beside the taps
+  load_taps<VEC, W>(w, bias, c0, tap, b);
+  for (int n = blockIdx.y; n < n_seqs; n += gridDim.y) {
+    if (n != static_cast<int>(blockIdx.y)) fetch(n);
+    const int64_t hbase = static_cast<int64_t>(n) * H * C + c0;
     float acc[VEC];
 #pragma unroll
     for (int e = 0; e < VEC; ++e) {
       acc[e] = b[e];
 #pragma unroll
-      for (int k = 0; k < W; ++k) acc[e] = fmaf(tap[k][e], u[k][e], acc[e]);
+      for (int k = 0; k < W; ++k) acc[e] = fmaf(tap[k][e], u[k].get(e), acc[e]);
     }
     activate<VEC, SILU>(acc);
 #pragma unroll
-    for (int r = 0; r < H; ++r) store_run<T, VEC>(hist_out + hbase + static_cast<int64_t>(r) * C, u[r + 1]);
+    for (int r = 0; r < H; ++r) u[r + 1].store(hist_out + hbase + static_cast<int64_t>(r) * C);
     store_run<T, VEC>(y + static_cast<int64_t>(n) * ldy + c0, acc);
   }
 }
