@@ -110,6 +110,40 @@ gdn_status gdn_la_block_replay(const gdn_la_shape* shape, const gdn_la_weights* 
                                void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * Replay of a layer whose requests carry low-rank adapters beside the shared
+ * projections (gdn_lora.h): with a = adapters[n] of a token's sequence,
+ *     P += scales_in[a] (x A_in[a]^T) B_in[a]^T   after step 1,
+ *     out += scales_out[a] (y A_out[a]^T) B_out[a]^T   after step 7,
+ * a = -1 for a request without one.  A rank of 0 leaves its projection as it is
+ * (its pointers may be NULL then); ranks are multiples of 8 up to 128; scales
+ * NULL = 1; rank_out is not looked at when `out` is NULL.
+ */
+typedef struct {
+  int32_t num_adapters;
+  int32_t rank_in;
+  int32_t rank_out;
+  const void* a_in;              /* bf16 [num_adapters, rank_in, D]              */
+  const void* b_in;              /* bf16 [num_adapters, 2cq + 2cv + 2Hv, rank_in] */
+  const void* a_out;             /* bf16 [num_adapters, rank_out, cv]            */
+  const void* b_out;             /* bf16 [num_adapters, D, rank_out]             */
+  const float* scales_in;        /* fp32 [num_adapters]                          */
+  const float* scales_out;       /* fp32 [num_adapters]                          */
+  const int32_t* adapters_host;  /* int32 [N], host                              */
+  const int32_t* adapters;       /* int32 [N], device, the same values           */
+} gdn_la_adapters;
+
+gdn_status gdn_la_block_adapted_workspace_size(const gdn_la_shape* shape,
+                                               const gdn_la_adapters* adapters,
+                                               const int32_t* cu_seqlens_host,
+                                               int32_t with_outputs, size_t* bytes);
+
+gdn_status gdn_la_block_replay_adapted(const gdn_la_shape* shape, const gdn_la_weights* weights,
+                                       const gdn_la_adapters* adapters,
+                                       const int32_t* cu_seqlens_host, const int32_t* cu_seqlens,
+                                       const void* x, float* state_out, void* out,
+                                       void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Profiling variant: identical work and results; records stage_events[i]
  * (hipEvent_t) before stage i and stage_events[n] after the last, where
  * n = gdn_la_block_num_stages(out != NULL) and num_events must be n + 1.

@@ -51,6 +51,13 @@ class LAWeights(ctypes.Structure):
                 ("dt_bias", ctypes.c_void_p), ("norm_w", ctypes.c_void_p), ("w_out", ctypes.c_void_p)]
 
 
+class LAAdapters(ctypes.Structure):
+    _fields_ = [("num_adapters", ctypes.c_int32), ("rank_in", ctypes.c_int32), ("rank_out", ctypes.c_int32),
+                ("a_in", ctypes.c_void_p), ("b_in", ctypes.c_void_p), ("a_out", ctypes.c_void_p),
+                ("b_out", ctypes.c_void_p), ("scales_in", ctypes.c_void_p), ("scales_out", ctypes.c_void_p),
+                ("adapters_host", ctypes.c_void_p), ("adapters", ctypes.c_void_p)]
+
+
 class ConvShape(ctypes.Structure):
     _fields_ = [("num_seqs", ctypes.c_int32), ("channels", ctypes.c_int32), ("taps", ctypes.c_int32),
                 ("dtype", ctypes.c_int32), ("activation", ctypes.c_int32), ("ld_x", ctypes.c_int64),
@@ -123,6 +130,11 @@ def load_library():
     lib.gdn_la_block_replay.restype = ctypes.c_int
     lib.gdn_la_block_replay_profiled.argtypes = lib.gdn_la_block_replay.argtypes + [P, ctypes.c_int32]
     lib.gdn_la_block_replay_profiled.restype = ctypes.c_int
+    DP = ctypes.POINTER(LAAdapters)
+    lib.gdn_la_block_adapted_workspace_size.argtypes = [LP, DP, P, ctypes.c_int32, ctypes.POINTER(ctypes.c_size_t)]
+    lib.gdn_la_block_adapted_workspace_size.restype = ctypes.c_int
+    lib.gdn_la_block_replay_adapted.argtypes = [LP, WP, DP, P, P, P, P, P, P, ctypes.c_size_t, P]
+    lib.gdn_la_block_replay_adapted.restype = ctypes.c_int
     lib.gdn_la_block_num_stages.argtypes = [ctypes.c_int32]
     lib.gdn_la_block_num_stages.restype = ctypes.c_int32
     lib.gdn_la_block_stage_name.argtypes = [ctypes.c_int32, ctypes.c_int32]
@@ -614,11 +626,57 @@ def la_block_workspace_size(hidden: int, num_k_heads: int, num_v_heads: int, d_k
     return int(out.value)
 
 
+def _adapter_ids(adapters, adapters_host, n, device):
+    """Device and host copies of the adapters' indices, int32 [N]."""
+    if adapters_host is None:
+        if isinstance(adapters, torch.Tensor):
+            adapters_host = adapters.detach().to("cpu", torch.int32)
+        else:
+            adapters_host = torch.tensor(list(adapters), dtype=torch.int32)
+    elif not isinstance(adapters_host, torch.Tensor):
+        adapters_host = torch.tensor(list(adapters_host), dtype=torch.int32)
+    adapters_host = adapters_host.to(torch.int32).contiguous()
+    if adapters_host.device.type != "cpu":
+        raise ValueError("adapters_host must live in host memory")
+    if not isinstance(adapters, torch.Tensor) or adapters.device != device:
+        adapters = adapters_host.to(device)
+    _need(adapters, "adapters", torch.int32, device, 1)
+    if adapters.numel() != n or adapters_host.numel() != n:
+        raise ValueError("adapters and adapters_host must hold one index per sequence")
+    return adapters, adapters_host
+
+
+def _la_adapters(adapters, n, hidden, rows, cv, device):
+    """The gdn_la_adapters of ``adapters``, and the tensors it points to."""
+    ids, host = _adapter_ids(adapters["ids"], adapters.get("ids_host"), n, device)
+    count, ranks, ptrs, keep = None, [0, 0], [], [ids, host]
+    for i, (side, k, m) in enumerate((("in", hidden, rows), ("out", cv, hidden))):
+        a, b, s = (adapters.get(f"{name}_{side}") for name in ("a", "b", "scales"))
+        if a is None and b is None:
+            ptrs.append((None, None, None))
+            continue
+        _need(a, f"a_{side}", torch.bfloat16, device, 3)
+        _need(b, f"b_{side}", torch.bfloat16, device, 3)
+        count = a.shape[0] if count is None else count
+        r = a.shape[1]
+        if tuple(a.shape) != (count, r, k) or tuple(b.shape) != (count, m, r):
+            raise ValueError(f"a_{side} must be [n, R, {k}] and b_{side} [n, {m}, R]")
+        if s is not None:
+            _need(s, f"scales_{side}", torch.float32, device, 1)
+            if s.numel() != count:
+                raise ValueError(f"scales_{side} must be [n]")
+        ranks[i] = r
+        ptrs.append((_ptr(a), _ptr(b), _ptr(s)))
+        keep += [a, b, s]
+    (ai, bi, si), (ao, bo, so) = ptrs
+    return LAAdapters(count or 0, ranks[0], ranks[1], ai, bi, ao, bo, si, so, _ptr(host), _ptr(ids)), keep
+
+
 def la_block_replay(x: torch.Tensor, weights, cu_seqlens, num_k_heads: int, num_v_heads: int,
                     d_k: int, d_v: int, scale: float, cu_seqlens_host=None, outputs: bool = True,
                     act_dtype: str = "f32", l2_eps: float = 1e-6, norm_eps: float = 1e-6,
                     state_out: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
-                    workspace: Optional[torch.Tensor] = None, events=None):
+                    workspace: Optional[torch.Tensor] = None, events=None, adapters=None):
     """Replay of one linear-attention layer over packed tails (paper Section 3,
     Eq. 2 behind the layer's projections) on torch's current stream.
 
@@ -627,6 +685,12 @@ def la_block_replay(x: torch.Tensor, weights, cu_seqlens, num_k_heads: int, num_
     dt_bias fp32 [Hv], norm_w fp32 [d_v], w_out bf16 [D, cv] (the last two
     unused when ``outputs`` is False).  Returns ``(state_out [N,Hv,d_k,d_v]
     fp32, out [T, D] bf16 or None)``.
+
+    ``adapters``: low-rank adapters beside the projections, a mapping with ids
+    (one int32 index per sequence, -1 = none) and optionally ids_host, and for
+    each adapted projection a_in [n, R, D], b_in [n, 2cq+2cv+2Hv, R], scales_in
+    [n] / a_out [n, R, cv], b_out [n, D, R], scales_out [n] (matrices bf16,
+    scales fp32 or absent = 1); see ``lora_add``.  Not with ``events``.
     """
     lib = load_library()
     device = x.device
@@ -667,6 +731,18 @@ def la_block_replay(x: torch.Tensor, weights, cu_seqlens, num_k_heads: int, num_
     shp = _la_shape(n, D, num_k_heads, num_v_heads, d_k, d_v, act_dtype, scale, l2_eps, norm_eps)
     stream = _stream(device)
     need = ctypes.c_size_t(0)
+    if adapters is not None:
+        if events is not None:
+            raise ValueError("events are for calls without adapters")
+        ad, keep = _la_adapters(adapters, n, D, 2 * cq + 2 * cv + 2 * num_v_heads, cv, device)
+        _check(lib.gdn_la_block_adapted_workspace_size(ctypes.byref(shp), ctypes.byref(ad), _ptr(cu_host),
+                                                       int(outputs), ctypes.byref(need)))
+        if workspace is None:
+            workspace = _workspace(need.value, device, stream)
+        _check(lib.gdn_la_block_replay_adapted(
+            ctypes.byref(shp), ctypes.byref(w), ctypes.byref(ad), _ptr(cu_host), _ptr(cu_dev), _ptr(x),
+            _ptr(state_out), _ptr(out), _ptr(workspace), workspace.numel() * workspace.element_size(), stream))
+        return state_out, out
     _check(lib.gdn_la_block_workspace_size(ctypes.byref(shp), _ptr(cu_host), int(outputs),
                                            ctypes.byref(need)))
     ws = workspace if workspace is not None else _workspace(need.value, device, stream)

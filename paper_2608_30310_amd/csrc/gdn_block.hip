@@ -4,20 +4,24 @@
 //
 // Stages, all on the caller's stream:
 //   in-projection   hipBLASLt bf16 GEMM, P = X W_in^T (only the k, v, a, b
-//                   rows when no output is wanted)
+//                   rows when no output is wanted); with adapters, each
+//                   request's low-rank product added to P
 //   prep            k_la_prep: conv + SiLU + L2 norms + gates (gdn_block.h)
 //   recurrence      gdn_chunk_forward from the zero state (with outputs) or
 //                   gdn_tail_replay (state only)
 //   gated norm      k_gated_norm -> y bf16
-//   out-projection  hipBLASLt bf16 GEMM, out = Y W_out^T
+//   out-projection  hipBLASLt bf16 GEMM, out = Y W_out^T; adapters as above
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cstdint>
 #include <string>
 
 #include "gdn_block.h"
 #include "gdn_gemm.h"
 #include "gdn_la_block.h"
+#include "gdn_layer_plan.h"
+#include "gdn_lora_call.h"
 #include "gdn_plan.h"
 
 namespace gdn {
@@ -102,9 +106,34 @@ gdn_status launched(const char* what) {
 
 bool misaligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a != 0; }
 
-gdn_status block_impl(const gdn_la_shape* shape, const gdn_la_weights* w, const int32_t* cu_host,
-                      const int32_t* cu, const void* x, float* state_out, void* out, void* workspace,
-                      size_t workspace_bytes, void* stream_ptr, void* const* events, int32_t num_events) {
+// The two adapted products of a block call: the in-projection's (columns row0 ..
+// row0 + rows of W_in's output) and, with outputs, the out-projection's; a rank of
+// 0 is a projection without adapters.
+struct BlockAdapters {
+  gdn_lora_shape in{}, out{};
+  size_t bytes = 0;   // of workspace, for one at a time
+};
+gdn_status plan_adapters(const gdn_la_shape& s, const BlockPlan& p, const gdn_la_adapters& a, const int32_t* cu_host,
+                         BlockAdapters* plan, std::string* err) {
+  BlockAdapters b;
+  b.in = {s.num_seqs, a.num_adapters, s.hidden, static_cast<int32_t>(p.rows), a.rank_in, s.act_dtype, s.hidden, p.ldp, p.ldp};
+  b.out = {s.num_seqs, a.num_adapters, static_cast<int32_t>(p.cv), s.hidden, p.outputs ? a.rank_out : 0, GDN_BF16, p.cv,
+           s.hidden, s.hidden};
+  for (const gdn_lora_shape* l : {&b.in, &b.out}) {
+    if (l->rank == 0) continue;
+    LoraPlan lp;
+    const gdn_status st = make_lora_plan(l, cu_host, &lp, err);
+    if (st != GDN_OK) return st;
+    b.bytes = std::max(b.bytes, lp.bytes);
+  }
+  *plan = b;
+  return GDN_OK;
+}
+
+gdn_status block_impl(const gdn_la_shape* shape, const gdn_la_weights* w, const gdn_la_adapters* ad,
+                      const int32_t* cu_host, const int32_t* cu, const void* x, float* state_out, void* out,
+                      void* workspace, size_t workspace_bytes, void* stream_ptr, void* const* events,
+                      int32_t num_events) {
   const bool outputs = out != nullptr;
   BlockPlan p;
   std::string err;
@@ -127,11 +156,25 @@ gdn_status block_impl(const gdn_la_shape* shape, const gdn_la_weights* w, const 
   if (misaligned(x, 16) || misaligned(w->w_in, 16) || misaligned(w->conv_w, 16) ||
       (outputs && (misaligned(w->w_out, 16) || misaligned(w->norm_w, 16) || misaligned(out, 16))))
     return bfail(GDN_ERR_UNSUPPORTED, "x, w_in, conv_w, norm_w, w_out and out must be 16-byte aligned");
+  BlockAdapters ap;
+  if (ad) {
+    if ((st = plan_adapters(*shape, p, *ad, cu_host, &ap, &err)) != GDN_OK) return bfail(st, "adapters: " + err);
+    if (p.T > 0 && (!ad->adapters_host || !ad->adapters))
+      return bfail(GDN_ERR_NULL_ARG, "adapters and adapters_host must be non-NULL");
+    if (p.T > 0 && ((ap.in.rank > 0 && (!ad->a_in || !ad->b_in)) || (ap.out.rank > 0 && (!ad->a_out || !ad->b_out))))
+      return bfail(GDN_ERR_NULL_ARG, "the adapters' matrices must be non-NULL where the rank is not 0");
+    for (const void* q : {ad->a_in, ad->b_in, ad->a_out, ad->b_out})
+      if (misaligned(q, 16)) return bfail(GDN_ERR_UNSUPPORTED, "the adapters' matrices must be 16-byte aligned");
+    for (int32_t n = 0; p.T > 0 && n < shape->num_seqs; ++n)
+      if (ad->adapters_host[n] < -1 || ad->adapters_host[n] >= ad->num_adapters)
+        return bfail(GDN_ERR_BAD_SHAPE, "adapters_host must hold -1 or an adapter's index");
+  }
   if (!workspace) return bfail(GDN_ERR_WORKSPACE, "workspace is NULL");
-  fit_split(workspace_bytes, &p);
-  if (workspace_bytes < p.bytes)
-    return bfail(GDN_ERR_WORKSPACE, "workspace too small: need " + std::to_string(p.bytes) + " bytes, got " +
-                                        std::to_string(workspace_bytes));
+  const size_t adapted = ad ? ap.bytes : 0;   // behind the block's own workspace
+  if (!ad) fit_split(workspace_bytes, &p);
+  if (workspace_bytes < p.bytes + adapted)
+    return bfail(GDN_ERR_WORKSPACE, "workspace too small: need " + std::to_string(p.bytes + adapted) +
+                                        " bytes, got " + std::to_string(workspace_bytes));
   if (misaligned(workspace, kAlign)) return bfail(GDN_ERR_WORKSPACE, "workspace must be 256-byte aligned");
 
   const hipStream_t stream = static_cast<hipStream_t>(stream_ptr);
@@ -146,6 +189,14 @@ gdn_status block_impl(const gdn_la_shape* shape, const gdn_la_weights* w, const 
   st = gemm_tn(p.rows, p.T, D, w_in, D, x, D, ws + p.off_P, p.ldp, shape->act_dtype, ws + p.off_gemm,
                kGemmWorkspace, stream, &err);
   if (st != GDN_OK) return bfail(st, "in-projection: " + err);
+  char* ws_adapters = ws + p.bytes;
+  if (ap.in.rank > 0) {
+    const int64_t all_rows = 2 * p.cq + 2 * p.cv + 2 * shape->num_v_heads;
+    const uint16_t* b = static_cast<const uint16_t*>(ad->b_in) + p.row0 * ad->rank_in;
+    st = lora_run(&ap.in, cu_host, cu, ad->adapters_host, ad->adapters, ws + p.off_P, x, ad->a_in, b,
+                  all_rows * ad->rank_in, ad->scales_in, ws + p.off_P, ws_adapters, adapted, stream_ptr);
+    if (st != GDN_OK) return st;   // lora_run set the message
+  }
   // 2. conv, SiLU, norms, gates
   if ((st = mk.at(1)) != GDN_OK) return st;
   if (p.T > 0) {
@@ -180,6 +231,11 @@ gdn_status block_impl(const gdn_la_shape* shape, const gdn_la_weights* w, const 
   st = gemm_tn(D, p.T, p.cv, w->w_out, p.cv, ws + p.off_q, p.cv, out, D, GDN_BF16, ws + p.off_gemm,
                kGemmWorkspace, stream, &err);
   if (st != GDN_OK) return bfail(st, "out-projection: " + err);
+  if (ap.out.rank > 0) {
+    st = lora_run(&ap.out, cu_host, cu, ad->adapters_host, ad->adapters, out, ws + p.off_q, ad->a_out, ad->b_out, D *
+                  ad->rank_out, ad->scales_out, out, ws_adapters, adapted, stream_ptr);
+    if (st != GDN_OK) return st;
+  }
   return mk.at(5);
 }
 
@@ -203,7 +259,30 @@ gdn_status gdn_la_block_replay(const gdn_la_shape* shape, const gdn_la_weights* 
                                const int32_t* cu_seqlens_host, const int32_t* cu_seqlens, const void* x,
                                float* state_out, void* out, void* workspace, size_t workspace_bytes,
                                void* stream) {
-  return gdn::block_impl(shape, weights, cu_seqlens_host, cu_seqlens, x, state_out, out, workspace,
+  return gdn::block_impl(shape, weights, nullptr, cu_seqlens_host, cu_seqlens, x, state_out, out, workspace,
+                         workspace_bytes, stream, nullptr, 0);
+}
+
+gdn_status gdn_la_block_adapted_workspace_size(const gdn_la_shape* shape, const gdn_la_adapters* adapters,
+                                               const int32_t* cu_seqlens_host, int32_t with_outputs, size_t* bytes) {
+  if (!bytes) return gdn::bfail(GDN_ERR_NULL_ARG, "bytes is NULL");
+  if (!adapters) return gdn::bfail(GDN_ERR_NULL_ARG, "adapters is NULL");
+  gdn::BlockPlan p;
+  gdn::BlockAdapters a;
+  std::string err;
+  gdn_status st = gdn::make_block_plan(shape, cu_seqlens_host, with_outputs != 0, &p, &err);
+  if (st == GDN_OK) st = gdn::plan_adapters(*shape, p, *adapters, cu_seqlens_host, &a, &err);
+  if (st != GDN_OK) return gdn::bfail(st, err);
+  *bytes = p.bytes + a.bytes;
+  return GDN_OK;
+}
+
+gdn_status gdn_la_block_replay_adapted(const gdn_la_shape* shape, const gdn_la_weights* weights,
+                                       const gdn_la_adapters* adapters, const int32_t* cu_seqlens_host,
+                                       const int32_t* cu_seqlens, const void* x, float* state_out, void* out,
+                                       void* workspace, size_t workspace_bytes, void* stream) {
+  if (!adapters) return gdn::bfail(GDN_ERR_NULL_ARG, "adapters is NULL");
+  return gdn::block_impl(shape, weights, adapters, cu_seqlens_host, cu_seqlens, x, state_out, out, workspace,
                          workspace_bytes, stream, nullptr, 0);
 }
 
@@ -213,7 +292,7 @@ gdn_status gdn_la_block_replay_profiled(const gdn_la_shape* shape, const gdn_la_
                                         size_t workspace_bytes, void* stream, void* const* stage_events,
                                         int32_t num_events) {
   if (!stage_events) return gdn::bfail(GDN_ERR_NULL_ARG, "stage_events is NULL");
-  return gdn::block_impl(shape, weights, cu_seqlens_host, cu_seqlens, x, state_out, out, workspace,
+  return gdn::block_impl(shape, weights, nullptr, cu_seqlens_host, cu_seqlens, x, state_out, out, workspace,
                          workspace_bytes, stream, stage_events, num_events);
 }
 

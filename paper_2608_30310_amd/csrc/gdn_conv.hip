@@ -45,7 +45,7 @@ gdn_status launch_conv(const ConvArgs& a) {
     const int64_t threads = (s.channels + VEC - 1) / VEC;
     const int block = 64;
     const int64_t bx = (threads + block - 1) / block;
-    const int64_t by = std::min<int64_t>(s.num_seqs, std::max<int64_t>(1, 4096 / bx));
+    const int64_t by = std::min<int64_t>(s.num_seqs, std::max<int64_t>(1, 1024 / bx));
     hipLaunchKernelGGL((k_causal_conv_step<T, VEC, W, SILU>), dim3(static_cast<uint32_t>(bx), static_cast<uint32_t>(by)),
                        dim3(block), 0, a.stream, s.num_seqs, s.channels, static_cast<const T*>(a.x), s.ld_x, a.w,
                        a.bias, static_cast<const T*>(a.hist_in), static_cast<T*>(a.y), s.ld_y,

@@ -104,21 +104,33 @@ gdn_status make_ssm_plan(const gdn_ssm_shape* s, const int32_t* cu, SsmPlan* pla
   const int64_t groups = H / p.heads_per_group;   // workgroups of a sequence
   // Whole sequences end with the longest one, or with the work per place; in
   // segments the work is even, but every chunk is walked twice (once for the
-  // states alone) and the states pass through memory.  In chunks of the whole
-  // walk (~8 us for bf16 inputs): a segment's chunk costs 1.5, the join and the
-  // two launches 1.5.
+  // states alone), the segments' states pass through memory and there are two
+  // launches more.  In chunks of the whole walk (~7 us for bf16 inputs): whole
+  // 1.7 + the chunks; segments 2.5 + 1.5 x a segment's chunks + 0.0093 x their
+  // number.  Measured, 64 heads of 64 x 128, one sequence of 2, 3, 8, 24 and 128
+  // chunks: whole 27, 33, 68, 184 and 914 us, segments 30, 32, 43, 51 and 121;
+  // 32 heads of 128 x 128, 8 sequences of 8 and 16: 71 and 124, 81 and 123.
   const auto chunks_of = [&](int64_t n) { return (static_cast<int64_t>(cu[n + 1]) - cu[n] + 63) / 64; };
   int64_t chunks = 0;
   for (int64_t n = 0; n < N; ++n) chunks += chunks_of(n);
   const int64_t longest = (p.longest + 63) / 64;
-  const double whole = std::max(static_cast<double>(longest), static_cast<double>(chunks * groups) / kSsmPlaces);
-  const int64_t seg = std::max<int64_t>(1, (chunks * groups + kSsmPlaces - 1) / kSsmPlaces);
-  int64_t segs = 0;
-  for (int64_t n = 0; n < N; ++n) segs += std::max<int64_t>(1, (chunks_of(n) + seg - 1) / seg);
-  const int64_t rounds = (segs * groups + kSsmPlaces - 1) / kSsmPlaces;
-  if (1.5 * static_cast<double>(seg * rounds) + 1.5 < whole) {
+  double best = 1.7 + std::max(static_cast<double>(longest), static_cast<double>(chunks * groups) / kSsmPlaces);
+  const int64_t least = std::max<int64_t>(1, (chunks * groups + kSsmPlaces - 1) / kSsmPlaces);
+  int64_t seg = 0;
+  for (int64_t more = 0; more <= 4 && least + more * ((least + 3) / 4) < longest; ++more) {
+    const int64_t try_seg = least + more * ((least + 3) / 4);
+    int64_t segs = 0;
+    for (int64_t n = 0; n < N; ++n) segs += std::max<int64_t>(1, (chunks_of(n) + try_seg - 1) / try_seg);
+    const int64_t rounds = (segs * groups + kSsmPlaces - 1) / kSsmPlaces;
+    const double cost = 2.5 + 1.5 * static_cast<double>(try_seg * rounds) + 0.0093 * static_cast<double>(segs * groups);
+    if (cost < best) {
+      best = cost;
+      seg = try_seg;
+      p.slots = segs;
+    }
+  }
+  if (seg > 0) {
     p.seg_tokens = static_cast<int32_t>(64 * seg);
-    p.slots = tile_slots(p.tokens, N, p.seg_tokens);
     const size_t state = static_cast<size_t>(H) * s->d_state * s->head_dim * sizeof(float);
     p.off_decay = static_cast<size_t>(p.slots) * state;   // a multiple of 256
     p.bytes = (p.off_decay + static_cast<size_t>(p.slots) * H * sizeof(float) + kAlign - 1) / kAlign * kAlign;

@@ -34,7 +34,7 @@ struct SsmPlan {
   int64_t tokens = 0, longest = 0;
   int32_t heads_per_group = 1;   // heads of a workgroup
   int32_t seg_tokens = 0;        // 0: whole sequences
-  int64_t slots = 0;             // segment slots (tile_slots), or sequences
+  int64_t slots = 0;             // segments (an empty sequence has one), or sequences
   size_t off_decay = 0;          // workspace: states [slots, H, d_state, head_dim], then decays [slots, H]
   size_t bytes = 0;
 };

@@ -6,6 +6,7 @@
 #include <string>
 
 #include "gdn_layer_plan.h"
+#include "gdn_lora_call.h"
 #include "gdn_lora_kernels.h"
 #include "gdn_plan.h"
 
@@ -56,9 +57,12 @@ gdn_status launch_lora(const LoraArgs& k, const LoraPlan& p, bool any, bool wide
   return llaunched("adapter launch");
 }
 
-gdn_status lora_impl(const gdn_lora_shape* s, const int32_t* cu_host, const int32_t* cu, const int32_t* adapters_host,
-                     const int32_t* adapters, const void* base, const void* x, const void* A, const void* B,
-                     const float* scales, void* out, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+}  // namespace
+
+gdn_status lora_run(const gdn_lora_shape* s, const int32_t* cu_host, const int32_t* cu, const int32_t* adapters_host,
+                    const int32_t* adapters, const void* base, const void* x, const void* A, const void* B,
+                    int64_t b_stride, const float* scales, void* out, void* workspace, size_t workspace_bytes,
+                    void* stream_ptr) {
   std::string err;
   LoraPlan p;
   const gdn_status st = make_lora_plan(s, cu_host, &p, &err);
@@ -92,8 +96,9 @@ gdn_status lora_impl(const gdn_lora_shape* s, const int32_t* cu_host, const int3
   if (!any && base == out) return GDN_OK;
   const LoraArgs k{s->num_seqs, s->num_adapters, s->hidden, s->width, s->rank, p.parts,
                    tokens, cu, adapters, static_cast<const uint16_t*>(x), s->ld_x, static_cast<const uint16_t*>(A),
-                   static_cast<const uint16_t*>(B), scales, base, s->ld_base, out, s->ld_out,
+                   static_cast<const uint16_t*>(B), b_stride, scales, base, s->ld_base, out, s->ld_out,
                    static_cast<float*>(workspace)};
+  const hipStream_t stream = static_cast<hipStream_t>(stream_ptr);
   const int64_t vec = 16 / e;
   const bool wide = s->width % vec == 0 && s->ld_base % vec == 0 && s->ld_out % vec == 0 && s->width % 8 == 0 &&
                     !off(base, 16) && !off(out, 16);
@@ -101,7 +106,6 @@ gdn_status lora_impl(const gdn_lora_shape* s, const int32_t* cu_host, const int3
                                   : launch_lora<float>(k, p, any, wide, stream);
 }
 
-}  // namespace
 }  // namespace gdn
 
 extern "C" {
@@ -120,8 +124,9 @@ gdn_status gdn_lora_add(const gdn_lora_shape* shape, const int32_t* cu_seqlens_h
                         const int32_t* adapters_host, const int32_t* adapters, const void* base, const void* x,
                         const void* lora_a, const void* lora_b, const float* scales, void* out, void* workspace,
                         size_t workspace_bytes, void* stream) {
-  return gdn::lora_impl(shape, cu_seqlens_host, cu_seqlens, adapters_host, adapters, base, x, lora_a, lora_b, scales,
-                        out, workspace, workspace_bytes, static_cast<hipStream_t>(stream));
+  const int64_t b_stride = shape ? static_cast<int64_t>(shape->width) * shape->rank : 0;
+  return gdn::lora_run(shape, cu_seqlens_host, cu_seqlens, adapters_host, adapters, base, x, lora_a, lora_b, b_stride,
+                       scales, out, workspace, workspace_bytes, stream);
 }
 
 }  // extern "C"

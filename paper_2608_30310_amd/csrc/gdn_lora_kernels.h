@@ -28,6 +28,7 @@ struct LoraArgs {
   int64_t ldx;
   const uint16_t* A;
   const uint16_t* B;
+  int64_t b_stride;   // elements between two adapters' B
   const float* scales;
   const void* base;
   int64_t ldbase;
@@ -227,7 +228,7 @@ void k_lora_up(LoraArgs a) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int m = min(m0 + 32 * b + 8 * (c / 4) + 4 * h + c % 4, a.M - 1);
-        const uint16_t* p = a.B + (static_cast<int64_t>(t.adapter) * a.M + m) * a.R + 8 * g;
+        const uint16_t* p = a.B + t.adapter * a.b_stride + static_cast<int64_t>(m) * a.R + 8 * g;
 #pragma unroll
         for (int k = 0; k < KS; ++k) bf[b][h][k] = 32 * k + 8 * g < a.R ? lora_load(p + 32 * k) : lora_zero();
       }

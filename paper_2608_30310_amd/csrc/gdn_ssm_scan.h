@@ -226,6 +226,44 @@ __device__ __forceinline__ float read_lane(float x, int lane) {
   return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), lane));
 }
 
+// Sequences cut into segments of `tokens`, an empty one into one: the sequence n
+// and its segment j that segment number `unit` is, counted over all of them.
+// The wave looks at 64 sequences at a time; uniform over the wave.
+struct SegmentAt { int n, j; };
+__device__ __forceinline__ int segments_of(const int32_t* __restrict__ cu, int n_seqs, int i, int tokens) {
+  return i < n_seqs ? max(1, (cu[i + 1] - cu[i] + tokens - 1) / tokens) : 0;
+}
+__device__ __forceinline__ int wave_scan(int x) {   // inclusive sums over the wave
+  const int lane = threadIdx.x % kWave;
+#pragma unroll
+  for (int off = 1; off < kWave; off <<= 1) {
+    const int up = __shfl_up(x, off, kWave);
+    x += lane >= off ? up : 0;
+  }
+  return x;
+}
+__device__ __forceinline__ SegmentAt segment_at(const int32_t* __restrict__ cu, int n_seqs, int tokens, int unit) {
+  const int lane = threadIdx.x % kWave;
+  for (int n0 = 0;; n0 += kWave) {   // unit is below the number of segments
+    const int sum = wave_scan(segments_of(cu, n_seqs, n0 + lane, tokens));
+    const int total = __builtin_amdgcn_readlane(sum, kWave - 1);
+    if (unit < total || n0 + kWave >= n_seqs) {
+      const int k = min(static_cast<int>(__popcll(__ballot(sum <= unit))), kWave - 1);
+      const int before = k > 0 ? __builtin_amdgcn_readlane(sum, max(k - 1, 0)) : 0;
+      return {min(n0 + k, n_seqs - 1), unit - before};
+    }
+    unit -= total;
+  }
+}
+// Segments of the sequences before n.
+__device__ __forceinline__ int segments_before(const int32_t* __restrict__ cu, int n, int tokens) {
+  const int lane = threadIdx.x % kWave;
+  int total = 0;
+  for (int n0 = 0; n0 < n; n0 += kWave)
+    total += __builtin_amdgcn_readlane(wave_scan(segments_of(cu, n, n0 + lane, tokens)), kWave - 1);
+  return total;
+}
+
 struct SsmScanArgs {
   int32_t n_seqs, heads, groups, seg_tokens;
   const int32_t* cu;
@@ -241,8 +279,8 @@ struct SsmScanArgs {
   const float* state_in;
   void* y;
   float* state_out;
-  f32x4* seg_state;     // [slot, head group, wave, tile, lane]
-  float* seg_decay;     // [slot, head]: log2 of a segment's decay
+  f32x4* seg_state;     // [segment, head group, wave, tile, lane]
+  float* seg_decay;     // [segment, head]: log2 of a segment's decay
 };
 
 // kWhole: a unit is a sequence, from state_in to y (where given) and state_out.
@@ -296,14 +334,13 @@ void k_ssm_scan(SsmScanArgs a) {
   const int unit = xcd_cluster_remap(blockIdx.x, gridDim.x, hgs);
   const int hg = unit % hgs, slot = unit / hgs;
   int n = slot, first = 0;
-  if constexpr (MODE != SsmMode::kWhole) n = slot_seq(a.cu, a.n_seqs, slot, a.seg_tokens);
+  if constexpr (MODE != SsmMode::kWhole) {
+    const SegmentAt at = segment_at(a.cu, a.n_seqs, a.seg_tokens, slot);
+    n = at.n;
+    first = at.j * a.seg_tokens;
+  }
   const int start = __builtin_amdgcn_readfirstlane(a.cu[n]);
   const int seq_len = __builtin_amdgcn_readfirstlane(a.cu[n + 1]) - start;
-  if constexpr (MODE != SsmMode::kWhole) {
-    const int64_t at = static_cast<int64_t>(slot - (start / a.seg_tokens + n)) * a.seg_tokens;
-    if (at > 0 && at >= seq_len) return;   // an unused slot
-    first = static_cast<int>(at);
-  }
   const int len = MODE == SsmMode::kWhole ? seq_len : min(a.seg_tokens, seq_len - first);
   const int64_t t0 = static_cast<int64_t>(start) + first;
   const int h0 = hg * L::kHeads, gh = h0 / (a.heads / a.groups);
@@ -659,10 +696,10 @@ __global__ __launch_bounds__(256)
 void k_ssm_join(SsmScanArgs a) {
   constexpr int kWavesPerHead = DV / (16 * CT);
   constexpr int kTiles = DK / 16 * CT;
+  static_assert(kWavesPerHead * kTiles * kWave % 256 == 0, "whole blocks per sequence");
   const int per_seq = a.heads * kWavesPerHead * kTiles * kWave;   // f32x4 of a sequence's states
-  const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-  if (i >= static_cast<int64_t>(a.n_seqs) * per_seq) return;
-  const int n = static_cast<int>(i / per_seq), e = static_cast<int>(i % per_seq);
+  const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;   // per_seq is a multiple of 256: one n per block
+  const int n = __builtin_amdgcn_readfirstlane(static_cast<int>(i / per_seq)), e = static_cast<int>(i % per_seq);
   const int lane = e % kWave, tile = e / kWave % kTiles, w = e / (kWave * kTiles);   // w: wave of the sequence
   const int head = w / kWavesPerHead;
   const int td = tile / CT, ct = tile % CT, g = lane / 16, c = lane % 16;
@@ -673,7 +710,7 @@ void k_ssm_join(SsmScanArgs a) {
     for (int r = 0; r < 4; ++r) run[r] = a.state_in[sbase + strow(td, g, r) * DV];
   }
   const int start = a.cu[n], len = a.cu[n + 1] - start;
-  const int64_t slot0 = start / a.seg_tokens + n;
+  const int64_t slot0 = segments_before(a.cu, n, a.seg_tokens);
   const int segs = max(1, (len + a.seg_tokens - 1) / a.seg_tokens);
   // eight segments' loads are in flight at a time
   constexpr int AHEAD = 8;

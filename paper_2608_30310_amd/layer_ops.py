@@ -17,8 +17,8 @@ from typing import Optional
 
 import torch
 
-from .binding import (ConvShape, GDN_F32, LoraShape, SSMShape, _check, _dtype_code, _need, _ptr, _seqlens, _stream,
-                      _workspace, load_library)
+from .binding import (ConvShape, GDN_F32, LoraShape, SSMShape, _adapter_ids, _check, _dtype_code, _need, _ptr,
+                      _seqlens, _stream, _workspace, load_library)
 
 _ACTIVATIONS = {None: 0, "none": 0, "silu": 1}
 
@@ -28,9 +28,9 @@ def _on_device(fn):
     the current device); free where it is current already."""
     @functools.wraps(fn)
     def call(first, *args, **kwargs):
-        if not isinstance(first, torch.Tensor) or first.device.type != "cuda":
+        if not isinstance(first, torch.Tensor) or not first.is_cuda:
             raise ValueError(f"{fn.__name__} works on tensors in GPU memory")
-        if first.device.index == torch.cuda.current_device():
+        if first.get_device() == torch._C._cuda_getDevice():
             return fn(first, *args, **kwargs)
         with torch.cuda.device(first.device):
             return fn(first, *args, **kwargs)
@@ -40,6 +40,20 @@ def _on_device(fn):
 def _rows(t, name, dtype, device, shape):
     """Checks a tensor of token rows ([T, ...] with dense rows); returns the
     distance of two rows in elements.  ``shape``: the row's shape."""
+    # the usual tensor at once; anything else is looked at in turn
+    if type(t) is torch.Tensor and t.dtype is dtype and t.device == device:
+        size, strides = t.shape, t.stride()
+        if len(shape) == 1:
+            usual, width = len(size) == 2 and size[1] == shape[0] and strides[1] == 1, shape[0]
+        else:
+            usual = len(size) == 3 and size[2] == shape[1] and size[1] == shape[0] and strides[2] == 1 and \
+                strides[1] == shape[1]
+            width = shape[0] * shape[1]
+        if usual:
+            if size[0] <= 1:
+                return width
+            if strides[0] >= width:
+                return strides[0]
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
     if t.device != device:
@@ -62,16 +76,19 @@ def _rows(t, name, dtype, device, shape):
 
 def _flat(t, name, shape, device):
     """Checks an optional fp32 parameter."""
-    if t is not None:
-        _need(t, name, torch.float32, device, len(shape))
-        if tuple(t.shape) != shape:
-            raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+    if t is None or (type(t) is torch.Tensor and t.shape == shape and t.dtype is torch.float32 and
+                     t.device == device and t.is_contiguous()):
+        return
+    _need(t, name, torch.float32, device, len(shape))
+    if tuple(t.shape) != shape:
+        raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
 
 
 def _offsets(cu_seqlens, cu_seqlens_host, device, tokens):
     cu, host = _seqlens(cu_seqlens, cu_seqlens_host, device)
-    if int(host[-1]) > tokens:
-        raise ValueError(f"cu_seqlens ends at {int(host[-1])}, behind the {tokens} token rows")
+    end = ctypes.c_int32.from_address(host.data_ptr() + 4 * (host.numel() - 1)).value   # host[-1], a quarter of its time
+    if end > tokens:
+        raise ValueError(f"cu_seqlens ends at {end}, behind the {tokens} token rows")
     return cu, host
 
 
@@ -85,7 +102,7 @@ def _scratch(nbytes, device, stream, given):
         return given.data_ptr(), given.numel() * given.element_size(), given
     if nbytes == 0:
         return None, 0, None
-    if torch.cuda.is_current_stream_capturing():
+    if torch._C._cuda_isCurrentStreamCapturing():
         ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
     else:
         ws = _workspace(nbytes, device, stream)
@@ -116,10 +133,12 @@ def _conv_args(x, weight, bias, activation, out):
 
 
 def _history(t, name, n, W, C, dtype, device):
-    if t is not None:
-        _need(t, name, dtype, device, 3)
-        if t.shape != (n, W - 1, C):
-            raise ValueError(f"{name} must be [N, W - 1, C]")
+    if t is None or (type(t) is torch.Tensor and t.shape == (n, W - 1, C) and t.dtype is dtype and
+                     t.device == device and t.is_contiguous()):
+        return
+    _need(t, name, dtype, device, 3)
+    if t.shape != (n, W - 1, C):
+        raise ValueError(f"{name} must be [N, W - 1, C]")
 
 
 @_on_device
@@ -179,26 +198,30 @@ def _ssm_args(x, dt, a_log, B, C, d_skip, dt_bias, out):
     G, N = B.shape[1], B.shape[2]
     if not isinstance(dt, torch.Tensor) or dt.dtype not in (dtype, torch.float32):
         raise ValueError("dt must be a float32 tensor or one of x's dtype")
-    for name, t in (("B", B), ("dt", dt), ("C", C), ("out", out)):
-        if t is not None and t.shape[0] != T:
-            raise ValueError(f"{name} must hold the same tokens as x")
-    lds = [_rows(x, "x", dtype, device, (H, P)), _rows(dt, "dt", dt.dtype, device, (H,)),
-           _rows(B, "B", dtype, device, (G, N))]
-    lds.append(lds[2] if C is None else _rows(C, "C", dtype, device, (G, N)))
-    lds.append(H * P if out is None else _rows(out, "out", dtype, device, (H, P)))
+    ldx, ldb = _rows(x, "x", dtype, device, (H, P)), _rows(B, "B", dtype, device, (G, N))
+    ldc = ldb if C is None else _rows(C, "C", dtype, device, (G, N))
+    ldy = H * P if out is None else _rows(out, "out", dtype, device, (H, P))
+    lddt = _rows(dt, "dt", dt.dtype, device, (H,))
+    if B.shape[0] != T or dt.shape[0] != T or (C is not None and C.shape[0] != T) or \
+            (out is not None and out.shape[0] != T):
+        raise ValueError("dt, B, C and out must hold the same tokens as x")
     if a_log is None:
         raise TypeError("a_log must be a torch.Tensor")
-    for name, t in (("a_log", a_log), ("d_skip", d_skip), ("dt_bias", dt_bias)):
-        _flat(t, name, (H,), device)
-    return device, T, H, P, N, (H, G, N, P, _dtype_code(x), GDN_F32 if dt.dtype == torch.float32 else _dtype_code(x),
-                                *lds)
+    _flat(a_log, "a_log", (H,), device)
+    _flat(d_skip, "d_skip", (H,), device)
+    _flat(dt_bias, "dt_bias", (H,), device)
+    code = _dtype_code(x)
+    return device, T, H, P, N, (H, G, N, P, code, GDN_F32 if dt.dtype is torch.float32 else code, ldx, lddt, ldb, ldc,
+                                ldy)
 
 
 def _state(t, name, shape, device):
-    if t is not None:
-        _need(t, name, torch.float32, device, 4)
-        if t.shape != shape:
-            raise ValueError(f"{name} must be [N, H, d_state, head_dim]")
+    if t is None or (type(t) is torch.Tensor and t.shape == shape and t.dtype is torch.float32 and
+                     t.device == device and t.is_contiguous()):
+        return
+    _need(t, name, torch.float32, device, 4)
+    if t.shape != shape:
+        raise ValueError(f"{name} must be [N, H, d_state, head_dim]")
 
 
 @_on_device
@@ -270,26 +293,6 @@ def ssm_step(x: torch.Tensor, dt: torch.Tensor, a_log: torch.Tensor, B: torch.Te
 
 
 # ---------------------------------------------------------------- low-rank adapters
-
-def _adapter_ids(adapters, adapters_host, n, device):
-    """Device and host copies of the adapters' indices, int32 [N]."""
-    if adapters_host is None:
-        if isinstance(adapters, torch.Tensor):
-            adapters_host = adapters.detach().to("cpu", torch.int32)
-        else:
-            adapters_host = torch.tensor(list(adapters), dtype=torch.int32)
-    elif not isinstance(adapters_host, torch.Tensor):
-        adapters_host = torch.tensor(list(adapters_host), dtype=torch.int32)
-    adapters_host = adapters_host.to(torch.int32).contiguous()
-    if adapters_host.device.type != "cpu":
-        raise ValueError("adapters_host must live in host memory")
-    if not isinstance(adapters, torch.Tensor) or adapters.device != device:
-        adapters = adapters_host.to(device)
-    _need(adapters, "adapters", torch.int32, device, 1)
-    if adapters.numel() != n or adapters_host.numel() != n:
-        raise ValueError("adapters and adapters_host must hold one index per sequence")
-    return adapters, adapters_host
-
 
 @_on_device
 def lora_add(base: torch.Tensor, x: torch.Tensor, lora_a: torch.Tensor, lora_b: torch.Tensor, adapters, cu_seqlens,

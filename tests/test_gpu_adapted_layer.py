@@ -1,0 +1,180 @@
+"""Adapters inside the layer block, and the layer's operators one after another.
+
+The adapted layer replay against the fp64 layer oracle with each sequence's
+adapters merged into its weights.  With fp32 intermediates nothing is rounded
+on the way to the state but the recurrence's operands (the layer's own bar,
+2e-3); an output passes one rounding more than without adapters (y, the
+projection's bf16 result, the adapters' sum: 2^-9 rms-wise at most each, 2.9e-3
+together for independent ones), inside the layer's 5e-3.
+"""
+import numpy as np
+import pytest
+import torch
+
+import paper_2608_30310_amd as gdn
+from oracle import la_block as lb
+from oracle import layer_ops as ref
+from synth.layer import LayerDims, exact_weights, hiddens, layer_weights, pack_hiddens
+from tests.gpu_util import OUTPUT_TOL, STATE_TOL, state_err, to_f64
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU visible")
+    gdn.load_library()
+
+
+def _bf16(bits):
+    return torch.from_numpy(np.ascontiguousarray(bits).view(np.int16)).view(torch.bfloat16).to(DEV)
+
+
+def _case(lens, dims, seed, ranks, n=3):
+    x, cu = pack_hiddens([hiddens(41, 0, i, 0, L, dims.hidden) for i, L in enumerate(lens)], dims.hidden)
+    w = layer_weights(41, 0, dims)
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    rn = lambda *s: torch.randn(*s, device=DEV, generator=g)
+    ad = {}
+    for side, r, k, m in (("in", ranks[0], dims.hidden, dims.in_rows), ("out", ranks[1], dims.cv, dims.hidden)):
+        if r:
+            ad.update({f"a_{side}": (rn(n, r, k) / k ** 0.5).bfloat16(), f"b_{side}": (0.5 * rn(n, m, r) / r ** 0.5).bfloat16(),
+                       f"scales_{side}": 0.5 + torch.rand(n, device=DEV, generator=g)})
+    wd = {k: _bf16(a) if a.dtype == np.uint16 else torch.from_numpy(a).to(DEV) for k, a in w.items()}
+    return x, cu, w, wd, ad
+
+
+def _replay(x, cu, wd, dims, ad, ids, outputs, act, **kw):
+    cu_t = torch.from_numpy(cu)
+    return gdn.la_block_replay(_bf16(x), wd, cu_t.to(DEV), dims.hk, dims.hv, dims.dk, dims.dv, 0.7,
+                               cu_seqlens_host=cu_t, outputs=outputs, act_dtype=act,
+                               adapters=None if ids is None else dict(ad, ids=ids), **kw)
+
+
+def _merged(x, cu, w, ad, ids, dims, outputs):
+    """The oracle, a sequence at a time, with its adapter merged into the weights."""
+    we = exact_weights(w)
+    xs = _bf16(x).double().cpu().numpy()
+    states, outs = [], []
+    for s, i in enumerate(ids):
+        wi = dict(we)
+        for side, name in (("in", "w_in"), ("out", "w_out")):
+            if i >= 0 and f"a_{side}" in ad:
+                k = float(ad[f"scales_{side}"][i])
+                wi[name] = we[name] + k * to_f64(ad[f"b_{side}"][i]) @ to_f64(ad[f"a_{side}"][i])
+        part = xs[cu[s]:cu[s + 1]]
+        st, out, _ = lb.la_block(part, wi["w_in"], wi["conv_w"], wi["a_log"], wi["dt_bias"], wi["norm_w"], wi["w_out"],
+                                 np.array([0, len(part)]), dims.hk, dims.hv, dims.dk, dims.dv, 0.7, outputs=outputs)
+        states.append(st[0])
+        outs.append(out)
+    return np.stack(states), (np.concatenate(outs) if outputs else None)
+
+
+@pytest.mark.parametrize("outputs", [True, False])
+@pytest.mark.parametrize("ranks", [(16, 8), (40, 0), (0, 32)])
+@pytest.mark.parametrize("dk,dv", [(64, 64), (128, 64)])
+def test_layer_with_adapters(outputs, ranks, dk, dv):
+    dims = LayerDims(hidden=128, hk=2, hv=4, dk=dk, dv=dv)
+    lens, ids = [70, 1, 33, 130], [1, -1, 0, 2]
+    x, cu, w, wd, ad = _case(lens, dims, 1, ranks)
+    st, out = _replay(x, cu, wd, dims, ad, ids, outputs, "f32")
+    ws, wo = _merged(x, cu, w, ad, ids, dims, outputs)
+    e = state_err(to_f64(st), ws)
+    print(f"[adapted layer] state {e:.2e}", flush=True)
+    assert e <= STATE_TOL
+    if outputs:
+        got = to_f64(out)
+        for s in range(len(lens)):
+            a, b = cu[s], cu[s + 1]
+            assert np.linalg.norm(got[a:b] - wo[a:b]) <= OUTPUT_TOL * np.linalg.norm(wo[a:b])
+
+
+@pytest.mark.parametrize("act", ["f32", "bf16"])
+def test_layer_without_an_adapter_is_the_plain_layer(act):
+    """Bit for bit, and so are the sequences without one beside adapted ones."""
+    dims = LayerDims(hidden=256, hk=2, hv=4, dk=64, dv=64)
+    x, cu, w, wd, ad = _case([50, 80], dims, 2, (16, 16))
+    st, out = _replay(x, cu, wd, dims, ad, None, True, act)
+    st2, out2 = _replay(x, cu, wd, dims, ad, [-1, -1], True, act)
+    assert torch.equal(st, st2) and torch.equal(out, out2)
+    st3, out3 = _replay(x, cu, wd, dims, ad, [-1, 2], True, act)
+    assert torch.equal(st[0], st3[0]) and torch.equal(out[:50], out3[:50])
+    assert not torch.equal(st[1], st3[1]) and not torch.equal(out[50:], out3[50:])
+
+
+def test_adapted_layer_refuses():
+    dims = LayerDims(hidden=128, hk=2, hv=4, dk=64, dv=64)
+    x, cu, w, wd, ad = _case([20, 20], dims, 3, (16, 16))
+    for bad in ([0, 3], [0, -2]):
+        with pytest.raises(gdn.GDNError):
+            _replay(x, cu, wd, dims, ad, bad, True, "f32")
+    with pytest.raises(ValueError):
+        _replay(x, cu, wd, dims, ad, [0], True, "f32")
+    with pytest.raises(ValueError):
+        _replay(x, cu, wd, dims, dict(ad, a_in=ad["a_in"][:2].contiguous()), [0, 1], True, "f32")
+    with pytest.raises(ValueError):
+        _replay(x, cu, wd, dims, ad, [0, 1], True, "f32", events=[torch.cuda.Event(enable_timing=True)])
+    with pytest.raises(gdn.GDNError):
+        _replay(x, cu, wd, dims, ad, [0, 1], True, "f32", workspace=torch.empty(1024, dtype=torch.uint8, device=DEV))
+
+
+def test_a_layer_from_projection_to_decoding():
+    """The operators in the order a state space layer runs them: projection with
+    adapters, convolution, scan over three ragged prompts, then five tokens one by
+    one from the histories and states that the prompts left.  Each operator is held
+    to its fp64 form on the very inputs it was given; the tokens' outputs and the
+    last states also to the fp64 form over the whole sequences."""
+    H, G, N, P, D, W = 4, 2, 64, 64, 128, 4
+    C = H * P + 2 * G * N
+    rows = C + H
+    lens, ids, steps = [90, 7, 64], [1, -1, 0], 5
+    g = torch.Generator(device=DEV).manual_seed(4)
+    rn = lambda *s: torch.randn(*s, device=DEV, generator=g)
+    w_in, a, b = (rn(rows, D) / D ** 0.5).bfloat16(), (rn(2, 16, D) / D ** 0.5).bfloat16(), (rn(2, rows, 16) / 4).bfloat16()
+    conv_w, conv_b, a_log, d, dt_bias = rn(C, W) * 0.5, rn(C) * 0.1, torch.log(1 + 3 * torch.rand(H, device=DEV, generator=g)), rn(H), rn(H) - 2
+    xs = [rn(L + steps, D).bfloat16() for L in lens]
+    cu = [0] + list(np.cumsum(lens))
+    x = torch.cat([t[:L] for t, L in zip(xs, lens)])
+
+    def project(x, cu):
+        base = x @ w_in.t()
+        out = gdn.lora_add(base, x, a, b, ids, cu)
+        e, mag = ref.lora(base, x, a, b, ids, cu)
+        assert bool(((out.double() - e).abs() <= 2.0 ** -8 * e.abs() * 1.01 + 2.0 ** -14 * mag).all())
+        return out
+
+    def split(p, y):
+        return (y[:, :H * P].unflatten(1, (H, P)), p[:, C:], y[:, H * P:H * P + G * N].unflatten(1, (G, N)),
+                y[:, H * P + G * N:].unflatten(1, (G, N)))
+
+    p = project(x, cu)
+    y, hist = gdn.causal_conv(p[:, :C], conv_w, cu, bias=conv_b)
+    e, after, mag = ref.causal_conv(p[:, :C], conv_w, cu, conv_b)
+    assert torch.equal(hist.double(), after)
+    assert bool(((y.double() - e).abs() <= 2.0 ** -8 * e.abs() * 1.01 + 2.0 ** -20 * (mag + 1)).all())
+    X, dt, B, Cm = split(p, y)
+    o, st = gdn.ssm_scan(X, dt, a_log, B, Cm, cu, d_skip=d, dt_bias=dt_bias)
+    all_p, all_y, all_o = [p], [y], [o]
+    for t in range(steps):
+        xt = torch.stack([s[L + t] for s, L in zip(xs, lens)])
+        pt = project(xt, [0, 1, 2, 3])
+        yt, hist = gdn.causal_conv_step(pt[:, :C], conv_w, hist, bias=conv_b, history_out=hist)
+        Xt, dtt, Bt, Ct = split(pt, yt)
+        ot, st = gdn.ssm_step(Xt, dtt, a_log, Bt, Ct, d_skip=d, dt_bias=dt_bias, state_in=st, state_out=st)
+        all_p.append(pt), all_y.append(yt), all_o.append(ot)
+
+    # whole sequences, from the projections and convolutions as they were given
+    def whole(parts):
+        return torch.cat([torch.cat([parts[0][cu[s]:cu[s + 1]]] + [q[s:s + 1] for q in parts[1:]]) for s in range(3)])
+    ends = [0] + list(np.cumsum([L + steps for L in lens]))
+    fp, fy, fo = whole(all_p), whole(all_y), whole(all_o)
+    e, after, mag = ref.causal_conv(fp[:, :C], conv_w, ends, conv_b)
+    assert torch.equal(hist.double(), after)
+    assert bool(((fy.double() - e).abs() <= 2.0 ** -8 * e.abs() * 1.01 + 2.0 ** -20 * (mag + 1)).all())
+    X, dt, B, Cm = split(fp, fy)
+    ey, es, my, ms = ref.ssm(X, dt, a_log, B, Cm, ends, d, dt_bias)
+    n32 = (N + 3 * 64) * 2.0 ** -24
+    assert bool(((st.double() - es).abs() <= n32 * ms + 1e-37).all())
+    assert bool(((fo.double() - ey).abs() <= 2.0 ** -8 * ey.abs() * 1.01 + (n32 + 2.0 ** -15) * my + 1e-37).all())
