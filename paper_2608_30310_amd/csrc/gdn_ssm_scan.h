@@ -29,18 +29,12 @@ constexpr int kSsmChunk = 64;
 template <typename T>
 struct Mx;
 
-// x rounded to a bf16 pair, and what the rounding left of it: exact, one
-// instruction per value (a dot product of the pair with (-1, 0) or (0, -1) added
-// to the value; the multiplier stays out of the instruction's inline constants,
-// whose packed form the compiler takes in the wrong half).
+// x rounded to a bf16 pair, and what the rounding left of it (exact).
 __device__ __forceinline__ uint32_t round_pair(f32x2& x) {
-  uint32_t first, second;
-  asm("s_mov_b32 %0, 0xbf80" : "=s"(first));
-  asm("s_mov_b32 %0, 0xbf800000" : "=s"(second));
-  const bf16x2 h = __builtin_convertvector(x, bf16x2);
-  x[0] = __builtin_amdgcn_fdot2_f32_bf16(h, __builtin_bit_cast(bf16x2, first), x[0], false);
-  x[1] = __builtin_amdgcn_fdot2_f32_bf16(h, __builtin_bit_cast(bf16x2, second), x[1], false);
-  return __builtin_bit_cast(uint32_t, h);
+  const uint32_t h = __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
+  x[0] -= __uint_as_float(h << 16);
+  x[1] -= __uint_as_float(h & 0xFFFF0000u);
+  return h;
 }
 __device__ __forceinline__ uint32_t last_pair(const f32x2& x) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
