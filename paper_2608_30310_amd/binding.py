@@ -628,6 +628,12 @@ def la_block_workspace_size(hidden: int, num_k_heads: int, num_v_heads: int, d_k
 
 def _adapter_ids(adapters, adapters_host, n, device):
     """Device and host copies of the adapters' indices, int32 [N]."""
+    # both in hand and as the library reads them: nothing to convert
+    if type(adapters) is torch.Tensor and type(adapters_host) is torch.Tensor and adapters.dtype is torch.int32 and \
+            adapters_host.dtype is torch.int32 and adapters_host.is_cpu and adapters.device == device and \
+            adapters.shape == (n,) and adapters_host.shape == (n,) and adapters.is_contiguous() and \
+            adapters_host.is_contiguous():
+        return adapters, adapters_host
     if adapters_host is None:
         if isinstance(adapters, torch.Tensor):
             adapters_host = adapters.detach().to("cpu", torch.int32)

@@ -18,7 +18,9 @@ from typing import Optional
 import torch
 
 from .binding import (ConvShape, GDN_F32, LoraShape, SSMShape, _adapter_ids, _check, _dtype_code, _need, _ptr,
-                      _seqlens, _stream, _workspace, load_library)
+                      _seqlens, _stream, _workspace, _WORKSPACES, load_library)
+
+GDN_ERR_WORKSPACE = 5
 
 _ACTIVATIONS = {None: 0, "none": 0, "silu": 1}
 
@@ -92,21 +94,31 @@ def _offsets(cu_seqlens, cu_seqlens_host, device, tokens):
     return cu, host
 
 
-def _scratch(nbytes, device, stream, given):
-    """The caller's workspace, or the one kept per (device, stream).  A call
-    that is being captured takes memory of its graph's own pool instead: no
-    other graph shares it, and no later call outside can replace it."""
+def _run_with_workspace(call, size, shape, host, device, stream, given):
+    """``call(workspace, its bytes)`` with the caller's workspace, or with the one
+    kept per (device, stream); the library refuses a workspace that is too small
+    before it enqueues anything, and only then its size is asked for.  A call
+    that is being captured takes memory of its graph's own pool instead: no other
+    graph shares it, and no later call outside can replace it."""
     if given is not None:
         if not isinstance(given, torch.Tensor) or given.device != device or not given.is_contiguous():
             raise ValueError(f"workspace must be a contiguous tensor on {device}")
-        return given.data_ptr(), given.numel() * given.element_size(), given
-    if nbytes == 0:
-        return None, 0, None
+        _check(call(given.data_ptr(), given.numel() * given.element_size()))
+        return
+    kept = None
+    if not torch._C._cuda_isCurrentStreamCapturing():
+        kept = _WORKSPACES.get((device.index, stream))
+        status = call(None, 0) if kept is None else call(kept.data_ptr(), kept.numel())
+        if status != GDN_ERR_WORKSPACE:
+            _check(status)
+            return
+    need = ctypes.c_size_t(0)
+    _check(size(ctypes.byref(shape), host, ctypes.byref(need)))
     if torch._C._cuda_isCurrentStreamCapturing():
-        ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        ws = torch.empty(max(need.value, 256), dtype=torch.uint8, device=device)
     else:
-        ws = _workspace(nbytes, device, stream)
-    return ws.data_ptr(), ws.numel(), ws
+        ws = _workspace(need.value, device, stream)
+    _check(call(ws.data_ptr(), ws.numel()))
 
 
 # ---------------------------------------------------------------- short convolution
@@ -165,8 +177,9 @@ def causal_conv(x: torch.Tensor, weight: torch.Tensor, cu_seqlens, cu_seqlens_ho
     if write_history and history_out is None:
         history_out = torch.empty((n, max(W - 1, 0), C), dtype=x.dtype, device=device)
     _history(history_out, "history_out", n, W, C, x.dtype, device)
-    _check(lib.gdn_causal_conv(ctypes.byref(ConvShape(n, *shape)), _ptr(host), _ptr(cu), _ptr(x), _ptr(weight),
-                               _ptr(bias), _ptr(history_in), _ptr(out), _ptr(history_out), _stream(device)))
+    _check(lib.gdn_causal_conv(ctypes.byref(ConvShape(n, *shape)), host.data_ptr(), cu.data_ptr(), x.data_ptr(),
+                               weight.data_ptr(), _ptr(bias), _ptr(history_in), out.data_ptr(), _ptr(history_out),
+                               _stream(device)))
     return out, history_out
 
 
@@ -183,8 +196,9 @@ def causal_conv_step(x: torch.Tensor, weight: torch.Tensor, history_in: Optional
     if history_out is None:
         history_out = torch.empty((n, max(W - 1, 0), C), dtype=x.dtype, device=device)
     _history(history_out, "history_out", n, W, C, x.dtype, device)
-    _check(lib.gdn_causal_conv_step(ctypes.byref(ConvShape(n, *shape)), _ptr(x), _ptr(weight), _ptr(bias),
-                                    _ptr(history_in), _ptr(out), _ptr(history_out), _stream(device)))
+    _check(lib.gdn_causal_conv_step(ctypes.byref(ConvShape(n, *shape)), x.data_ptr(), weight.data_ptr(),
+                                    _ptr(bias), _ptr(history_in), out.data_ptr(), history_out.data_ptr(),
+                                    _stream(device)))
     return out, history_out
 
 
@@ -260,12 +274,11 @@ def ssm_scan(x: torch.Tensor, dt: torch.Tensor, a_log: torch.Tensor, B: torch.Te
     _state(state_out, "state_out", (n, H, N, P), device)
     shp = SSMShape(n, *shape)
     stream = _stream(device)
-    need = ctypes.c_size_t(0)
-    _check(lib.gdn_ssm_workspace_size(ctypes.byref(shp), _ptr(host), ctypes.byref(need)))
-    ws, nbytes, keep = _scratch(need.value, device, stream, workspace)
-    _check(lib.gdn_ssm_scan(ctypes.byref(shp), _ptr(host), _ptr(cu), _ptr(x), _ptr(dt), _ptr(a_log), _ptr(B), _ptr(C),
-                            _ptr(d_skip), _ptr(dt_bias), _ptr(state_in), _ptr(out), _ptr(state_out), ws, nbytes,
-                            stream))
+    lens = host.data_ptr()
+    args = (ctypes.byref(shp), lens, cu.data_ptr(), x.data_ptr(), dt.data_ptr(), a_log.data_ptr(), B.data_ptr(), _ptr(C),
+            _ptr(d_skip), _ptr(dt_bias), _ptr(state_in), _ptr(out), _ptr(state_out))
+    _run_with_workspace(lambda ws, nbytes: lib.gdn_ssm_scan(*args, ws, nbytes, stream), lib.gdn_ssm_workspace_size, shp,
+                        lens, device, stream, workspace)
     return out, state_out
 
 
@@ -286,9 +299,9 @@ def ssm_step(x: torch.Tensor, dt: torch.Tensor, a_log: torch.Tensor, B: torch.Te
     if state_out is None:
         state_out = torch.empty((n, H, N, P), dtype=torch.float32, device=device)
     _state(state_out, "state_out", (n, H, N, P), device)
-    _check(lib.gdn_ssm_step(ctypes.byref(SSMShape(n, *shape)), _ptr(x), _ptr(dt), _ptr(a_log), _ptr(B), _ptr(C),
-                            _ptr(d_skip), _ptr(dt_bias), _ptr(state_in), _ptr(out), _ptr(state_out),
-                            _stream(device)))
+    _check(lib.gdn_ssm_step(ctypes.byref(SSMShape(n, *shape)), x.data_ptr(), dt.data_ptr(), a_log.data_ptr(), B.data_ptr(),
+                            C.data_ptr(), _ptr(d_skip), _ptr(dt_bias), _ptr(state_in), out.data_ptr(),
+                            state_out.data_ptr(), _stream(device)))
     return out, state_out
 
 
@@ -334,9 +347,9 @@ def lora_add(base: torch.Tensor, x: torch.Tensor, lora_a: torch.Tensor, lora_b: 
     ids, ids_host = _adapter_ids(adapters, adapters_host, n, device)
     shp = LoraShape(n, na, K, M, R, _dtype_code(base), ldx, ldbase, ldout)
     stream = _stream(device)
-    need = ctypes.c_size_t(0)
-    _check(lib.gdn_lora_workspace_size(ctypes.byref(shp), _ptr(host), ctypes.byref(need)))
-    ws, nbytes, keep = _scratch(need.value, device, stream, workspace)
-    _check(lib.gdn_lora_add(ctypes.byref(shp), _ptr(host), _ptr(cu), _ptr(ids_host), _ptr(ids), _ptr(base), _ptr(x),
-                            _ptr(lora_a), _ptr(lora_b), _ptr(scales), _ptr(out), ws, nbytes, stream))
+    lens = host.data_ptr()
+    args = (ctypes.byref(shp), lens, cu.data_ptr(), ids_host.data_ptr(), ids.data_ptr(), base.data_ptr(), x.data_ptr(),
+            lora_a.data_ptr(), lora_b.data_ptr(), _ptr(scales), out.data_ptr())
+    _run_with_workspace(lambda ws, nbytes: lib.gdn_lora_add(*args, ws, nbytes, stream), lib.gdn_lora_workspace_size, shp,
+                        lens, device, stream, workspace)
     return out
