@@ -743,7 +743,9 @@ def la_block_replay(x: torch.Tensor, weights, cu_seqlens, num_k_heads: int, num_
         ad, keep = _la_adapters(adapters, n, D, 2 * cq + 2 * cv + 2 * num_v_heads, cv, device)
         _check(lib.gdn_la_block_adapted_workspace_size(ctypes.byref(shp), ctypes.byref(ad), _ptr(cu_host),
                                                        int(outputs), ctypes.byref(need)))
-        if workspace is None:
+        if workspace is None and torch.cuda.is_current_stream_capturing():
+            workspace = torch.empty(need.value, dtype=torch.uint8, device=device)   # of the graph's own pool
+        elif workspace is None:
             workspace = _workspace(need.value, device, stream)
         _check(lib.gdn_la_block_replay_adapted(
             ctypes.byref(shp), ctypes.byref(w), ctypes.byref(ad), _ptr(cu_host), _ptr(cu_dev), _ptr(x),

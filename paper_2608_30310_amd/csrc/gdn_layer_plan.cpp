@@ -117,7 +117,8 @@ gdn_status make_ssm_plan(const gdn_ssm_shape* s, const int32_t* cu, SsmPlan* pla
   double best = 1.7 + std::max(static_cast<double>(longest), static_cast<double>(chunks * groups) / kSsmPlaces);
   const int64_t least = std::max<int64_t>(1, (chunks * groups + kSsmPlaces - 1) / kSsmPlaces);
   int64_t seg = 0;
-  for (int64_t more = 0; more <= 4 && least + more * ((least + 3) / 4) < longest; ++more) {
+  const bool joinable = N * H * s->d_state * s->head_dim / 4 <= kMaxGrid;   // a thread of the join takes four elements
+  for (int64_t more = 0; joinable && more <= 4 && least + more * ((least + 3) / 4) < longest; ++more) {
     const int64_t try_seg = least + more * ((least + 3) / 4);
     int64_t segs = 0;
     for (int64_t n = 0; n < N; ++n) segs += std::max<int64_t>(1, (chunks_of(n) + try_seg - 1) / try_seg);

@@ -430,7 +430,8 @@ void k_ssm_scan(SsmScanArgs a) {
       float delta = 0.0f, la = 0.0f;
       if (lane < rows) {
         delta = softplus_f(__uint_as_float(a.dt_bf16 ? pdt << 16 : pdt) + dt_bias);
-        la = fmaxf(neg_a2 * delta, -150.0f);   // 2^-150 rounds to zero
+        la = neg_a2 * delta;
+        if (la < -150.0f) la = -150.0f;   // 2^-150 rounds to zero, and sums of it stay finite; NaN stays NaN
       }
       // sums over the 16-token tiles (a tile is a DPP row): up to the token, and behind it
       const float l = row_scan<0x110>(la), s = row_scan<0x100>(dpp<0x101>(la));

@@ -135,12 +135,13 @@ def _conv_args(x, weight, bias, activation, out):
     _flat(bias, "bias", (C,), device)
     if activation not in _ACTIVATIONS:
         raise ValueError("activation must be 'silu' or 'none'")
-    if out is None:
-        out = torch.empty((T, C), dtype=x.dtype, device=device)
-    elif out.shape[0] != T:
-        raise ValueError("out must hold as many token rows as x")
     ldx = _rows(x, "x", x.dtype, device, (C,))
-    ldy = _rows(out, "out", x.dtype, device, (C,))
+    if out is None:
+        out, ldy = torch.empty((T, C), dtype=x.dtype, device=device), C
+    else:
+        ldy = _rows(out, "out", x.dtype, device, (C,))
+        if out.shape[0] != T:
+            raise ValueError("out must hold as many token rows as x")
     return device, T, C, W, out, (C, W, _dtype_code(x), _ACTIVATIONS[activation], ldx, ldy)
 
 
@@ -338,10 +339,11 @@ def lora_add(base: torch.Tensor, x: torch.Tensor, lora_a: torch.Tensor, lora_b: 
         raise ValueError("lora_a must be [n, R, K] and lora_b [n, M, R]")
     _flat(scales, "scales", (na,), device)
     if out is None:
-        out = torch.empty((T, M), dtype=base.dtype, device=device)
-    elif out.shape[0] != T:
-        raise ValueError("out must hold the same tokens as base")
-    ldout = _rows(out, "out", base.dtype, device, (M,))
+        out, ldout = torch.empty((T, M), dtype=base.dtype, device=device), M
+    else:
+        ldout = _rows(out, "out", base.dtype, device, (M,))
+        if out.shape[0] != T:
+            raise ValueError("out must hold the same tokens as base")
     cu, host = _offsets(cu_seqlens, cu_seqlens_host, device, T)
     n = host.numel() - 1
     ids, ids_host = _adapter_ids(adapters, adapters_host, n, device)

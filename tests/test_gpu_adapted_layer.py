@@ -104,6 +104,27 @@ def test_layer_without_an_adapter_is_the_plain_layer(act):
     assert not torch.equal(st[1], st3[1]) and not torch.equal(out[50:], out3[50:])
 
 
+def test_adapted_layer_in_a_graph():
+    dims = LayerDims(hidden=128, hk=2, hv=4, dk=64, dv=64)
+    x, cu, w, wd, ad = _case([70, 33], dims, 5, (16, 8))
+    ids = torch.tensor([1, -1], dtype=torch.int32)
+    cu_t = torch.from_numpy(cu)
+    xd, cu_d, both = _bf16(x), cu_t.to(DEV), dict(ad, ids=ids.to(DEV), ids_host=ids)
+    call = lambda **kw: gdn.la_block_replay(xd, wd, cu_d, 2, 4, 64, 64, 0.7, cu_seqlens_host=cu_t, adapters=both, **kw)
+    st0, out0 = call()
+    st, out = torch.empty_like(st0), torch.empty_like(out0)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(state_out=st, out=out)
+    for _ in range(3):
+        st.zero_(), out.zero_()
+        graph.replay()
+        x2, cu2, _, wd2, ad2 = _case([300], dims, 6, (16, 8))
+        _replay(x2, cu2, wd2, dims, ad2, [0], True, "f32")
+        torch.cuda.synchronize()
+        assert torch.equal(st, st0) and torch.equal(out, out0)
+
+
 def test_adapted_layer_refuses():
     dims = LayerDims(hidden=128, hk=2, hv=4, dk=64, dv=64)
     x, cu, w, wd, ad = _case([20, 20], dims, 3, (16, 16))

@@ -157,3 +157,25 @@ def test_graph_replays():
         conv(inputs([500], 264, seed=8))
         torch.cuda.synchronize()
         assert torch.equal(y, y0) and torch.equal(h, h0) and torch.equal(s, s0) and torch.equal(g, g0)
+
+
+def test_many_sequences():
+    """More sequences than one look of a wave, empty ones among them."""
+    i = inputs([k % 4 for k in range(5000)], 24, seed=9)
+    check(i, *conv(i))
+
+
+def test_refuses():
+    i = inputs([5, 3], 64, seed=10)
+    x, w = i["x"], i["w"]
+    for bad in (dict(w=w[:3]), dict(w=w.bfloat16()), dict(bias=w[:, 0]), dict(activation="relu"), dict(cu=[0, 9]),
+                dict(history_in=torch.zeros(2, 3, 64, device=DEV)), dict(history_in=x[:3].repeat(2, 1).view(2, 3, 64)[:1]),
+                dict(out=x[:7]), dict(out=[1]), dict(x=x.half()), dict(x=x.t()), dict(x=x.cpu())):
+        kw = dict(dict(x=x, w=w, cu=i["cu_host"].tolist()), **bad)
+        first = [kw.pop(k) for k in ("x", "w", "cu")]
+        with pytest.raises((ValueError, TypeError)):
+            gdn.causal_conv(*first, **kw)
+    for kw in (dict(out=x), dict(cu=[0, 5, 4]), dict(w=w[:, :1].contiguous()), dict(w=torch.zeros(64, 5, device=DEV))):
+        kw = dict(dict(w=w, cu=[0, 8]), **kw)
+        with pytest.raises(gdn.GDNError):
+            gdn.causal_conv(x, kw.pop("w"), kw.pop("cu"), **kw)

@@ -131,3 +131,26 @@ def test_no_tokens_and_no_adapters():
     i = inputs([4], [-1], seed=8)
     i.update(a=i["a"][:0], b=i["b"][:0], scales=None)
     assert torch.equal(lora(i), i["base"])
+
+
+def test_many_sequences():
+    i = inputs([k % 3 for k in range(700)], [k % 4 - 1 for k in range(700)], 72, 136, 16, seed=9)
+    check(i, lora(i))
+
+
+def test_refuses():
+    i = inputs([5, 3], [0, 1], 64, 96, 16, seed=10)
+    base, x, a, b = i["base"], i["x"], i["a"], i["b"]
+    for bad in (dict(x=x[:7]), dict(x=x.float()), dict(a=a[:, :, :56].contiguous()), dict(b=b[:2]), dict(a=a.float()),
+                dict(ids=[0]), dict(ids=[0, 1, 0]), dict(scales=torch.ones(2, device=DEV)), dict(out=base[:7]),
+                dict(out=base.float()), dict(cu=[0, 5, 9]), dict(base=base.cpu()), dict(base=base.half())):
+        kw = dict(dict(base=base, x=x, a=a, b=b, ids=[0, 1], cu=[0, 5, 8]), **bad)
+        first = [kw.pop(k) for k in ("base", "x", "a", "b", "ids", "cu")]
+        with pytest.raises((ValueError, TypeError)):
+            gdn.lora_add(*first, **kw)
+    for kw in (dict(ids=[0, 3]), dict(ids=[-2, 0]), dict(cu=[0, 8, 5]), dict(a=a[:, :12].contiguous(), b=b[:, :, :12].contiguous()),
+               dict(workspace=torch.empty(64, dtype=torch.uint8, device=DEV))):
+        kw = dict(dict(base=base, x=x, a=a, b=b, ids=[0, 1], cu=[0, 5, 8]), **kw)
+        first = [kw.pop(k) for k in ("base", "x", "a", "b", "ids", "cu")]
+        with pytest.raises(gdn.GDNError):
+            gdn.lora_add(*first, **kw)

@@ -260,6 +260,49 @@ def test_two_streams_at_once():
         assert torch.equal(y, wy) and torch.equal(s, ws)
 
 
+def test_many_sequences():
+    """More sequences than a wave has lanes, with one long enough for segments among them."""
+    i = inputs([3] * 100 + [1500] + [0] * 40 + [200, 1], H=4, G=1, N=64, seed=19)
+    check(i, *scan(i))
+
+
+def test_a_head_without_a_number():
+    """A decay that is not a number makes that head's outputs and states so, and no other's."""
+    i = inputs([70, 1500], H=4, G=2, seed=21)
+    y, st = scan(i)
+    bad = dict(i, a_log=i["a_log"].clone())
+    bad["a_log"][2] = float("nan")
+    y2, st2 = scan(bad)
+    keep = [0, 1, 3]
+    assert torch.equal(y[:, keep], y2[:, keep]) and torch.equal(st[:, keep], st2[:, keep])
+    assert torch.isnan(st2[:, 2]).all() and torch.isnan(y2[1:, 2][:60]).all()
+    y3, st3 = gdn.ssm_step(i["x"][:2], i["dt"][:2], bad["a_log"], i["B"][:2], i["C"][:2], state_in=i["state"])
+    assert torch.isnan(st3[:, 2]).all() and torch.isfinite(st3[:, keep]).all()
+
+
+def test_refuses():
+    i = inputs([5, 3], seed=22)
+    x, dt, a, B, C = (i[k] for k in ("x", "dt", "a_log", "B", "C"))
+    for bad in (dict(x=x[:, :3]), dict(B=B[:, :1]), dict(C=C[:7]), dict(dt=dt.double()), dict(dt=dt[:, :3]), dict(a_log=a[:3]),
+                dict(x=x.half()), dict(d_skip=a.bfloat16()), dict(dt_bias=a[:1]), dict(state_in=torch.zeros(2, 4, 64, 32, device=DEV)),
+                dict(state_in=torch.zeros(3, 4, 64, 64, device=DEV)), dict(cu=[0, 5, 9]), dict(out=torch.empty(8, 4, 64, device=DEV)),
+                dict(out=torch.empty(7, 4, 64, dtype=x.dtype, device=DEV)), dict(x=x.cpu()), dict(a_log=a.cpu()), dict(C=None),
+                dict(outputs=False, out=torch.empty_like(x)), dict(workspace=torch.empty(8))):
+        kw = dict(dict(x=x, dt=dt, a_log=a, B=B, C=C, cu=i["cu_host"].tolist()), **bad)
+        first = [kw.pop(k) for k in ("x", "dt", "a_log", "B", "C", "cu")]
+        with pytest.raises((ValueError, TypeError)):
+            gdn.ssm_scan(*first, **kw)
+    for cu in ([1, 5, 8], [0, 6, 3, 8]):
+        with pytest.raises(gdn.GDNError):
+            gdn.ssm_scan(x, dt, a, B, C, cu)
+    with pytest.raises(gdn.GDNError):   # rows that do not start at 16 bytes
+        big = torch.zeros(8, 4 * 64 + 8, dtype=x.dtype, device=DEV)
+        gdn.ssm_scan(big[:, 4:260].unflatten(1, (4, 64)), dt, a, B, C, i["cu"])
+    with pytest.raises(gdn.GDNError):   # in place over x
+        y = x.contiguous()
+        gdn.ssm_scan(y, dt, a, B, C, i["cu"], out=y)
+
+
 def test_no_tokens():
     i = inputs([0, 0], seed=18)
     y, st = scan(i)
