@@ -157,6 +157,22 @@ struct RowsLds {
       return r;
     }
   }
+  // writes elements 8 e8 .. + 7 of row `up` + row
+  static __device__ __forceinline__ void put8(char* base, int up, int row, int e8, const float (&x)[8]) {
+    base += up * kPitch;
+    if constexpr (sizeof(T) == 2) {
+      u32x4 w;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const f32x2 pair = {x[2 * j], x[2 * j + 1]};
+        w[j] = __builtin_bit_cast(uint32_t, __builtin_convertvector(pair, bf16x2));
+      }
+      *reinterpret_cast<u32x4*>(base + at(row, e8)) = w;
+    } else {
+      *reinterpret_cast<f32x4*>(base + at(row, 2 * e8)) = f32x4{x[0], x[1], x[2], x[3]};
+      *reinterpret_cast<f32x4*>(base + at(row, 2 * e8 + 1)) = f32x4{x[4], x[5], x[6], x[7]};
+    }
+  }
   // address of row + k STEP
   template <int STEP>
   static __device__ __forceinline__ int at_step(int row, int k, int piece) {
@@ -165,22 +181,7 @@ struct RowsLds {
   }
 };
 
-// Eight elements to a buffer at byte offset `off`; a row behind the buffer's end is dropped.
-__device__ __forceinline__ void buffer_store8(__amdgpu_buffer_rsrc_t r, uint32_t off, const float (&x)[8], uint16_t*) {
-  u32x4 w;
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const f32x2 pair = {x[2 * j], x[2 * j + 1]};
-    w[j] = __builtin_bit_cast(uint32_t, __builtin_convertvector(pair, bf16x2));
-  }
-  __builtin_amdgcn_raw_buffer_store_b128(w, r, off, 0, 0);
-}
-__device__ __forceinline__ void buffer_store8(__amdgpu_buffer_rsrc_t r, uint32_t off, const float (&x)[8], float*) {
-  const f32x4 a = {x[0], x[1], x[2], x[3]}, b = {x[4], x[5], x[6], x[7]};
-  __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, a), r, off, 0, 0);
-  __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, b), r, off + 16, 0, 0);
-}
-// Raw buffer of `bytes` bytes: a load behind its end gives zero.
+// Raw buffer of `bytes` bytes: a load behind its end gives zero, a store is dropped.
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_buffer(const void* base, uint32_t bytes) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, bytes, 0x00020000);
 }
@@ -380,6 +381,10 @@ void k_ssm_scan(SsmScanArgs a) {
   const uint32_t rowk = tid / KRows::kPieces, colk = tid % KRows::kPieces, rowx = tid / XP, colx = tid % XP;
   constexpr uint32_t KSTEP = L::kThreads / KRows::kPieces, XSTEP = L::kThreads / XP;   // rows from k to k + 1
   static_assert(KSTEP * KRows::kPieces == L::kThreads && XSTEP * XP == L::kThreads, "whole rows per step");
+  const auto x_at = [&](int k) {   // where piece k of x lies in LDS
+    return L::kOffX + static_cast<int>(colx / XRows::kPieces) * XRows::kBytes +
+           XRows::template at_step<XSTEP>(rowx, k, colx % XRows::kPieces);
+  };
   const auto fetch = [&](int at) {
     const uint32_t rows = min(kSsmChunk, len - at);
     uint32_t vb = rowk * ldb + colk * 16, vc = rowk * ldc + colk * 16, vx = rowx * ldx + colx * 16;
@@ -412,9 +417,23 @@ void k_ssm_scan(SsmScanArgs a) {
       X::put4(pf + 3 * X::kF2Bytes, 32 + lane % 32, lane / 32, zero);
     }
   }
+  // The outputs of the chunk at `at`, which lie where its x lay.  A thread takes
+  // the very pieces that it writes the next chunk's x to, so no barrier comes
+  // between.
+  const auto write_y = [&](int at) {
+    const uint32_t rows = min(kSsmChunk, len - at);
+    const __amdgpu_buffer_rsrc_t ry = rows_buffer(static_cast<T*>(a.y) + (t0 + at) * a.ldy + static_cast<int64_t>(h0) * DV,
+                                                  (rows - 1) * ldy + L::kHeads * DV * E);
+    uint32_t vy = rowx * ldy + colx * 16;
+    asm volatile("" : "+v"(vy));
+#pragma unroll
+    for (int k = 0; k < KX; ++k)
+      __builtin_amdgcn_raw_buffer_store_b128(*reinterpret_cast<const u32x4*>(lds + x_at(k)), ry, vy + k * XSTEP * ldy, 0, 0);
+  };
   if (len > 0) fetch(0);
   for (int at = 0; at < len; at += kSsmChunk) {
     const int rows = min(kSsmChunk, len - at);
+    if (OUT && at > 0) write_y(at - kSsmChunk);
     // registers -> LDS
 #pragma unroll
     for (int k = 0; k < KB; ++k) {
@@ -422,9 +441,7 @@ void k_ssm_scan(SsmScanArgs a) {
       if constexpr (OUT) *reinterpret_cast<u32x4*>(lds + L::kOffC + KRows::template at_step<KSTEP>(rowk, k, colk)) = pc[k];
     }
 #pragma unroll
-    for (int k = 0; k < KX; ++k)
-      *reinterpret_cast<u32x4*>(lds + L::kOffX + (colx / XRows::kPieces) * XRows::kBytes +
-                                XRows::template at_step<XSTEP>(rowx, k, colx % XRows::kPieces)) = px[k];
+    for (int k = 0; k < KX; ++k) *reinterpret_cast<u32x4*>(lds + x_at(k)) = px[k];
     if (wave < L::kHeads) {
       // this head's steps, a token per lane
       float delta = 0.0f, la = 0.0f;
@@ -552,32 +569,50 @@ void k_ssm_scan(SsmScanArgs a) {
       lds_barrier();   // C B^T is whole
       // P^T = (C B^T o L o delta)^T, the head's tiles shared by its waves: the four
       // values of a lane are half of one lane's operand for x^T P^T
-      int own = wave % L::kWavesPerHead;
+      constexpr int WPH = L::kWavesPerHead, ND = 4 / WPH, NO = (6 + WPH - 1) / WPH;   // tiles on and below the diagonal
+      static_assert(4 % WPH == 0, "diagonal tiles per wave");
+      int own = wave % WPH;
       asm volatile("" : "+s"(own));
+      f32x4 cd[ND], jd[ND], co[NO], jo[NO];
+      float ed[ND], eo[NO];
+      int ti_o[NO], tj_o[NO];
 #pragma unroll
-      for (int k = 0; k < (10 + L::kWavesPerHead - 1) / L::kWavesPerHead; ++k) {
-        const int t = own + k * L::kWavesPerHead;
-        if (10 % L::kWavesPerHead != 0 && t >= 10) break;
-        int ti, tj;
-        tile_rows(t, ti, tj);
-        const f32x4 cbt = *reinterpret_cast<const f32x4*>(lds + L::kOffCb + 1024 * t + 16 * lane);
+      for (int k = 0; k < ND; ++k) {
+        const int ti = own + k * WPH;
+        cd[k] = *reinterpret_cast<const f32x4*>(lds + L::kOffCb + 1024 * (ti * (ti + 3) / 2) + 16 * lane);
+        jd[k] = *reinterpret_cast<const f32x4*>(hs.same + 16 * ti + 4 * g);
+        ed[k] = hs.l[16 * ti + c];
+      }
+#pragma unroll
+      for (int k = 0; k < NO; ++k) {
+        const int o = min(own + k * WPH, 5);   // (1,0) (2,0) (2,1) (3,0) (3,1) (3,2)
+        ti_o[k] = o < 1 ? 1 : o < 3 ? 2 : 3;
+        tj_o[k] = o - ti_o[k] * (ti_o[k] - 1) / 2;
+        const int t = ti_o[k] * (ti_o[k] + 1) / 2 + tj_o[k];
+        co[k] = *reinterpret_cast<const f32x4*>(lds + L::kOffCb + 1024 * t + 16 * lane);
+        jo[k] = *reinterpret_cast<const f32x4*>(hs.past + 16 * tj_o[k] + 4 * g);
+        eo[k] = hs.row[16 * ti_o[k] + c] * hs.between[t];
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      const auto put = [&](int ti, int tj, const float (&v)[4]) {
+        X::put4(pt + (ti < 2 ? ti : 2 * ti - 2 + tj / 2) * X::kF2Bytes, 16 * (2 * (tj & 1) + g / 2) + c, g & 1, v);
+      };
+#pragma unroll
+      for (int k = 0; k < ND; ++k) {
         float v[4];
-        if (tj < ti) {   // uniform
-          const f32x4 pj = *reinterpret_cast<const f32x4*>(hs.past + 16 * tj + 4 * g);
-          const float e = hs.row[16 * ti + c] * hs.between[t];
 #pragma unroll
-          for (int r = 0; r < 4; ++r) v[r] = cbt[r] * (e * pj[r]);
-        } else {
-          const f32x4 pj = *reinterpret_cast<const f32x4*>(hs.same + 16 * tj + 4 * g);
-          const float e = hs.l[16 * ti + c];
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const float p = cbt[r] * __builtin_amdgcn_exp2f(e + pj[r]);
-            v[r] = 4 * g + r < c ? p : 4 * g + r == c ? p + skip : 0.0f;   // d_skip x rides on the diagonal
-          }
+        for (int r = 0; r < 4; ++r) {
+          const float p = cd[k][r] * __builtin_amdgcn_exp2f(ed[k] + jd[k][r]);
+          v[r] = 4 * g + r < c ? p : 4 * g + r == c ? p + skip : 0.0f;   // d_skip x rides on the diagonal
         }
-        X::put4(pt + (ti < 2 ? ti : ti == 2 ? 2 + tj / 2 : 4 + tj / 2) * X::kF2Bytes, 16 * (2 * (tj & 1) + g / 2) + c,
-                g & 1, v);
+        put(own + k * WPH, own + k * WPH, v);
+      }
+#pragma unroll
+      for (int k = 0; k < NO; ++k) {
+        float v[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[r] = co[k][r] * (eo[k] * jo[k][r]);
+        if (6 % WPH == 0 || own + k * WPH < 6) put(ti_o[k], tj_o[k], v);
       }
     } else {
       load_x();
@@ -648,10 +683,10 @@ void k_ssm_scan(SsmScanArgs a) {
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct)
               yt[ti][ct] = X::mul(xf[kk][ct], pf[ti < 2 ? ti : 2 * ti - 2 + kk].part[k], yt[ti][ct]);
-      const __amdgpu_buffer_rsrc_t ry = rows_buffer(static_cast<T*>(a.y) + (t0 + at) * a.ldy + static_cast<int64_t>(head) * DV + p0,
-                                                    (rows - 1) * ldy + L::kCols * E);
-      uint32_t vy = c * ldy + 8 * g * E;
-      asm volatile("" : "+v"(vy));
+      // over the chunk's x, which every wave has in registers by now; write_y sends
+      // whole token rows from there (a wave's own 64-byte pieces of 16 rows per
+      // store kept the CU's memory path busy more than twice as long)
+      char* yl = lds + L::kOffX + hl * XRows::kBytes;
 #pragma unroll
       for (int ti = 0; ti < 4; ++ti)
 #pragma unroll
@@ -659,11 +694,12 @@ void k_ssm_scan(SsmScanArgs a) {
           float o[8];
 #pragma unroll
           for (int j = 0; j < 8; ++j) o[j] = yt[ti][2 * b + j / 4][j & 3];
-          buffer_store8(ry, vy + 16 * ti * ldy + 32 * b * E, o, static_cast<T*>(nullptr));
+          XRows::put8(yl, 16 * ti, c, (p0 + 32 * b) / 8 + g, o);
         }
     }
-    lds_barrier();   // the chunk's LDS has been read
+    lds_barrier();   // the chunk's LDS has been read, its outputs are whole
   }
+  if (OUT && len > 0) write_y((len - 1) / kSsmChunk * kSsmChunk);
 
   if constexpr (MODE == SsmMode::kLocal) {
 #pragma unroll
