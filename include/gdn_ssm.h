@@ -102,8 +102,8 @@ gdn_status gdn_ssm_workspace_size(const gdn_ssm_shape* shape, const int32_t* cu_
  * y NULL = no outputs (the state alone, as where a tail is replayed; C and
  * d_skip are not read then and may be NULL); state_out NULL = not written
  * (one of the two is required).  state_out may equal state_in and must not
- * otherwise overlap it; y must not overlap an input.  A zero-length sequence
- * writes its state_in (or zeros) to state_out.
+ * otherwise overlap it, nor another input; y must not overlap an input or a
+ * state.  A zero-length sequence writes its state_in (or zeros) to state_out.
  * x, B, C and y must be 16-byte aligned, their row strides multiples of 16
  * bytes (GDN_ERR_UNSUPPORTED otherwise).
  * workspace: at least gdn_ssm_workspace_size bytes, 256-byte aligned; NULL is

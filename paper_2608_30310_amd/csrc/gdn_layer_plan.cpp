@@ -98,23 +98,25 @@ gdn_status make_ssm_plan(const gdn_ssm_shape* s, const int32_t* cu, SsmPlan* pla
   if (st == GDN_OK) st = check_seqlens(s->num_seqs, cu, &p.tokens, &p.longest, err);
   if (st != GDN_OK) return st;
   const int64_t H = s->num_heads, N = s->num_seqs;
-  const int32_t share = (s->dtype == GDN_BF16 ? kSsmCols : kSsmColsF32) / s->head_dim;
-  p.heads_per_group = H / s->num_groups % share == 0 ? share : 1;
+  const bool bf16 = s->dtype == GDN_BF16;
+  int32_t share = (bf16 ? kSsmCols : kSsmColsF32) / s->head_dim;
+  while (H / s->num_groups % share != 0) share /= 2;
+  p.heads_per_group = share;
   p.slots = N;
-  const int64_t groups = H / p.heads_per_group;   // workgroups of a sequence
+  int64_t groups = H / share;   // workgroups of a sequence
   // Whole sequences end with the longest one, or with the work per place; in
   // segments the work is even, but every chunk is walked twice (once for the
   // states alone), the segments' states pass through memory and there are two
-  // launches more.  In chunks of the whole walk (~7 us for bf16 inputs): whole
-  // 1.7 + the chunks; segments 2.5 + 1.5 x a segment's chunks + 0.0093 x their
+  // launches more.  In chunks of the whole walk (~6.5 us for bf16 inputs): whole
+  // 0.8 + the chunks; segments 2.5 + 1.5 x a segment's chunks + 0.0093 x their
   // number.  Measured, 64 heads of 64 x 128, one sequence of 2, 3, 8, 24 and 128
-  // chunks: whole 27, 33, 68, 184 and 914 us, segments 30, 32, 43, 51 and 121;
-  // 32 heads of 128 x 128, 8 sequences of 8 and 16: 71 and 124, 81 and 123.
+  // chunks: whole 18, 25, 55, 152 and 776 us, segments 24, 26, 37, 44 and 105;
+  // 32 heads of 128 x 128, 8 sequences of 8 and 16, 4 of 64: 58, 104 and 397, 73, 110 and 190.
   const auto chunks_of = [&](int64_t n) { return (static_cast<int64_t>(cu[n + 1]) - cu[n] + 63) / 64; };
   int64_t chunks = 0;
   for (int64_t n = 0; n < N; ++n) chunks += chunks_of(n);
   const int64_t longest = (p.longest + 63) / 64;
-  double best = 1.7 + std::max(static_cast<double>(longest), static_cast<double>(chunks * groups) / kSsmPlaces);
+  double best = 0.8 + std::max(static_cast<double>(longest), static_cast<double>(chunks * groups) / kSsmPlaces);
   const int64_t least = std::max<int64_t>(1, (chunks * groups + kSsmPlaces - 1) / kSsmPlaces);
   int64_t seg = 0;
   const bool joinable = N * H * s->d_state * s->head_dim / 4 <= kMaxGrid;   // a thread of the join takes four elements
@@ -129,6 +131,18 @@ gdn_status make_ssm_plan(const gdn_ssm_shape* s, const int32_t* cu, SsmPlan* pla
       seg = try_seg;
       p.slots = segs;
     }
+  }
+  // Four heads of 64 columns in pairs instead, whole sequences, while there is a
+  // place for every pair: twice the CUs at 0.77 of the time a chunk.  Measured, 64
+  // heads of 64 x 128: one sequence of 1, 2 and 3 chunks 9.6, 14.4 and 19.4 us in
+  // pairs, 12.2, 18.4 and 24.5 in fours; 8 of 1, 3 and 13: 14.5, 25.5 and 72.9, 16.6,
+  // 29.8 and 89.7; but 32 of 32 chunks 676, 486.  (Two heads of 128 columns gain
+  // nothing one by one: 8 sequences of 3 chunks 31.5 us, 28.8 in pairs.)
+  if (bf16 && share == 4 && N * (H / 2) <= kSsmPlaces && 0.7 + 0.77 * static_cast<double>(longest) < best) {
+    p.heads_per_group = 2;
+    p.slots = N;
+    groups = H / 2;
+    seg = 0;
   }
   if (seg > 0) {
     p.seg_tokens = static_cast<int32_t>(64 * seg);
@@ -174,14 +188,21 @@ gdn_status make_lora_plan(const gdn_lora_shape* s, const int32_t* cu, LoraPlan* 
   int64_t longest = 0;
   if (st == GDN_OK) st = check_seqlens(s->num_seqs, cu, &p.tokens, &longest, err);
   if (st != GDN_OK) return st;
-  const bool tokenwise = p.tokens <= 16 * static_cast<int64_t>(s->num_seqs);
+  // Small tiles where larger ones would be mostly empty, or too few for the CUs.
+  // Measured (2048 -> 12352, us, small and large tiles): 64 sequences of 1, 8 and 32
+  // tokens at rank 16 12.3, 16.5 and 30.6, 16.6, 20.4 and 28.6; at rank 64 8 of 32
+  // tokens 17.4, 23.3, one of 819 27.8, 31.1, 8 of 128 33.5 both, of 512 88, 61.
+  const bool tokenwise = p.tokens <= std::max<int64_t>(1024, 16 * static_cast<int64_t>(s->num_seqs));
   p.down_tile = tokenwise ? 16 : 32;
   p.up_tile = tokenwise ? 16 : 64;
   p.down_slots = tile_slots(p.tokens, s->num_seqs, p.down_tile);
   p.up_slots = tile_slots(p.tokens, s->num_seqs, p.up_tile);
-  // x A^T in enough workgroups for every CU, each with at least two 32-wide steps
-  // for each of its four waves; every part is read by all column tiles
-  const int64_t most = std::max<int64_t>(1, s->hidden / 256);
+  // x A^T in parts of K until there are workgroups for every CU (64 sequences of 4
+  // tokens, rank 16: 14.1 us in four parts, 15.7 in one), each with at least two
+  // 32-wide steps for each of its four waves.  Every column tile reads every part,
+  // so no more than 1 KB of them a token (8 x 32 tokens, rank 64: 15.6 us in 4 parts,
+  // 17.6 in 8, 20.9 in one; one sequence of 1500 36.8 in 4, 38.7 in 6).
+  const int64_t most = std::max<int64_t>(1, std::min<int64_t>(s->hidden / 256, 256 / s->rank));
   p.parts = static_cast<int32_t>(std::min(most, std::max<int64_t>(1, kLoraGroups / std::max<int64_t>(1, p.down_slots))));
   const int64_t tiles = (static_cast<int64_t>(s->width) + 255) / 256;
   if (p.down_slots * p.parts > kMaxGrid / 256 || p.up_slots * tiles > kMaxGrid / 256) {

@@ -11,8 +11,9 @@
 
 namespace gdn {
 
-// State columns of a workgroup of the state space scan, where a B/C group has
-// that many heads to share them (bf16, fp32); one head's otherwise.
+// State columns of a workgroup of the state space scan (bf16, fp32), where a B/C
+// group has that many heads to share them; fewer heads otherwise, and where
+// make_ssm_plan says so.
 constexpr int32_t kSsmCols = 256, kSsmColsF32 = 128;
 
 // Packed sequences cut into tiles of `tile` tokens, each sequence from its own
@@ -45,7 +46,7 @@ gdn_status check_lora(const gdn_lora_shape* s, std::string* err);
 struct LoraPlan {
   int64_t tokens = 0;
   // tokens of a tile of the first and of the second product (32 and 64, or 16
-  // where sequences are short) and their slots
+  // where there are few tokens) and their slots
   int32_t down_tile = 0, up_tile = 0;
   int64_t down_slots = 0, up_slots = 0;
   int32_t parts = 1;   // pieces of the first product's contraction over K

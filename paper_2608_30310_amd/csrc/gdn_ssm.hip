@@ -83,11 +83,14 @@ gdn_status launch_scan(const SsmArgs& a) {
 template <typename T, int DK, int DV>
 gdn_status launch_ssm(const SsmArgs& a) {
   if (!a.p) return launch_step<T, DK, DV>(a);
-  constexpr int CT = 2;
-  constexpr int cols = sizeof(T) == 2 ? kSsmCols : kSsmColsF32;
-  if constexpr (cols > DV)
-    if (a.p->heads_per_group > 1) return launch_scan<T, DK, DV, CT, cols / (16 * CT)>(a);
-  return launch_scan<T, DK, DV, CT, DV / (16 * CT)>(a);
+  constexpr int CT = 2, WPH = DV / (16 * CT);   // waves of a head
+  constexpr int share = (sizeof(T) == 2 ? kSsmCols : kSsmColsF32) / DV;
+  const int heads = a.p->heads_per_group;
+  if constexpr (share >= 4)
+    if (heads == 4) return launch_scan<T, DK, DV, CT, 4 * WPH>(a);
+  if constexpr (share >= 2)
+    if (heads == 2) return launch_scan<T, DK, DV, CT, 2 * WPH>(a);
+  return launch_scan<T, DK, DV, CT, WPH>(a);
 }
 
 template <typename T>
@@ -110,13 +113,20 @@ gdn_status ssm_impl(const SsmArgs& a) {
   const size_t states = static_cast<size_t>(s.num_seqs) * s.num_heads * s.d_state * s.head_dim * sizeof(float);
   if (a.state_in && a.state_out && a.state_in != a.state_out && overlap(a.state_in, states, a.state_out, states))
     return sfail(GDN_ERR_BAD_SHAPE, "state_out overlaps state_in without being equal");
-  if (a.y && a.tokens > 0) {
+  if (a.tokens > 0) {
     const int64_t wy = static_cast<int64_t>(s.num_heads) * s.head_dim * e, wb = static_cast<int64_t>(s.num_groups) * s.d_state * e;
-    if (rows_overlap(a.y, wy, s.ld_y * e, a.x, wy, s.ld_x * e, a.tokens) ||
-        rows_overlap(a.y, wy, s.ld_y * e, a.B, wb, s.ld_b * e, a.tokens) ||
-        rows_overlap(a.y, wy, s.ld_y * e, a.C, wb, s.ld_c * e, a.tokens) ||
-        rows_overlap(a.y, wy, s.ld_y * e, a.dt, s.num_heads * edt, s.ld_dt * edt, a.tokens))
-      return sfail(GDN_ERR_BAD_SHAPE, "y overlaps an input");
+    const struct { const void* p; int64_t width, ld; } in[] = {
+        {a.x, wy, s.ld_x * e}, {a.B, wb, s.ld_b * e}, {a.y ? a.C : nullptr, wb, s.ld_c * e}, {a.dt, s.num_heads * edt, s.ld_dt * edt}};
+    for (const auto& r : in) {
+      if (!r.p) continue;
+      if (a.y && rows_overlap(a.y, wy, s.ld_y * e, r.p, r.width, r.ld, a.tokens))
+        return sfail(GDN_ERR_BAD_SHAPE, "y overlaps an input");
+      if (a.state_out && overlap(a.state_out, states, r.p, (a.tokens - 1) * r.ld + r.width))
+        return sfail(GDN_ERR_BAD_SHAPE, "state_out overlaps an input");
+    }
+    const size_t ey = (a.tokens - 1) * s.ld_y * e + wy;
+    if (a.y && ((a.state_in && overlap(a.state_in, states, a.y, ey)) || (a.state_out && overlap(a.state_out, states, a.y, ey))))
+      return sfail(GDN_ERR_BAD_SHAPE, "y overlaps a state");
   }
   return s.dtype == GDN_BF16 ? ssm_dims<uint16_t>(a) : ssm_dims<float>(a);
 }

@@ -372,7 +372,7 @@ void k_ssm_scan(SsmScanArgs a) {
 
   // A thread's pieces of a chunk: rows tid / pieces + k (threads / pieces).  A
   // chunk is a buffer from its first row: its offsets fit 32 bits (row strides
-  // are below 2^24 elements), rows behind the sequence's last one read as zero.
+  // are at most 2^23 elements), rows behind the sequence's last one read as zero.
   constexpr uint32_t E = sizeof(T);
   u32x4 pb[KB], pc[OUT ? KB : 1], px[KX];
   uint32_t pdt = 0;   // dt as loaded

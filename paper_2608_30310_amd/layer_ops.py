@@ -28,14 +28,17 @@ _ACTIVATIONS = {None: 0, "none": 0, "silu": 1}
 def _on_device(fn):
     """Runs the call with its first tensor's device current (kernels launch on
     the current device); free where it is current already."""
+    name = fn.__code__.co_varnames[0]
+
     @functools.wraps(fn)
-    def call(first, *args, **kwargs):
+    def call(*args, **kwargs):
+        first = args[0] if args else kwargs.get(name)
         if not isinstance(first, torch.Tensor) or not first.is_cuda:
             raise ValueError(f"{fn.__name__} works on tensors in GPU memory")
         if first.get_device() == torch._C._cuda_getDevice():
-            return fn(first, *args, **kwargs)
+            return fn(*args, **kwargs)
         with torch.cuda.device(first.device):
-            return fn(first, *args, **kwargs)
+            return fn(*args, **kwargs)
     return call
 
 

@@ -266,6 +266,24 @@ def test_many_sequences():
     check(i, *scan(i))
 
 
+@pytest.mark.parametrize("N", [64, 128])
+def test_as_many_sequences_as_places(N):
+    """Heads of a workgroup by fours where there are enough sequences, by twos where there are few."""
+    i = inputs([70] * 39 + [130], H=16, G=2, N=N, seed=23)
+    y, st = scan(i)
+    check(i, y, st)
+    one = inputs([130], H=16, G=2, N=N, seed=24)
+    check(one, *scan(one))
+
+
+def test_arguments_by_name():
+    i = inputs([40, 30], seed=25)
+    y, st = scan(i)
+    y2, st2 = gdn.ssm_scan(cu_seqlens=i["cu"], C=i["C"], B=i["B"], a_log=i["a_log"], dt=i["dt"], x=i["x"], d_skip=i["d_skip"],
+                           dt_bias=i["dt_bias"], state_in=i["state"])
+    assert torch.equal(y, y2) and torch.equal(st, st2)
+
+
 def test_a_head_without_a_number():
     """A decay that is not a number makes that head's outputs and states so, and no other's."""
     i = inputs([70, 1500], H=4, G=2, seed=21)
