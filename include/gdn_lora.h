@@ -10,7 +10,10 @@
  * projection gave.
  *
  * Conventions as in gdn_tail_replay.h; token rows may be strided and rows at or
- * behind cu_seqlens[N] are left alone, as in gdn_ssm.h.
+ * behind cu_seqlens[N] are left alone, as in gdn_ssm.h.  x A^T is summed in
+ * fp32; for fp32 outputs it enters the second product with 24 bits, for bf16
+ * outputs with 16.  A token whose x A^T is not finite gets outputs that are not
+ * (NaN also where the formula gives an infinity), and no other token does.
  */
 #ifndef GDN_LORA_H
 #define GDN_LORA_H

@@ -191,16 +191,31 @@ struct Cols8<T, false> {
   }
 };
 
+// w rounded to bf16; w keeps what the rounding left (exact).
+__device__ __forceinline__ bf16x8 round_off8(float (&w)[8]) {
+  u32x4 r;
+#pragma unroll
+  for (int p = 0; p < 4; ++p) {
+    const f32x2 pair = {w[2 * p], w[2 * p + 1]};
+    r[p] = __builtin_bit_cast(uint32_t, __builtin_convertvector(pair, bf16x2));
+    w[2 * p] -= __uint_as_float(r[p] << 16);
+    w[2 * p + 1] -= __uint_as_float(r[p] & 0xFFFF0000u);
+  }
+  return __builtin_bit_cast(bf16x8, r);
+}
+
 // grid: slots x column tiles, an XCD takes neighbouring ones (they share u, and
 // the adapter's B stays in its L2).  A workgroup: a token tile x 256 columns, 64
 // of them a wave's, KS steps over the rank.  The tile's u goes through LDS once
-// for the four waves, as operands of two bf16 parts (within 2^-16).  A tile's
-// rows of B are taken in the order in which a lane ends up with eight
-// neighbouring columns of a token.
+// for the four waves, as operands of bf16 parts: two (within 2^-16) where the
+// outputs are bf16, three (24 bits) where they are fp32.  A tile's rows of B are
+// taken in the order in which a lane ends up with eight neighbouring columns of
+// a token.
 template <typename T, int TT, int KS, bool WIDE>
 __global__ __launch_bounds__(kLoraThreads)
 void k_lora_up(LoraArgs a) {
-  __shared__ bf16x8 uf[TT * KS][2][kWave];
+  constexpr int NP = sizeof(T) == 2 ? 2 : 3;
+  __shared__ bf16x8 uf[TT * KS][NP][kWave];
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int g = lane / 16, c = lane % 16;
   const int tiles = (a.M + kLoraCols - 1) / kLoraCols;
@@ -248,9 +263,8 @@ void k_lora_up(LoraArgs a) {
           for (int e = 0; e < 8; ++e) w[e] += q[e];
         }
       }
-      const Frag fr = split8(w);
-      uf[f + wave][0][lane] = fr.hi;
-      uf[f + wave][1][lane] = fr.lo;
+#pragma unroll
+      for (int p = 0; p < NP; ++p) uf[f + wave][p][lane] = round_off8(w);
     }
   }
   __syncthreads();
@@ -264,11 +278,14 @@ void k_lora_up(LoraArgs a) {
     if (adapted) {
 #pragma unroll
       for (int k = 0; k < KS; ++k) {
-        const Frag fr = {uf[i * KS + k][0][lane], uf[i * KS + k][1][lane]};
 #pragma unroll
-        for (int b = 0; b < BLOCKS; ++b)
+        for (int p = 0; p < NP; ++p) {
+          const bf16x8 u = uf[i * KS + k][p][lane];
 #pragma unroll
-          for (int h = 0; h < 2; ++h) acc[b][h] = mma_x2(bf[b][h][k], fr, acc[b][h]);   // rows columns, columns tokens
+          for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) acc[b][h] = mma(bf[b][h][k], u, acc[b][h]);   // rows columns, columns tokens
+        }
       }
     }
 #pragma unroll

@@ -1,8 +1,9 @@
 """Low-rank adapters beside a shared projection against their fp64 form.
 
 Bounds.  x A^T is summed over K and its product with B^T over R products in
-fp32, the first factor through the matrix cores in two bf16 parts (2^-16): the
-result is within (K + R + 8) 2^-24 + 2^-16 of the sum over magnitudes; a bf16
+fp32: the result is within (K + R + 8) 2^-24 of the sum over magnitudes.  For a
+bf16 output the first factor goes through the matrix cores in two bf16 parts
+(2^-16), for an fp32 one in three (24 bits, one more rounding of 2^-24), and the
 output is rounded by 2^-8 of itself.
 """
 import pytest
@@ -41,8 +42,9 @@ def check(i, out):
     T = int(i["cu_host"][-1])
     e, mag = ref.lora(i["base"], i["x"], i["a"], i["b"], i["ids"], i["cu_host"].tolist(), i["scales"])
     K, R = i["x"].shape[1], i["a"].shape[1]
-    bound = ((K + R + 8) * 2.0 ** -24 + 2.0 ** -16) * mag
+    bound = (K + R + 9) * 2.0 ** -24 * mag
     if out.dtype == torch.bfloat16:
+        bound = bound + 2.0 ** -16 * mag
         bound = bound + 2.0 ** -8 * e.abs() * (1 + 2.0 ** -7)
     off = (out.double() - e).abs()[:T]
     worst = float((off / (bound[:T] + 1e-37)).max()) if off.numel() else 0.0
