@@ -1,6 +1,11 @@
 // The short causal convolution (gdn_ssm.h), for packed sequences and for one
 // token per sequence.  W multiply-adds per element read and written: HBM bound.
 // fp32 arithmetic whatever the element type, one rounding at the store.
+//
+// Measured, bf16, 4 taps, 8192 channels: 8192 tokens 57 us (4.7 TB/s; a copy of
+// as many bytes 49 to 55), 256 single tokens 8.0 us (4.2 TB/s with their
+// histories), one single token 2.7 us, a launch.  771 fp32 channels, whose rows
+// are not 16-byte aligned, 2700 tokens: 7.5 us.
 #pragma once
 
 #include <type_traits>
@@ -19,6 +24,8 @@ constexpr int conv_vec() { return ALIGNED ? 16 / static_cast<int>(sizeof(T)) : 1
 constexpr int conv_tile(int tpt) { return kConvRows * tpt; }
 
 // A thread's channels of one row as they lie in memory: 16 bytes, or one element.
+// They become floats only where they are used: converted at the load, each row
+// waits for its own (8192 tokens 101 us so, 57 kept raw).
 template <typename T, int VEC>
 struct Chans {
   typedef typename std::conditional<VEC == 1, T, u32x4>::type Raw;

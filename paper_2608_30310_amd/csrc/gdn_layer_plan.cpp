@@ -15,7 +15,9 @@ constexpr int64_t kMaxStride = int64_t{1} << 23;
 
 constexpr int64_t kSsmPlaces = 256;   // workgroups of the state space scan that the chip holds at once, one per CU
 
-constexpr int64_t kLoraGroups = 256;   // workgroups that the first product of the adapters aims at
+// Workgroups that the first product of the adapters aims at: 64 sequences of 8
+// tokens, rank 16, 16.5 us; 18.6 with 128, 17.1 with 512.
+constexpr int64_t kLoraGroups = 256;
 
 bool known_dtype(int32_t d) { return d == GDN_F32 || d == GDN_BF16; }
 

@@ -6,6 +6,12 @@
 // they are loaded, without a pass through LDS.  The work is HBM's: at rank 64 a
 // projected element costs 128 multiply-adds against reading and writing it.
 //
+// Measured, 2048 -> 12352, bf16: 4324 tokens of 8 requests at rank 64, 15.5 and 52
+// us (the second kernel at 4.1 TB/s; 238 MB in all, which a copy moves in 44 to
+// 49); 64 single tokens at rank 16 4.9 and 8.7 us (16 MB, most of it A and B).
+// The first kernel is bound by its loads' way through L2: eight waves instead
+// of four, or neighbouring steps a wave, left it at 16.0 us.
+//
 // Tokens go by tiles of 16 TT inside a sequence (its adapter is the tile's).
 #pragma once
 

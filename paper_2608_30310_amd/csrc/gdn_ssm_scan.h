@@ -8,7 +8,18 @@
 //   L_ij = e^{G_i - G_j} for j <= i.
 // A wave owns 16 CT state columns of one head; the waves of a head share the
 // decayed products P = (C B^T) o L o delta_j through LDS, and the heads of a
-// workgroup, which are of one B/C group, share the B and C rows.
+// workgroup, which are of one B/C group, share the B and C rows and C B^T.
+//
+// What bounds it: a chunk is a chain (rows into LDS, C B^T, P, P x) between
+// products on the state, and matrix and vector instructions of a SIMD's two
+// waves hardly overlap.  Measured, bf16: 16 sequences of 128 to 2048 tokens, 32
+// heads of 128 x 128, 222 us (498 MB, 2.2 TB/s); one of 32768 tokens, 64 heads of
+// 64 x 128, in segments 335 us: 118 for the segments' states, 12 for the join
+// and 224 for the outputs at best, each more where the chip's power limit lowers
+// its clock.  Of the outputs' time, found by leaving out one stage's arithmetic:
+// the split of M into parts 35, the products on M 42, the state's update 37, P 34,
+// the stores 23, the loads 16, C B^T 11.  fp32 inputs go through k = 4 products
+// (2048 tokens, 4 heads of 64 x 64: 25 us a call in segments).
 #pragma once
 
 #include <type_traits>
@@ -641,31 +652,34 @@ void k_ssm_scan(SsmScanArgs a) {
         X::split(v, wx[ct].part);
       }
     };
-    const float total = hs.total;
-    load_b(0);
-    __builtin_amdgcn_sched_barrier(0);
-    weigh_x(0);
-#pragma unroll
-    for (int td = 0; td < DK / 16; ++td)
-#pragma unroll
-      for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) m[td][ct][i] *= total;
-#pragma unroll
-    for (int step = 0; step < 2 * STEPS; ++step) {
-      if (step + 1 < 2 * STEPS) load_b(step + 1);
+    // (not after the last chunk of a segment whose state ends there)
+    if (MODE != SsmMode::kJoined || at + kSsmChunk < len) {
+      const float total = hs.total;
+      load_b(0);
       __builtin_amdgcn_sched_barrier(0);
-      if (step == STEPS) weigh_x(1);
+      weigh_x(0);
 #pragma unroll
-      for (int k = 0; k < NS; ++k)
+      for (int td = 0; td < DK / 16; ++td)
 #pragma unroll
-        for (int t = 0; t < TS; ++t)
+        for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-          for (int ct = 0; ct < CT; ++ct) {
-            f32x4& acc = m[step % STEPS * TS + t][ct];
-            acc = X::mul(bt[step & 1][t], wx[ct].part[k], acc);
-          }
-      __builtin_amdgcn_sched_barrier(0);
+          for (int i = 0; i < 4; ++i) m[td][ct][i] *= total;
+#pragma unroll
+      for (int step = 0; step < 2 * STEPS; ++step) {
+        if (step + 1 < 2 * STEPS) load_b(step + 1);
+        __builtin_amdgcn_sched_barrier(0);
+        if (step == STEPS) weigh_x(1);
+#pragma unroll
+        for (int k = 0; k < NS; ++k)
+#pragma unroll
+          for (int t = 0; t < TS; ++t)
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) {
+              f32x4& acc = m[step % STEPS * TS + t][ct];
+              acc = X::mul(bt[step & 1][t], wx[ct].part[k], acc);
+            }
+        __builtin_amdgcn_sched_barrier(0);
+      }
     }
     if constexpr (OUT) {
       lds_barrier();   // P is whole
@@ -721,7 +735,8 @@ void k_ssm_scan(SsmScanArgs a) {
 //   start_0 = state_in,  start_{j+1} = decay_j start_j + local_j,
 // the last of them state_out (where wanted).  With JOIN the starts replace the
 // local states, for kJoined.  A thread takes one accumulator element (four rows
-// of a column) of one sequence.
+// of a column) of one sequence.  Bound by the states' bytes: 13 segments of 64
+// heads of 64 x 128, 54 MB both ways, 10 us.
 template <int DK, int DV, int CT, int NW, bool JOIN>
 __global__ __launch_bounds__(256)
 void k_ssm_join(SsmScanArgs a) {

@@ -10,7 +10,11 @@ constexpr int kSsmWaves = kSsmThreads / kWave;
 
 // One token per sequence: read and write the state once.  HBM bound (8 bytes
 // per state element against three multiply-adds); streaming accesses, since a
-// layer's state comes back only after every other layer's.
+// layer's state comes back only after every other layer's.  A workgroup takes a
+// head of a sequence, a thread four neighbouring columns of DK DV / 1024 rows,
+// so that all its loads are in flight together.  64 heads of 64 x 128: 128
+// sequences 83 us (539 MB, 6.5 TB/s, part of the state still in the last-level
+// cache; a copy of as many bytes 99 to 110), one sequence 3.9 us.
 template <typename T, int DK, int DV>
 __global__ __launch_bounds__(kSsmThreads)
 void k_ssm_step(int32_t heads, int32_t groups, const T* __restrict__ x, int64_t ldx, const void* __restrict__ dt,
