@@ -11,6 +11,7 @@ from __future__ import annotations
 import ctypes
 import functools
 import os
+import threading
 from fractions import Fraction
 from typing import Optional, Sequence, Union
 
@@ -278,15 +279,23 @@ def _need(t, name, dtype, device, ndim):
         raise ValueError(f"{name} must be contiguous")
 
 
-_WORKSPACES = {}
+class _Workspaces(threading.local):
+    """The workspaces kept per (device, stream), each thread its own: the launches
+    of two threads' calls may take turns on one stream."""
+
+    def __init__(self):
+        self.kept = {}
+
+
+_WORKSPACES = _Workspaces()
 
 
 def _workspace(nbytes: int, device: torch.device, stream) -> torch.Tensor:
     key = (device.index, stream)
-    ws = _WORKSPACES.get(key)
+    ws = _WORKSPACES.kept.get(key)
     if ws is None or ws.numel() < nbytes:
         ws = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
-        _WORKSPACES[key] = ws
+        _WORKSPACES.kept[key] = ws
     if ws.data_ptr() % 256:
         raise RuntimeError("workspace allocation is not 256-byte aligned")
     return ws

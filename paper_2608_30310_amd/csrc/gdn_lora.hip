@@ -69,9 +69,9 @@ gdn_status lora_run(const gdn_lora_shape* s, const int32_t* cu_host, const int32
   if (st != GDN_OK) return lfail(st, err);
   const int64_t tokens = p.tokens;
   if (s->num_seqs == 0) return GDN_OK;
-  if (!adapters_host) return lfail(GDN_ERR_NULL_ARG, "adapters_host is NULL");
+  if (tokens > 0 && !adapters_host) return lfail(GDN_ERR_NULL_ARG, "adapters_host is NULL");
   bool any = false;
-  for (int32_t n = 0; n < s->num_seqs; ++n) {
+  for (int32_t n = 0; adapters_host && n < s->num_seqs; ++n) {
     if (adapters_host[n] < -1 || adapters_host[n] >= s->num_adapters)
       return lfail(GDN_ERR_BAD_SHAPE, "adapters_host must hold -1 or an adapter's index");
     any = any || (adapters_host[n] >= 0 && cu_host[n + 1] > cu_host[n]);

@@ -99,7 +99,7 @@ def _offsets(cu_seqlens, cu_seqlens_host, device, tokens):
 
 def _run_with_workspace(call, size, shape, host, device, stream, given):
     """``call(workspace, its bytes)`` with the caller's workspace, or with the one
-    kept per (device, stream); the library refuses a workspace that is too small
+    kept per thread, device and stream; the library refuses a workspace that is too small
     before it enqueues anything, and only then its size is asked for.  A call
     that is being captured takes memory of its graph's own pool instead: no other
     graph shares it, and no later call outside can replace it."""
@@ -110,7 +110,7 @@ def _run_with_workspace(call, size, shape, host, device, stream, given):
         return
     kept = None
     if not torch._C._cuda_isCurrentStreamCapturing():
-        kept = _WORKSPACES.get((device.index, stream))
+        kept = _WORKSPACES.kept.get((device.index, stream))
         status = call(None, 0) if kept is None else call(kept.data_ptr(), kept.numel())
         if status != GDN_ERR_WORKSPACE:
             _check(status)

@@ -10,6 +10,7 @@ import ctypes
 import os
 import shutil
 import subprocess
+import threading
 
 import pytest
 import torch
@@ -155,6 +156,7 @@ def test_nothing_to_do_is_no_error():
     assert conv(lens=(0, 0), cu=None, x=None, y=None, w=None) == 0
     assert scan(lens=(), cu=None, x=None) == 0
     assert lora(lens=(0, 0), base=None, x=None, out=None, ws=None) == 0
+    assert lora(lens=(0, 0), ids=None, dev_ids=None, base=None, x=None, out=None, ws=None) == 0
     assert lora(lens=(), ids=(), host="lens") == 0
 
 
@@ -172,6 +174,14 @@ def test_adapted_layer_workspace():
     for bad in (LAAdapters(2, 12, 8), LAAdapters(2, 16, 200), LAAdapters(-1, 16, 8)):
         assert lib.gdn_la_block_adapted_workspace_size(ctypes.byref(shp), ctypes.byref(bad), c, 1, ctypes.byref(adapted))
     assert lib.gdn_la_block_adapted_workspace_size(ctypes.byref(shp), None, c, 1, ctypes.byref(adapted)) == NULL
+
+
+def test_workspaces_are_a_threads_own():
+    seen = []
+    t = threading.Thread(target=lambda: seen.append(binding._WORKSPACES.kept))
+    t.start()
+    t.join()
+    assert seen[0] == {} and seen[0] is not binding._WORKSPACES.kept
 
 
 def test_calls_refuse_host_tensors():

@@ -9,6 +9,8 @@ matrix cores in bf16 parts: in the states three of them (24 bits, nothing
 added), in the outputs two (within 2^-16 each for the state and for the decayed
 products, so 2^-15).  A bf16 output is rounded once more, by 2^-8 of itself.
 """
+import threading
+
 import pytest
 import torch
 
@@ -258,6 +260,29 @@ def test_two_streams_at_once():
     torch.cuda.synchronize()
     for (y, s), wy, ws in got:
         assert torch.equal(y, wy) and torch.equal(s, ws)
+
+
+def test_two_threads_on_one_stream():
+    """Launches of two threads' calls may take turns on a stream: each has a workspace of its own."""
+    both = [inputs([1500], H=4, G=1, N=128, seed=26), inputs([1800], H=4, G=1, N=128, seed=27)]
+    want_ = [scan(i) for i in both]
+    torch.cuda.synchronize()
+    got = [[], []]
+
+    def work(k):
+        for _ in range(40):
+            got[k].append(scan(both[k]))
+
+    threads = [threading.Thread(target=work, args=(k,)) for k in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join(60)
+    torch.cuda.synchronize()
+    for k in range(2):
+        assert len(got[k]) == 40
+        for y, s in got[k]:
+            assert torch.equal(y, want_[k][0]) and torch.equal(s, want_[k][1])
 
 
 def test_many_sequences():
