@@ -320,8 +320,13 @@ struct SsmLayout {
 // Row and first column of state tile (td, ct) of lane (g, c); see strow.
 __device__ __forceinline__ int ssm_col(int ct, int c) { return 32 * (ct >> 1) + 8 * (c / 4) + 4 * (ct & 1) + c % 4; }
 
+// Waves of a SIMD that the registers are kept for: two for bf16 inputs, where a
+// CU's LDS holds enough workgroups.
+template <typename T, int NW, int BYTES>
+constexpr int ssm_waves() { return sizeof(T) == 2 && 160 * 1024 / BYTES * NW / 4 >= 2 ? 2 : 1; }
+
 template <typename T, int DK, int DV, int CT, int NW, SsmMode MODE, bool OUT>
-__global__ __launch_bounds__(NW * kWave, sizeof(T) == 2 ? 2 : 1)
+__global__ __launch_bounds__(NW * kWave, (ssm_waves<T, NW, SsmLayout<T, DK, DV, CT, NW, OUT>::kBytes>()))
 void k_ssm_scan(SsmScanArgs a) {
   typedef SsmLayout<T, DK, DV, CT, NW, OUT> L;
   typedef typename L::KRows KRows;
