@@ -134,16 +134,16 @@ gdn_status make_ssm_plan(const gdn_ssm_shape* s, const int32_t* cu, SsmPlan* pla
       p.slots = segs;
     }
   }
-  // Four heads of 64 columns in pairs instead, whole sequences, while there is a
-  // place for every pair: twice the CUs at 0.77 of the time a chunk.  Measured, 64
-  // heads of 64 x 128: one sequence of 1, 2 and 3 chunks 9.6, 14.4 and 19.4 us in
-  // pairs, 12.2, 18.4 and 24.5 in fours; 8 of 1, 3 and 13: 14.5, 25.5 and 72.9, 16.6,
-  // 29.8 and 89.7; but 32 of 32 chunks 676, 486.  (Two heads of 128 columns gain
-  // nothing one by one: 8 sequences of 3 chunks 31.5 us, 28.8 in pairs.)
-  if (bf16 && share == 4 && N * (H / 2) <= kSsmPlaces && 0.7 + 0.77 * static_cast<double>(longest) < best) {
-    p.heads_per_group = 2;
+  // Half the heads a workgroup instead, whole sequences, while there is a place for
+  // every workgroup: twice the CUs at 0.77 of the time a chunk.  Measured, 64
+  // heads of 64 x 128: one sequence of 1, 2 and 3 chunks 9.6, 14.4 and 19.4 us by
+  // twos, 12.2, 18.4 and 24.5 by fours; 8 of 1, 3 and 13: 14.5, 25.5 and 72.9, 16.6,
+  // 29.8 and 89.7; but 32 of 32 chunks 676, 486.
+  if (bf16 && share * s->head_dim == kSsmCols && N * (H / (share / 2)) <= kSsmPlaces &&
+      0.7 + 0.77 * static_cast<double>(longest) < best) {
+    p.heads_per_group = share / 2;
     p.slots = N;
-    groups = H / 2;
+    groups = H / p.heads_per_group;
     seg = 0;
   }
   if (seg > 0) {

@@ -321,12 +321,18 @@ struct SsmLayout {
 __device__ __forceinline__ int ssm_col(int ct, int c) { return 32 * (ct >> 1) + 8 * (c / 4) + 4 * (ct & 1) + c % 4; }
 
 // Waves of a SIMD that the registers are kept for: two for bf16 inputs, where a
-// CU's LDS holds enough workgroups.
-template <typename T, int NW, int BYTES>
-constexpr int ssm_waves() { return sizeof(T) == 2 && 160 * 1024 / BYTES * NW / 4 >= 2 ? 2 : 1; }
+// CU's LDS holds enough workgroups.  Whole sequences with outputs and 128 state
+// rows want more than 256 registers, for which four waves a workgroup can give up
+// the second one: 32 heads of 128 x 128, one a workgroup, 8 sequences of 512 tokens
+// 47 us with one, 66 with two, 16 of 2048 334 and 383 (71 registers spilled).
+template <typename T, int DK, int NW, SsmMode MODE, bool OUT, int BYTES>
+constexpr int ssm_waves() {
+  if (sizeof(T) != 2 || 160 * 1024 / BYTES * NW / 4 < 2) return 1;
+  return MODE == SsmMode::kWhole && OUT && DK == 128 && NW <= 4 ? 1 : 2;
+}
 
 template <typename T, int DK, int DV, int CT, int NW, SsmMode MODE, bool OUT>
-__global__ __launch_bounds__(NW * kWave, (ssm_waves<T, NW, SsmLayout<T, DK, DV, CT, NW, OUT>::kBytes>()))
+__global__ __launch_bounds__(NW * kWave, (ssm_waves<T, DK, NW, MODE, OUT, SsmLayout<T, DK, DV, CT, NW, OUT>::kBytes>()))
 void k_ssm_scan(SsmScanArgs a) {
   typedef SsmLayout<T, DK, DV, CT, NW, OUT> L;
   typedef typename L::KRows KRows;
