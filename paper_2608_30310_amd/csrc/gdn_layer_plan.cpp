@@ -4,6 +4,7 @@
 #include "gdn_plan.h"
 
 #include <algorithm>
+#include <functional>
 #include <limits>
 
 namespace gdn {
@@ -18,6 +19,31 @@ constexpr int64_t kSsmPlaces = 256;   // workgroups of the state space scan that
 // Workgroups that the first product of the adapters aims at: 64 sequences of 8
 // tokens, rank 16, 16.5 us; 18.6 with 128, 17.1 with 512.
 constexpr int64_t kLoraGroups = 256;
+
+int64_t chunks_of(const int32_t* cu, int64_t n) { return (static_cast<int64_t>(cu[n + 1]) - cu[n] + 63) / 64; }
+
+constexpr int64_t kXcds = 8;
+
+// Chunks after which the last of n <= kSsmOrdered sequences ends: the longest
+// first, dealt to the XCDs there and back, `lanes` of them at once on each, where the
+// next starts as one ends.
+double longest_first(const int32_t* cu, int64_t n, int64_t lanes) {
+  int64_t chunks[kSsmOrdered];
+  for (int64_t i = 0; i < n; ++i) chunks[i] = chunks_of(cu, i);
+  std::sort(chunks, chunks + n, std::greater<int64_t>());
+  int64_t end = 0;
+  for (int64_t x = 0; x < kXcds; ++x) {
+    int64_t busy[kSsmOrdered] = {};   // a heap, the lane that is free first in front
+    for (int64_t row = 0; row * kXcds < n; ++row) {
+      const int64_t r = row * kXcds + (row % 2 != 0 && (row + 1) * kXcds <= n ? kXcds - 1 - x : x);
+      if (r >= n) continue;
+      std::pop_heap(busy, busy + lanes, std::greater<int64_t>());
+      end = std::max(end, busy[lanes - 1] += chunks[r]);
+      std::push_heap(busy, busy + lanes, std::greater<int64_t>());
+    }
+  }
+  return static_cast<double>(end);
+}
 
 bool known_dtype(int32_t d) { return d == GDN_F32 || d == GDN_BF16; }
 
@@ -103,9 +129,23 @@ gdn_status make_ssm_plan(const gdn_ssm_shape* s, const int32_t* cu, SsmPlan* pla
   const bool bf16 = s->dtype == GDN_BF16;
   int32_t share = (bf16 ? kSsmCols : kSsmColsF32) / s->head_dim;
   while (H / s->num_groups % share != 0) share /= 2;
-  p.heads_per_group = share;
-  p.slots = N;
-  int64_t groups = H / share;   // workgroups of a sequence
+  // Whole sequences: the longest one, or what the places' shares of the work come to.
+  const int64_t longest = (p.longest + 63) / 64;
+  int64_t chunks = 0;
+  for (int64_t n = 0; n < N; ++n) chunks += chunks_of(cu, n);
+  // More sequences than fit at once start with the longest, unless there is so much
+  // work that the last one's length does not matter (us, 32 heads of 128 x 128: 24
+  // sequences of 1 to 1000 tokens 146, as they come 196; 40 of 1 to 800 187 and 215; 64
+  // of 1 to 300 151 and 139).
+  const auto orderable = [&](int64_t groups) {
+    return N * groups > kSsmPlaces && N <= kSsmOrdered && groups <= kSsmPlaces / kXcds &&
+           2 * longest * kSsmPlaces >= chunks * groups;
+  };
+  const auto whole = [&](int64_t groups) {
+    if (N * groups <= kSsmPlaces) return static_cast<double>(longest);
+    if (orderable(groups)) return longest_first(cu, N, std::min<int64_t>(kSsmOrdered, kSsmPlaces / kXcds / groups));
+    return std::max(static_cast<double>(longest), static_cast<double>(chunks * groups) / kSsmPlaces);
+  };
   // Whole sequences end with the longest one, or with the work per place; in
   // segments the work is even, but every chunk is walked twice (once for the
   // states alone), the segments' states pass through memory and there are two
@@ -114,38 +154,38 @@ gdn_status make_ssm_plan(const gdn_ssm_shape* s, const int32_t* cu, SsmPlan* pla
   // number.  Measured, 64 heads of 64 x 128, one sequence of 2, 3, 8, 24 and 128
   // chunks: whole 18, 25, 55, 152 and 776 us, segments 24, 26, 37, 44 and 105;
   // 32 heads of 128 x 128, 8 sequences of 8 and 16, 4 of 64: 58, 104 and 397, 73, 110 and 190.
-  const auto chunks_of = [&](int64_t n) { return (static_cast<int64_t>(cu[n + 1]) - cu[n] + 63) / 64; };
-  int64_t chunks = 0;
-  for (int64_t n = 0; n < N; ++n) chunks += chunks_of(n);
-  const int64_t longest = (p.longest + 63) / 64;
-  double best = 0.8 + std::max(static_cast<double>(longest), static_cast<double>(chunks * groups) / kSsmPlaces);
+  int64_t groups = H / share;   // workgroups of a sequence
+  double best = 0.8 + whole(groups);
+  p.heads_per_group = share;
+  p.slots = N;
+  // Half the heads a workgroup, whole sequences: twice the CUs at 0.77 of the time
+  // a chunk.  Measured, 64 heads of 64 x 128: one sequence of 1, 2 and 3 chunks
+  // 9.6, 14.4 and 19.4 us by twos, 12.2, 18.4 and 24.5 by fours; 8 of 1, 3 and 13:
+  // 14.5, 25.5 and 72.9, 16.6, 29.8 and 89.7; but 32 of 32 chunks 676, 486.  And 32 heads
+  // of 128 x 128, 16 of 2 to 32 chunks: 202 one by one, 223 by twos.
+  if (bf16 && share * s->head_dim == kSsmCols)
+    if (const double cost = 0.7 + 0.77 * whole(2 * groups); cost < best) {
+      best = cost;
+      p.heads_per_group = share / 2;
+    }
   const int64_t least = std::max<int64_t>(1, (chunks * groups + kSsmPlaces - 1) / kSsmPlaces);
   int64_t seg = 0;
   const bool joinable = N * H * s->d_state * s->head_dim / 4 <= kMaxGrid;   // a thread of the join takes four elements
   for (int64_t more = 0; joinable && more <= 4 && least + more * ((least + 3) / 4) < longest; ++more) {
     const int64_t try_seg = least + more * ((least + 3) / 4);
     int64_t segs = 0;
-    for (int64_t n = 0; n < N; ++n) segs += std::max<int64_t>(1, (chunks_of(n) + try_seg - 1) / try_seg);
+    for (int64_t n = 0; n < N; ++n) segs += std::max<int64_t>(1, (chunks_of(cu, n) + try_seg - 1) / try_seg);
     const int64_t rounds = (segs * groups + kSsmPlaces - 1) / kSsmPlaces;
     const double cost = 2.5 + 1.5 * static_cast<double>(try_seg * rounds) + 0.0093 * static_cast<double>(segs * groups);
     if (cost < best) {
       best = cost;
       seg = try_seg;
       p.slots = segs;
+      p.heads_per_group = share;
     }
   }
-  // Half the heads a workgroup instead, whole sequences, while there is a place for
-  // every workgroup: twice the CUs at 0.77 of the time a chunk.  Measured, 64
-  // heads of 64 x 128: one sequence of 1, 2 and 3 chunks 9.6, 14.4 and 19.4 us by
-  // twos, 12.2, 18.4 and 24.5 by fours; 8 of 1, 3 and 13: 14.5, 25.5 and 72.9, 16.6,
-  // 29.8 and 89.7; but 32 of 32 chunks 676, 486.
-  if (bf16 && share * s->head_dim == kSsmCols && N * (H / (share / 2)) <= kSsmPlaces &&
-      0.7 + 0.77 * static_cast<double>(longest) < best) {
-    p.heads_per_group = share / 2;
-    p.slots = N;
-    groups = H / p.heads_per_group;
-    seg = 0;
-  }
+  groups = H / p.heads_per_group;
+  p.ordered = seg == 0 && orderable(groups);
   if (seg > 0) {
     p.seg_tokens = static_cast<int32_t>(64 * seg);
     const size_t state = static_cast<size_t>(H) * s->d_state * s->head_dim * sizeof(float);

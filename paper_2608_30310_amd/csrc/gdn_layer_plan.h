@@ -17,6 +17,8 @@ namespace gdn {
 // 16 sequences of 2048 tokens, 32 heads of 128 x 128, 251 and 354 us; one of 8192,
 // 64 heads of 64 x 128, 105 and 124.
 constexpr int32_t kSsmCols = 256, kSsmColsF32 = 128;
+// Sequences that the scan's workgroups rank by themselves, one a lane.
+constexpr int32_t kSsmOrdered = 64;
 
 // Packed sequences cut into tiles of `tile` tokens, each sequence from its own
 // start: tile j of sequence n is slot cu[n] / tile + n + j.  The map is
@@ -37,6 +39,7 @@ struct SsmPlan {
   int64_t tokens = 0, longest = 0;
   int32_t heads_per_group = 1;   // heads of a workgroup
   int32_t seg_tokens = 0;        // 0: whole sequences
+  bool ordered = false;          // whole sequences, more than the chip holds: the longest first
   int64_t slots = 0;             // segments (an empty sequence has one), or sequences
   size_t off_decay = 0;          // workspace: states [slots, H, d_state, head_dim], then decays [slots, H]
   size_t bytes = 0;

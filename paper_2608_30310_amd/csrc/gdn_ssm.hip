@@ -57,7 +57,7 @@ template <typename T, int DK, int DV, int CT, int NW>
 gdn_status launch_scan(const SsmArgs& a) {
   const gdn_ssm_shape& s = *a.s;
   const SsmPlan& p = *a.p;
-  SsmScanArgs k{s.num_seqs, s.num_heads, s.num_groups, p.seg_tokens, a.cu, a.x, a.dt, a.B, a.C,
+  SsmScanArgs k{s.num_seqs, s.num_heads, s.num_groups, p.seg_tokens, p.ordered, a.cu, a.x, a.dt, a.B, a.C,
                 s.ld_x, s.ld_dt, s.ld_b, s.ld_c, s.ld_y, s.dt_dtype == GDN_BF16, a.a_log, a.d_skip, a.dt_bias,
                 a.state_in, a.y, a.state_out, reinterpret_cast<f32x4*>(a.ws),
                 reinterpret_cast<float*>(a.ws + p.off_decay)};

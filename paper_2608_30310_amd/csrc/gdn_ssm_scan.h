@@ -11,15 +11,15 @@
 // workgroup, which are of one B/C group, share the B and C rows and C B^T.
 //
 // What bounds it: a chunk is a chain (rows into LDS, C B^T, P, P x) between
-// products on the state, and matrix and vector instructions of a SIMD's two
-// waves hardly overlap.  Measured, bf16: 16 sequences of 128 to 2048 tokens, 32
-// heads of 128 x 128, 222 us (498 MB, 2.2 TB/s); one of 32768 tokens, 64 heads of
-// 64 x 128, in segments 335 us: 118 for the segments' states, 12 for the join
+// products on the state, and matrix and vector instructions of a SIMD's waves
+// hardly overlap.  Measured, bf16: 16 sequences of 128 to 2048 tokens, 32
+// heads of 128 x 128, 195 us (498 MB, 2.6 TB/s); one of 32768 tokens, 64 heads of
+// 64 x 128, in segments 338 us: 118 for the segments' states, 12 for the join
 // and 224 for the outputs at best, each more where the chip's power limit lowers
 // its clock.  Of the outputs' time, found by leaving out one stage's arithmetic:
 // the split of M into parts 35, the products on M 42, the state's update 37, P 34,
 // the stores 23, the loads 16, C B^T 11.  fp32 inputs go through k = 4 products
-// (2048 tokens, 4 heads of 64 x 64: 25 us a call in segments).
+// (2048 tokens, 4 heads of 64 x 64: 23 us a call in segments).
 #pragma once
 
 #include <type_traits>
@@ -270,8 +270,22 @@ __device__ __forceinline__ int segments_before(const int32_t* __restrict__ cu, i
   return total;
 }
 
+// The sequence of rank r by chunks, the longest first, equal ones as they come;
+// at most 64 sequences.  Uniform over the wave.
+__device__ __forceinline__ int nth_longest(const int32_t* __restrict__ cu, int n_seqs, int r) {
+  const int lane = threadIdx.x % kWave;
+  const int mine = lane < n_seqs ? (cu[lane + 1] - cu[lane] + kSsmChunk - 1) / kSsmChunk : -1;
+  int rank = 0;
+  for (int j = 0; j < n_seqs; ++j) {
+    const int other = __builtin_amdgcn_readlane(mine, j);
+    rank += other > mine || (other == mine && j < lane) ? 1 : 0;
+  }
+  return max(__ffsll(static_cast<unsigned long long>(__ballot(lane < n_seqs && rank == r))) - 1, 0);
+}
+
 struct SsmScanArgs {
   int32_t n_seqs, heads, groups, seg_tokens;
+  bool ordered;   // kWhole: unit r is the sequence of rank r
   const int32_t* cu;
   const void* x;
   const void* dt;
@@ -351,7 +365,14 @@ void k_ssm_scan(SsmScanArgs a) {
   const int unit = xcd_cluster_remap(blockIdx.x, gridDim.x, hgs);
   const int hg = unit % hgs, slot = unit / hgs;
   int n = slot, first = 0;
-  if constexpr (MODE != SsmMode::kWhole) {
+  if constexpr (MODE == SsmMode::kWhole) {
+    // a sequence's workgroups go to one XCD, its neighbours' to the next: every other
+    // row of eight backwards, so that the first XCD does not get the longest of each
+    if (a.ordered) {
+      const int rank = (slot & kXcds) && (slot | (kXcds - 1)) < a.n_seqs ? slot ^ (kXcds - 1) : slot;
+      n = __builtin_amdgcn_readfirstlane(nth_longest(a.cu, a.n_seqs, rank));
+    }
+  } else {
     const SegmentAt at = segment_at(a.cu, a.n_seqs, a.seg_tokens, slot);
     n = at.n;
     first = at.j * a.seg_tokens;

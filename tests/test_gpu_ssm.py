@@ -301,6 +301,16 @@ def test_as_many_sequences_as_places(N):
     check(one, *scan(one))
 
 
+@pytest.mark.parametrize("n", [13, 20, 64, 65])
+@pytest.mark.parametrize("H,G,P", [(64, 1, 64), (32, 8, 64), (32, 16, 128)])
+def test_more_sequences_than_places(n, H, G, P):
+    """Ragged batches whose workgroups do not fit at once: the longest start first."""
+    some = [200, 3, 0, 64, 65, 1, 130, 17, 2, 80, 5, 9, 33]
+    lens = [some[k % 13] if k < 13 else (7 * k) % 40 for k in range(n)]
+    i = inputs(lens, H=H, G=G, N=64, P=P, seed=n, spare=2)
+    check(i, *scan(i))
+
+
 def test_arguments_by_name():
     i = inputs([40, 30], seed=25)
     y, st = scan(i)
