@@ -231,12 +231,14 @@ gdn_status make_lora_plan(const gdn_lora_shape* s, const int32_t* cu, LoraPlan* 
   if (st == GDN_OK) st = check_seqlens(s->num_seqs, cu, &p.tokens, &longest, err);
   if (st != GDN_OK) return st;
   // Small tiles where larger ones would be mostly empty, or too few for the CUs.
-  // Measured (2048 -> 12352, us, small and large tiles): 64 sequences of 1, 8 and 32
-  // tokens at rank 16 12.3, 16.5 and 30.6, 16.6, 20.4 and 28.6; at rank 64 8 of 32
+  // Measured (2048 -> 12352, us), tiles of 16 tokens and of 32 and 64: 64 sequences of 1, 8
+  // and 32 tokens at rank 16 12.3, 16.5 and 30.6, 16.6, 20.4 and 28.6; at rank 64 8 of 32
   // tokens 17.4, 23.3, one of 819 27.8, 31.1, 8 of 128 33.5 both, of 512 88, 61.
+  // Second product, tiles of 32 and of 64: 64 sequences of 32 tokens 26.7, 35.1, at rank
+  // 64 8 of 512 56.6, 58.9, of 1500 182.7, 162.3.
   const bool tokenwise = p.tokens <= std::max<int64_t>(1024, 16 * static_cast<int64_t>(s->num_seqs));
   p.down_tile = tokenwise ? 16 : 32;
-  p.up_tile = tokenwise ? 16 : 64;
+  p.up_tile = tokenwise ? 16 : p.tokens > 6144 && p.tokens >= 64 * static_cast<int64_t>(s->num_seqs) ? 64 : 32;
   p.down_slots = tile_slots(p.tokens, s->num_seqs, p.down_tile);
   p.up_slots = tile_slots(p.tokens, s->num_seqs, p.up_tile);
   // x A^T in parts of K until there are workgroups for every CU (64 sequences of 4

@@ -50,8 +50,8 @@ gdn_status check_lora(const gdn_lora_shape* s, std::string* err);
 
 struct LoraPlan {
   int64_t tokens = 0;
-  // tokens of a tile of the first and of the second product (32 and 64, or 16
-  // where there are few tokens) and their slots
+  // tokens of a tile of the first and of the second product (32, 64 in the second
+  // where there are many, 16 in both where there are few) and their slots
   int32_t down_tile = 0, up_tile = 0;
   int64_t down_slots = 0, up_slots = 0;
   int32_t parts = 1;   // pieces of the first product's contraction over K

@@ -4,6 +4,7 @@
 
 #include <algorithm>
 #include <string>
+#include <type_traits>
 
 #include "gdn_layer_plan.h"
 #include "gdn_lora_call.h"
@@ -45,15 +46,17 @@ void launch_down(const LoraArgs& k, int64_t slots, hipStream_t stream) {
 
 template <typename T>
 gdn_status launch_lora(const LoraArgs& k, const LoraPlan& p, bool any, bool wide, hipStream_t stream) {
-  if (p.up_tile == lora_tile(4)) {
-    if (any) launch_down<2>(k, p.down_slots, stream);
-    if (wide) launch_up<T, 4, true>(k, p.up_slots, stream);
-    else launch_up<T, 4, false>(k, p.up_slots, stream);
-  } else {
-    if (any) launch_down<1>(k, p.down_slots, stream);
-    if (wide) launch_up<T, 1, true>(k, p.up_slots, stream);
-    else launch_up<T, 1, false>(k, p.up_slots, stream);
+  if (any) {
+    if (p.down_tile == lora_tile(2)) launch_down<2>(k, p.down_slots, stream);
+    else launch_down<1>(k, p.down_slots, stream);
   }
+  const auto up = [&](auto tt) {
+    if (wide) launch_up<T, tt.value, true>(k, p.up_slots, stream);
+    else launch_up<T, tt.value, false>(k, p.up_slots, stream);
+  };
+  if (p.up_tile == lora_tile(4)) up(std::integral_constant<int, 4>{});
+  else if (p.up_tile == lora_tile(2)) up(std::integral_constant<int, 2>{});
+  else up(std::integral_constant<int, 1>{});
   return llaunched("adapter launch");
 }
 

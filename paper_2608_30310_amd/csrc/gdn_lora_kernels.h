@@ -6,9 +6,9 @@
 // they are loaded, without a pass through LDS.  The work is HBM's: at rank 64 a
 // projected element costs 128 multiply-adds against reading and writing it.
 //
-// Measured, 2048 -> 12352, bf16: 4324 tokens of 8 requests at rank 64, 15.5 and 52
-// us (the second kernel at 4.1 TB/s; 238 MB in all, which a copy moves in 44 to
-// 49); 64 single tokens at rank 16 4.9 and 8.7 us (16 MB, most of it A and B).
+// Measured, 2048 -> 12352, bf16: 4324 tokens of 8 requests at rank 64, 15.3 and 48
+// us (the second kernel at 4.5 TB/s; 238 MB in all, which a copy moves in 44 to
+// 49); 64 single tokens at rank 16 5.1 and 8.7 us (16 MB, most of it A and B).
 // The first kernel is bound by its loads' way through L2: eight waves instead
 // of four, or neighbouring steps a wave, left it at 16.0 us.
 //
@@ -210,15 +210,24 @@ __device__ __forceinline__ bf16x8 round_off8(float (&w)[8]) {
   return __builtin_bit_cast(bf16x8, r);
 }
 
+// Tiles of bf16 tokens pass through LDS, so that base and out move as whole rows
+// of 512 bytes: 4324 tokens 47.5 us, 52 by 64-byte pieces of 16 rows from the lanes.
+// (Those of fp32 are 128 bytes.)
+constexpr int kLoraPitch = 2 * kLoraCols + 64;
+template <typename T, int TT, bool WIDE>
+constexpr bool lora_rows() { return sizeof(T) == 2 && WIDE; }
+
 // grid: slots x column tiles, an XCD takes neighbouring ones (they share u, and
 // the adapter's B stays in its L2).  A workgroup: a token tile x 256 columns, 64
 // of them a wave's, KS steps over the rank.  The tile's u goes through LDS once
 // for the four waves, as operands of bf16 parts: two (within 2^-16) where the
 // outputs are bf16, three (24 bits) where they are fp32.  A tile's rows of B are
 // taken in the order in which a lane ends up with eight neighbouring columns of
-// a token.
+// a token.  Rows through LDS: registers for as many waves as it holds workgroups
+// (left alone the compiler reads all of a tile ahead, with one wave a SIMD 81 us
+// for those 47.5).
 template <typename T, int TT, int KS, bool WIDE>
-__global__ __launch_bounds__(kLoraThreads)
+__global__ __launch_bounds__(kLoraThreads, (lora_rows<T, TT, WIDE>() ? (TT == 4 ? (KS < 4 ? 3 : 2) : 4) : 1))
 void k_lora_up(LoraArgs a) {
   constexpr int NP = sizeof(T) == 2 ? 2 : 3;
   __shared__ bf16x8 uf[TT * KS][NP][kWave];
@@ -234,14 +243,27 @@ void k_lora_up(LoraArgs a) {
   const T* base = static_cast<const T*>(a.base) + t.t0 * a.ldbase;
   T* out = static_cast<T*>(a.out) + t.t0 * a.ldout;
   // everything that is read is on its way before anything waits
-  Cols8<T, WIDE> was[TT][BLOCKS];
+  constexpr bool ROWS = lora_rows<T, TT, WIDE>();
+  constexpr int PIECES = kLoraCols / 8, STEP = kLoraThreads / PIECES, NPC = ROWS ? lora_tile(TT) / STEP : 1;
+  __shared__ __attribute__((aligned(16))) char tile[ROWS ? lora_tile(TT) * kLoraPitch : 16];
+  const int prow = threadIdx.x / PIECES, pcol = threadIdx.x % PIECES;
+  const int pm = unit % tiles * kLoraCols + 8 * pcol;
+  u32x4 piece[NPC];
+  Cols8<T, WIDE> was[ROWS ? 1 : TT][BLOCKS];
+  if constexpr (ROWS) {
 #pragma unroll
-  for (int i = 0; i < TT; ++i)
+    for (int k = 0; k < NPC; ++k)
+      if (prow + k * STEP < t.rows && pm < a.M)
+        piece[k] = *reinterpret_cast<const u32x4*>(base + (prow + k * STEP) * a.ldbase + pm);
+  } else {
 #pragma unroll
-    for (int b = 0; b < BLOCKS; ++b) {
-      const int row = 16 * i + c, m = m0 + 32 * b + 8 * g;
-      if (row < t.rows && m < a.M) was[i][b].load(base + row * a.ldbase + m, a.M - m);
-    }
+    for (int i = 0; i < TT; ++i)
+#pragma unroll
+      for (int b = 0; b < BLOCKS; ++b) {
+        const int row = 16 * i + c, m = m0 + 32 * b + 8 * g;
+        if (row < t.rows && m < a.M) was[i][b].load(base + row * a.ldbase + m, a.M - m);
+      }
+  }
   bf16x8 bf[BLOCKS][2][KS];
   if (adapted) {
 #pragma unroll
@@ -273,9 +295,16 @@ void k_lora_up(LoraArgs a) {
       for (int p = 0; p < NP; ++p) uf[f + wave][p][lane] = round_off8(w);
     }
   }
+  if constexpr (ROWS) {
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int k = 0; k < NPC; ++k)
+      *reinterpret_cast<u32x4*>(tile + (prow + k * STEP) * kLoraPitch + 16 * pcol) = piece[k];
+  }
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < TT; ++i) {
+    if constexpr (ROWS) __builtin_amdgcn_sched_barrier(0);
     f32x4 acc[BLOCKS][2];
 #pragma unroll
     for (int b = 0; b < BLOCKS; ++b)
@@ -297,12 +326,29 @@ void k_lora_up(LoraArgs a) {
 #pragma unroll
     for (int b = 0; b < BLOCKS; ++b) {
       const int row = 16 * i + c, m = m0 + 32 * b + 8 * g;
-      if (row >= t.rows || m >= a.M) continue;
       float v[8];
+      if constexpr (ROWS) {
+        if (!adapted) continue;
+        T* place = reinterpret_cast<T*>(tile + row * kLoraPitch) + wave * kLoraWaveCols + 32 * b + 8 * g;
+        was[0][b].load(place, 8);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = adapted ? was[i][b].get(e) + acc[b][e / 4][e % 4] : was[i][b].get(e);
-      Cols8<T, WIDE>::store(out + row * a.ldout + m, a.M - m, v);
+        for (int e = 0; e < 8; ++e) v[e] = was[0][b].get(e) + acc[b][e / 4][e % 4];
+        Cols8<T, WIDE>::store(place, 8, v);
+      } else {
+        if (row >= t.rows || m >= a.M) continue;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = adapted ? was[i][b].get(e) + acc[b][e / 4][e % 4] : was[i][b].get(e);
+        Cols8<T, WIDE>::store(out + row * a.ldout + m, a.M - m, v);
+      }
     }
+  }
+  if constexpr (ROWS) {
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < NPC; ++k)
+      if (prow + k * STEP < t.rows && pm < a.M)
+        *reinterpret_cast<u32x4*>(out + (prow + k * STEP) * a.ldout + pm) =
+            *reinterpret_cast<const u32x4*>(tile + (prow + k * STEP) * kLoraPitch + 16 * pcol);
   }
 }
 

@@ -127,6 +127,19 @@ def test_graph_replays():
         assert torch.equal(o, o0)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("pads", [(0, 0), (8, 3)])
+@pytest.mark.parametrize("lens", [[600, 0, 500, 47], [6000, 1, 400]])
+def test_many_tokens(dtype, pads, lens):
+    """Tiles of every size, in place and not, with a request that has no adapter."""
+    i = inputs(lens, [1, 0, -1, 2][:len(lens)], K=64, M=264, R=40, dtype=dtype, seed=len(lens), pads=pads, spare=3)
+    out = lora(i)
+    check(i, out)
+    same = i["base"].clone() if pads[1] == 0 else i["base"]
+    again = dict(i, base=same)
+    assert torch.equal(lora(again, out=same)[:sum(lens)], out[:sum(lens)])
+
+
 def test_no_tokens_and_no_adapters():
     i = inputs([0, 0], [0, -1], seed=8)
     assert lora(i).shape == (0, 96)
