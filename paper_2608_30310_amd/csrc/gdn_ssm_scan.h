@@ -200,11 +200,15 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_buffer(const void* base, 
 // Per head and chunk, in base 2: with l the inclusive cumulative log alpha inside
 // a token's 16-token tile and s what is left of the tile after it, e^{G_i - G_j}
 // = 2^(l_i - l_j) within a tile and 2^l_i 2^between 2^s_j across tiles, three
-// factors of at most one: exponents are sums of terms of one sign, never the
-// difference of two long ones, and no factor overflows.
+// factors of at most one, so no factor overflows.  Across tiles exponents are sums
+// of terms of one sign.  Within a tile they are the difference of two sums that
+// may be far longer (l reaches -2400, where fp32 steps by 2^-12: outputs off by
+// 1e-4): l is summed in 64 bits there and kept as two floats, whose differences
+// are as good as the sum of the steps between.
 struct HeadScalars {
-  float l[kSsmChunk];      // l
-  float same[kSsmChunk];   // log2 delta - l
+  float high[kSsmChunk];   // l rounded
+  float low[kSsmChunk];    // l - high
+  float same[kSsmChunk];   // log2 delta - low
   float row[kSsmChunk];    // 2^l
   float past[kSsmChunk];   // 2^s delta
   float pre[kSsmChunk];    // e^G
@@ -226,6 +230,21 @@ __device__ __forceinline__ float row_scan(float x) {
   x += dpp<SHIFT + 2>(x);
   x += dpp<SHIFT + 4>(x);
   x += dpp<SHIFT + 8>(x);
+  return x;
+}
+// The same from the row's start, in 64 bits.
+template <int CTRL>
+__device__ __forceinline__ double dpp(double x) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, x);
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, static_cast<int>(u), CTRL, 0xf, 0xf, true);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, static_cast<int>(u >> 32), CTRL, 0xf, 0xf, true);
+  return __builtin_bit_cast(double, static_cast<uint64_t>(hi) << 32 | lo);
+}
+__device__ __forceinline__ double row_scan_wide(double x) {
+  x += dpp<0x111>(x);
+  x += dpp<0x112>(x);
+  x += dpp<0x114>(x);
+  x += dpp<0x118>(x);
   return x;
 }
 __device__ __forceinline__ float read_lane(float x, int lane) {
@@ -499,16 +518,21 @@ void k_ssm_scan(SsmScanArgs a) {
       const float before = g == 0 ? 0.0f : g == 1 ? q0 : g == 2 ? q0 + q1 : q0 + q1 + q2;
       const float after = g == 3 ? 0.0f : g == 2 ? q3 : g == 1 ? q2 + q3 : q1 + (q2 + q3);
       HeadScalars& o = sc[wave];
+      int place = lane;
+      asm volatile("" : "+v"(place));   // addresses are made here, not kept in registers over the chunks
       if constexpr (OUT) {
-        const float ld = __log2f(delta);
-        o.l[lane] = l;
-        o.same[lane] = ld - l;
-        o.row[lane] = __builtin_amdgcn_exp2f(l);
-        o.past[lane] = __builtin_amdgcn_exp2f(s) * delta;
-        o.pre[lane] = __builtin_amdgcn_exp2f(before + l);
-        if (lane < 10) o.between[lane] = __builtin_amdgcn_exp2f(lane == 3 ? q1 : lane == 6 ? q1 + q2 : lane == 7 ? q2 : 0.0f);
+        const double wide = row_scan_wide(la);
+        const float high = static_cast<float>(wide), low = static_cast<float>(wide - high);
+        o.high[place] = high;
+        o.low[place] = low;
+        o.same[place] = __log2f(delta) - low;
+        o.row[place] = __builtin_amdgcn_exp2f(l);
+        o.past[place] = __builtin_amdgcn_exp2f(s) * delta;
+        o.pre[place] = __builtin_amdgcn_exp2f(before + l);
+        if (place < 10)
+          o.between[place] = __builtin_amdgcn_exp2f(place == 3 ? q1 : place == 6 ? q1 + q2 : place == 7 ? q2 : 0.0f);
       }
-      o.suf[lane] = __builtin_amdgcn_exp2f(s + after) * delta;
+      o.suf[place] = __builtin_amdgcn_exp2f(s + after) * delta;
       const float sum = (q0 + q1) + (q2 + q3);
       log_total += sum;
       if (lane == 0) o.total = __builtin_amdgcn_exp2f(sum);
@@ -616,15 +640,19 @@ void k_ssm_scan(SsmScanArgs a) {
       static_assert(4 % WPH == 0, "diagonal tiles per wave");
       int own = wave % WPH;
       asm volatile("" : "+s"(own));
-      f32x4 cd[ND], jd[ND], co[NO], jo[NO];
-      float ed[ND], eo[NO];
+      int gg = g, cc = c;
+      asm volatile("" : "+v"(gg), "+v"(cc));   // so are the places of the exponents
+      f32x4 cd[ND], hd[ND], jd[ND], co[NO];
+      float ed[ND], ld[ND], eo[NO];
       int ti_o[NO], tj_o[NO];
 #pragma unroll
       for (int k = 0; k < ND; ++k) {
         const int ti = own + k * WPH;
         cd[k] = *reinterpret_cast<const f32x4*>(lds + L::kOffCb + 1024 * (ti * (ti + 3) / 2) + 16 * lane);
-        jd[k] = *reinterpret_cast<const f32x4*>(hs.same + 16 * ti + 4 * g);
-        ed[k] = hs.l[16 * ti + c];
+        hd[k] = *reinterpret_cast<const f32x4*>(hs.high + 16 * ti + 4 * gg);
+        jd[k] = *reinterpret_cast<const f32x4*>(hs.same + 16 * ti + 4 * gg);
+        ed[k] = hs.high[16 * ti + cc];
+        ld[k] = hs.low[16 * ti + cc];
       }
 #pragma unroll
       for (int k = 0; k < NO; ++k) {
@@ -633,7 +661,6 @@ void k_ssm_scan(SsmScanArgs a) {
         tj_o[k] = o - ti_o[k] * (ti_o[k] - 1) / 2;
         const int t = ti_o[k] * (ti_o[k] + 1) / 2 + tj_o[k];
         co[k] = *reinterpret_cast<const f32x4*>(lds + L::kOffCb + 1024 * t + 16 * lane);
-        jo[k] = *reinterpret_cast<const f32x4*>(hs.past + 16 * tj_o[k] + 4 * g);
         eo[k] = hs.row[16 * ti_o[k] + c] * hs.between[t];
       }
       __builtin_amdgcn_sched_barrier(0);
@@ -645,16 +672,18 @@ void k_ssm_scan(SsmScanArgs a) {
         float v[4];
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const float p = cd[k][r] * __builtin_amdgcn_exp2f(ed[k] + jd[k][r]);
+          const float p = cd[k][r] * __builtin_amdgcn_exp2f((ed[k] - hd[k][r]) + (ld[k] + jd[k][r]));
           v[r] = 4 * g + r < c ? p : 4 * g + r == c ? p + skip : 0.0f;   // d_skip x rides on the diagonal
         }
         put(own + k * WPH, own + k * WPH, v);
       }
 #pragma unroll
       for (int k = 0; k < NO; ++k) {
+        // (read here: with the operands above it would be a register too many)
+        const f32x4 jo = *reinterpret_cast<const f32x4*>(hs.past + 16 * tj_o[k] + 4 * g);
         float v[4];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) v[r] = co[k][r] * (eo[k] * jo[k][r]);
+        for (int r = 0; r < 4; ++r) v[r] = co[k][r] * (eo[k] * jo[r]);
         if (6 % WPH == 0 || own + k * WPH < 6) put(ti_o[k], tj_o[k], v);
       }
     } else {

@@ -133,6 +133,33 @@ def test_steps_that_forget_everything(dtype):
     check(i, *scan(i))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("steps", ["3 each", "10 each", "8 of 5", 7, 12, 15])
+@pytest.mark.parametrize("length,N,P", [(200, 64, 64), (200, 128, 128), (1500, 128, 64)])
+def test_short_decays_after_long_ones(dtype, steps, length, N, P):
+    """Tokens that forget nearly everything, and ordinary ones behind them in the
+    same 16 tokens: the decays between the ordinary ones are sums of few short
+    steps, whatever came before.  x, B and C are positive, so that every output is
+    its own sum over magnitudes and the bound is one on its relative error.
+    `steps`: softplus(dt) of about 3 or 10 everywhere (a decay of e^-48 or e^-160 a
+    token); of each 16 tokens the first 8 of about 5; the first 7, 12 or 15 of 200."""
+    i = inputs([length], H=4, G=2, N=N, P=P, dtype=dtype, seed=28, state=False, dt32=True)
+    noise = torch.randn(length, 4, device=DEV, generator=torch.Generator(DEV).manual_seed(29))
+    place = (torch.arange(length, device=DEV) % 16)[:, None]
+    if isinstance(steps, int):
+        dt = torch.where(place < steps, 200.0, noise - 1.5)
+    elif steps == "8 of 5":
+        dt = torch.where(place < 8, noise + 5.0, noise - 3.0)
+    else:
+        dt = noise + float(steps.split()[0])
+    i.update(x=i["x"].abs(), B=i["B"].abs(), C=i["C"].abs(), dt=dt, dt_bias=None, d_skip=None,
+             a_log=torch.full((4,), 16.0, device=DEV).log())
+    y, st = scan(i)
+    ey, _, my, _ = want(i)
+    assert torch.allclose(ey, my, rtol=1e-12)
+    check(i, y, st)
+
+
 def test_all_outputs_choices_agree():
     """Outputs alone, states alone and both are the same numbers; so is a state updated in place."""
     for lens in ([100, 65], [1500]):
