@@ -88,9 +88,9 @@ typedef struct {
   int64_t ld_b;         /* >= G d_state                                      */
   int64_t ld_c;         /* >= G d_state                                      */
   int64_t ld_y;         /* >= H head_dim                                     */
-} gdn_ssm_shape;
+} gdn_ssm_shape;        /* ld_c and ld_y are looked at only where y is given */
 
-/* Workspace bytes of gdn_ssm_scan (0 where the sequences run unsplit). */
+/* Workspace bytes of gdn_ssm_scan, with or without y (0 where the sequences run unsplit). */
 gdn_status gdn_ssm_workspace_size(const gdn_ssm_shape* shape, const int32_t* cu_seqlens_host,
                                   size_t* bytes);
 
@@ -104,8 +104,8 @@ gdn_status gdn_ssm_workspace_size(const gdn_ssm_shape* shape, const int32_t* cu_
  * (one of the two is required).  state_out may equal state_in and must not
  * otherwise overlap it, nor another input; y must not overlap an input or a
  * state.  A zero-length sequence writes its state_in (or zeros) to state_out.
- * x, B, C and y must be 16-byte aligned, their row strides multiples of 16
- * bytes (GDN_ERR_UNSUPPORTED otherwise).
+ * x, B, C, y and the states must be 16-byte aligned, the row strides of x, B, C
+ * and y multiples of 16 bytes (GDN_ERR_UNSUPPORTED otherwise).
  * workspace: at least gdn_ssm_workspace_size bytes, 256-byte aligned; NULL is
  * accepted where that is 0.
  */
@@ -118,7 +118,7 @@ gdn_status gdn_ssm_scan(const gdn_ssm_shape* shape, const int32_t* cu_seqlens_ho
 /*
  * One token per sequence (T = N): the state is advanced once, y and state_out
  * are required, state_out may equal state_in.  One kernel, no workspace.
- * Alignment as for gdn_ssm_scan, the states 16-byte aligned as well.
+ * Alignment as for gdn_ssm_scan.
  */
 gdn_status gdn_ssm_step(const gdn_ssm_shape* shape, const void* x, const void* dt,
                         const float* a_log, const void* B, const void* C, const float* d_skip,

@@ -83,7 +83,7 @@ gdn_status check_conv(const gdn_conv_shape* s, std::string* err) {
   return st != GDN_OK ? st : check_stride("ld_y", s->ld_y, s->channels, err);
 }
 
-gdn_status check_ssm(const gdn_ssm_shape* s, std::string* err) {
+gdn_status check_ssm(const gdn_ssm_shape* s, std::string* err, bool outputs) {
   if (!s) { *err = "shape is NULL"; return GDN_ERR_NULL_ARG; }
   if (s->num_seqs < 0) { *err = "num_seqs must be >= 0"; return GDN_ERR_BAD_SHAPE; }
   if (s->num_heads < 1 || s->num_groups < 1) { *err = "head counts must be >= 1"; return GDN_ERR_BAD_SHAPE; }
@@ -103,13 +103,18 @@ gdn_status check_ssm(const gdn_ssm_shape* s, std::string* err) {
     return GDN_ERR_UNSUPPORTED;
   }
   const int64_t H = s->num_heads, G = s->num_groups, vec = s->dtype == GDN_BF16 ? 8 : 4;
-  struct { const char* name; int64_t ld, least; bool aligned; } rows[] = {
-      {"ld_x", s->ld_x, H * s->head_dim, true}, {"ld_dt", s->ld_dt, H, false}, {"ld_b", s->ld_b, G * s->d_state, true},
-      {"ld_c", s->ld_c, G * s->d_state, true},  {"ld_y", s->ld_y, H * s->head_dim, true}};
-  for (const auto& r : rows)
+  struct { const char* name; int64_t ld, least; bool used, aligned; } rows[] = {
+      {"ld_x", s->ld_x, H * s->head_dim, true, true},
+      {"ld_dt", s->ld_dt, H, true, false},
+      {"ld_b", s->ld_b, G * s->d_state, true, true},
+      {"ld_c", s->ld_c, G * s->d_state, outputs, true},
+      {"ld_y", s->ld_y, H * s->head_dim, outputs, true}};
+  for (const auto& r : rows) {
+    if (!r.used) continue;
     if (const gdn_status st = check_stride(r.name, r.ld, r.least, err); st != GDN_OK) return st;
+  }
   for (const auto& r : rows)
-    if (r.aligned && r.ld % vec != 0) {
+    if (r.used && r.aligned && r.ld % vec != 0) {
       *err = std::string(r.name) + " must be a multiple of 16 bytes";
       return GDN_ERR_UNSUPPORTED;
     }
@@ -120,8 +125,8 @@ gdn_status check_ssm(const gdn_ssm_shape* s, std::string* err) {
   return GDN_OK;
 }
 
-gdn_status make_ssm_plan(const gdn_ssm_shape* s, const int32_t* cu, SsmPlan* plan, std::string* err) {
-  gdn_status st = check_ssm(s, err);
+gdn_status make_ssm_plan(const gdn_ssm_shape* s, const int32_t* cu, SsmPlan* plan, std::string* err, bool outputs) {
+  gdn_status st = check_ssm(s, err, outputs);
   SsmPlan p;
   if (st == GDN_OK) st = check_seqlens(s->num_seqs, cu, &p.tokens, &p.longest, err);
   if (st != GDN_OK) return st;

@@ -31,7 +31,8 @@ inline int64_t tile_slots(int64_t tokens, int64_t seqs, int64_t tile) { return s
 gdn_status check_seqlens(int32_t n, const int32_t* cu, int64_t* tokens, int64_t* longest, std::string* err);
 
 gdn_status check_conv(const gdn_conv_shape* s, std::string* err);
-gdn_status check_ssm(const gdn_ssm_shape* s, std::string* err);
+// outputs: y is given (ld_c and ld_y are not looked at otherwise)
+gdn_status check_ssm(const gdn_ssm_shape* s, std::string* err, bool outputs = true);
 
 // How gdn_ssm_scan runs: which heads share a workgroup and whether sequences
 // are worked on in segments.
@@ -44,7 +45,7 @@ struct SsmPlan {
   size_t off_decay = 0;          // workspace: states [slots, H, d_state, head_dim], then decays [slots, H]
   size_t bytes = 0;
 };
-gdn_status make_ssm_plan(const gdn_ssm_shape* s, const int32_t* cu, SsmPlan* p, std::string* err);
+gdn_status make_ssm_plan(const gdn_ssm_shape* s, const int32_t* cu, SsmPlan* p, std::string* err, bool outputs = true);
 
 gdn_status check_lora(const gdn_lora_shape* s, std::string* err);
 

@@ -140,7 +140,7 @@ gdn_status gdn_ssm_workspace_size(const gdn_ssm_shape* shape, const int32_t* cu_
   if (!bytes) return gdn::sfail(GDN_ERR_NULL_ARG, "bytes is NULL");
   std::string err;
   gdn::SsmPlan p;
-  const gdn_status st = gdn::make_ssm_plan(shape, cu_seqlens_host, &p, &err);
+  const gdn_status st = gdn::make_ssm_plan(shape, cu_seqlens_host, &p, &err, false);
   if (st != GDN_OK) return gdn::sfail(st, err);
   *bytes = p.bytes;
   return GDN_OK;
@@ -152,7 +152,7 @@ gdn_status gdn_ssm_scan(const gdn_ssm_shape* shape, const int32_t* cu_seqlens_ho
                         void* workspace, size_t workspace_bytes, void* stream) {
   std::string err;
   gdn::SsmPlan p;
-  const gdn_status st = gdn::make_ssm_plan(shape, cu_seqlens_host, &p, &err);
+  const gdn_status st = gdn::make_ssm_plan(shape, cu_seqlens_host, &p, &err, y != nullptr);
   if (st != GDN_OK) return gdn::sfail(st, err);
   if (shape->num_seqs == 0) return GDN_OK;
   if (!cu_seqlens) return gdn::sfail(GDN_ERR_NULL_ARG, "cu_seqlens (device) is NULL");

@@ -126,6 +126,29 @@ def test_scan_refuses(status, kw):
 
 
 @needs_no_gpu
+@pytest.mark.parametrize("bad", [dict(ld_c=0), dict(ld_y=0), dict(ld_c=0, ld_y=0), dict(ld_c=132, ld_y=257), dict(ld_y=1 << 24)])
+def test_scan_of_states_alone_has_no_rows_of_C_and_y(bad):
+    """Their strides are not looked at without y: such a call is refused for its
+    workspace alone, whose size does not ask for them either."""
+    need = ctypes.c_size_t(0)
+    size = lambda **kw: gdn.load_library().gdn_ssm_workspace_size(ctypes.byref(ssm_shape(1, **kw)), ctypes.cast(
+        cu_of((2000,)), ctypes.c_void_p), ctypes.byref(need))
+    assert size() == 0 and need.value > 0
+    whole = need.value
+    assert size(**bad) == 0 and need.value == whole
+    assert scan(lens=(2000,), C=None, y=None, **bad) == WORKSPACE
+    assert scan(lens=(2000,), **bad) in (SHAPE, UNSUPPORTED)
+    assert step(**bad) in (SHAPE, UNSUPPORTED)
+    assert scan(lens=(2000,), C=None, y=None, **dict(bad, ld_b=64)) == SHAPE
+
+
+@needs_no_gpu
+@pytest.mark.parametrize("kw", [dict(sin=0x600004), dict(sout=0x500008), dict(sin=0x600004, y=None, C=None)])
+def test_scan_refuses_states_off_16_bytes(kw):
+    assert scan(**kw) == UNSUPPORTED
+
+
+@needs_no_gpu
 @pytest.mark.parametrize("status,kw", [
     (NULL, dict(x=None)), (NULL, dict(y=None)), (NULL, dict(sout=None)), (NULL, dict(C=None)), (NULL, dict(a_log=None)),
     (UNSUPPORTED, dict(sin=0x500004)), (SHAPE, dict(sin=0x500010)), (SHAPE, dict(y=0x100000)),
