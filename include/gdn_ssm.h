@@ -101,7 +101,7 @@ gdn_status gdn_ssm_workspace_size(const gdn_ssm_shape* shape, const int32_t* cu_
  *   state_in, state_out [N, H, d_state, head_dim] fp32.
  * y NULL = no outputs (the state alone, as where a tail is replayed; C and
  * d_skip are not read then and may be NULL); state_out NULL = not written
- * (one of the two is required).  state_out may equal state_in and must not
+ * (one of the two is required where there are tokens).  state_out may equal state_in and must not
  * otherwise overlap it, nor another input; y must not overlap an input or a
  * state.  A zero-length sequence writes its state_in (or zeros) to state_out.
  * x, B, C, y and the states must be 16-byte aligned, the row strides of x, B, C

@@ -154,7 +154,7 @@ gdn_status gdn_ssm_scan(const gdn_ssm_shape* shape, const int32_t* cu_seqlens_ho
   gdn::SsmPlan p;
   const gdn_status st = gdn::make_ssm_plan(shape, cu_seqlens_host, &p, &err, y != nullptr);
   if (st != GDN_OK) return gdn::sfail(st, err);
-  if (shape->num_seqs == 0) return GDN_OK;
+  if (shape->num_seqs == 0 || (p.tokens == 0 && !state_out)) return GDN_OK;
   if (!cu_seqlens) return gdn::sfail(GDN_ERR_NULL_ARG, "cu_seqlens (device) is NULL");
   if (!y && !state_out) return gdn::sfail(GDN_ERR_NULL_ARG, "y and state_out are both NULL");
   if (p.bytes > 0 && !workspace) return gdn::sfail(GDN_ERR_WORKSPACE, "workspace is NULL");

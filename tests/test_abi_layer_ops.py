@@ -183,6 +183,12 @@ def test_nothing_to_do_is_no_error():
     assert lora(lens=(), ids=(), host="lens") == 0
 
 
+def test_outputs_of_no_tokens_alone_are_no_error():
+    """An empty tensor of outputs has no address; without tokens there is nothing to write."""
+    assert scan(lens=(0, 0), cu=None, x=None, dt=None, B=None, C=None, y=None, sout=None) == 0
+    assert scan(lens=(0, 0), cu=None, x=None, dt=None, B=None, C=None, sout=None) == 0
+
+
 def test_adapted_layer_workspace():
     """The adapters' workspace lies behind the layer's own."""
     lib = gdn.load_library()

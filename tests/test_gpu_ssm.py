@@ -389,3 +389,9 @@ def test_no_tokens():
     assert y.shape == (0, 4, 64) and torch.equal(st, i["state"])
     i = inputs([0, 0], seed=18, state=False)
     assert not scan(i)[1].any()
+
+
+def test_outputs_of_no_tokens_alone():
+    i = inputs([0, 0], seed=18)
+    y, st = scan(i, write_state=False)
+    assert y.shape == (0, 4, 64) and st is None
