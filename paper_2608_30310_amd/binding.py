@@ -281,7 +281,9 @@ def _need(t, name, dtype, device, ndim):
 
 class _Workspaces(threading.local):
     """The workspaces kept per (device, stream), each thread its own: the launches
-    of two threads' calls may take turns on one stream."""
+    of two threads' calls may take turns on one stream.  A thread's go with it; a
+    program that makes a thread for every request allocates one for each, unless
+    it passes ``workspace``."""
 
     def __init__(self):
         self.kept = {}
@@ -291,11 +293,16 @@ _WORKSPACES = _Workspaces()
 
 
 def _workspace(nbytes: int, device: torch.device, stream) -> torch.Tensor:
+    """The kept workspace of at least ``nbytes``.  A call that is being captured
+    takes memory of its graph's own pool instead: no other graph or call shares
+    it, and nothing frees it before the graph."""
     key = (device.index, stream)
-    ws = _WORKSPACES.kept.get(key)
+    capturing = torch._C._cuda_isCurrentStreamCapturing()
+    ws = None if capturing else _WORKSPACES.kept.get(key)
     if ws is None or ws.numel() < nbytes:
         ws = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
-        _WORKSPACES.kept[key] = ws
+        if not capturing:
+            _WORKSPACES.kept[key] = ws
     if ws.data_ptr() % 256:
         raise RuntimeError("workspace allocation is not 256-byte aligned")
     return ws
@@ -752,9 +759,7 @@ def la_block_replay(x: torch.Tensor, weights, cu_seqlens, num_k_heads: int, num_
         ad, keep = _la_adapters(adapters, n, D, 2 * cq + 2 * cv + 2 * num_v_heads, cv, device)
         _check(lib.gdn_la_block_adapted_workspace_size(ctypes.byref(shp), ctypes.byref(ad), _ptr(cu_host),
                                                        int(outputs), ctypes.byref(need)))
-        if workspace is None and torch.cuda.is_current_stream_capturing():
-            workspace = torch.empty(need.value, dtype=torch.uint8, device=device)   # of the graph's own pool
-        elif workspace is None:
+        if workspace is None:
             workspace = _workspace(need.value, device, stream)
         _check(lib.gdn_la_block_replay_adapted(
             ctypes.byref(shp), ctypes.byref(w), ctypes.byref(ad), _ptr(cu_host), _ptr(cu_dev), _ptr(x),

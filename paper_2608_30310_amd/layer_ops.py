@@ -100,15 +100,13 @@ def _offsets(cu_seqlens, cu_seqlens_host, device, tokens):
 def _run_with_workspace(call, size, shape, host, device, stream, given):
     """``call(workspace, its bytes)`` with the caller's workspace, or with the one
     kept per thread, device and stream; the library refuses a workspace that is too small
-    before it enqueues anything, and only then its size is asked for.  A call
-    that is being captured takes memory of its graph's own pool instead: no other
-    graph shares it, and no later call outside can replace it."""
+    before it enqueues anything, and only then its size is asked for.  (While a
+    graph is captured, ``_workspace`` gives memory of the graph's.)"""
     if given is not None:
         if not isinstance(given, torch.Tensor) or given.device != device or not given.is_contiguous():
             raise ValueError(f"workspace must be a contiguous tensor on {device}")
         _check(call(given.data_ptr(), given.numel() * given.element_size()))
         return
-    kept = None
     if not torch._C._cuda_isCurrentStreamCapturing():
         kept = _WORKSPACES.kept.get((device.index, stream))
         status = call(None, 0) if kept is None else call(kept.data_ptr(), kept.numel())
@@ -117,10 +115,7 @@ def _run_with_workspace(call, size, shape, host, device, stream, given):
             return
     need = ctypes.c_size_t(0)
     _check(size(ctypes.byref(shape), host, ctypes.byref(need)))
-    if torch._C._cuda_isCurrentStreamCapturing():
-        ws = torch.empty(max(need.value, 256), dtype=torch.uint8, device=device)
-    else:
-        ws = _workspace(need.value, device, stream)
+    ws = _workspace(need.value, device, stream)
     _check(call(ws.data_ptr(), ws.numel()))
 
 

@@ -213,6 +213,29 @@ def test_workspaces_are_a_threads_own():
     assert seen[0] == {} and seen[0] is not binding._WORKSPACES.kept
 
 
+def test_a_captured_call_takes_memory_of_its_own(monkeypatch):
+    """Neither the workspace that is kept, which a later call or the end of its
+    thread would free under the graph, nor one that is kept from then on."""
+    def aligned(n, dtype, device):
+        t = torch.zeros(n + 256, dtype=dtype, device=device)
+        return t[-t.data_ptr() % 256:][:n]
+    monkeypatch.setattr(torch, "empty", aligned)
+    capturing = [False]
+    monkeypatch.setattr(torch._C, "_cuda_isCurrentStreamCapturing", lambda: capturing[0])
+    monkeypatch.setattr(binding._WORKSPACES, "kept", {})
+    cpu = torch.device("cpu")
+    kept = binding._workspace(1000, cpu, 7)
+    assert binding._workspace(500, cpu, 7) is kept
+    capturing[0] = True
+    for n in (500, 1000, 5000):
+        ws = binding._workspace(n, cpu, 7)
+        assert ws.numel() >= n and ws is not kept
+        assert binding._WORKSPACES.kept == {(None, 7): kept}
+    assert binding._workspace(300, cpu, 8).numel() >= 300 and (None, 8) not in binding._WORKSPACES.kept
+    capturing[0] = False
+    assert binding._workspace(1000, cpu, 7) is kept
+
+
 def test_calls_refuse_host_tensors():
     x, w = torch.zeros(2, 8), torch.zeros(8, 4)
     for call in (lambda: gdn.causal_conv(x, w, [0, 2]), lambda: gdn.causal_conv_step(x, w),
