@@ -642,6 +642,17 @@ def la_block_workspace_size(hidden: int, num_k_heads: int, num_v_heads: int, d_k
     return int(out.value)
 
 
+def _indices(values, name):
+    """Indices, given as integers of any type, as the library reads them on the host."""
+    t = values.detach().cpu() if isinstance(values, torch.Tensor) else torch.tensor(list(values))
+    if t.numel() == 0:
+        return torch.empty(0, dtype=torch.int32)
+    if t.dim() != 1 or t.dtype not in (torch.int8, torch.uint8, torch.int16, torch.int32, torch.int64) or \
+            (t.dtype is torch.int64 and not torch.equal(t, t.to(torch.int32).to(torch.int64))):
+        raise ValueError(f"{name} must be a row of 32-bit integers")
+    return t.to(torch.int32).contiguous()
+
+
 def _adapter_ids(adapters, adapters_host, n, device):
     """Device and host copies of the adapters' indices, int32 [N]."""
     # both in hand and as the library reads them: nothing to convert
@@ -650,17 +661,15 @@ def _adapter_ids(adapters, adapters_host, n, device):
             adapters.shape == (n,) and adapters_host.shape == (n,) and adapters.is_contiguous() and \
             adapters_host.is_contiguous():
         return adapters, adapters_host
-    if adapters_host is None:
-        if isinstance(adapters, torch.Tensor):
-            adapters_host = adapters.detach().to("cpu", torch.int32)
-        else:
-            adapters_host = torch.tensor(list(adapters), dtype=torch.int32)
-    elif not isinstance(adapters_host, torch.Tensor):
-        adapters_host = torch.tensor(list(adapters_host), dtype=torch.int32)
-    adapters_host = adapters_host.to(torch.int32).contiguous()
-    if adapters_host.device.type != "cpu":
+    on_device = isinstance(adapters, torch.Tensor) and adapters.device == device
+    if isinstance(adapters_host, torch.Tensor) and not adapters_host.is_cpu:
         raise ValueError("adapters_host must live in host memory")
-    if not isinstance(adapters, torch.Tensor) or adapters.device != device:
+    in_host = not isinstance(adapters, torch.Tensor) or adapters.is_cpu
+    given = _indices(adapters, "adapters") if adapters_host is None or in_host else None
+    adapters_host = given if adapters_host is None else _indices(adapters_host, "adapters_host")
+    if given is not None and not torch.equal(given, adapters_host):
+        raise ValueError("adapters and adapters_host must hold the same indices")
+    if not on_device:
         adapters = adapters_host.to(device)
     _need(adapters, "adapters", torch.int32, device, 1)
     if adapters.numel() != n or adapters_host.numel() != n:

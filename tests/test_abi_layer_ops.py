@@ -236,6 +236,22 @@ def test_a_captured_call_takes_memory_of_its_own(monkeypatch):
     assert binding._workspace(1000, cpu, 7) is kept
 
 
+def test_adapter_indices():
+    """Integers that fit 32 bits, however they come; what is rounded, cut off or contradicts itself is refused."""
+    cpu = torch.device("cpu")
+    ids = lambda a, host=None: binding._adapter_ids(a, host, 2, cpu)
+    i32 = torch.tensor([1, -1], dtype=torch.int32)
+    for a, host in ((i32, None), (i32, i32), ([1, -1], None), ((1, -1), i32), ([1, -1], torch.tensor([1, -1])), (i32, [1, -1])):
+        dev, back = ids(a, host)
+        assert dev.dtype == back.dtype == torch.int32 and dev.tolist() == back.tolist() == [1, -1]
+    assert binding._adapter_ids([], None, 0, cpu)[1].numel() == 0
+    for a, host in (([0.0, 1.9], None), ([True, False], None), ([0, 2 ** 32], None), ([0, 1], torch.tensor([2 ** 32, 1])),
+                    ([0, 1], [0.5, 1]), (i32, torch.tensor([1.0, -1.0])), ([0, 1], [1, 0]), ([0, 1], i32), ([0], None),
+                    (i32, [1]), ([0, -2 ** 31 - 1], None), (torch.tensor([[1, -1]]), None)):
+        with pytest.raises((ValueError, TypeError)):
+            ids(a, host)
+
+
 def test_calls_refuse_host_tensors():
     x, w = torch.zeros(2, 8), torch.zeros(8, 4)
     for call in (lambda: gdn.causal_conv(x, w, [0, 2]), lambda: gdn.causal_conv_step(x, w),
