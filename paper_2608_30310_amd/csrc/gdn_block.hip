@@ -161,13 +161,21 @@ gdn_status block_impl(const gdn_la_shape* shape, const gdn_la_weights* w, const 
     if ((st = plan_adapters(*shape, p, *ad, cu_host, &ap, &err)) != GDN_OK) return bfail(st, "adapters: " + err);
     if (p.T > 0 && (!ad->adapters_host || !ad->adapters))
       return bfail(GDN_ERR_NULL_ARG, "adapters and adapters_host must be non-NULL");
-    if (p.T > 0 && ((ap.in.rank > 0 && (!ad->a_in || !ad->b_in)) || (ap.out.rank > 0 && (!ad->a_out || !ad->b_out))))
-      return bfail(GDN_ERR_NULL_ARG, "the adapters' matrices must be non-NULL where the rank is not 0");
-    for (const void* q : {ad->a_in, ad->b_in, ad->a_out, ad->b_out})
-      if (misaligned(q, 16)) return bfail(GDN_ERR_UNSUPPORTED, "the adapters' matrices must be 16-byte aligned");
-    for (int32_t n = 0; p.T > 0 && n < shape->num_seqs; ++n)
+    bool any = false;
+    for (int32_t n = 0; p.T > 0 && n < shape->num_seqs; ++n) {
       if (ad->adapters_host[n] < -1 || ad->adapters_host[n] >= ad->num_adapters)
         return bfail(GDN_ERR_BAD_SHAPE, "adapters_host must hold -1 or an adapter's index");
+      any = any || ad->adapters_host[n] >= 0;
+    }
+    const struct { int32_t rank; const void* a; const void* b; } sides[] = {{ap.in.rank, ad->a_in, ad->b_in},
+                                                                           {ap.out.rank, ad->a_out, ad->b_out}};
+    for (const auto& q : sides) {
+      if (q.rank == 0) continue;
+      if (any && (!q.a || !q.b))
+        return bfail(GDN_ERR_NULL_ARG, "the adapters' matrices must be non-NULL where the rank is not 0");
+      if (misaligned(q.a, 16) || misaligned(q.b, 16))
+        return bfail(GDN_ERR_UNSUPPORTED, "the adapters' matrices must be 16-byte aligned");
+    }
   }
   if (!workspace) return bfail(GDN_ERR_WORKSPACE, "workspace is NULL");
   const size_t adapted = ad ? ap.bytes : 0;   // behind the block's own workspace

@@ -205,6 +205,35 @@ def test_adapted_layer_workspace():
     assert lib.gdn_la_block_adapted_workspace_size(ctypes.byref(shp), None, c, 1, ctypes.byref(adapted)) == NULL
 
 
+def adapted(ids=(-1, -1), ws=None, out=0x700000, **kw):
+    shp = binding.LAShape(2, 128, 2, 4, 64, 64, 4, GDN_BF16, 1.0, 0.0, 0.0)
+    w = binding.LAWeights(0x100000, 0x200000, 0x300000, 0x400000, 0x500000, 0x600000)
+    host = (ctypes.c_int32 * 2)(*ids)
+    ad = LAAdapters(**dict(dict(num_adapters=0, rank_in=16, rank_out=8, adapters_host=ctypes.addressof(host), adapters=0x800000),
+                           **kw))
+    return gdn.load_library().gdn_la_block_replay_adapted(
+        ctypes.byref(shp), ctypes.byref(w), ctypes.byref(ad), ctypes.cast(cu_of((5, 3)), ctypes.c_void_p), P(0x900000),
+        P(0xa00000), P(0xb00000), P(out), P(ws), 1 << 30, None)
+
+
+@needs_no_gpu
+def test_adapted_layer_looks_at_the_matrices_in_use():
+    """Refused for the missing workspace alone: no adapters and no request that has
+    one; matrices of a projection that is not adapted, or not run."""
+    mats = dict(a_in=0x10000, b_in=0x20000, a_out=0x30000, b_out=0x40000)
+    assert adapted() == WORKSPACE
+    assert adapted(num_adapters=2) == WORKSPACE
+    assert adapted(rank_in=0, rank_out=0, a_in=2, b_out=8) == WORKSPACE
+    assert adapted(ids=(1, -1), out=None, num_adapters=2, **dict(mats, a_out=None, b_out=2)) == WORKSPACE
+    assert adapted(ids=(1, -1), num_adapters=2, **mats) == WORKSPACE
+    # and those that are
+    assert adapted(ids=(1, -1), num_adapters=2, **dict(mats, a_in=None)) == NULL
+    assert adapted(ids=(1, -1), num_adapters=2, **dict(mats, b_out=None)) == NULL
+    assert adapted(ids=(1, -1), num_adapters=2, **dict(mats, b_in=0x20008)) == UNSUPPORTED
+    assert adapted(ids=(0, -1)) == SHAPE
+    assert adapted(adapters=None) == NULL
+
+
 def test_workspaces_are_a_threads_own():
     seen = []
     t = threading.Thread(target=lambda: seen.append(binding._WORKSPACES.kept))

@@ -104,6 +104,14 @@ def test_layer_without_an_adapter_is_the_plain_layer(act):
     assert not torch.equal(st[1], st3[1]) and not torch.equal(out[50:], out3[50:])
 
 
+def test_layer_with_no_adapters_at_all():
+    dims = LayerDims(hidden=128, hk=2, hv=4, dk=64, dv=64)
+    x, cu, w, wd, ad = _case([50, 9], dims, 7, (16, 8))
+    st, out = _replay(x, cu, wd, dims, ad, None, True, "bf16")
+    st2, out2 = _replay(x, cu, wd, dims, {k: v[:0] for k, v in ad.items()}, [-1, -1], True, "bf16")
+    assert torch.equal(st, st2) and torch.equal(out, out2)
+
+
 def test_adapted_layer_in_a_graph():
     dims = LayerDims(hidden=128, hk=2, hv=4, dk=64, dv=64)
     x, cu, w, wd, ad = _case([70, 33], dims, 5, (16, 8))
