@@ -160,6 +160,24 @@ def test_short_decays_after_long_ones(dtype, steps, length, N, P):
     check(i, y, st)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("length", [150, 1500])
+def test_steps_of_nothing_and_of_everything(dtype, length):
+    """Tokens whose step is masked out (dt of -infinity or near it: delta is zero)
+    beside ones with enormous steps; one head has no other tokens than masked ones."""
+    i = inputs([length, 3], H=4, G=2, dtype=dtype, seed=30, dt32=True)
+    g = torch.Generator(DEV).manual_seed(31)
+    kinds = torch.tensor([-float("inf"), -1e30, -90.0, 0.0, 90.0, 1e4], device=DEV)
+    i["dt"] = kinds[torch.randint(0, 6, (length + 3, 4), device=DEV, generator=g)]
+    i["dt"][:, 1] = -float("inf")
+    y, st = scan(i)
+    check(i, y, st)
+    assert torch.equal(st[:, 1], i["state"][:, 1])
+    one = dict(i, x=i["x"][:2], B=i["B"][:2], C=i["C"][:2], dt=i["dt"][:2], cu_host=torch.tensor([0, 1, 2]))
+    check(one, *gdn.ssm_step(one["x"], one["dt"], i["a_log"], one["B"], one["C"], d_skip=i["d_skip"], dt_bias=i["dt_bias"],
+                             state_in=i["state"]))
+
+
 def test_all_outputs_choices_agree():
     """Outputs alone, states alone and both are the same numbers; so is a state updated in place."""
     for lens in ([100, 65], [1500]):
