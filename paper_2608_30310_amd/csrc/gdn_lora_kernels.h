@@ -6,11 +6,14 @@
 // they are loaded, without a pass through LDS.  The work is HBM's: at rank 64 a
 // projected element costs 128 multiply-adds against reading and writing it.
 //
-// Measured, 2048 -> 12352, bf16: 4324 tokens of 8 requests at rank 64, 15.3 and 48
-// us (the second kernel at 4.5 TB/s; 238 MB in all, which a copy moves in 44 to
-// 49); 64 single tokens at rank 16 5.1 and 8.7 us (16 MB, most of it A and B).
-// The first kernel is bound by its loads' way through L2: eight waves instead
-// of four, or neighbouring steps a wave, left it at 16.0 us.
+// Measured, 2048 -> 12352, on inputs that are not in the last-level cache: bf16,
+// 4324 tokens of 8 requests at rank 64, 19 and 64 us (the second kernel moves 214
+// MB of base and out, 3.3 TB/s; 238 MB in all, which a copy moves in 44 to 49),
+// fp32 19 and 119; 64 single tokens at rank 16 5.9 and 9.1 us (16 MB, most of it A
+// and B).  With the same inputs call after call, as for the figures below, part of
+// them stays in that cache: 16 and 48 us.  The first kernel has 143 workgroups
+// there for 256 CUs, each bound by its loads' way through L2: eight waves instead of
+// four, or neighbouring steps a wave, left it at 16.0 us.
 //
 // Tokens go by tiles of 16 TT inside a sequence (its adapter is the tile's).
 #pragma once

@@ -13,10 +13,10 @@
 // What bounds it: a chunk is a chain (rows into LDS, C B^T, P, P x) between
 // products on the state, and matrix and vector instructions of a SIMD's waves
 // hardly overlap.  Measured, bf16: 16 sequences of 128 to 2048 tokens, 32
-// heads of 128 x 128, 195 us (498 MB, 2.6 TB/s); one of 32768 tokens, 64 heads of
-// 64 x 128, in segments 338 us: 118 for the segments' states, 12 for the join
-// and 224 for the outputs at best, each more where the chip's power limit lowers
-// its clock.  Of the outputs' time, found by leaving out one stage's arithmetic:
+// heads of 128 x 128, 198 us (498 MB, 2.5 TB/s); one of 32768 tokens, 64 heads of
+// 64 x 128, in segments 342 us: 117 for the segments' states, 12 for the join
+// and 226 for the outputs at best, each more where the chip's power limit lowers
+// its clock.  States alone: 82 and 119 us.  Of the outputs' time, found by leaving out one stage's arithmetic:
 // the split of M into parts 35, the products on M 42, the state's update 37, P 34,
 // the stores 23, the loads 16, C B^T 11.  fp32 inputs go through k = 4 products
 // (2048 tokens, 4 heads of 64 x 64: 23 us a call in segments).
