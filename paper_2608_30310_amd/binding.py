@@ -78,6 +78,38 @@ class LoraShape(ctypes.Structure):
                 ("ld_x", ctypes.c_int64), ("ld_base", ctypes.c_int64), ("ld_out", ctypes.c_int64)]
 
 
+class LinearShape(ctypes.Structure):
+    _fields_ = [("num_seqs", ctypes.c_int32), ("num_k_heads", ctypes.c_int32), ("num_v_heads", ctypes.c_int32),
+                ("d_k", ctypes.c_int32), ("d_v", ctypes.c_int32), ("dtype", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("ld_q", ctypes.c_int64), ("ld_k", ctypes.c_int64), ("ld_v", ctypes.c_int64), ("ld_o", ctypes.c_int64)]
+
+
+class PagesShape(ctypes.Structure):
+    _fields_ = [("num_seqs", ctypes.c_int32), ("table_width", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("num_free", ctypes.c_int32), ("first", ctypes.c_int32)]
+
+
+class QkShape(ctypes.Structure):
+    _fields_ = [("num_tokens", ctypes.c_int32), ("num_heads", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32), ("rotary_dim", ctypes.c_int32),
+                ("interleaved", ctypes.c_int32), ("num_positions", ctypes.c_int32), ("eps", ctypes.c_float),
+                ("num_pages", ctypes.c_int32), ("page_size", ctypes.c_int32), ("ld_q", ctypes.c_int64),
+                ("ld_k", ctypes.c_int64), ("ld_v", ctypes.c_int64), ("ld_q_out", ctypes.c_int64),
+                ("ld_k_out", ctypes.c_int64), ("k_page", ctypes.c_int64), ("k_token", ctypes.c_int64),
+                ("k_head", ctypes.c_int64), ("v_page", ctypes.c_int64), ("v_token", ctypes.c_int64),
+                ("v_head", ctypes.c_int64)]
+
+
+class AttnShape(ctypes.Structure):
+    _fields_ = [("num_seqs", ctypes.c_int32), ("num_heads", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32), ("num_pages", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("table_width", ctypes.c_int32), ("prefix_len", ctypes.c_int32),
+                ("max_len", ctypes.c_int32), ("scale", ctypes.c_float), ("ld_q", ctypes.c_int64),
+                ("ld_out", ctypes.c_int64), ("k_page", ctypes.c_int64), ("k_token", ctypes.c_int64),
+                ("k_head", ctypes.c_int64), ("v_page", ctypes.c_int64), ("v_token", ctypes.c_int64),
+                ("v_head", ctypes.c_int64)]
+
+
 _lib = None
 
 
@@ -156,6 +188,24 @@ def load_library():
     lib.gdn_lora_workspace_size.restype = ctypes.c_int
     lib.gdn_lora_add.argtypes = [AP, P, P, P, P, P, P, P, P, P, P, P, ctypes.c_size_t, P]
     lib.gdn_lora_add.restype = ctypes.c_int
+    NP, GP = ctypes.POINTER(LinearShape), ctypes.POINTER(PagesShape)
+    QP, TP = ctypes.POINTER(QkShape), ctypes.POINTER(AttnShape)
+    lib.gdn_linear_attention_workspace_size.argtypes = [NP, P, ZP]
+    lib.gdn_linear_attention_workspace_size.restype = ctypes.c_int
+    lib.gdn_linear_attention.argtypes = [NP, P, P, P, P, P, P, P, P, P, P, ctypes.c_size_t, P]
+    lib.gdn_linear_attention.restype = ctypes.c_int
+    lib.gdn_linear_attention_step.argtypes = [NP, P, P, P, P, P, P, P, P]
+    lib.gdn_linear_attention_step.restype = ctypes.c_int
+    lib.gdn_extend_pages_workspace_size.argtypes = [GP, P, ZP]
+    lib.gdn_extend_pages_workspace_size.restype = ctypes.c_int
+    lib.gdn_extend_pages.argtypes = [GP, P, P, P, P, P, P, P, P, P, P, P, P, ctypes.c_size_t, P]
+    lib.gdn_extend_pages.restype = ctypes.c_int
+    lib.gdn_qk_norm_rope.argtypes = [QP, P, P, P, P, P, P, P, P, P, P, P, P, P]
+    lib.gdn_qk_norm_rope.restype = ctypes.c_int
+    lib.gdn_prefix_attention_workspace_size.argtypes = [TP, P, ZP]
+    lib.gdn_prefix_attention_workspace_size.restype = ctypes.c_int
+    lib.gdn_prefix_attention.argtypes = [TP, P, P, P, P, P, P, P, P, P, P, ctypes.c_size_t, P]
+    lib.gdn_prefix_attention.restype = ctypes.c_int
     lib.gdn_replay_len.argtypes = [ctypes.c_int64, ctypes.c_int64, ctypes.c_int64]
     lib.gdn_replay_len.restype = ctypes.c_int64
     lib.gdn_status_string.argtypes = [ctypes.c_int]

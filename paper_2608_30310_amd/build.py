@@ -8,6 +8,8 @@ from __future__ import annotations
 import os
 import shutil
 import subprocess
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -16,7 +18,7 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB_NAME = "libgdn_tailreplay.so"
 LIB_PATH = os.path.join(HERE, LIB_NAME)
 SOURCES = ["gdn_plan.cpp", "gdn_layer_plan.cpp", "gdn_gemm.cpp", "gdn_api.hip", "gdn_block.hip", "gdn_conv.hip",
-           "gdn_ssm.hip", "gdn_lora.hip"]
+           "gdn_ssm.hip", "gdn_linear.hip", "gdn_lora.hip", "gdn_attn_plan.cpp", "gdn_pages.hip", "gdn_attn.hip"]
 ROCM_LIB = "/opt/rocm/lib"
 ARCH = "gfx950"
 
@@ -30,23 +32,34 @@ def hipcc() -> str:
 
 def build(verbose: bool = False) -> str:
     tmp = LIB_PATH + ".tmp"
-    cmd = [hipcc(), f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", "-shared",
-           # packed fp32 instructions stay off on this target
-           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
-           # MFMA results in ordinary VGPRs: the scan feeds them to VALU work
-           # every step, and accumulator-register copies would serialise it
-           "-mllvm", "-amdgpu-mfma-vgpr-form",
-           "-Wall", "-I", INCLUDE, "-I", CSRC, "-o", tmp]
-    cmd += [os.path.join(CSRC, s) for s in SOURCES]
-    # the layer block's projections run through hipBLASLt
-    cmd += ["-L", ROCM_LIB, "-Wl,-rpath," + ROCM_LIB, "-lhipblaslt"]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    res = subprocess.run(cmd, capture_output=True, text=True)
+    flags = [f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC",
+             # packed fp32 instructions stay off on this target
+             "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
+             # MFMA results in ordinary VGPRs: the scan feeds them to VALU work
+             # every step, and accumulator-register copies would serialise it
+             "-mllvm", "-amdgpu-mfma-vgpr-form",
+             "-Wall", "-I", INCLUDE, "-I", CSRC]
     noise = "is not a recognized feature for this target"
-    msgs = [l for l in (res.stdout + res.stderr).splitlines() if noise not in l]
-    if res.returncode != 0:
-        raise RuntimeError("hipcc failed:\n" + "\n".join(msgs))
+
+    def run(cmd):
+        res = subprocess.run(cmd, capture_output=True, text=True)
+        msgs = [l for l in (res.stdout + res.stderr).splitlines() if noise not in l]
+        if res.returncode != 0:
+            raise RuntimeError("hipcc failed:\n" + " ".join(cmd) + "\n" + "\n".join(msgs))
+        return msgs
+
+    # the sources side by side, as many as there are CPUs for (about 1 GiB each)
+    with tempfile.TemporaryDirectory() as objs:
+        pairs = [(os.path.join(CSRC, s), os.path.join(objs, s + ".o")) for s in SOURCES]
+        cmds = [[hipcc(), *flags, "-c", "-o", obj, src] for src, obj in pairs]
+        # the layer block's projections run through hipBLASLt
+        link = [hipcc(), f"--offload-arch={ARCH}", "-shared", "-fPIC", "-o", tmp, *(obj for _, obj in pairs),
+                "-L", ROCM_LIB, "-Wl,-rpath," + ROCM_LIB, "-lhipblaslt"]
+        if verbose:
+            print("\n".join(" ".join(c) for c in cmds + [link]), flush=True)
+        with ThreadPoolExecutor(max_workers=max(1, min(8, os.cpu_count() or 1))) as pool:
+            msgs = [m for out in pool.map(run, cmds) for m in out]
+        msgs += run(link)
     if verbose and msgs:
         print("\n".join(msgs))
     os.replace(tmp, LIB_PATH)

@@ -1,0 +1,207 @@
+// Pages and slots from lengths, and norm and rotation of queries and keys on
+// their way into the pages (C ABI in gdn_attn.h).
+#pragma once
+
+#include "gdn_varlen.h"
+
+namespace gdn {
+
+// ---------------------------------------------------------------- pages
+struct PagesArgs {
+  int32_t n_seqs, width, page_size, num_free, first;
+  const int32_t* cu;
+  const int32_t* table_in;
+  const int32_t* lens_in;
+  const int32_t* free_pages;
+  const int32_t* taken_in;
+  int32_t* table_out;
+  int32_t* lens_out;
+  int32_t* taken_out;
+  int32_t* slots;
+  int32_t* positions;
+  int32_t* have;    // workspace [N]: pages that a sequence holds already
+  int32_t* index;   // [N]: where its new pages begin in free_pages
+  int32_t* held;    // [N]: its tokens before the call
+};
+constexpr int32_t kMaxToken = 0x7FFFFFFF;
+
+__device__ __forceinline__ int32_t pages_of(int64_t tokens, int32_t page_size, int32_t width) {
+  const int64_t p = (tokens + page_size - 1) / page_size;
+  return static_cast<int32_t>(p < width ? p : width);
+}
+__device__ __forceinline__ int32_t clamp_token(int64_t x) { return static_cast<int32_t>(x < kMaxToken ? x : kMaxToken); }
+
+__device__ __forceinline__ int wave_sums(int x) {   // inclusive sums over the wave
+  const int lane = threadIdx.x % kWave;
+#pragma unroll
+  for (int off = 1; off < kWave; off <<= 1) {
+    const int up = __shfl_up(x, off, kWave);
+    x += lane >= off ? up : 0;
+  }
+  return x;
+}
+
+// One workgroup: the exclusive sums of what the sequences take.  The old lengths
+// go to the workspace, since lens_out may be lens_in.
+constexpr int kPagesPlanThreads = 1024;
+__global__ __launch_bounds__(kPagesPlanThreads)
+void k_pages_plan(PagesArgs a) {
+  constexpr int NW = kPagesPlanThreads / kWave;
+  __shared__ int sums[NW];
+  const int tid = threadIdx.x, wave = tid / kWave, lane = tid % kWave;
+  int64_t base = a.taken_in ? max(a.taken_in[0], 0) : 0;
+  for (int n0 = 0; n0 < a.n_seqs; n0 += kPagesPlanThreads) {
+    const int n = n0 + tid;
+    int32_t held = 0, have = 0, more = 0;
+    int64_t len = 0;
+    if (n < a.n_seqs) {
+      held = max(a.lens_in[n], 0);
+      len = static_cast<int64_t>(held) + (a.cu[n + 1] - a.cu[n]);
+      have = pages_of(held, a.page_size, a.width);
+      more = pages_of(clamp_token(len), a.page_size, a.width) - have;
+    }
+    const int up_to = wave_sums(more);
+    if (lane == kWave - 1) sums[wave] = up_to;
+    __syncthreads();
+    int before = 0, all = 0;
+    for (int w = 0; w < NW; ++w) {
+      before += w < wave ? sums[w] : 0;
+      all += sums[w];
+    }
+    if (n < a.n_seqs) {
+      a.have[n] = have;
+      a.index[n] = clamp_token(base + before + up_to - more);
+      a.held[n] = held;
+      a.lens_out[n] = clamp_token(len);
+    }
+    base += all;
+    __syncthreads();
+  }
+  if (tid == 0) a.taken_out[0] = clamp_token(base);
+}
+
+// A workgroup takes TILE new tokens of a sequence, the first of a sequence its
+// table row too.  Where table_out is table_in, entries below `have` are only read
+// and those from it on only written.
+constexpr int kPagesThreads = 256;
+template <int TILE>
+__global__ __launch_bounds__(kPagesThreads)
+void k_pages_fill(PagesArgs a) {
+  const int tid = threadIdx.x;
+  const int n = slot_seq(a.cu, a.n_seqs, blockIdx.x, TILE);
+  const int start = a.cu[n], count = a.cu[n + 1] - start;
+  const int64_t from = (static_cast<int64_t>(blockIdx.x) - (start / TILE + n)) * TILE;   // first new token of the tile
+  const int32_t have = a.have[n], index = a.index[n], held = a.held[n];
+  const int64_t row = static_cast<int64_t>(n) * a.width;
+  const auto page_at = [&](int32_t c) {
+    if (c < have) return a.table_in[row + c];
+    const int64_t i = static_cast<int64_t>(index) + (c - have);
+    return i < a.num_free ? a.free_pages[i] : -1;
+  };
+  if (from == 0) {
+    const int32_t need = pages_of(clamp_token(static_cast<int64_t>(held) + count), a.page_size, a.width);
+    const bool in_place = a.table_in == a.table_out;
+    for (int c = in_place ? have + tid : tid; c < (in_place ? need : a.width); c += kPagesThreads)
+      a.table_out[row + c] = c < need ? page_at(c) : a.table_in[row + c];
+  }
+  const int64_t end = from + TILE < count ? from + TILE : count;
+  for (int64_t i = from + tid; i < end; i += kPagesThreads) {
+    const int64_t at = held + i, c = at / a.page_size;
+    const int32_t page = c < a.width ? page_at(static_cast<int32_t>(c)) : -1;
+    const int64_t slot = static_cast<int64_t>(page) * a.page_size + (at - c * a.page_size);
+    a.slots[start + i] = page >= 0 && slot <= kMaxToken ? static_cast<int32_t>(slot) : -1;
+    a.positions[start + i] = clamp_token(a.first + at);
+  }
+}
+
+// ---------------------------------------------------------------- norm and rotation
+struct QkArgs {
+  int32_t tokens, heads, kv_heads, rotary, num_positions, slots_end, page_size;
+  float eps;
+  const void* q;
+  const void* k;
+  const void* v;
+  int64_t ldq, ldk, ldv, ldqo, ldko;
+  const int32_t* positions;
+  const float* cos_sin;
+  const float* q_weight;
+  const float* k_weight;
+  const int32_t* slots;
+  void* q_out;
+  void* k_out;
+  void* k_cache;
+  void* v_cache;
+  int64_t kp, kt, kh, vp, vt, vh;
+};
+
+// A thread takes eight elements of a head row, D / 8 neighbouring lanes a row.
+constexpr int kQkThreads = 256;
+template <typename T, int D, bool INTERLEAVED>
+__global__ __launch_bounds__(kQkThreads)
+void k_qk_norm_rope(QkArgs a) {
+  constexpr int LPR = D / 8, UNITS = kQkThreads / LPR;
+  const int lane = threadIdx.x % LPR, per = a.heads + (a.v ? 2 : 1) * a.kv_heads;
+  const int64_t unit = static_cast<int64_t>(blockIdx.x) * UNITS + threadIdx.x / LPR;
+  if (unit >= static_cast<int64_t>(a.tokens) * per) return;
+  const int t = static_cast<int>(unit / per), u = static_cast<int>(unit - static_cast<int64_t>(t) * per);
+  const int pos = a.positions[t];
+  if (pos < 0 || pos >= a.num_positions) return;   // whole rows of lanes leave together
+  const bool is_q = u < a.heads, is_v = u >= a.heads + a.kv_heads;
+  const int h = is_q ? u : is_v ? u - a.heads - a.kv_heads : u - a.heads;
+  const T* src = is_q ? static_cast<const T*>(a.q) + t * a.ldq
+                      : is_v ? static_cast<const T*>(a.v) + t * a.ldv : static_cast<const T*>(a.k) + t * a.ldk;
+  float x[8];
+  load_run<T, 8>(src + h * D + 8 * lane, x);
+  const float* w = is_q ? a.q_weight : is_v ? nullptr : a.k_weight;
+  if (w) {
+    float s = 0.0f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s = fmaf(x[j], x[j], s);
+#pragma unroll
+    for (int off = 1; off < LPR; off <<= 1) s += __shfl_xor(s, off, LPR);
+    const float r = rsqrtf(s * (1.0f / D) + a.eps);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = x[j] * r * w[8 * lane + j];
+  }
+  if (!is_v) {
+    const float* cs = a.cos_sin + static_cast<int64_t>(pos) * a.rotary;
+    const int half = a.rotary / 2;
+    if constexpr (INTERLEAVED) {
+      if (8 * lane < a.rotary) {
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+          const float c = cs[4 * lane + p], s = cs[half + 4 * lane + p], e = x[2 * p], o = x[2 * p + 1];
+          x[2 * p] = e * c - o * s;
+          x[2 * p + 1] = o * c + e * s;
+        }
+      }
+    } else {
+      const bool turned = 8 * lane < a.rotary, first = 8 * lane < half;
+      const int other = turned ? (first ? lane + half / 8 : lane - half / 8) : lane;
+      float y[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) y[j] = __shfl(x[j], other, LPR);
+      if (turned) {
+        const int p = 8 * lane - (first ? 0 : half);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float c = cs[p + j], s = cs[half + p + j];
+          x[j] = first ? x[j] * c - y[j] * s : x[j] * c + y[j] * s;
+        }
+      }
+    }
+  }
+  if (is_q) {
+    store8(static_cast<T*>(a.q_out) + t * a.ldqo + h * D + 8 * lane, x);
+    return;
+  }
+  if (!is_v && a.k_out) store8(static_cast<T*>(a.k_out) + t * a.ldko + h * D + 8 * lane, x);
+  T* cache = static_cast<T*>(is_v ? a.v_cache : a.k_cache);
+  if (!cache) return;
+  const int slot = a.slots[t];
+  if (slot < 0 || slot >= a.slots_end) return;
+  const int64_t page = slot / a.page_size, r = slot % a.page_size;
+  store8(cache + (is_v ? page * a.vp + r * a.vt + h * a.vh : page * a.kp + r * a.kt + h * a.kh) + 8 * lane, x);
+}
+
+}  // namespace gdn

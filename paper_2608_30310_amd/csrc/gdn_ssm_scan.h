@@ -304,6 +304,7 @@ __device__ __forceinline__ int nth_longest(const int32_t* __restrict__ cu, int n
 
 struct SsmScanArgs {
   int32_t n_seqs, heads, groups, seg_tokens;
+  float scale;    // of the outputs (fixed decays)
   bool ordered;   // kWhole: unit r is the sequence of rank r
   const int32_t* cu;
   const void* x;
@@ -312,7 +313,7 @@ struct SsmScanArgs {
   const void* C;
   int64_t ldx, ld_dt, ldb, ldc, ldy;
   bool dt_bf16;
-  const float* a_log;
+  const float* a_log;   // fixed decays: log alpha
   const float* d_skip;
   const float* dt_bias;
   const float* state_in;
@@ -326,6 +327,13 @@ struct SsmScanArgs {
 // kLocal: a unit is a segment from the zero state to seg_state and seg_decay.
 // kJoined: a unit is a segment from seg_state to y.
 enum class SsmMode { kWhole, kLocal, kJoined };
+
+// 2^e of an exponent in 64 bits: as good as exp2's own rounding whatever |e|.
+__device__ __forceinline__ float exp2_wide(double e) {
+  const float high = static_cast<float>(e), low = static_cast<float>(e - high);
+  const float p = __builtin_amdgcn_exp2f(high);
+  return fmaf(p, low * 0.693147180559945f, p);
+}
 
 template <typename T, int DK, int DV, int CT, int NW, bool OUT>
 struct SsmLayout {
@@ -364,7 +372,11 @@ constexpr int ssm_waves() {
   return MODE == SsmMode::kWhole && OUT && DK == 128 && NW <= 4 ? 1 : 2;
 }
 
-template <typename T, int DK, int DV, int CT, int NW, SsmMode MODE, bool OUT>
+// FIXED: linear attention with a decay for each head (gdn_linear.h), M <- alpha M +
+// k v^T, y = scale M^T q: x is v, B is k, C is q, a step has delta = 1 and there is
+// no dt.  The scalars of a whole chunk are the same for every chunk, so they are
+// made once, from exponents in 64 bits, and again for a sequence's last, shorter one.
+template <typename T, int DK, int DV, int CT, int NW, SsmMode MODE, bool OUT, bool FIXED = false>
 __global__ __launch_bounds__(NW * kWave, (ssm_waves<T, DK, NW, MODE, OUT, SsmLayout<T, DK, DV, CT, NW, OUT>::kBytes>()))
 void k_ssm_scan(SsmScanArgs a) {
   typedef SsmLayout<T, DK, DV, CT, NW, OUT> L;
@@ -427,9 +439,14 @@ void k_ssm_scan(SsmScanArgs a) {
       }
     }
 
-  const float neg_a2 = wave < L::kHeads ? -expf(a.a_log[h0 + wave]) * 1.44269504088896f : 0.0f;
-  const float dt_bias = wave < L::kHeads && a.dt_bias ? a.dt_bias[h0 + wave] : 0.0f;
-  const float skip = OUT && a.d_skip ? a.d_skip[head] : 0.0f;
+  const float neg_a2 = !FIXED && wave < L::kHeads ? -expf(a.a_log[h0 + wave]) * 1.44269504088896f : 0.0f;
+  const float dt_bias = !FIXED && wave < L::kHeads && a.dt_bias ? a.dt_bias[h0 + wave] : 0.0f;
+  const float skip = !FIXED && OUT && a.d_skip ? a.d_skip[head] : 0.0f;
+  double rate = 0.0;   // log2 alpha (FIXED)
+  if (FIXED && wave < L::kHeads) {
+    rate = static_cast<double>(a.a_log[h0 + wave]) * 1.4426950408889634;
+    if (rate < -150.0) rate = -150.0;   // as below
+  }
   float log_total = 0.0f;   // of the whole segment (kLocal)
 
   // A thread's pieces of a chunk: rows tid / pieces + k (threads / pieces).  A
@@ -462,7 +479,7 @@ void k_ssm_scan(SsmScanArgs a) {
     const __amdgpu_buffer_rsrc_t rx = rows_buffer(xb + at * a.ldx, (rows - 1) * ldx + L::kHeads * DV * E);
 #pragma unroll
     for (int k = 0; k < KX; ++k) px[k] = __builtin_amdgcn_raw_buffer_load_b128(rx, vx + k * XSTEP * ldx, 0, 0);
-    if (wave < L::kHeads) {
+    if (!FIXED && wave < L::kHeads) {
       const int64_t base = (t0 + at) * a.ld_dt + h0 + wave;
       const uint32_t off = min(static_cast<uint32_t>(lane), rows - 1) * static_cast<uint32_t>(a.ld_dt);
       if (a.dt_bf16) pdt = (static_cast<const uint16_t*>(a.dt) + base)[off];
@@ -504,7 +521,30 @@ void k_ssm_scan(SsmScanArgs a) {
     }
 #pragma unroll
     for (int k = 0; k < KX; ++k) *reinterpret_cast<u32x4*>(lds + x_at(k)) = px[k];
-    if (wave < L::kHeads) {
+    if (FIXED && wave < L::kHeads && (at == 0 || rows < kSsmChunk)) {
+      // this head's decays, a token per lane: its tile holds `in_tile` tokens, `upto` of them up to this one
+      const int in_tile = max(0, min(16, rows - 16 * g)), upto = min(c + 1, in_tile), behind = max(0, rows - 1 - lane);
+      const bool there = lane < rows;
+      HeadScalars& o = sc[wave];
+      if constexpr (OUT) {
+        const double wide = rate * upto;
+        const float high = static_cast<float>(wide), low = static_cast<float>(wide - high);
+        o.high[lane] = high;
+        o.low[lane] = low;
+        o.same[lane] = there ? -low : -INFINITY;
+        o.row[lane] = exp2_wide(wide) * a.scale;
+        o.past[lane] = there ? exp2_wide(rate * (in_tile - upto)) : 0.0f;
+        o.pre[lane] = exp2_wide(rate * min(lane + 1, rows)) * a.scale;
+        // the tokens of the tiles between those of tile pair t, see tile_rows
+        if (lane < 10) {
+          const int t1 = max(0, min(16, rows - 16)), t2 = max(0, min(16, rows - 32));
+          o.between[lane] = exp2_wide(rate * (lane == 3 ? t1 : lane == 6 ? t1 + t2 : lane == 7 ? t2 : 0));
+        }
+      }
+      o.suf[lane] = there ? exp2_wide(rate * behind) : 0.0f;
+      if (lane == 0) o.total = exp2_wide(rate * rows);
+    }
+    if (!FIXED && wave < L::kHeads) {
       // this head's steps, a token per lane
       float delta = 0.0f, la = 0.0f;
       if (lane < rows) {
@@ -672,7 +712,8 @@ void k_ssm_scan(SsmScanArgs a) {
         float v[4];
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const float p = cd[k][r] * __builtin_amdgcn_exp2f((ed[k] - hd[k][r]) + (ld[k] + jd[k][r]));
+          float p = cd[k][r] * __builtin_amdgcn_exp2f((ed[k] - hd[k][r]) + (ld[k] + jd[k][r]));
+          if (FIXED) p *= a.scale;
           v[r] = 4 * g + r < c ? p : 4 * g + r == c ? p + skip : 0.0f;   // d_skip x rides on the diagonal
         }
         put(own + k * WPH, own + k * WPH, v);
@@ -781,7 +822,8 @@ void k_ssm_scan(SsmScanArgs a) {
     for (int td = 0; td < DK / 16; ++td)
 #pragma unroll
       for (int ct = 0; ct < CT; ++ct) seg[(td * CT + ct) * kWave] = m[td][ct];
-    if (wave < L::kHeads && lane == 0) a.seg_decay[static_cast<int64_t>(slot) * a.heads + h0 + wave] = log_total;
+    if (wave < L::kHeads && lane == 0)
+      a.seg_decay[static_cast<int64_t>(slot) * a.heads + h0 + wave] = FIXED ? static_cast<float>(rate * len) : log_total;
   } else if (MODE == SsmMode::kWhole && a.state_out) {
 #pragma unroll
     for (int td = 0; td < DK / 16; ++td)

@@ -15,13 +15,15 @@ constexpr int kSsmWaves = kSsmThreads / kWave;
 // so that all its loads are in flight together.  64 heads of 64 x 128: 128
 // sequences 83 us (539 MB, 6.5 TB/s, part of the state still in the last-level
 // cache; a copy of as many bytes 99 to 110), one sequence 3.9 us.
-template <typename T, int DK, int DV>
+// FIXED: the same for linear attention with a decay for each head (gdn_linear.h):
+// delta = 1, a_log is log alpha, the output is scaled.
+template <typename T, int DK, int DV, bool FIXED = false>
 __global__ __launch_bounds__(kSsmThreads)
 void k_ssm_step(int32_t heads, int32_t groups, const T* __restrict__ x, int64_t ldx, const void* __restrict__ dt,
                 bool dt_bf16, int64_t ld_dt, const float* __restrict__ a_log, const T* __restrict__ B, int64_t ldb,
                 const T* __restrict__ Cm, int64_t ldc, const float* __restrict__ d_skip,
                 const float* __restrict__ dt_bias, const float* state_in, T* __restrict__ y, int64_t ldy,
-                float* state_out) {
+                float* state_out, float scale) {
   constexpr int CQ = DV / 4;
   constexpr int RP = kSsmThreads / CQ;
   constexpr int RPT = DK / RP;
@@ -43,8 +45,8 @@ void k_ssm_step(int32_t heads, int32_t groups, const T* __restrict__ x, int64_t 
   load_run<T, 4>(x + n * ldx + h * DV + 4 * cq, xv);
   load_run<T, RPT>(B + n * ldb + gh * DK + rp * RPT, bv);
   load_run<T, RPT>(Cm + n * ldc + gh * DK + rp * RPT, cv);
-  const float delta = softplus_f(load_dt(dt, dt_bf16, n * ld_dt + h) + (dt_bias ? dt_bias[h] : 0.0f));
-  const float alpha = expf(-expf(a_log[h]) * delta), skip = d_skip ? d_skip[h] : 0.0f;
+  const float delta = FIXED ? 1.0f : softplus_f(load_dt(dt, dt_bf16, n * ld_dt + h) + (dt_bias ? dt_bias[h] : 0.0f));
+  const float alpha = expf(FIXED ? a_log[h] : -expf(a_log[h]) * delta), skip = !FIXED && d_skip ? d_skip[h] : 0.0f;
   f32x4 p = zero4();
 #pragma unroll
   for (int i = 0; i < RPT; ++i) {
@@ -58,7 +60,7 @@ void k_ssm_step(int32_t heads, int32_t groups, const T* __restrict__ x, int64_t 
   const f32x4 o = decode_reduce<CQ>(p, red, lane, wave, cq);
   if (rp == 0) {
 #pragma unroll
-    for (int c = 0; c < 4; ++c) store_elt(y, n * ldy + h * DV + 4 * cq + c, fmaf(skip, xv[c], o[c]));
+    for (int c = 0; c < 4; ++c) store_elt(y, n * ldy + h * DV + 4 * cq + c, FIXED ? scale * o[c] : fmaf(skip, xv[c], o[c]));
   }
 }
 

@@ -1,7 +1,7 @@
 """ctypes binding of a recurrent layer's other operators: the short causal
-convolution, the selective state space scan, each for packed sequences and for
-one token per sequence, and low-rank adapters beside a shared projection
-(``include/gdn_ssm.h``, ``include/gdn_lora.h``).
+convolution, the selective state space scan, linear attention with a decay for
+each head, each for packed sequences and for one token per sequence, and low-rank adapters beside a shared projection
+(``include/gdn_ssm.h``, ``include/gdn_linear.h``, ``include/gdn_lora.h``).
 
 Argument checks and marshalling only, as in ``binding``.  Token rows may be
 strided (columns of a projection's rows are passed as views, nothing is
@@ -17,7 +17,7 @@ from typing import Optional
 
 import torch
 
-from .binding import (ConvShape, GDN_F32, LoraShape, SSMShape, _adapter_ids, _check, _dtype_code, _need, _ptr,
+from .binding import (ConvShape, GDN_F32, LinearShape, LoraShape, SSMShape, _adapter_ids, _check, _dtype_code, _need, _ptr,
                       _seqlens, _stream, _workspace, _WORKSPACES, load_library)
 
 GDN_ERR_WORKSPACE = 5
@@ -25,14 +25,14 @@ GDN_ERR_WORKSPACE = 5
 _ACTIVATIONS = {None: 0, "none": 0, "silu": 1}
 
 
-def _on_device(fn):
-    """Runs the call with its first tensor's device current (kernels launch on
-    the current device); free where it is current already."""
-    name = fn.__code__.co_varnames[0]
+def _on_device(fn, at=0):
+    """Runs the call with the device of its argument number ``at`` current (kernels
+    launch on the current device); free where it is current already."""
+    name = fn.__code__.co_varnames[at]
 
     @functools.wraps(fn)
     def call(*args, **kwargs):
-        first = args[0] if args else kwargs.get(name)
+        first = args[at] if len(args) > at else kwargs.get(name)
         if not isinstance(first, torch.Tensor) or not first.is_cuda:
             raise ValueError(f"{fn.__name__} works on tensors in GPU memory")
         if first.get_device() == torch._C._cuda_getDevice():
@@ -228,13 +228,13 @@ def _ssm_args(x, dt, a_log, B, C, d_skip, dt_bias, out):
                                 ldy)
 
 
-def _state(t, name, shape, device):
+def _state(t, name, shape, device, dims="[N, H, d_state, head_dim]"):
     if t is None or (type(t) is torch.Tensor and t.shape == shape and t.dtype is torch.float32 and
                      t.device == device and t.is_contiguous()):
         return
     _need(t, name, torch.float32, device, 4)
     if t.shape != shape:
-        raise ValueError(f"{name} must be [N, H, d_state, head_dim]")
+        raise ValueError(f"{name} must be {dims}")
 
 
 @_on_device
@@ -301,6 +301,90 @@ def ssm_step(x: torch.Tensor, dt: torch.Tensor, a_log: torch.Tensor, B: torch.Te
     _check(lib.gdn_ssm_step(ctypes.byref(SSMShape(n, *shape)), x.data_ptr(), dt.data_ptr(), a_log.data_ptr(), B.data_ptr(),
                             C.data_ptr(), _ptr(d_skip), _ptr(dt_bias), _ptr(state_in), out.data_ptr(),
                             state_out.data_ptr(), _stream(device)))
+    return out, state_out
+
+
+# ---------------------------------------------------------------- linear attention
+
+def _linear_args(q, k, v, g, scale, out):
+    device, dtype = v.device, v.dtype
+    if v.dim() != 3 or not isinstance(k, torch.Tensor) or k.dim() != 3:
+        raise ValueError("k must be [T, Hk, d_k] and v [T, Hv, d_v]")
+    T, Hv, V = v.shape
+    Hk, K = k.shape[1], k.shape[2]
+    ldk, ldv = _rows(k, "k", dtype, device, (Hk, K)), _rows(v, "v", dtype, device, (Hv, V))
+    ldq = ldk if q is None else _rows(q, "q", dtype, device, (Hk, K))
+    ldo = Hv * V if out is None else _rows(out, "out", dtype, device, (Hv, V))
+    if k.shape[0] != T or (q is not None and q.shape[0] != T) or (out is not None and out.shape[0] != T):
+        raise ValueError("q, k and out must hold the same tokens as v")
+    if g is None:
+        raise TypeError("g must be a torch.Tensor")
+    _flat(g, "g", (Hv,), device)
+    return device, T, Hv, K, V, (Hk, Hv, K, V, _dtype_code(v), float(scale), ldq, ldk, ldv, ldo)
+
+
+@functools.partial(_on_device, at=1)   # q may be None
+def linear_attention(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, g: torch.Tensor, cu_seqlens,
+                     cu_seqlens_host=None, scale: float = 1.0, state_in: Optional[torch.Tensor] = None,
+                     outputs: bool = True, out: Optional[torch.Tensor] = None,
+                     state_out: Optional[torch.Tensor] = None, write_state: bool = True,
+                     workspace: Optional[torch.Tensor] = None):
+    """Linear attention with a decay for each head, of packed sequences, on
+    torch's current stream.
+
+    Per token and value head: M = exp(g) M + k v^T, o = scale M^T q.  q, k
+    [T, Hk, d_k], v [T, Hv, d_v] (bf16 or fp32, token rows may be strided; head h
+    reads key head h / (Hv / Hk)), g [Hv] fp32 (log decays, <= 0), state_in
+    [N, Hv, d_k, d_v] fp32 (None = zero states).  Returns ``(o [T, Hv, d_v] in
+    v's dtype, state_out)``; with ``outputs=False`` only the states are computed
+    (a replayed tail's; o is None, q is not read and may be None).  ``state_out``
+    may be ``state_in``.  Rows of ``out`` behind the last sequence are left alone.
+    """
+    lib = load_library()
+    if not outputs:
+        if out is not None or not write_state:
+            raise ValueError("outputs=False computes the states alone: out must be None and write_state true")
+        q = None
+    elif q is None:
+        raise TypeError("q must be a torch.Tensor")
+    device, T, Hv, K, V, shape = _linear_args(q, k, v, g, scale, out)
+    cu, host = _offsets(cu_seqlens, cu_seqlens_host, device, T)
+    n = host.numel() - 1
+    if outputs and out is None:
+        out = torch.empty((T, Hv, V), dtype=v.dtype, device=device)
+    _state(state_in, "state_in", (n, Hv, K, V), device, "[N, Hv, d_k, d_v]")
+    if write_state and state_out is None:
+        state_out = torch.empty((n, Hv, K, V), dtype=torch.float32, device=device)
+    _state(state_out, "state_out", (n, Hv, K, V), device, "[N, Hv, d_k, d_v]")
+    shp = LinearShape(n, *shape)
+    stream = _stream(device)
+    lens = host.data_ptr()
+    args = (ctypes.byref(shp), lens, cu.data_ptr(), _ptr(q), k.data_ptr(), v.data_ptr(), g.data_ptr(), _ptr(state_in),
+            _ptr(out), _ptr(state_out))
+    _run_with_workspace(lambda ws, nbytes: lib.gdn_linear_attention(*args, ws, nbytes, stream),
+                        lib.gdn_linear_attention_workspace_size, shp, lens, device, stream, workspace)
+    return out, state_out
+
+
+@_on_device
+def linear_attention_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, g: torch.Tensor,
+                          state_in: Optional[torch.Tensor] = None, scale: float = 1.0,
+                          out: Optional[torch.Tensor] = None, state_out: Optional[torch.Tensor] = None):
+    """``linear_attention`` for one token per sequence (T = N).  Returns ``(o [N,
+    Hv, d_v], state_out)``; pass ``state_out=state_in`` to update in place."""
+    lib = load_library()
+    if q is None:
+        raise TypeError("q must be a torch.Tensor")
+    device, n, Hv, K, V, shape = _linear_args(q, k, v, g, scale, out)
+    if out is None:
+        out = torch.empty((n, Hv, V), dtype=v.dtype, device=device)
+    _state(state_in, "state_in", (n, Hv, K, V), device, "[N, Hv, d_k, d_v]")
+    if state_out is None:
+        state_out = torch.empty((n, Hv, K, V), dtype=torch.float32, device=device)
+    _state(state_out, "state_out", (n, Hv, K, V), device, "[N, Hv, d_k, d_v]")
+    _check(lib.gdn_linear_attention_step(ctypes.byref(LinearShape(n, *shape)), q.data_ptr(), k.data_ptr(), v.data_ptr(),
+                                         g.data_ptr(), _ptr(state_in), out.data_ptr(), state_out.data_ptr(),
+                                         _stream(device)))
     return out, state_out
 
 
