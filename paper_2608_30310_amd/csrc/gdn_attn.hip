@@ -2,6 +2,9 @@
 // in gdn_attn.h).
 #include "gdn_attn_kernels.h"
 
+#include <algorithm>
+#include <cmath>
+#include <limits>
 #include <string>
 
 #include "gdn_attn_plan.h"
@@ -16,9 +19,13 @@ gdn_status afail(gdn_status st, const std::string& msg) {
 }
 
 template <typename T, int D>
-gdn_status launch_attn(const AttnArgs& a, hipStream_t stream) {
-  const int64_t units = static_cast<int64_t>(a.tokens) * a.heads, nw = kAttnThreads / kWave;
-  hipLaunchKernelGGL((k_attn<T, D>), dim3(static_cast<uint32_t>((units + nw - 1) / nw)), dim3(kAttnThreads), 0, stream, a);
+gdn_status launch_attn(const AttnArgs& a, const AttnPlan& p, hipStream_t stream) {
+  static_assert(kAttnRows == kPlanRows && kAttnTile == kPlanTile, "the plan's tiles");
+  hipLaunchKernelGGL((k_attn<T, D>), dim3(static_cast<uint32_t>(p.shared_items + p.own_items)), dim3(kAttnThreads), 0, stream, a);
+  if (p.joined) {
+    const int64_t tiles = (p.rows + kAttnRows - 1) / kAttnRows * a.kv_heads;
+    hipLaunchKernelGGL((k_attn_join<T, D>), dim3(static_cast<uint32_t>(tiles)), dim3(kAttnThreads), 0, stream, a);
+  }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return afail(GDN_ERR_HIP, std::string("attention launch: ") + hipGetErrorString(e));
   return GDN_OK;
@@ -74,12 +81,34 @@ gdn_status gdn_prefix_attention(const gdn_attn_shape* shape, const int32_t* cu_s
                                         std::to_string(workspace_bytes));
   if (p.bytes > 0 && reinterpret_cast<uintptr_t>(workspace) % kAlign != 0)
     return afail(GDN_ERR_WORKSPACE, "workspace must be 256-byte aligned");
-  const AttnArgs a{s.num_seqs, s.num_heads, s.num_kv_heads, s.num_pages, s.page_size, s.table_width, s.prefix_len, p.max_len,
-                   static_cast<int32_t>(p.tokens), s.scale, cu_seqlens, table, lens, prefix_pages, q, k_cache, v_cache, out,
-                   s.ld_q, s.ld_out, s.k_page, s.k_token, s.k_head, s.v_page, s.v_token, s.v_head};
+  // n / d = mulhi(n, m) >> (l - 1) for n < 2^31: m = 2^(31 + l) / d rounded up, l = ceil(log2 d)
+  int l = 0;
+  while ((int64_t{1} << l) < s.page_size) ++l;
+  const uint32_t mul = l ? static_cast<uint32_t>((uint64_t{1} << (31 + l)) / s.page_size + 1) : 0;
+  const int64_t vec = 16 / e;
+  const auto units = [&](int64_t stride) { return static_cast<uint32_t>(stride / vec); };
+  AttnArgs a{};
+  a.n_seqs = s.num_seqs, a.kv_heads = s.num_kv_heads, a.groups = p.groups, a.num_pages = s.num_pages;
+  a.page_size = s.page_size, a.width = s.table_width, a.prefix_len = s.prefix_len, a.max_len = p.max_len;
+  a.page_mul = mul, a.page_shift = l ? l - 1 : 0;
+  // (not below the least normal number: a masked score of -inf stays one)
+  a.scale2 = std::max(std::fabs(s.scale) * 1.44269504088896f, std::numeric_limits<float>::min());
+  a.flip = std::signbit(s.scale) ? 0x80000000u : 0u;
+  a.shared_splits = p.shared_splits, a.shared_chunk = p.shared_chunk;
+  a.shared_tiles = static_cast<int32_t>(p.shared_tiles), a.shared_items = static_cast<int32_t>(p.shared_items);
+  a.own_tile = p.own_tile, a.own_splits = p.own_splits, a.own_chunk = p.own_chunk;
+  a.own_slots = static_cast<int32_t>(p.own_slots), a.rows = static_cast<int32_t>(p.rows);
+  a.cu = cu_seqlens, a.table = table, a.lens = lens, a.prefix_pages = prefix_pages;
+  a.q = q, a.k = k_cache, a.v = v_cache, a.out = out, a.ldq = s.ld_q, a.ldo = s.ld_out;
+  a.kp = units(s.k_page), a.kt = units(s.k_token), a.vp = units(s.v_page), a.vt = units(s.v_token);
+  a.kh = s.k_head * e, a.vh = s.v_head * e;
+  if (p.joined) {
+    a.part = static_cast<f32x4*>(workspace);
+    a.part_ml = reinterpret_cast<f32x2*>(static_cast<char*>(workspace) + p.off_ml);
+  }
   const hipStream_t hs = static_cast<hipStream_t>(stream);
-  if (s.dtype == GDN_BF16) return s.head_dim == 64 ? launch_attn<uint16_t, 64>(a, hs) : launch_attn<uint16_t, 128>(a, hs);
-  return s.head_dim == 64 ? launch_attn<float, 64>(a, hs) : launch_attn<float, 128>(a, hs);
+  if (s.dtype == GDN_BF16) return s.head_dim == 64 ? launch_attn<uint16_t, 64>(a, p, hs) : launch_attn<uint16_t, 128>(a, p, hs);
+  return s.head_dim == 64 ? launch_attn<float, 64>(a, p, hs) : launch_attn<float, 128>(a, p, hs);
 }
 
 }  // extern "C"

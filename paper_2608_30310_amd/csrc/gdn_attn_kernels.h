@@ -1,14 +1,44 @@
-// Attention over a shared prefix and each sequence's own pages (C ABI in
-// gdn_attn.h).
+// Attention over a shared prefix and each sequence's own pages on the matrix
+// cores (C ABI in gdn_attn.h).
+//
+// Rows.  The Hq / Hkv query heads of a K/V head read the same keys, so a row of
+// a tile is one head of one token, r = token * G + head % G, and keys are read
+// once for all of them.  A work item is a tile of rows, one K/V head and a range
+// of keys: of the prefix, of a sequence's own tokens, or of both one after the
+// other.
+//
+// A tile of scores is formed transposed, S^T = K Q^T (32 x 32 x 16 products): a
+// lane holds one row's scores, 16 keys of 32 (the other half wave the rest), so
+// maximum and sum are per lane but for one exchange of halves, and the scores'
+// registers are, key for key, the operand of O^T = V^T P^T.  Which keys lie in
+// which registers does not matter to that product as long as V's operand has them
+// in the same order.  One pass, with the running maximum m and sum l of each row:
+//   p = 2^(s - m),  l += sum p,  O += p V,  out = O / l,
+// where m moves (and O and l are scaled) only when a row's maximum passes it by
+// more than 8: p stays below 2^8, which neither bf16's range nor fp32 sums mind.
 #pragma once
 
 #include "gdn_varlen.h"
 
 namespace gdn {
 
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+constexpr int kAttnThreads = 256;
+constexpr int kAttnWaves = kAttnThreads / kWave;
+constexpr int kAttnRows = 32;                        // of a wave
+constexpr int kAttnTile = kAttnRows * kAttnWaves;    // of a workgroup whose waves take rows of their own
+
 struct AttnArgs {
-  int32_t n_seqs, heads, kv_heads, num_pages, page_size, width, prefix_len, max_len, tokens;
-  float scale;
+  int32_t n_seqs, kv_heads, groups, num_pages, page_size, width, prefix_len, max_len;
+  uint32_t page_mul;      // n / page_size = mulhi(n, page_mul) >> page_shift (page_size > 1)
+  int32_t page_shift;
+  float scale2;           // |scale| log2 e
+  uint32_t flip;          // sign bits of the queries where scale is negative
+  // items: shared ones over the prefix alone, all rows packed (shared_splits 0: none), then own ones
+  int32_t shared_splits, shared_chunk, shared_tiles, shared_items;
+  int32_t own_tile, own_splits, own_chunk, own_slots;
+  int32_t rows;           // T G
   const int32_t* cu;
   const int32_t* table;
   const int32_t* lens;
@@ -17,75 +47,728 @@ struct AttnArgs {
   const void* k;
   const void* v;
   void* out;
-  int64_t ldq, ldo, kp, kt, kh, vp, vt, vh;
+  int64_t ldq, ldo;
+  uint32_t kp, kt, vp, vt;   // strides of the caches' pages and tokens, in 16 bytes
+  int64_t kh, vh;            // of their heads, in bytes
+  // partial results of the items (NULL: items write out): shared ones, then own ones
+  f32x4* part;            // [item][wave tile][D / 8][lane]: four columns of a row
+  f32x2* part_ml;         // [item][wave tile][32]: m and l of a row
 };
 
-// A wave takes one query head of one token and 64 keys at a time, a key a lane
-// for the scores, D / 64 columns a lane for the values.
-constexpr int kAttnThreads = 256;
-template <typename T, int D>
-__global__ __launch_bounds__(kAttnThreads)
-void k_attn(AttnArgs a) {
-  constexpr int NW = kAttnThreads / kWave, C = D / 64;
-  __shared__ float qs[NW][D];
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
-  const int64_t unit = static_cast<int64_t>(blockIdx.x) * NW + wave;
-  if (unit >= static_cast<int64_t>(a.tokens) * a.heads) return;
-  const int t = static_cast<int>(unit / a.heads), h = static_cast<int>(unit % a.heads), kvh = h / (a.heads / a.kv_heads);
-  // the sequence of token t: the first whose end lies behind it
-  int lo = 0, hi = a.n_seqs - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi) / 2;
-    if (a.cu[mid + 1] > t) hi = mid;
-    else lo = mid + 1;
+// ---------------------------------------------------------------- operands
+// 32 x 32 x 16 products: lane (h, r) supplies elements 8 h + j (j = 0..7) of row r
+// of either operand and holds rows 8 (i / 4) + 4 h + i % 4 (i = 0..15) of column r.
+template <typename T>
+struct Mm;
+template <>
+struct Mm<uint16_t> {
+  typedef bf16x8 R;
+  static __device__ __forceinline__ f32x16 mul(const R& a, const R& b, const f32x16& c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
   }
-  const int n = lo, len = min(max(a.lens[n], 0), a.max_len);
-  const int own = max(min(len, len - (a.cu[n + 1] - t) + 1), 0);   // own tokens that the query sees
-  const T* q = static_cast<const T*>(a.q) + t * a.ldq + h * D;
-  for (int d = lane; d < D; d += kWave) qs[wave][d] = load_elt(q, d);
-  __builtin_amdgcn_wave_barrier();
-  float top = -INFINITY, sum = 0.0f, acc[C] = {};
-  const auto walk = [&](const int32_t* pages, int count) {
-    for (int j0 = 0; j0 < count; j0 += kWave) {
-      const int j = j0 + lane;
-      const int page = j < count ? pages[j / a.page_size] : -1, r = j % a.page_size;
-      const bool seen = page >= 0 && page < a.num_pages;
-      float s = -INFINITY;
-      if (seen) {
-        const T* k = static_cast<const T*>(a.k) + page * a.kp + r * a.kt + kvh * a.kh;
-        s = 0.0f;
-        for (int d = 0; d < D; d += 8) {
-          float x[8];
-          load_run<T, 8>(k + d, x);
-          for (int e = 0; e < 8; ++e) s = fmaf(x[e], qs[wave][d + e], s);
-        }
-        s *= a.scale;
-      }
-      float m = s;
-      for (int off = 1; off < kWave; off <<= 1) m = fmaxf(m, __shfl_xor(m, off, kWave));
-      const float next = fmaxf(top, m), at = next == -INFINITY ? 0.0f : next;
-      const float keep = expf(top - at), p = seen ? expf(s - at) : 0.0f;
-      top = next;
-      float ps = p;
-      for (int off = 1; off < kWave; off <<= 1) ps += __shfl_xor(ps, off, kWave);
-      sum = sum * keep + ps;
-      for (int c = 0; c < C; ++c) acc[c] *= keep;
-      for (int i = 0; i < kWave; ++i) {
-        const int pg = __shfl(page, i, kWave), ri = __shfl(r, i, kWave);
-        const float w = __shfl(p, i, kWave);
-        if (pg < 0 || pg >= a.num_pages) continue;
-        const T* v = static_cast<const T*>(a.v) + pg * a.vp + ri * a.vt + kvh * a.vh + C * lane;
-        for (int c = 0; c < C; ++c) acc[c] = fmaf(w, load_elt(v, c), acc[c]);
+  // p: eight weights, rounded to bf16 as the product takes them
+  static __device__ __forceinline__ R pack(const float (&p)[8]) {
+    u32x4 w;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const f32x2 x = {p[2 * j], p[2 * j + 1]};
+      w[j] = __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
+    }
+    return __builtin_bit_cast(R, w);
+  }
+  static __device__ __forceinline__ R flip(const R& a, uint32_t sign) {
+    u32x4 w = __builtin_bit_cast(u32x4, a);
+    w ^= sign | sign >> 16;
+    return __builtin_bit_cast(R, w);
+  }
+};
+template <>
+struct Mm<float> {
+  typedef f32x8 R;
+  static __device__ __forceinline__ f32x16 mul(const R& a, const R& b, f32x16 c) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], c, 0, 0, 0);
+    return c;
+  }
+  static __device__ __forceinline__ R pack(const float (&p)[8]) { return R{p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7]}; }
+  static __device__ __forceinline__ R flip(const R& a, uint32_t sign) {
+    R r;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) r[j] = __uint_as_float(__float_as_uint(a[j]) ^ sign);
+    return r;
+  }
+};
+
+// Rows of D elements in LDS as they lie in memory, 16-byte piece p of row r at
+// p ^ swz(r).  The swizzle is a permutation of the low row bits, so the operand
+// reads of K (32 rows of one piece) meet every bank once; those of V (four rows
+// of four pieces, transposed on the way) do because rows 0..3 differ in the high
+// bits of the piece.  (fp32: rows r and r + 4 differ in the highest, for V's
+// 4-byte reads.)
+template <typename T, int D>
+struct KvRows {
+  static constexpr int kPitch = D * static_cast<int>(sizeof(T));
+  static constexpr int kPieces = kPitch / 16;
+  static constexpr int kRowsPerDma = kWave / kPieces;   // a DMA moves 64 pieces
+  static __device__ __forceinline__ constexpr int swz(int r) {
+    if (sizeof(T) == 4) return (r & 7) << 1 | (r >> 3 & 1);
+    return D == 128 ? (r & 3) << 2 | (r >> 2 & 3) : (r >> 1 & 1) << 2 | (r >> 2 & 3);
+  }
+  static __device__ __forceinline__ int at(int r, int piece) { return r * kPitch + ((piece ^ swz(r)) << 4); }
+  // elements 8 e8 .. + 7 of row r
+  static __device__ __forceinline__ typename Mm<T>::R row_frag(const char* base, int r, int e8) {
+    if constexpr (sizeof(T) == 2) {
+      return __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(base + at(r, e8)));
+    } else {
+      const f32x4 a = *reinterpret_cast<const f32x4*>(base + at(r, 2 * e8));
+      const f32x4 b = *reinterpret_cast<const f32x4*>(base + at(r, 2 * e8 + 1));
+      return f32x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+    }
+  }
+  // column 32 dt + lane % 32 of rows r0 + 8 (j / 4) + 4 h + j % 4, j = 0..7 (r0 a multiple of 16)
+  static __device__ __forceinline__ typename Mm<T>::R col_frag(const char* base, int r0, int dt, int lane) {
+    const int h = lane / 32;
+    if constexpr (sizeof(T) == 2) {
+      const int row = 4 * h + lane % 16 / 4, piece = 4 * dt + lane / 16 % 2 * 2 + lane % 4 / 2, half = lane % 2 * 8;
+      base += r0 * kPitch;
+      const u32x2 a = lds_read_tr16(base + at(row, piece) + half);
+      const u32x2 b = lds_read_tr16(base + at(row + 8, piece) + half);
+      return join_halves(a, b);
+    } else {
+      f32x8 x;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] = elt(base, r0 + 8 * (j / 4) + 4 * h + j % 4, 32 * dt + lane % 32);
+      return x;
+    }
+  }
+  static __device__ __forceinline__ float elt(const char* base, int r, int col) {
+    const int b = col * static_cast<int>(sizeof(T));
+    const char* p = base + at(r, b / 16) + b % 16;
+    if constexpr (sizeof(T) == 2) return bf2f(*reinterpret_cast<const uint16_t*>(p));
+    else return *reinterpret_cast<const float*>(p);
+  }
+};
+
+__device__ __forceinline__ bool not_finite(float x) { return (__float_as_uint(x) & 0x7F800000u) == 0x7F800000u; }
+// An operand with its infinities and NaNs replaced by zero; *found: there were some.
+__device__ __forceinline__ bf16x8 finite_only(const bf16x8& a, bool* found) {
+  u32x4 w = __builtin_bit_cast(u32x4, a);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const bool lo = (w[j] & 0x7F80u) == 0x7F80u, hi = (w[j] & 0x7F800000u) == 0x7F800000u;
+    *found |= lo || hi;
+    w[j] &= (lo ? 0u : 0xFFFFu) | (hi ? 0u : 0xFFFF0000u);
+  }
+  return __builtin_bit_cast(bf16x8, w);
+}
+__device__ __forceinline__ f32x8 finite_only(const f32x8& a, bool* found) {
+  f32x8 r;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const bool bad = not_finite(a[j]);
+    *found |= bad;
+    r[j] = bad ? 0.0f : a[j];
+  }
+  return r;
+}
+
+// The larger of a lane's value and its counterpart's in the other half wave, and their sum.
+__device__ __forceinline__ float half_max(float x) {
+  const u32x2 s = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false));
+  return fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1]));
+}
+__device__ __forceinline__ float half_sum(float x) {
+  const u32x2 s = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false));
+  return __uint_as_float(s[0]) + __uint_as_float(s[1]);
+}
+
+// ---------------------------------------------------------------- keys
+// The keys that an item walks, in tiles of KT: `count0` tokens of the prefix from
+// `first0` on, then `count1` of a sequence's own from `first1` on.
+struct KeyRange {
+  const int32_t* list0;
+  const int32_t* list1;
+  int first0, count0, first1, count1;
+  template <int KT>
+  __device__ __forceinline__ int tiles() const { return (count0 + KT - 1) / KT + (count1 + KT - 1) / KT; }
+};
+struct KeyTile {
+  const int32_t* list;
+  int base, count;   // its first token, and how many there are of KT
+  bool own;
+};
+template <int KT>
+__device__ __forceinline__ KeyTile key_tile(const KeyRange& k, int j) {
+  const int t0 = (k.count0 + KT - 1) / KT;
+  const bool own = j >= t0;
+  const int from = (own ? j - t0 : j) * KT;
+  return {own ? k.list1 : k.list0, (own ? k.first1 : k.first0) + from, min(KT, (own ? k.count1 : k.count0) - from), own};
+}
+
+// The page and its row that hold token base + lane % KT of a tile (lanes behind its end: of its last token).
+struct PageOf { int page, row; };
+template <int KT>
+__device__ __forceinline__ PageOf find_pages(const AttnArgs& a, const KeyTile& t) {
+  const int key = t.base + min(static_cast<int>(threadIdx.x) % KT, t.count - 1);
+  const int c = a.page_size == 1 ? key : static_cast<int>(__umulhi(key, a.page_mul) >> a.page_shift);
+  return {t.list[c], key - c * a.page_size};
+}
+
+// Where a K/V head's rows are in the caches.
+struct CacheAt { const char* k; const char* v; };
+
+// DMA of rows [i0, i0 + N) kRowsPerDma of a tile into LDS (both of K and V, or one of them).
+template <typename T, int D, int N, bool K, bool V>
+__device__ __forceinline__ void load_rows(const AttnArgs& a, const CacheAt& c, const PageOf& at, uint64_t there, bool whole,
+                                          lds_byte* kl, lds_byte* vl, int i0, int lane) {
+  typedef KvRows<T, D> Rows;
+  constexpr int RPD = Rows::kRowsPerDma;
+  const int j = lane / Rows::kPieces;
+  if (whole && a.page_size % RPD == 0) {
+    // the rows of a DMA lie in one page
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int r = (i0 + i) * RPD;
+      const uint64_t page = static_cast<uint32_t>(__builtin_amdgcn_readlane(at.page, r)),
+                     row = static_cast<uint32_t>(__builtin_amdgcn_readlane(at.row, r));
+      const uint32_t piece = lane % Rows::kPieces ^ Rows::swz(r + j);
+      if (K) dma16(c.k + 16 * (page * a.kp + row * a.kt) + 16 * static_cast<uint64_t>(j * a.kt + piece), kl + (i0 + i) * 1024);
+      if (V) dma16(c.v + 16 * (page * a.vp + row * a.vt) + 16 * static_cast<uint64_t>(j * a.vt + piece), vl + (i0 + i) * 1024);
+    }
+  } else {
+    // rows that are none are taken from the cache's first
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int r = (i0 + i) * RPD + j;
+      const bool ok = there >> r & 1;
+      const int pg = __shfl(at.page, r, kWave), rw = __shfl(at.row, r, kWave);
+      const uint64_t page = static_cast<uint32_t>(ok ? pg : 0), row = static_cast<uint32_t>(ok ? rw : 0);
+      const uint32_t piece = lane % Rows::kPieces ^ Rows::swz(r);
+      if (K) dma16(c.k + 16 * (page * a.kp + row * a.kt + piece), kl + (i0 + i) * 1024);
+      if (V) dma16(c.v + 16 * (page * a.vp + row * a.vt + piece), vl + (i0 + i) * 1024);
+    }
+  }
+}
+
+// ---------------------------------------------------------------- a wave's rows
+template <typename T, int D>
+struct AttnWave {
+  typedef KvRows<T, D> Rows;
+  typedef typename Mm<T>::R R;
+  R q[D / 16];
+  f32x16 o[D / 32];   // O^T: columns 32 dt + .. of row lane % 32
+  float m, l;         // l: this half wave's part
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[dt][i] = 0.0f;
+    m = -INFINITY;
+    l = 0.0f;
+  }
+  __device__ __forceinline__ void load_q(const T* row, uint32_t flip, int h) {
+#pragma unroll
+    for (int u = 0; u < D / 16; ++u) {
+      float x[8];
+      if constexpr (sizeof(T) == 2) {
+        q[u] = Mm<T>::flip(__builtin_bit_cast(R, *reinterpret_cast<const u32x4*>(row + 16 * u + 8 * h)), flip);
+      } else {
+        load_run<T, 8>(row + 16 * u + 8 * h, x);
+        q[u] = Mm<T>::flip(R{x[0], x[1], x[2], x[3], x[4], x[5], x[6], x[7]}, flip);
       }
     }
+  }
+  // S^T of 32 keys from row r0 of the tile
+  __device__ __forceinline__ f32x16 scores(const char* kl, int r0, int lane) const {
+    f32x16 s;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = 0.0f;
+#pragma unroll
+    for (int u = 0; u < D / 16; ++u) s = Mm<T>::mul(Rows::row_frag(kl, r0 + lane % 32, 2 * u + lane / 32), q[u], s);
+    return s;
+  }
+  // scores -> weights, for NB blocks of 32 keys
+  template <int NB>
+  __device__ __forceinline__ void weigh(f32x16 (&s)[NB], float scale2) {
+    float top = s[0][0];
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
+    top = half_max(top) * scale2;
+    // each row by itself: what one row meets does not change another's rounding
+    const bool moves = top > m + 8.0f || m == -INFINITY;
+    if (__any(moves)) {
+      const float next = moves ? fmaxf(m, top) : m;
+      const float keep = moves ? __builtin_amdgcn_exp2f(m - (next == -INFINITY ? 0.0f : next)) : 1.0f;
+      m = next;
+      l *= keep;
+#pragma unroll
+      for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[dt][i] *= keep;
+    }
+    const float at = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        s[b][i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], scale2, -at));
+        l += s[b][i];
+      }
+  }
+  // O^T += V^T P^T over 32 keys.  CHECK: some rows do not see some of the keys (weight
+  // zero), whose values may be anything: those that are not finite stay out of the
+  // product and are added, element by element, to the rows that see them (`seen`: bit
+  // i is for key 8 (i / 4) + 4 h + i % 4).
+  template <bool CHECK>
+  __device__ __forceinline__ void values(const char* vl, int r0, const f32x16& p, int lane, uint32_t seen) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      float w[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) w[j] = p[8 * s + j];
+      const R pf = Mm<T>::pack(w);
+      bool odd = false;
+#pragma unroll
+      for (int dt = 0; dt < D / 32; ++dt) {
+        R vf = Rows::col_frag(vl, r0 + 16 * s, dt, lane);
+        if (CHECK) vf = finite_only(vf, &odd);
+        o[dt] = Mm<T>::mul(vf, pf, o[dt]);
+      }
+      if (CHECK && __any(odd)) {
+        for (int k = 0; k < 16; ++k) {   // key k of these: register 8 s + 4 (k / 8) + k % 4 of half k / 4 % 2
+          const int reg = 8 * s + 4 * (k / 8) + k % 4, from = k / 4 % 2 * 32 + lane % 32;
+          float pk = 0.0f;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) pk = reg == i ? p[i] : pk;
+          pk = __shfl(pk, from, kWave);
+          const bool sees = __shfl(static_cast<int>(seen >> reg & 1), from, kWave);
+#pragma unroll
+          for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const float x = Rows::elt(vl, r0 + 16 * s + k, 32 * dt + 8 * (i / 4) + 4 * (lane / 32) + i % 4);
+              if (sees && not_finite(x)) o[dt][i] = fmaf(pk, x, o[dt][i]);
+            }
+        }
+      }
+    }
+  }
+  // A tile of NB blocks of 32 keys.  limit: keys of the tile that this lane's row may
+  // see; there: keys that exist; whole: all rows see all keys
+  template <int NB>
+  __device__ __forceinline__ void masked_scores(f32x16 (&s)[NB], uint32_t (&seen)[NB], int limit, uint64_t there, int lane) {
+    const int h4 = lane / 32 * 4;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      const uint32_t bits = static_cast<uint32_t>(there >> (32 * b)) >> h4;
+      seen[b] = 0;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int key = 8 * (i / 4) + i % 4;
+        const bool sees = 32 * b + key + h4 < limit && (bits >> key & 1);
+        s[b][i] = sees ? s[b][i] : -INFINITY;
+        seen[b] |= sees ? 1u << i : 0u;
+      }
+    }
+  }
+};
+
+// Waits for this wave's LDS accesses; keeps memory accesses on their side of it.
+__device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+// ---------------------------------------------------------------- items
+template <typename T, int D>
+struct AttnLds {
+  typedef KvRows<T, D> Rows;
+  static constexpr int kTileKeys = sizeof(T) == 2 ? 64 : 32;   // of a workgroup whose waves take rows of their own
+  static constexpr int kTileBytes = kTileKeys * Rows::kPitch;
+  static constexpr int kOwnBytes = 32 * Rows::kPitch;          // tiles of a wave that takes keys of its own
+  static constexpr int kRows = 4 * kTileBytes;                 // K and V, two of each
+  static constexpr int kKeys = 2 * kAttnWaves * kOwnBytes;
+  static constexpr int kMerge = kAttnWaves * D * kAttnRows * 4 + kAttnWaves * kAttnRows * 8;
+  static constexpr int kBytes = kRows > kKeys ? (kRows > kMerge ? kRows : kMerge) : (kKeys > kMerge ? kKeys : kMerge);
+};
+
+struct AttnItem {
+  int kvh;
+  int row0;            // first row, counted over all packed rows
+  int rows;            // of the item, from row0 on
+  int len, tail;       // own tokens; row r of the item is token (row0 + r) / G, and sees own tokens below
+  int first_row;       // tail + 1 + (row0 + r - first_row) / G
+  KeyRange keys;
+  int64_t part;        // its first wave tile among the partial results
+};
+
+// Own tokens that row r of the item sees.
+__device__ __forceinline__ int own_limit(const AttnItem& it, int groups, int r) {
+  const int i = static_cast<int>(static_cast<uint32_t>(it.row0 - it.first_row + r) / static_cast<uint32_t>(groups));
+  return max(min(it.tail + 1 + i, it.len), 0);
+}
+
+// The token and query head of row r of the item.
+struct RowAt { int64_t token; int head; };
+__device__ __forceinline__ RowAt row_at(const AttnArgs& a, const AttnItem& it, int r) {
+  const uint32_t row = it.row0 + r, token = row / static_cast<uint32_t>(a.groups);
+  return {token, static_cast<int>(it.kvh * a.groups + (row - token * a.groups))};
+}
+
+template <typename T, int D>
+__device__ __forceinline__ void store_out(const AttnArgs& a, const AttnItem& it, const f32x16& o, int dt, float l, int r, int lane) {
+  if (r >= it.rows) return;
+  const RowAt at = row_at(a, it, r);
+  T* out = static_cast<T*>(a.out) + at.token * a.ldo + static_cast<int64_t>(at.head) * D + 32 * dt + 4 * (lane / 32);
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+#pragma unroll
+  for (int i4 = 0; i4 < 4; ++i4) {
+    float x[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = l == 0.0f ? 0.0f : o[4 * i4 + i] * inv;
+    if constexpr (sizeof(T) == 2) {
+      u32x2 w;
+      w[0] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{x[0], x[1]}), bf16x2));
+      w[1] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{x[2], x[3]}), bf16x2));
+      *reinterpret_cast<u32x2*>(out + 8 * i4) = w;
+    } else {
+      *reinterpret_cast<f32x4*>(out + 8 * i4) = f32x4{x[0], x[1], x[2], x[3]};
+    }
+  }
+}
+
+// Results of wave tile `wt` of the item (rows 32 wt ..): out, or partial results.
+template <typename T, int D>
+__device__ __forceinline__ void put_columns(const AttnArgs& a, const AttnItem& it, int wt, const f32x16& o, int dt, float m, float l,
+                                            int lane) {
+  const int r = kAttnRows * wt + lane % 32;
+  if (!a.part) {
+    store_out<T, D>(a, it, o, dt, l, r, lane);
+    return;
+  }
+  if (r >= it.rows) return;
+  f32x4* p = a.part + ((it.part + wt) * (D / 8) + 4 * dt) * kWave + lane;
+#pragma unroll
+  for (int i4 = 0; i4 < 4; ++i4) p[i4 * kWave] = f32x4{o[4 * i4], o[4 * i4 + 1], o[4 * i4 + 2], o[4 * i4 + 3]};
+  if (dt == 0 && lane < 32) a.part_ml[(it.part + wt) * kAttnRows + lane] = f32x2{m, l};
+}
+
+// Waves take rows of their own and share tiles of keys.
+template <typename T, int D>
+__device__ __forceinline__ void attend_rows(const AttnArgs& a, const AttnItem& it, const CacheAt& cache, char* lds) {
+  typedef AttnLds<T, D> L;
+  typedef typename L::Rows Rows;
+  constexpr int KT = L::kTileKeys, NB = KT / 32, N = KT / Rows::kRowsPerDma / kAttnWaves;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
+  const int w0 = kAttnRows * wave, r = min(w0 + lane % 32, it.rows - 1);
+  const RowAt at = row_at(a, it, r);
+  AttnWave<T, D> w;
+  w.load_q(static_cast<const T*>(a.q) + at.token * a.ldq + static_cast<int64_t>(at.head) * D, a.flip, lane / 32);
+  w.clear();
+  const bool idle = w0 >= it.rows;
+  const int mine = own_limit(it, a.groups, r);
+  const int least = __builtin_amdgcn_readfirstlane(own_limit(it, a.groups, min(w0, it.rows - 1))),
+            most = __builtin_amdgcn_readfirstlane(own_limit(it, a.groups, min(w0 + kAttnRows, it.rows) - 1));
+  lds_byte* dst = (lds_byte*)lds;
+  const int tiles = it.keys.tiles<KT>();
+  const auto present = [&](const KeyTile& t, const PageOf& p) {   // a bit for each key
+    return __ballot(lane < t.count && p.page >= 0 && p.page < a.num_pages);
   };
-  walk(a.prefix_pages, a.prefix_len);
-  walk(a.table + static_cast<int64_t>(n) * a.width, own);
-  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-  T* o = static_cast<T*>(a.out) + t * a.ldo + h * D + C * lane;
+  constexpr uint64_t kAll = KT == 64 ? ~0ull : (1ull << (KT % 64)) - 1;
+  KeyTile cur{}, next{};
+  uint64_t there = 0, there_next = 0;
+  PageOf pages{};
+  if (tiles > 0) {
+    next = key_tile<KT>(it.keys, 0);
+    pages = find_pages<KT>(a, next);
+    there_next = present(next, pages);
+    load_rows<T, D, N, true, true>(a, cache, pages, there_next, there_next == kAll, dst, dst + L::kTileBytes, N * wave, lane);
+    if (tiles > 1) pages = find_pages<KT>(a, key_tile<KT>(it.keys, 1));
+  }
+  for (int j = 0; j < tiles; ++j) {
+    cur = next;
+    there = there_next;
+    wait_dma();
+    lds_barrier();
+    const char* kl = lds + (j & 1) * 2 * L::kTileBytes;
+    char* vl = lds + (j & 1) * 2 * L::kTileBytes + L::kTileBytes;
+    if (there != kAll) {   // values of keys that are none count as zeros
+      for (int p = threadIdx.x; p < KT * Rows::kPieces; p += kAttnThreads)
+        if (!(there >> (p / Rows::kPieces) & 1)) *reinterpret_cast<u32x4*>(vl + 16 * p) = u32x4{0, 0, 0, 0};
+      lds_barrier();
+    }
+    if (j + 1 < tiles) {
+      next = key_tile<KT>(it.keys, j + 1);
+      there_next = present(next, pages);
+      lds_byte* to = dst + ((j + 1) & 1) * 2 * L::kTileBytes;
+      load_rows<T, D, N, true, true>(a, cache, pages, there_next, there_next == kAll, to, to + L::kTileBytes, N * wave, lane);
+      if (j + 2 < tiles) pages = find_pages<KT>(a, key_tile<KT>(it.keys, j + 2));
+    }
+    if (idle || (cur.own && most <= cur.base)) continue;
+    f32x16 s[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) s[b] = w.scores(kl, 32 * b, lane);
+    const bool whole = there == kAll && (!cur.own || least >= cur.base + KT);
+    if (whole) {
+      w.weigh(s, a.scale2);
+#pragma unroll
+      for (int b = 0; b < NB; ++b) w.template values<false>(vl, 32 * b, s[b], lane, 0);
+    } else {
+      uint32_t seen[NB];
+      w.masked_scores(s, seen, cur.own ? mine - cur.base : KT, there, lane);
+      w.weigh(s, a.scale2);
+#pragma unroll
+      for (int b = 0; b < NB; ++b) w.template values<true>(vl, 32 * b, s[b], lane, seen[b]);
+    }
+  }
+  if (idle) return;
+  w.l = half_sum(w.l);
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt) put_columns<T, D>(a, it, wave, w.o[dt], dt, w.m, w.l, lane);
+}
+
+// At most 32 rows: waves take keys of their own, and their results are joined.
+template <typename T, int D>
+__device__ __forceinline__ void attend_keys(const AttnArgs& a, const AttnItem& it, const CacheAt& cache, char* lds) {
+  typedef AttnLds<T, D> L;
+  typedef typename L::Rows Rows;
+  constexpr int KT = 32, N = KT / Rows::kRowsPerDma;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
+  const int r = min(lane % 32, it.rows - 1);
+  const RowAt at = row_at(a, it, r);
+  AttnWave<T, D> w;
+  w.load_q(static_cast<const T*>(a.q) + at.token * a.ldq + static_cast<int64_t>(at.head) * D, a.flip, lane / 32);
+  w.clear();
+  const int mine = own_limit(it, a.groups, r), least = __builtin_amdgcn_readfirstlane(own_limit(it, a.groups, 0));
+  const char* kl = lds + wave * 2 * L::kOwnBytes;
+  char* vl = lds + wave * 2 * L::kOwnBytes + L::kOwnBytes;
+  lds_byte* kd = (lds_byte*)lds + wave * 2 * L::kOwnBytes;
+  lds_byte* vd = kd + L::kOwnBytes;
+  const int tiles = it.keys.tiles<KT>();
+  const auto present = [&](const KeyTile& t, const PageOf& p) {
+    return __ballot(lane < t.count && p.page >= 0 && p.page < a.num_pages);
+  };
+  constexpr uint64_t kAll = 0xFFFFFFFFull;
+  // K of the next tile is on its way while the weights are made, its V while the next
+  // scores are; pages are looked up a tile further ahead, between the two
+  KeyTile cur{}, next{};
+  uint64_t there = 0, there_next = 0;
+  PageOf pages{}, ahead{};
+  if (wave < tiles) {
+    cur = key_tile<KT>(it.keys, wave);
+    pages = find_pages<KT>(a, cur);
+    there = present(cur, pages);
+    load_rows<T, D, N, true, false>(a, cache, pages, there, there == kAll, kd, vd, 0, lane);
+    if (wave + kAttnWaves < tiles) {
+      next = key_tile<KT>(it.keys, wave + kAttnWaves);
+      ahead = find_pages<KT>(a, next);
+    }
+    load_rows<T, D, N, false, true>(a, cache, pages, there, there == kAll, kd, vd, 0, lane);
+  }
+  for (int j = wave; j < tiles; j += kAttnWaves) {
+    const bool more = j + kAttnWaves < tiles;
+    wait_dma_but<N>();   // this tile's K and the next one's pages are here, V may be on its way
+    f32x16 s[1] = {w.scores(kl, 0, lane)};
+    wait_lds();
+    KeyTile after{};
+    if (more) {
+      pages = ahead;
+      there_next = present(next, pages);
+      load_rows<T, D, N, true, false>(a, cache, pages, there_next, there_next == kAll, kd, vd, 0, lane);
+      if (j + 2 * kAttnWaves < tiles) {
+        after = key_tile<KT>(it.keys, j + 2 * kAttnWaves);
+        ahead = find_pages<KT>(a, after);
+      }
+    }
+    const bool whole = there == kAll && (!cur.own || least >= cur.base + KT);
+    uint32_t seen[1] = {0};
+    if (!whole) w.masked_scores(s, seen, cur.own ? mine - cur.base : KT, there, lane);
+    w.weigh(s, a.scale2);
+    if (more) wait_dma_but<N>();   // (the last of N + 1 where pages were looked up)
+    else wait_dma();
+    if (there != kAll) {
+      for (int p = lane; p < KT * Rows::kPieces; p += kWave)
+        if (!(there >> (p / Rows::kPieces) & 1)) *reinterpret_cast<u32x4*>(vl + 16 * p) = u32x4{0, 0, 0, 0};
+      wait_lds();
+    }
+    if (whole) w.template values<false>(vl, 0, s[0], lane, 0);
+    else w.template values<true>(vl, 0, s[0], lane, seen[0]);
+    wait_lds();
+    if (more) load_rows<T, D, N, false, true>(a, cache, pages, there_next, there_next == kAll, kd, vd, 0, lane);
+    cur = next;
+    next = after;
+    there = there_next;
+  }
+  // the waves' results into one: every wave's maximum, then the scaled sums of 32 columns a wave
+  w.l = half_sum(w.l);
+  f32x4* os = reinterpret_cast<f32x4*>(lds);   // [wave][D / 8][lane]
+  f32x2* mls = reinterpret_cast<f32x2*>(lds + kAttnWaves * D * kAttnRows * 4);
+  lds_barrier();
+  if (lane < 32) mls[wave * kAttnRows + lane] = f32x2{w.m, w.l};
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+    for (int i4 = 0; i4 < 4; ++i4)
+      os[(wave * (D / 8) + 4 * dt + i4) * kWave + lane] =
+          f32x4{w.o[dt][4 * i4], w.o[dt][4 * i4 + 1], w.o[dt][4 * i4 + 2], w.o[dt][4 * i4 + 3]};
+  lds_barrier();
+  if (wave >= D / 32) return;
+  float m = -INFINITY, l = 0.0f, f[kAttnWaves];
+#pragma unroll
+  for (int x = 0; x < kAttnWaves; ++x) m = fmaxf(m, mls[x * kAttnRows + lane % 32][0]);
+  const float base = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+  for (int x = 0; x < kAttnWaves; ++x) {
+    const f32x2 ml = mls[x * kAttnRows + lane % 32];
+    f[x] = __builtin_amdgcn_exp2f(ml[0] - base);
+    l = fmaf(f[x], ml[1], l);
+  }
+  f32x16 o;
+#pragma unroll
+  for (int i4 = 0; i4 < 4; ++i4) {
+    f32x4 sum = zero4();
+#pragma unroll
+    for (int x = 0; x < kAttnWaves; ++x) {
+      const f32x4 p = os[(x * (D / 8) + 4 * wave + i4) * kWave + lane];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sum[i] = fmaf(f[x], p[i], sum[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[4 * i4 + i] = sum[i];
+  }
+  put_columns<T, D>(a, it, 0, o, wave, m, l, lane);
+}
+
+// Largest n in [0, N) with cu[n] G / tile + n <= slot (see slot_seq).
+__device__ __forceinline__ int row_slot_seq(const int32_t* __restrict__ cu, int n_seqs, int slot, int groups, int tile) {
+  const int lane = threadIdx.x % kWave;
+  int lo = 0, hi = n_seqs;
+  while (hi - lo > 1) {
+    const int step = (hi - lo + kWave - 1) / kWave;
+    const int at = lo + lane * step;
+    const bool below = at < hi && static_cast<int64_t>(cu[at]) * groups / tile + at <= slot;
+    const int found = __popcll(__ballot(below));
+    lo += (found - 1) * step;
+    hi = min(hi, lo + step);
+  }
+  return __builtin_amdgcn_readfirstlane(lo);
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(kAttnThreads, sizeof(T) == 2 ? 2 : 1)
+void k_attn(AttnArgs a) {
+  __shared__ __attribute__((aligned(1024))) char lds[AttnLds<T, D>::kBytes];
+  AttnItem it;
+  int b = blockIdx.x;
+  if (b < a.shared_items) {
+    // [split][row tile][K/V head]
+    it.kvh = b % a.kv_heads;
+    const int u = b / a.kv_heads, tile = u % a.shared_tiles, split = u / a.shared_tiles;
+    it.row0 = tile * kAttnTile;
+    it.rows = min(kAttnTile, a.rows - it.row0);
+    it.len = it.tail = 0;
+    it.first_row = it.row0;
+    const int first = split * a.shared_chunk;
+    it.keys = {a.prefix_pages, nullptr, first, min(a.shared_chunk, a.prefix_len - first), 0, 0};
+    it.part = ((static_cast<int64_t>(split) * a.shared_tiles + tile) * a.kv_heads + it.kvh) * kAttnWaves;
+  } else {
+    b -= a.shared_items;
+    // [slot, the last first][split][K/V head]
+    it.kvh = b % a.kv_heads;
+    const int u = b / a.kv_heads, split = u % a.own_splits, slot = a.own_slots - 1 - u / a.own_splits;
+    const int n = row_slot_seq(a.cu, a.n_seqs, slot, a.groups, a.own_tile);
+    const int start = a.cu[n], count = a.cu[n + 1] - start;
+    it.first_row = start * a.groups;
+    const int from = (slot - (it.first_row / a.own_tile + n)) * a.own_tile;
+    const int left = count * a.groups - from;
+    if (left <= 0) return;
+    it.row0 = it.first_row + from;
+    it.rows = min(a.own_tile, left);
+    it.len = min(max(a.lens[n], 0), a.max_len);
+    it.tail = it.len - count;
+    const int end = own_limit(it, a.groups, it.rows - 1);
+    const int64_t first = static_cast<int64_t>(split) * a.own_chunk;
+    const int64_t own = min(static_cast<int64_t>(a.own_chunk), end - first);
+    const bool both = a.shared_items == 0;
+    it.keys = {a.prefix_pages, a.table + static_cast<int64_t>(n) * a.width, 0, both ? a.prefix_len : 0, static_cast<int>(first),
+               static_cast<int>(max(own, static_cast<int64_t>(0)))};
+    it.part = static_cast<int64_t>(a.shared_items) * kAttnWaves +
+              ((static_cast<int64_t>(slot) * a.own_splits + split) * a.kv_heads + it.kvh) * (a.own_tile / kAttnRows);
+  }
+  const CacheAt cache = {static_cast<const char*>(a.k) + it.kvh * a.kh, static_cast<const char*>(a.v) + it.kvh * a.vh};
+  if (it.rows <= kAttnRows) attend_keys<T, D>(a, it, cache, lds);
+  else attend_rows<T, D>(a, it, cache, lds);
+}
+
+// The items' partial results of a row into one.  A workgroup takes 32 packed rows
+// of a K/V head, a wave D / 32 of the D / 8 groups of columns: lane (h, r) four
+// columns of row r.
+template <typename T, int D>
+__global__ __launch_bounds__(kAttnThreads)
+void k_attn_join(AttnArgs a) {
+  constexpr int C = D / 8 / kAttnWaves;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
+  const int kvh = blockIdx.x % a.kv_heads;
+  const int wt = blockIdx.x / a.kv_heads;
+  const bool there = wt * kAttnRows + lane % 32 < a.rows;
+  const int row = there ? wt * kAttnRows + lane % 32 : a.rows - 1;
+  const int token = static_cast<int>(static_cast<uint32_t>(row) / static_cast<uint32_t>(a.groups));
+  int lo = 0, hi = a.n_seqs - 1;   // the sequence of the token: the first whose end lies behind it
+  while (lo < hi) {
+    const int mid = (lo + hi) / 2;
+    if (a.cu[mid + 1] > token) hi = mid;
+    else lo = mid + 1;
+  }
+  const int first = a.cu[lo] * a.groups, rs = row - first;
+  const int slot = first / a.own_tile + lo + rs / a.own_tile;
+  // wave tiles of the shared items are this workgroup's rows, those of the own ones are found by sequence
+  const auto tile_of = [&](int s) {
+    if (s < a.shared_splits)
+      return ((static_cast<int64_t>(s) * a.shared_tiles + wt / kAttnWaves) * a.kv_heads + kvh) * kAttnWaves + wt % kAttnWaves;
+    return static_cast<int64_t>(a.shared_items) * kAttnWaves +
+           ((static_cast<int64_t>(slot) * a.own_splits + (s - a.shared_splits)) * a.kv_heads + kvh) * (a.own_tile / kAttnRows) +
+           rs % a.own_tile / kAttnRows;
+  };
+  const auto lane_of = [&](int s) { return s < a.shared_splits ? lane % 32 : rs % kAttnRows; };
+  const int parts = a.shared_splits + a.own_splits;
+  float m = -INFINITY;
+  for (int s = 0; s < parts; ++s) m = fmaxf(m, a.part_ml[tile_of(s) * kAttnRows + lane_of(s)][0]);
+  const float at = m == -INFINITY ? 0.0f : m;
+  float l = 0.0f;
+  f32x4 sum[C];
+#pragma unroll
+  for (int c = 0; c < C; ++c) sum[c] = zero4();
+  for (int s = 0; s < parts; ++s) {
+    const int64_t t = tile_of(s);
+    const int r = lane_of(s);
+    const f32x2 ml = a.part_ml[t * kAttnRows + r];
+    if (ml[1] == 0.0f) continue;   // nothing seen there (nor anything written)
+    const float f = __builtin_amdgcn_exp2f(ml[0] - at);
+    l = fmaf(f, ml[1], l);
+    const f32x4* p = a.part + (t * (D / 8) + C * wave) * kWave + lane / 32 * 32 + r;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const f32x4 x = p[c * kWave];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sum[c][i] = fmaf(f, x[i], sum[c][i]);
+    }
+  }
+  if (!there) return;
+  const int head = kvh * a.groups + (row - token * a.groups);
+  T* out = static_cast<T*>(a.out) + token * a.ldo + static_cast<int64_t>(head) * D + 8 * C * wave + 4 * (lane / 32);
+  const float inv = 1.0f / l;
+#pragma unroll
   for (int c = 0; c < C; ++c) {
-    const float x[1] = {acc[c] * inv};
-    store_run<T, 1>(o + c, x);
+    float x[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = l == 0.0f ? 0.0f : sum[c][i] * inv;
+    if constexpr (sizeof(T) == 2) {
+      u32x2 w;
+      w[0] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{x[0], x[1]}), bf16x2));
+      w[1] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{x[2], x[3]}), bf16x2));
+      *reinterpret_cast<u32x2*>(out + 8 * c) = w;
+    } else {
+      *reinterpret_cast<f32x4*>(out + 8 * c) = f32x4{x[0], x[1], x[2], x[3]};
+    }
   }
 }
 

@@ -13,6 +13,10 @@ namespace {
 constexpr int64_t kMaxInt = std::numeric_limits<int32_t>::max();
 constexpr int64_t kMaxStride = int64_t{1} << 23;
 
+// Workgroups of the attention that the chip holds at once, and the fewest keys of
+// a piece of a split range.
+constexpr int64_t kAttnPlaces = 512, kLeastChunk = 256;
+
 gdn_status bad(std::string* err, const std::string& what, gdn_status st = GDN_ERR_BAD_SHAPE) {
   *err = what;
   return st;
@@ -31,7 +35,7 @@ gdn_status check_ld(const char* name, int64_t ld, int64_t least, int64_t vec, st
   return GDN_OK;
 }
 
-// Strides of a cache: its rows of `dim` elements are apart, their offsets fit 61 bits.
+// Strides of a cache: its rows of `dim` elements are apart; in 16 bytes they fit 31 bits.
 gdn_status check_cache(const char* name, int32_t pages, int32_t page_size, int32_t heads, int32_t dim, int64_t page,
                        int64_t token, int64_t head, int64_t vec, std::string* err) {
   if (pages < 1 || page_size < 1) return bad(err, "num_pages and page_size must be >= 1");
@@ -39,8 +43,8 @@ gdn_status check_cache(const char* name, int32_t pages, int32_t page_size, int32
     return bad(err, "a cache must hold at most 2^31 - 1 tokens", GDN_ERR_UNSUPPORTED);
   struct { int64_t stride, count; } d[3] = {{page, pages}, {token, page_size}, {head, heads}};
   for (const auto& x : d) {
-    if (x.stride < 0 || x.stride > (int64_t{1} << 60) / x.count)
-      return bad(err, std::string("strides of ") + name + " must not be negative or enormous");
+    if (x.stride < 0) return bad(err, std::string("strides of ") + name + " must not be negative");
+    if (x.stride / vec >= int64_t{1} << 31) return bad(err, std::string("strides of ") + name + " must be below 2^31 x 16 bytes", GDN_ERR_UNSUPPORTED);
     if (x.stride % vec != 0)
       return bad(err, std::string("strides of ") + name + " must be multiples of 16 bytes", GDN_ERR_UNSUPPORTED);
   }
@@ -161,7 +165,37 @@ gdn_status make_attn_plan(const gdn_attn_shape* s, const int32_t* cu, AttnPlan* 
   if (st == GDN_OK) st = check_seqlens(s->num_seqs, cu, &p.tokens, &p.longest, err);
   if (st != GDN_OK) return st;
   p.max_len = s->max_len ? s->max_len : s->table_width * s->page_size;
+  p.groups = s->num_heads / s->num_kv_heads;
   if (p.tokens * s->num_heads > kMaxInt) return bad(err, "too many tokens for one call", GDN_ERR_UNSUPPORTED);
+  const int64_t G = p.groups, H = s->num_kv_heads, N = s->num_seqs, P = s->prefix_len;
+  p.rows = p.tokens * G;
+  p.own_tile = p.longest * G <= kPlanRows ? kPlanRows : kPlanTile;
+  int64_t tiles = 0;
+  for (int64_t n = 0; n < N; ++n) tiles += ((static_cast<int64_t>(cu[n + 1]) - cu[n]) * G + p.own_tile - 1) / p.own_tile;
+  p.own_slots = tile_slots(p.rows, N, p.own_tile);
+  const auto pieces = [](int64_t keys, int64_t items, int32_t* splits, int32_t* chunk) {
+    const int64_t most = std::max<int64_t>(1, (keys + kLeastChunk - 1) / kLeastChunk);
+    int64_t n = std::min(most, std::max<int64_t>(1, kAttnPlaces / std::max<int64_t>(1, items)));
+    const int64_t each = std::max<int64_t>(64, ((keys + n - 1) / n + 63) / 64 * 64);
+    *chunk = static_cast<int32_t>(each);
+    *splits = static_cast<int32_t>(std::max<int64_t>(1, (keys + each - 1) / each));
+  };
+  if (P > 0 && (tiles * H < kAttnPlaces || p.rows < tiles * p.own_tile * 3 / 5)) {
+    p.shared_tiles = (p.rows + kPlanTile - 1) / kPlanTile;
+    pieces(P, p.shared_tiles * H, &p.shared_splits, &p.shared_chunk);
+    p.shared_items = p.shared_tiles * H * p.shared_splits;
+  }
+  if (P == 0 || p.shared_items > 0) pieces(p.max_len, tiles * H, &p.own_splits, &p.own_chunk);
+  else p.own_chunk = (p.max_len + 63) / 64 * 64;
+  p.own_items = p.own_slots * H * p.own_splits;
+  p.joined = p.shared_items > 0 || p.own_splits > 1;
+  if (p.shared_items + p.own_items > kMaxInt / 256) return bad(err, "too many tokens for one call", GDN_ERR_UNSUPPORTED);
+  if (p.joined) {
+    const size_t waves = static_cast<size_t>(p.shared_items) * (kPlanTile / kPlanRows) +
+                         static_cast<size_t>(p.own_items) * (p.own_tile / kPlanRows);
+    p.off_ml = waves * kPlanRows * s->head_dim * sizeof(float);
+    p.bytes = (p.off_ml + waves * kPlanRows * 2 * sizeof(float) + kAlign - 1) / kAlign * kAlign;
+  }
   *plan = p;
   return GDN_OK;
 }

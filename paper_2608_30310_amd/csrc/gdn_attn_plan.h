@@ -26,9 +26,25 @@ gdn_status check_qk(const gdn_qk_shape* s, bool k_out, bool k_cache, bool v, std
 
 gdn_status check_attn(const gdn_attn_shape* s, std::string* err);
 
+// Rows (one query head of one token, the heads of a K/V head next to each other)
+// of a wave, and of a workgroup whose waves take rows of their own.
+constexpr int32_t kPlanRows = 32, kPlanTile = 128;
+
+// How gdn_prefix_attention runs.  Shared items: tiles of all packed rows against
+// `shared_splits` pieces of the prefix.  Own items: tiles of a sequence's rows
+// against `own_splits` pieces of its own tokens, and against the whole prefix
+// before them where there are no shared items.
 struct AttnPlan {
   int64_t tokens = 0, longest = 0;
-  int32_t max_len = 0;   // own tokens of a sequence at most
+  int32_t groups = 1;        // query heads of a K/V head
+  int32_t max_len = 0;       // own tokens of a sequence at most
+  int64_t rows = 0;          // tokens * groups
+  int32_t shared_splits = 0, shared_chunk = 0;
+  int64_t shared_tiles = 0, shared_items = 0;
+  int32_t own_tile = kPlanTile, own_splits = 1, own_chunk = 0;
+  int64_t own_slots = 0, own_items = 0;
+  bool joined = false;       // items leave partial results, which a second kernel joins
+  size_t off_ml = 0;         // workspace: partial outputs, then maxima and sums
   size_t bytes = 0;
 };
 gdn_status make_attn_plan(const gdn_attn_shape* s, const int32_t* cu, AttnPlan* p, std::string* err);

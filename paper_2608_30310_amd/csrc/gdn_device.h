@@ -49,6 +49,23 @@ __device__ __forceinline__ int xcd_cluster_remap(int b, int total, int cs) {
 // across it.
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
+// ---------------------------------------------------------------- global -> LDS
+typedef __attribute__((address_space(3))) void* lds_ptr_t;
+typedef __attribute__((address_space(3))) unsigned char lds_byte;   // LDS bytes
+
+// 16 bytes per lane from `src` (per lane) to LDS `dst + 16 * lane` (dst uniform).
+__device__ __forceinline__ void dma16(const void* src, lds_byte* dst) {
+  __builtin_amdgcn_global_load_lds(src, (lds_ptr_t)dst, 16, 0, 0);
+}
+
+__device__ __forceinline__ void wait_dma() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+// The same, but for the N youngest.
+template <int N>
+__device__ __forceinline__ void wait_dma_but() {
+  static_assert(N < 64, "vmcnt holds six bits");
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+
 // ---------------------------------------------------------------- bf16
 __device__ __forceinline__ uint16_t f2bf(float x) {
   // round to nearest, ties to even (finite values)

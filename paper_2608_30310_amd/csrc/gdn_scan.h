@@ -41,23 +41,7 @@ namespace gdn {
 
 constexpr int kLdsBytes = 160 * 1024;
 
-typedef __attribute__((address_space(3))) void* lds_ptr_t;
-typedef __attribute__((address_space(3))) unsigned char lds_byte;   // LDS bytes
-
-// 16 bytes per lane from `src` (per lane) to LDS `dst + 16 * lane` (dst uniform).
-__device__ __forceinline__ void dma16(const void* src, lds_byte* dst) {
-  __builtin_amdgcn_global_load_lds(src, (lds_ptr_t)dst, 16, 0, 0);
-}
-
-__device__ __forceinline__ void wait_dma() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
-// The same, but for the N youngest.
-template <int N>
-__device__ __forceinline__ void wait_dma_but() {
-  static_assert(N < 64, "vmcnt holds six bits");
-  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
-}
-
-// The same from `base + off`: a uniform base and a 32-bit lane offset, so the
+// dma16 from `base + off`: a uniform base and a 32-bit lane offset, so the
 // load takes the scalar-base form and its address costs no 64-bit lane
 // arithmetic.  Offsets stay below 2^32: a chunk spans 64 rows of at most
 // 65535 heads x 128 x 4 bytes.
