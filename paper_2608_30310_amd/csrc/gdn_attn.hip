@@ -18,6 +18,9 @@ gdn_status afail(gdn_status st, const std::string& msg) {
   return st;
 }
 
+// Whether a few rows that are `units` of 16 bytes apart have 32-bit offsets.
+bool a_stride_fits(int64_t units) { return units < int64_t{1} << 24; }
+
 template <typename T, int D>
 gdn_status launch_attn(const AttnArgs& a, const AttnPlan& p, hipStream_t stream) {
   static_assert(kAttnRows == kPlanRows && kAttnTile == kPlanTile, "the plan's tiles");
@@ -93,6 +96,9 @@ gdn_status gdn_prefix_attention(const gdn_attn_shape* shape, const int32_t* cu_s
   a.page_mul = mul, a.page_shift = l ? l - 1 : 0;
   // (not below the least normal number: a masked score of -inf stays one)
   a.scale2 = std::max(std::fabs(s.scale) * 1.44269504088896f, std::numeric_limits<float>::min());
+  // rows of a DMA: 1 KiB of rows
+  const int64_t rows = 1024 / (s.head_dim * e);
+  a.dma_in_page = s.page_size % rows == 0 && a_stride_fits(s.k_token / vec) && a_stride_fits(s.v_token / vec);
   a.flip = std::signbit(s.scale) ? 0x80000000u : 0u;
   a.shared_splits = p.shared_splits, a.shared_chunk = p.shared_chunk;
   a.shared_tiles = static_cast<int32_t>(p.shared_tiles), a.shared_items = static_cast<int32_t>(p.shared_items);

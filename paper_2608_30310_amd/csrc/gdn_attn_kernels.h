@@ -35,6 +35,7 @@ struct AttnArgs {
   int32_t page_shift;
   float scale2;           // |scale| log2 e
   uint32_t flip;          // sign bits of the queries where scale is negative
+  int32_t dma_in_page;    // the rows of a DMA never lie in two pages, and their offsets fit 32 bits
   // items: shared ones over the prefix alone, all rows packed (shared_splits 0: none), then own ones
   int32_t shared_splits, shared_chunk, shared_tiles, shared_items;
   int32_t own_tile, own_splits, own_chunk, own_slots;
@@ -115,29 +116,40 @@ struct KvRows {
     return D == 128 ? (r & 3) << 2 | (r >> 2 & 3) : (r >> 1 & 1) << 2 | (r >> 2 & 3);
   }
   static __device__ __forceinline__ int at(int r, int piece) { return r * kPitch + ((piece ^ swz(r)) << 4); }
-  // elements 8 e8 .. + 7 of row r
-  static __device__ __forceinline__ typename Mm<T>::R row_frag(const char* base, int r, int e8) {
+  // Operand of 32 rows, elements 16 u + 8 h ..: `at` is at(r, h) for lane (h, r) (fp32:
+  // of 4-byte elements, at(r, 2 h)), turned by kFragStep u; r multiples of 16 above, the
+  // swizzle is the same.
+  static constexpr int kFragStep = 2 * 16 * static_cast<int>(sizeof(T)) / 2;
+  static __device__ __forceinline__ int frag_start(int lane) { return at(lane % 32, lane / 32 * static_cast<int>(sizeof(T)) / 2); }
+  static __device__ __forceinline__ typename Mm<T>::R frag_at(const char* base, int at) {
     if constexpr (sizeof(T) == 2) {
-      return __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(base + at(r, e8)));
+      return __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(base + at));
     } else {
-      const f32x4 a = *reinterpret_cast<const f32x4*>(base + at(r, 2 * e8));
-      const f32x4 b = *reinterpret_cast<const f32x4*>(base + at(r, 2 * e8 + 1));
+      const f32x4 a = *reinterpret_cast<const f32x4*>(base + at);
+      const f32x4 b = *reinterpret_cast<const f32x4*>(base + (at ^ 16));
       return f32x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
     }
   }
-  // column 32 dt + lane % 32 of rows r0 + 8 (j / 4) + 4 h + j % 4, j = 0..7 (r0 a multiple of 16)
-  static __device__ __forceinline__ typename Mm<T>::R col_frag(const char* base, int r0, int dt, int lane) {
+  // Operand of 16 rows, transposed: column 32 dt + lane % 32 of rows 8 (j / 4) + 4 h + j % 4,
+  // j = 0..7.  col_start: where a lane's first read begins for dt = 0.
+  static __device__ __forceinline__ int col_start(int lane) {
     const int h = lane / 32;
+    if constexpr (sizeof(T) == 2) return at(4 * h + lane % 16 / 4, lane / 16 % 2 * 2 + lane % 4 / 2) + lane % 2 * 8;
+    else return at(4 * h, lane % 32 / 4) + lane % 4 * 4;
+  }
+  static __device__ __forceinline__ typename Mm<T>::R col_frag(const char* base, int at, int dt) {
     if constexpr (sizeof(T) == 2) {
-      const int row = 4 * h + lane % 16 / 4, piece = 4 * dt + lane / 16 % 2 * 2 + lane % 4 / 2, half = lane % 2 * 8;
-      base += r0 * kPitch;
-      const u32x2 a = lds_read_tr16(base + at(row, piece) + half);
-      const u32x2 b = lds_read_tr16(base + at(row + 8, piece) + half);
+      // four pieces on is the bits 4 dt of the piece; eight rows on turn it by swz(8)
+      const u32x2 a = lds_read_tr16(base + (at ^ 64 * dt));
+      const u32x2 b = lds_read_tr16(base + (at ^ 64 * dt ^ 16 * swz(8)) + 8 * kPitch);
       return join_halves(a, b);
     } else {
       f32x8 x;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] = elt(base, r0 + 8 * (j / 4) + 4 * h + j % 4, 32 * dt + lane % 32);
+      for (int j = 0; j < 8; ++j) {
+        const int row = 8 * (j / 4) + j % 4;   // bits apart from those of 4 h
+        x[j] = *reinterpret_cast<const float*>(base + (at ^ 128 * dt ^ 16 * swz(row)) + row * kPitch);
+      }
       return x;
     }
   }
@@ -150,26 +162,19 @@ struct KvRows {
 };
 
 __device__ __forceinline__ bool not_finite(float x) { return (__float_as_uint(x) & 0x7F800000u) == 0x7F800000u; }
-// An operand with its infinities and NaNs replaced by zero; *found: there were some.
-__device__ __forceinline__ bf16x8 finite_only(const bf16x8& a, bool* found) {
-  u32x4 w = __builtin_bit_cast(u32x4, a);
+// A piece of a row with its infinities and NaNs replaced by zero.
+template <typename T>
+__device__ __forceinline__ u32x4 finite_only(u32x4 w) {
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    const bool lo = (w[j] & 0x7F80u) == 0x7F80u, hi = (w[j] & 0x7F800000u) == 0x7F800000u;
-    *found |= lo || hi;
-    w[j] &= (lo ? 0u : 0xFFFFu) | (hi ? 0u : 0xFFFF0000u);
+    if constexpr (sizeof(T) == 2) {
+      const bool lo = (w[j] & 0x7F80u) == 0x7F80u, hi = (w[j] & 0x7F800000u) == 0x7F800000u;
+      w[j] &= (lo ? 0u : 0xFFFFu) | (hi ? 0u : 0xFFFF0000u);
+    } else {
+      w[j] = not_finite(__uint_as_float(w[j])) ? 0u : w[j];
+    }
   }
-  return __builtin_bit_cast(bf16x8, w);
-}
-__device__ __forceinline__ f32x8 finite_only(const f32x8& a, bool* found) {
-  f32x8 r;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const bool bad = not_finite(a[j]);
-    *found |= bad;
-    r[j] = bad ? 0.0f : a[j];
-  }
-  return r;
+  return w;
 }
 
 // The larger of a lane's value and its counterpart's in the other half wave, and their sum.
@@ -214,39 +219,81 @@ __device__ __forceinline__ PageOf find_pages(const AttnArgs& a, const KeyTile& t
   return {t.list[c], key - c * a.page_size};
 }
 
-// Where a K/V head's rows are in the caches.
-struct CacheAt { const char* k; const char* v; };
+// Where a K/V head's rows are in the caches, and a lane's place in a DMA of
+// kRowsPerDma rows: the swizzle is linear over XOR, so piece p of row r + j (r a
+// multiple of kRowsPerDma) comes from piece (p ^ swz(j)) ^ swz(r).
+template <typename T, int D>
+struct CacheAt {
+  const char* k;
+  const char* v;
+  uint32_t krow, vrow, piece;
+  __device__ __forceinline__ CacheAt(const AttnArgs& a, int kvh) {
+    typedef KvRows<T, D> Rows;
+    const int lane = threadIdx.x % kWave, j = lane / Rows::kPieces;
+    k = static_cast<const char*>(a.k) + kvh * a.kh;
+    v = static_cast<const char*>(a.v) + kvh * a.vh;
+    krow = 16 * j * a.kt;
+    vrow = 16 * j * a.vt;
+    piece = 16 * (lane % Rows::kPieces ^ Rows::swz(j));
+  }
+};
 
 // DMA of rows [i0, i0 + N) kRowsPerDma of a tile into LDS (both of K and V, or one of them).
 template <typename T, int D, int N, bool K, bool V>
-__device__ __forceinline__ void load_rows(const AttnArgs& a, const CacheAt& c, const PageOf& at, uint64_t there, bool whole,
-                                          lds_byte* kl, lds_byte* vl, int i0, int lane) {
+__device__ __forceinline__ void load_rows(const AttnArgs& a, const CacheAt<T, D>& c, const PageOf& at, uint64_t there, bool whole,
+                                          lds_byte* kl, lds_byte* vl, int i0) {
   typedef KvRows<T, D> Rows;
   constexpr int RPD = Rows::kRowsPerDma;
-  const int j = lane / Rows::kPieces;
-  if (whole && a.page_size % RPD == 0) {
-    // the rows of a DMA lie in one page
+  if (whole && a.dma_in_page) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int r = (i0 + i) * RPD;
       const uint64_t page = static_cast<uint32_t>(__builtin_amdgcn_readlane(at.page, r)),
                      row = static_cast<uint32_t>(__builtin_amdgcn_readlane(at.row, r));
-      const uint32_t piece = lane % Rows::kPieces ^ Rows::swz(r + j);
-      if (K) dma16(c.k + 16 * (page * a.kp + row * a.kt) + 16 * static_cast<uint64_t>(j * a.kt + piece), kl + (i0 + i) * 1024);
-      if (V) dma16(c.v + 16 * (page * a.vp + row * a.vt) + 16 * static_cast<uint64_t>(j * a.vt + piece), vl + (i0 + i) * 1024);
+      const uint32_t turn = 16 * Rows::swz(r);
+      if (K) dma16(c.k + 16 * (page * a.kp + row * a.kt) + (c.krow + (c.piece ^ turn)), kl + (i0 + i) * 1024);
+      if (V) dma16(c.v + 16 * (page * a.vp + row * a.vt) + (c.vrow + (c.piece ^ turn)), vl + (i0 + i) * 1024);
     }
   } else {
-    // rows that are none are taken from the cache's first
-#pragma unroll
+    // row by row; rows that are none are taken from the cache's first
+    const int lane = threadIdx.x % kWave, j = lane / Rows::kPieces;
+#pragma unroll 1
     for (int i = 0; i < N; ++i) {
       const int r = (i0 + i) * RPD + j;
       const bool ok = there >> r & 1;
       const int pg = __shfl(at.page, r, kWave), rw = __shfl(at.row, r, kWave);
       const uint64_t page = static_cast<uint32_t>(ok ? pg : 0), row = static_cast<uint32_t>(ok ? rw : 0);
-      const uint32_t piece = lane % Rows::kPieces ^ Rows::swz(r);
-      if (K) dma16(c.k + 16 * (page * a.kp + row * a.kt + piece), kl + (i0 + i) * 1024);
-      if (V) dma16(c.v + 16 * (page * a.vp + row * a.vt + piece), vl + (i0 + i) * 1024);
+      const uint32_t piece = 16 * (lane % Rows::kPieces ^ Rows::swz(r));
+      if (K) dma16(c.k + 16 * (page * a.kp + row * a.kt) + piece, kl + (i0 + i) * 1024);
+      if (V) dma16(c.v + 16 * (page * a.vp + row * a.vt) + piece, vl + (i0 + i) * 1024);
     }
+  }
+}
+
+// Values of rows that are not there count as zeros.  Returns whether a row that is
+// holds an infinity or a NaN in this thread's part (of `threads` threads).
+template <typename T, int D, int KT>
+__device__ __forceinline__ bool clean_values(char* vl, uint64_t there, int thread, int threads) {
+  typedef KvRows<T, D> Rows;
+  bool odd = false;
+#pragma unroll 1
+  for (int p = thread; p < KT * Rows::kPieces; p += threads) {
+    u32x4* at = reinterpret_cast<u32x4*>(vl + 16 * p);
+    if (there >> (p / Rows::kPieces) & 1) {
+      const u32x4 w = *at, f = finite_only<T>(w);
+      odd |= w[0] != f[0] || w[1] != f[1] || w[2] != f[2] || w[3] != f[3];
+    } else {
+      *at = u32x4{0, 0, 0, 0};
+    }
+  }
+  return odd;
+}
+template <typename T, int D, int KT>
+__device__ __forceinline__ void drop_odd_values(char* vl, int thread, int threads) {
+#pragma unroll 1
+  for (int p = thread; p < KT * KvRows<T, D>::kPieces; p += threads) {
+    u32x4* at = reinterpret_cast<u32x4*>(vl + 16 * p);
+    *at = finite_only<T>(*at);
   }
 }
 
@@ -278,14 +325,30 @@ struct AttnWave {
       }
     }
   }
-  // S^T of 32 keys from row r0 of the tile
-  __device__ __forceinline__ f32x16 scores(const char* kl, int r0, int lane) const {
-    f32x16 s;
+  // S^T of the tile's NB blocks of 32 keys; operands are read a step ahead of their products
+  template <int NB>
+  __device__ __forceinline__ void scores(const char* kl, f32x16 (&s)[NB], int lane) const {
+    constexpr int U = D / 16;
+    int at = Rows::frag_start(lane);
+    asm volatile("" : "+v"(at));   // addresses are made here, not kept in registers over the tiles
+    R kf[2][NB];
+    const auto load = [&](int u) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) s[i] = 0.0f;
+      for (int b = 0; b < NB; ++b) kf[u & 1][b] = Rows::frag_at(kl + 32 * b * Rows::kPitch, at ^ Rows::kFragStep * u);
+    };
 #pragma unroll
-    for (int u = 0; u < D / 16; ++u) s = Mm<T>::mul(Rows::row_frag(kl, r0 + lane % 32, 2 * u + lane / 32), q[u], s);
-    return s;
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[b][i] = 0.0f;
+    load(0);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (u + 1 < U) load(u + 1);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int b = 0; b < NB; ++b) s[b] = Mm<T>::mul(kf[u & 1][b], q[u], s[b]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
   }
   // scores -> weights, for NB blocks of 32 keys
   template <int NB>
@@ -317,60 +380,73 @@ struct AttnWave {
         l += s[b][i];
       }
   }
-  // O^T += V^T P^T over 32 keys.  CHECK: some rows do not see some of the keys (weight
-  // zero), whose values may be anything: those that are not finite stay out of the
-  // product and are added, element by element, to the rows that see them (`seen`: bit
-  // i is for key 8 (i / 4) + 4 h + i % 4).
-  template <bool CHECK>
-  __device__ __forceinline__ void values(const char* vl, int r0, const f32x16& p, int lane, uint32_t seen) {
+  // O^T += V^T P^T over the tile's NB blocks of 32 keys
+  template <int NB>
+  __device__ __forceinline__ void values(const char* vl, const f32x16 (&p)[NB], int lane) {
+    constexpr int DT = D / 32, S = 2 * NB;
+    int at = Rows::col_start(lane);
+    asm volatile("" : "+v"(at));
+    R vf[2][DT];
+    const auto load = [&](int s) {
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
+      for (int dt = 0; dt < DT; ++dt) vf[s & 1][dt] = Rows::col_frag(vl + 16 * s * Rows::kPitch, at, dt);
+    };
+    load(0);
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+      if (s + 1 < S) load(s + 1);
+      __builtin_amdgcn_sched_barrier(0);
       float w[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) w[j] = p[8 * s + j];
+      for (int j = 0; j < 8; ++j) w[j] = p[s / 2][8 * (s % 2) + j];
       const R pf = Mm<T>::pack(w);
-      bool odd = false;
 #pragma unroll
-      for (int dt = 0; dt < D / 32; ++dt) {
-        R vf = Rows::col_frag(vl, r0 + 16 * s, dt, lane);
-        if (CHECK) vf = finite_only(vf, &odd);
-        o[dt] = Mm<T>::mul(vf, pf, o[dt]);
-      }
-      if (CHECK && __any(odd)) {
-        for (int k = 0; k < 16; ++k) {   // key k of these: register 8 s + 4 (k / 8) + k % 4 of half k / 4 % 2
-          const int reg = 8 * s + 4 * (k / 8) + k % 4, from = k / 4 % 2 * 32 + lane % 32;
-          float pk = 0.0f;
-#pragma unroll
-          for (int i = 0; i < 16; ++i) pk = reg == i ? p[i] : pk;
-          pk = __shfl(pk, from, kWave);
-          const bool sees = __shfl(static_cast<int>(seen >> reg & 1), from, kWave);
-#pragma unroll
-          for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const float x = Rows::elt(vl, r0 + 16 * s + k, 32 * dt + 8 * (i / 4) + 4 * (lane / 32) + i % 4);
-              if (sees && not_finite(x)) o[dt][i] = fmaf(pk, x, o[dt][i]);
-            }
-        }
-      }
+      for (int dt = 0; dt < DT; ++dt) o[dt] = Mm<T>::mul(vf[s & 1][dt], pf, o[dt]);
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
-  // A tile of NB blocks of 32 keys.  limit: keys of the tile that this lane's row may
-  // see; there: keys that exist; whole: all rows see all keys
+  // Scores of keys that the lane's row does not see: limit keys of the tile may be
+  // seen, of those that are `there`.
   template <int NB>
-  __device__ __forceinline__ void masked_scores(f32x16 (&s)[NB], uint32_t (&seen)[NB], int limit, uint64_t there, int lane) {
+  __device__ __forceinline__ void mask(f32x16 (&s)[NB], int limit, uint64_t there, int lane) {
     const int h4 = lane / 32 * 4;
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
       const uint32_t bits = static_cast<uint32_t>(there >> (32 * b)) >> h4;
-      seen[b] = 0;
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const int key = 8 * (i / 4) + i % 4;
-        const bool sees = 32 * b + key + h4 < limit && (bits >> key & 1);
-        s[b][i] = sees ? s[b][i] : -INFINITY;
-        seen[b] |= sees ? 1u << i : 0u;
+        s[b][i] = 32 * b + key + h4 < limit && (bits >> key & 1) ? s[b][i] : -INFINITY;
       }
+    }
+  }
+  // Adds the values of a tile that are not finite to the rows that see them, element by
+  // element (they stay out of the product, where the weights of rows that do not are
+  // zero).  Rare, so small rather than fast.
+  template <int NB>
+  __device__ __forceinline__ void add_odd_values(const char* vl, const f32x16 (&p)[NB], int limit, uint64_t there, int lane) {
+#pragma unroll 1
+    for (int key = 0; key < 32 * NB; ++key) {
+      bool odd = false;
+#pragma unroll
+      for (int d = 0; d < D / kWave; ++d) odd |= not_finite(Rows::elt(vl, key, kWave * d + lane));
+      if (!__any(odd)) continue;
+      // the key's weight: register 4 (key / 8) + key % 4 of half key / 4 % 2
+      const int reg = 16 * (key / 32) + 4 * (key % 32 / 8) + key % 4;
+      float pk = 0.0f;
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) pk = reg == 16 * b + i ? p[b][i] : pk;
+      pk = __shfl(pk, key / 4 % 2 * 32 + lane % 32, kWave);
+      const bool sees = key < limit && (there >> key & 1);
+#pragma unroll
+      for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const float x = Rows::elt(vl, key, 32 * dt + 8 * (i / 4) + 4 * (lane / 32) + i % 4);
+          if (sees && not_finite(x)) o[dt][i] = fmaf(pk, x, o[dt][i]);
+        }
     }
   }
 };
@@ -388,7 +464,9 @@ struct AttnLds {
   static constexpr int kRows = 4 * kTileBytes;                 // K and V, two of each
   static constexpr int kKeys = 2 * kAttnWaves * kOwnBytes;
   static constexpr int kMerge = kAttnWaves * D * kAttnRows * 4 + kAttnWaves * kAttnRows * 8;
-  static constexpr int kBytes = kRows > kKeys ? (kRows > kMerge ? kRows : kMerge) : (kKeys > kMerge ? kKeys : kMerge);
+  static constexpr int kMost = kRows > kKeys ? (kRows > kMerge ? kRows : kMerge) : (kKeys > kMerge ? kKeys : kMerge);
+  static constexpr int kOffOdd = kMost;                        // a word for each wave
+  static constexpr int kBytes = kMost + 4 * kAttnWaves;
 };
 
 struct AttnItem {
@@ -454,7 +532,7 @@ __device__ __forceinline__ void put_columns(const AttnArgs& a, const AttnItem& i
 
 // Waves take rows of their own and share tiles of keys.
 template <typename T, int D>
-__device__ __forceinline__ void attend_rows(const AttnArgs& a, const AttnItem& it, const CacheAt& cache, char* lds) {
+__device__ __forceinline__ void attend_rows(const AttnArgs& a, const AttnItem& it, const CacheAt<T, D>& cache, char* lds) {
   typedef AttnLds<T, D> L;
   typedef typename L::Rows Rows;
   constexpr int KT = L::kTileKeys, NB = KT / 32, N = KT / Rows::kRowsPerDma / kAttnWaves;
@@ -466,59 +544,67 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, const AttnItem& i
   w.clear();
   const bool idle = w0 >= it.rows;
   const int mine = own_limit(it, a.groups, r);
+  const int first = own_limit(it, a.groups, 0);   // the least of the workgroup, then the wave's least and most
   const int least = __builtin_amdgcn_readfirstlane(own_limit(it, a.groups, min(w0, it.rows - 1))),
             most = __builtin_amdgcn_readfirstlane(own_limit(it, a.groups, min(w0 + kAttnRows, it.rows) - 1));
   lds_byte* dst = (lds_byte*)lds;
+  uint32_t* odds = reinterpret_cast<uint32_t*>(lds + L::kOffOdd);
   const int tiles = it.keys.tiles<KT>();
   const auto present = [&](const KeyTile& t, const PageOf& p) {   // a bit for each key
     return __ballot(lane < t.count && p.page >= 0 && p.page < a.num_pages);
   };
   constexpr uint64_t kAll = KT == 64 ? ~0ull : (1ull << (KT % 64)) - 1;
-  KeyTile cur{}, next{};
-  uint64_t there = 0, there_next = 0;
+  KeyTile next{};
+  uint64_t there_next = 0;
   PageOf pages{};
-  if (tiles > 0) {
-    next = key_tile<KT>(it.keys, 0);
-    pages = find_pages<KT>(a, next);
+  const auto fetch = [&](int j) {
+    next = key_tile<KT>(it.keys, j);
     there_next = present(next, pages);
-    load_rows<T, D, N, true, true>(a, cache, pages, there_next, there_next == kAll, dst, dst + L::kTileBytes, N * wave, lane);
+    lds_byte* to = dst + (j & 1) * 2 * L::kTileBytes;
+    load_rows<T, D, N, true, true>(a, cache, pages, there_next, there_next == kAll, to, to + L::kTileBytes, N * wave);
+  };
+  if (tiles > 0) {
+    pages = find_pages<KT>(a, key_tile<KT>(it.keys, 0));
+    fetch(0);
     if (tiles > 1) pages = find_pages<KT>(a, key_tile<KT>(it.keys, 1));
   }
   for (int j = 0; j < tiles; ++j) {
-    cur = next;
-    there = there_next;
+    const KeyTile cur = next;
+    const uint64_t there = there_next;
     wait_dma();
     lds_barrier();
     const char* kl = lds + (j & 1) * 2 * L::kTileBytes;
     char* vl = lds + (j & 1) * 2 * L::kTileBytes + L::kTileBytes;
-    if (there != kAll) {   // values of keys that are none count as zeros
-      for (int p = threadIdx.x; p < KT * Rows::kPieces; p += kAttnThreads)
-        if (!(there >> (p / Rows::kPieces) & 1)) *reinterpret_cast<u32x4*>(vl + 16 * p) = u32x4{0, 0, 0, 0};
-      lds_barrier();
-    }
     if (j + 1 < tiles) {
-      next = key_tile<KT>(it.keys, j + 1);
-      there_next = present(next, pages);
-      lds_byte* to = dst + ((j + 1) & 1) * 2 * L::kTileBytes;
-      load_rows<T, D, N, true, true>(a, cache, pages, there_next, there_next == kAll, to, to + L::kTileBytes, N * wave, lane);
+      fetch(j + 1);
       if (j + 2 < tiles) pages = find_pages<KT>(a, key_tile<KT>(it.keys, j + 2));
     }
-    if (idle || (cur.own && most <= cur.base)) continue;
-    f32x16 s[NB];
+    // tiles that some rows of the workgroup do not see whole
+    bool odd = false;
+    if (there != kAll || (cur.own && first < cur.base + KT)) {
+      const bool found = clean_values<T, D, KT>(vl, there, threadIdx.x, kAttnThreads);
+      if (lane == 0) odds[wave] = 0;
+      if (found) odds[wave] = 1;
+      lds_barrier();
 #pragma unroll
-    for (int b = 0; b < NB; ++b) s[b] = w.scores(kl, 32 * b, lane);
-    const bool whole = there == kAll && (!cur.own || least >= cur.base + KT);
-    if (whole) {
-      w.weigh(s, a.scale2);
-#pragma unroll
-      for (int b = 0; b < NB; ++b) w.template values<false>(vl, 32 * b, s[b], lane, 0);
-    } else {
-      uint32_t seen[NB];
-      w.masked_scores(s, seen, cur.own ? mine - cur.base : KT, there, lane);
-      w.weigh(s, a.scale2);
-#pragma unroll
-      for (int b = 0; b < NB; ++b) w.template values<true>(vl, 32 * b, s[b], lane, seen[b]);
+      for (int x = 0; x < kAttnWaves; ++x) odd |= odds[x] != 0;
+      odd = __builtin_amdgcn_readfirstlane(odd);
     }
+    const bool active = !idle && !(cur.own && most <= cur.base);
+    const int limit = cur.own ? mine - cur.base : KT;
+    f32x16 s[NB];
+    if (active) {
+      w.scores(kl, s, lane);
+      if (there != kAll || (cur.own && least < cur.base + KT)) w.mask(s, limit, there, lane);
+      w.weigh(s, a.scale2);
+    }
+    if (odd) {
+      if (active) w.add_odd_values(vl, s, limit, there, lane);
+      lds_barrier();
+      drop_odd_values<T, D, KT>(vl, threadIdx.x, kAttnThreads);
+      lds_barrier();
+    }
+    if (active) w.values(vl, s, lane);
   }
   if (idle) return;
   w.l = half_sum(w.l);
@@ -528,7 +614,7 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, const AttnItem& i
 
 // At most 32 rows: waves take keys of their own, and their results are joined.
 template <typename T, int D>
-__device__ __forceinline__ void attend_keys(const AttnArgs& a, const AttnItem& it, const CacheAt& cache, char* lds) {
+__device__ __forceinline__ void attend_keys(const AttnArgs& a, const AttnItem& it, const CacheAt<T, D>& cache, char* lds) {
   typedef AttnLds<T, D> L;
   typedef typename L::Rows Rows;
   constexpr int KT = 32, N = KT / Rows::kRowsPerDma;
@@ -557,43 +643,46 @@ __device__ __forceinline__ void attend_keys(const AttnArgs& a, const AttnItem& i
     cur = key_tile<KT>(it.keys, wave);
     pages = find_pages<KT>(a, cur);
     there = present(cur, pages);
-    load_rows<T, D, N, true, false>(a, cache, pages, there, there == kAll, kd, vd, 0, lane);
+    load_rows<T, D, N, true, false>(a, cache, pages, there, there == kAll, kd, vd, 0);
     if (wave + kAttnWaves < tiles) {
       next = key_tile<KT>(it.keys, wave + kAttnWaves);
       ahead = find_pages<KT>(a, next);
     }
-    load_rows<T, D, N, false, true>(a, cache, pages, there, there == kAll, kd, vd, 0, lane);
+    load_rows<T, D, N, false, true>(a, cache, pages, there, there == kAll, kd, vd, 0);
   }
   for (int j = wave; j < tiles; j += kAttnWaves) {
     const bool more = j + kAttnWaves < tiles;
     wait_dma_but<N>();   // this tile's K and the next one's pages are here, V may be on its way
-    f32x16 s[1] = {w.scores(kl, 0, lane)};
+    f32x16 s[1];
+    w.scores(kl, s, lane);
     wait_lds();
     KeyTile after{};
     if (more) {
       pages = ahead;
       there_next = present(next, pages);
-      load_rows<T, D, N, true, false>(a, cache, pages, there_next, there_next == kAll, kd, vd, 0, lane);
+      load_rows<T, D, N, true, false>(a, cache, pages, there_next, there_next == kAll, kd, vd, 0);
       if (j + 2 * kAttnWaves < tiles) {
         after = key_tile<KT>(it.keys, j + 2 * kAttnWaves);
         ahead = find_pages<KT>(a, after);
       }
     }
+    const int limit = cur.own ? mine - cur.base : KT;
     const bool whole = there == kAll && (!cur.own || least >= cur.base + KT);
-    uint32_t seen[1] = {0};
-    if (!whole) w.masked_scores(s, seen, cur.own ? mine - cur.base : KT, there, lane);
+    if (!whole) w.mask(s, limit, there, lane);
     w.weigh(s, a.scale2);
     if (more) wait_dma_but<N>();   // (the last of N + 1 where pages were looked up)
     else wait_dma();
-    if (there != kAll) {
-      for (int p = lane; p < KT * Rows::kPieces; p += kWave)
-        if (!(there >> (p / Rows::kPieces) & 1)) *reinterpret_cast<u32x4*>(vl + 16 * p) = u32x4{0, 0, 0, 0};
+    if (!whole) {
+      if (__any(clean_values<T, D, KT>(vl, there, lane, kWave))) {
+        w.add_odd_values(vl, s, limit, there, lane);
+        wait_lds();
+        drop_odd_values<T, D, KT>(vl, lane, kWave);
+      }
       wait_lds();
     }
-    if (whole) w.template values<false>(vl, 0, s[0], lane, 0);
-    else w.template values<true>(vl, 0, s[0], lane, seen[0]);
+    w.values(vl, s, lane);
     wait_lds();
-    if (more) load_rows<T, D, N, false, true>(a, cache, pages, there_next, there_next == kAll, kd, vd, 0, lane);
+    if (more) load_rows<T, D, N, false, true>(a, cache, pages, there_next, there_next == kAll, kd, vd, 0);
     cur = next;
     next = after;
     there = there_next;
@@ -694,7 +783,7 @@ void k_attn(AttnArgs a) {
     it.part = static_cast<int64_t>(a.shared_items) * kAttnWaves +
               ((static_cast<int64_t>(slot) * a.own_splits + split) * a.kv_heads + it.kvh) * (a.own_tile / kAttnRows);
   }
-  const CacheAt cache = {static_cast<const char*>(a.k) + it.kvh * a.kh, static_cast<const char*>(a.v) + it.kvh * a.vh};
+  const CacheAt<T, D> cache(a, it.kvh);
   if (it.rows <= kAttnRows) attend_keys<T, D>(a, it, cache, lds);
   else attend_rows<T, D>(a, it, cache, lds);
 }
