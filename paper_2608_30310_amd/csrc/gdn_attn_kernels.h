@@ -56,6 +56,10 @@ struct AttnArgs {
   f32x2* part_ml;         // [item][wave tile][32]: m and l of a row
 };
 
+// Branches that registers are not to be allotted for (rare loops would come before
+// the ones around them).
+__device__ __forceinline__ bool rarely(bool x) { return __builtin_expect(x, 0); }
+
 // ---------------------------------------------------------------- operands
 // 32 x 32 x 16 products: lane (h, r) supplies elements 8 h + j (j = 0..7) of row r
 // of either operand and holds rows 8 (i / 4) + 4 h + i % 4 (i = 0..15) of column r.
@@ -188,84 +192,155 @@ __device__ __forceinline__ float half_sum(float x) {
 }
 
 // ---------------------------------------------------------------- keys
-// The keys that an item walks, in tiles of KT: `count0` tokens of the prefix from
-// `first0` on, then `count1` of a sequence's own from `first1` on.
+// The keys that an item walks: `count0` tokens of the prefix from `first0` on, then
+// `count1` of a sequence's own from `first1` on.
 struct KeyRange {
   const int32_t* list0;
   const int32_t* list1;
   int first0, count0, first1, count1;
-  template <int KT>
-  __device__ __forceinline__ int tiles() const { return (count0 + KT - 1) / KT + (count1 + KT - 1) / KT; }
 };
+// A tile of KT of them: tokens base .. of a list of pages, `count` of them left in
+// their part of the range.
 struct KeyTile {
   const int32_t* list;
-  int base, count;   // its first token, and how many there are of KT
+  int base, count;
   bool own;
 };
+__device__ __forceinline__ void key_part(const KeyRange& k, KeyTile& t) {   // t.own: into the second part
+  t.list = t.own ? k.list1 : k.list0;
+  t.base = t.own ? k.first1 : k.first0;
+  t.count = t.own ? k.count1 : k.count0;
+}
+__device__ __forceinline__ KeyTile first_tile(const KeyRange& k) {
+  KeyTile t;
+  t.own = k.count0 <= 0;
+  key_part(k, t);
+  return t;
+}
+// KT tokens on; no tile where its count is not positive.
 template <int KT>
-__device__ __forceinline__ KeyTile key_tile(const KeyRange& k, int j) {
-  const int t0 = (k.count0 + KT - 1) / KT;
-  const bool own = j >= t0;
-  const int from = (own ? j - t0 : j) * KT;
-  return {own ? k.list1 : k.list0, (own ? k.first1 : k.first0) + from, min(KT, (own ? k.count1 : k.count0) - from), own};
+__device__ __forceinline__ void next_tile(const KeyRange& k, KeyTile& t) {
+  t.base += KT;
+  t.count -= KT;
+  if (t.count <= 0 && !t.own) {
+    t.own = true;
+    key_part(k, t);
+  }
 }
 
-// The page and its row that hold token base + lane % KT of a tile (lanes behind its end: of its last token).
-struct PageOf { int page, row; };
-template <int KT>
-__device__ __forceinline__ PageOf find_pages(const AttnArgs& a, const KeyTile& t) {
-  const int key = t.base + min(static_cast<int>(threadIdx.x) % KT, t.count - 1);
-  const int c = a.page_size == 1 ? key : static_cast<int>(__umulhi(key, a.page_mul) >> a.page_shift);
-  return {t.list[c], key - c * a.page_size};
+// Loads into LDS that the compiler does not count: it would wait for all of them
+// before the next transposing read of LDS, which may be of another buffer.  Whoever
+// reads what they write waits by wait_dma or wait_dma_but first.
+__device__ __forceinline__ uint32_t lds_address(lds_byte* p) {
+  return __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(reinterpret_cast<uintptr_t>(p)));
+}
+__device__ __forceinline__ void async_piece(const void* src, lds_byte* dst) {   // 16 bytes a lane
+  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_address(dst)), "v"(src) : "memory");
+}
+__device__ __forceinline__ void async_piece(uint64_t base, uint32_t off, lds_byte* dst) {   // from a uniform base
+  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds_address(dst)), "v"(off), "s"(base) : "memory");
+}
+__device__ __forceinline__ void async_word(const void* src, lds_byte* dst) {   // 4 bytes a lane
+  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, off" ::"s"(lds_address(dst)), "v"(src) : "memory");
 }
 
+// What the loop over tiles needs of the arguments: each value a register of its own
+// (left in the tuples that they are loaded in, they do not fit the scalar registers and
+// every use restores a whole tuple).
+template <typename X>
+__device__ __forceinline__ X apart(X x) {
+  asm("" : "+s"(x));
+  return x;
+}
 // Where a K/V head's rows are in the caches, and a lane's place in a DMA of
 // kRowsPerDma rows: the swizzle is linear over XOR, so piece p of row r + j (r a
 // multiple of kRowsPerDma) comes from piece (p ^ swz(j)) ^ swz(r).
 template <typename T, int D>
 struct CacheAt {
-  const char* k;
-  const char* v;
+  uint64_t k, v;
+  uint32_t kp, kt, vp, vt, page_mul;
+  int page_shift, page_size, num_pages, dma_in_page;
   uint32_t krow, vrow, piece;
   __device__ __forceinline__ CacheAt(const AttnArgs& a, int kvh) {
     typedef KvRows<T, D> Rows;
     const int lane = threadIdx.x % kWave, j = lane / Rows::kPieces;
-    k = static_cast<const char*>(a.k) + kvh * a.kh;
-    v = static_cast<const char*>(a.v) + kvh * a.vh;
+    k = apart(reinterpret_cast<uint64_t>(a.k) + kvh * a.kh);
+    v = apart(reinterpret_cast<uint64_t>(a.v) + kvh * a.vh);
+    kp = apart(a.kp), kt = apart(a.kt), vp = apart(a.vp), vt = apart(a.vt), page_mul = apart(a.page_mul);
+    page_shift = apart(a.page_shift), page_size = apart(a.page_size), num_pages = apart(a.num_pages);
+    dma_in_page = apart(a.dma_in_page);
     krow = 16 * j * a.kt;
     vrow = 16 * j * a.vt;
     piece = 16 * (lane % Rows::kPieces ^ Rows::swz(j));
   }
+  // The page index of token base + lane % KT of a tile (lanes behind its end: of its
+  // last token), and the token's row there.
+  template <int KT>
+  __device__ __forceinline__ int page_index(const KeyTile& t, int* row) const {
+    const int key = t.base + min(static_cast<int>(threadIdx.x) % KT, t.count - 1);
+    const int c = page_size == 1 ? key : static_cast<int>(__umulhi(key, page_mul) >> page_shift);
+    *row = key - c * page_size;
+    return c;
+  }
+  // The page numbers come through LDS, 64 of a wave's own.
+  template <int KT>
+  __device__ __forceinline__ void ask_pages(const KeyTile& t, lds_byte* to) const {
+    int row;
+    async_word(t.list + page_index<KT>(t, &row), to);
+  }
+  // Addresses of the rows of a tile, one a lane, and which of them are there; rows that
+  // are not have the cache's first.
+  struct RowsAt { uint64_t k, v; };
+  template <int KT>
+  __device__ __forceinline__ RowsAt find_rows(const KeyTile& t, const lds_byte* numbers, uint64_t* there) const {
+    const int lane = threadIdx.x % kWave;
+    int row;
+    page_index<KT>(t, &row);
+    const int page = ((const __attribute__((address_space(3))) int32_t*)numbers)[lane];
+    const bool ok = lane < min(KT, t.count) && page >= 0 && page < num_pages;
+    *there = __ballot(ok);
+    const uint64_t p = ok ? page : 0;
+    const uint32_t r = ok ? row : 0;
+    return {k + 16 * (p * kp + static_cast<uint64_t>(r) * kt), v + 16 * (p * vp + static_cast<uint64_t>(r) * vt)};
+  }
 };
 
-// DMA of rows [i0, i0 + N) kRowsPerDma of a tile into LDS (both of K and V, or one of them).
-template <typename T, int D, int N, bool K, bool V>
-__device__ __forceinline__ void load_rows(const AttnArgs& a, const CacheAt<T, D>& c, const PageOf& at, uint64_t there, bool whole,
-                                          lds_byte* kl, lds_byte* vl, int i0) {
+__device__ __forceinline__ KeyRange apart_range(const KeyRange& k) {
+  return {reinterpret_cast<const int32_t*>(apart(reinterpret_cast<uint64_t>(k.list0))),
+          reinterpret_cast<const int32_t*>(apart(reinterpret_cast<uint64_t>(k.list1))), apart(k.first0), apart(k.count0),
+          apart(k.first1), apart(k.count1)};
+}
+
+__device__ __forceinline__ uint64_t uniform_at(uint64_t x, int lane) {
+  const uint32_t lo = __builtin_amdgcn_readlane(static_cast<uint32_t>(x), lane),
+                 hi = __builtin_amdgcn_readlane(static_cast<uint32_t>(x >> 32), lane);
+  return static_cast<uint64_t>(hi) << 32 | lo;
+}
+__device__ __forceinline__ uint64_t lane_at(uint64_t x, int lane) {
+  const uint32_t lo = __shfl(static_cast<uint32_t>(x), lane, kWave), hi = __shfl(static_cast<uint32_t>(x >> 32), lane, kWave);
+  return static_cast<uint64_t>(hi) << 32 | lo;
+}
+
+// DMA of rows [i0, i0 + N) kRowsPerDma of a tile into LDS; row_off: krow or vrow.
+// Where a DMA's rows lie in one page they are read from its first row's address on:
+// rows behind the last token that way too, which are in the page and masked later.
+template <typename T, int D, int N>
+__device__ __forceinline__ void load_rows(const CacheAt<T, D>& c, uint64_t rows_at, uint32_t row_off, lds_byte* to, int i0) {
   typedef KvRows<T, D> Rows;
   constexpr int RPD = Rows::kRowsPerDma;
-  if (whole && a.dma_in_page) {
+  if (!rarely(!c.dma_in_page)) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int r = (i0 + i) * RPD;
-      const uint64_t page = static_cast<uint32_t>(__builtin_amdgcn_readlane(at.page, r)),
-                     row = static_cast<uint32_t>(__builtin_amdgcn_readlane(at.row, r));
-      const uint32_t turn = 16 * Rows::swz(r);
-      if (K) dma16(c.k + 16 * (page * a.kp + row * a.kt) + (c.krow + (c.piece ^ turn)), kl + (i0 + i) * 1024);
-      if (V) dma16(c.v + 16 * (page * a.vp + row * a.vt) + (c.vrow + (c.piece ^ turn)), vl + (i0 + i) * 1024);
+      async_piece(uniform_at(rows_at, r), row_off + (c.piece ^ 16 * Rows::swz(r)), to + (i0 + i) * 1024);
     }
   } else {
-    // row by row; rows that are none are taken from the cache's first
-    const int lane = threadIdx.x % kWave, j = lane / Rows::kPieces;
-#pragma unroll 1
+    const int lane = threadIdx.x % kWave;
+#pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int r = (i0 + i) * RPD + j;
-      const bool ok = there >> r & 1;
-      const int pg = __shfl(at.page, r, kWave), rw = __shfl(at.row, r, kWave);
-      const uint64_t page = static_cast<uint32_t>(ok ? pg : 0), row = static_cast<uint32_t>(ok ? rw : 0);
-      const uint32_t piece = 16 * (lane % Rows::kPieces ^ Rows::swz(r));
-      if (K) dma16(c.k + 16 * (page * a.kp + row * a.kt) + piece, kl + (i0 + i) * 1024);
-      if (V) dma16(c.v + 16 * (page * a.vp + row * a.vt) + piece, vl + (i0 + i) * 1024);
+      const int r = (i0 + i) * RPD;
+      const uint64_t at = lane_at(rows_at, r + lane / Rows::kPieces);
+      async_piece(reinterpret_cast<const void*>(at + (c.piece ^ 16 * Rows::swz(r))), to + (i0 + i) * 1024);
     }
   }
 }
@@ -276,6 +351,7 @@ template <typename T, int D, int KT>
 __device__ __forceinline__ bool clean_values(char* vl, uint64_t there, int thread, int threads) {
   typedef KvRows<T, D> Rows;
   bool odd = false;
+  asm volatile("" : "+v"(thread));
 #pragma unroll 1
   for (int p = thread; p < KT * Rows::kPieces; p += threads) {
     u32x4* at = reinterpret_cast<u32x4*>(vl + 16 * p);
@@ -290,6 +366,7 @@ __device__ __forceinline__ bool clean_values(char* vl, uint64_t there, int threa
 }
 template <typename T, int D, int KT>
 __device__ __forceinline__ void drop_odd_values(char* vl, int thread, int threads) {
+  asm volatile("" : "+v"(thread));
 #pragma unroll 1
   for (int p = thread; p < KT * KvRows<T, D>::kPieces; p += threads) {
     u32x4* at = reinterpret_cast<u32x4*>(vl + 16 * p);
@@ -361,7 +438,7 @@ struct AttnWave {
     top = half_max(top) * scale2;
     // each row by itself: what one row meets does not change another's rounding
     const bool moves = top > m + 8.0f || m == -INFINITY;
-    if (__any(moves)) {
+    if (rarely(__any(moves))) {
       const float next = moves ? fmaxf(m, top) : m;
       const float keep = moves ? __builtin_amdgcn_exp2f(m - (next == -INFINITY ? 0.0f : next)) : 1.0f;
       m = next;
@@ -409,14 +486,16 @@ struct AttnWave {
   // seen, of those that are `there`.
   template <int NB>
   __device__ __forceinline__ void mask(f32x16 (&s)[NB], int limit, uint64_t there, int lane) {
-    const int h4 = lane / 32 * 4;
+    int h4 = lane / 32 * 4;
+    asm volatile("" : "+v"(h4));   // what follows is made here, not kept in registers over the tiles
+    const int left = limit - h4;
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
       const uint32_t bits = static_cast<uint32_t>(there >> (32 * b)) >> h4;
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const int key = 8 * (i / 4) + i % 4;
-        s[b][i] = 32 * b + key + h4 < limit && (bits >> key & 1) ? s[b][i] : -INFINITY;
+        s[b][i] = 32 * b + key < left && (bits >> key & 1) ? s[b][i] : -INFINITY;
       }
     }
   }
@@ -425,12 +504,13 @@ struct AttnWave {
   // zero).  Rare, so small rather than fast.
   template <int NB>
   __device__ __forceinline__ void add_odd_values(const char* vl, const f32x16 (&p)[NB], int limit, uint64_t there, int lane) {
+    asm volatile("" : "+v"(lane));
 #pragma unroll 1
     for (int key = 0; key < 32 * NB; ++key) {
       bool odd = false;
 #pragma unroll
       for (int d = 0; d < D / kWave; ++d) odd |= not_finite(Rows::elt(vl, key, kWave * d + lane));
-      if (!__any(odd)) continue;
+      if (!rarely(__any(odd))) continue;
       // the key's weight: register 4 (key / 8) + key % 4 of half key / 4 % 2
       const int reg = 16 * (key / 32) + 4 * (key % 32 / 8) + key % 4;
       float pk = 0.0f;
@@ -446,6 +526,7 @@ struct AttnWave {
         for (int i = 0; i < 16; ++i) {
           const float x = Rows::elt(vl, key, 32 * dt + 8 * (i / 4) + 4 * (lane / 32) + i % 4);
           if (sees && not_finite(x)) o[dt][i] = fmaf(pk, x, o[dt][i]);
+          if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);   // few registers, for the sake of the others
         }
     }
   }
@@ -466,8 +547,17 @@ struct AttnLds {
   static constexpr int kMerge = kAttnWaves * D * kAttnRows * 4 + kAttnWaves * kAttnRows * 8;
   static constexpr int kMost = kRows > kKeys ? (kRows > kMerge ? kRows : kMerge) : (kKeys > kMerge ? kKeys : kMerge);
   static constexpr int kOffOdd = kMost;                        // a word for each wave
-  static constexpr int kBytes = kMost + 4 * kAttnWaves;
+  static constexpr int kOffPages = kOffOdd + 64;               // 64 page numbers for each wave
+  static constexpr int kBytes = kOffPages + 4 * kAttnThreads;
 };
+
+// The kernel's arguments, loaded anew: what is used at the end alone is not kept in
+// scalar registers over the loop.
+__device__ __forceinline__ AttnArgs args_again() {
+  auto p = __builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  return *(const AttnArgs*)p;
+}
 
 struct AttnItem {
   int kvh;
@@ -538,9 +628,9 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, const AttnItem& i
   constexpr int KT = L::kTileKeys, NB = KT / 32, N = KT / Rows::kRowsPerDma / kAttnWaves;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
   const int w0 = kAttnRows * wave, r = min(w0 + lane % 32, it.rows - 1);
-  const RowAt at = row_at(a, it, r);
+  const RowAt mine_at = row_at(a, it, r);
   AttnWave<T, D> w;
-  w.load_q(static_cast<const T*>(a.q) + at.token * a.ldq + static_cast<int64_t>(at.head) * D, a.flip, lane / 32);
+  w.load_q(static_cast<const T*>(a.q) + mine_at.token * a.ldq + static_cast<int64_t>(mine_at.head) * D, a.flip, lane / 32);
   w.clear();
   const bool idle = w0 >= it.rows;
   const int mine = own_limit(it, a.groups, r);
@@ -549,40 +639,40 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, const AttnItem& i
             most = __builtin_amdgcn_readfirstlane(own_limit(it, a.groups, min(w0 + kAttnRows, it.rows) - 1));
   lds_byte* dst = (lds_byte*)lds;
   uint32_t* odds = reinterpret_cast<uint32_t*>(lds + L::kOffOdd);
-  const int tiles = it.keys.tiles<KT>();
-  const auto present = [&](const KeyTile& t, const PageOf& p) {   // a bit for each key
-    return __ballot(lane < t.count && p.page >= 0 && p.page < a.num_pages);
-  };
+  const float scale2 = apart(a.scale2);
+  const KeyRange keys = apart_range(it.keys);
+  lds_byte* numbers = dst + L::kOffPages + 4 * kWave * wave;
   constexpr uint64_t kAll = KT == 64 ? ~0ull : (1ull << (KT % 64)) - 1;
-  KeyTile next{};
-  uint64_t there_next = 0;
-  PageOf pages{};
-  const auto fetch = [&](int j) {
-    next = key_tile<KT>(it.keys, j);
-    there_next = present(next, pages);
-    lds_byte* to = dst + (j & 1) * 2 * L::kTileBytes;
-    load_rows<T, D, N, true, true>(a, cache, pages, there_next, there_next == kAll, to, to + L::kTileBytes, N * wave);
-  };
-  if (tiles > 0) {
-    pages = find_pages<KT>(a, key_tile<KT>(it.keys, 0));
-    fetch(0);
-    if (tiles > 1) pages = find_pages<KT>(a, key_tile<KT>(it.keys, 1));
-  }
-  for (int j = 0; j < tiles; ++j) {
-    const KeyTile cur = next;
-    const uint64_t there = there_next;
+  // `cur` is looked at while `next` comes in, and the pages of the one after it
+  KeyTile cur{}, next = first_tile(keys);
+  uint64_t there = 0;
+  bool any = false;
+  int side = 0;   // the buffer of `cur`
+  if (next.count > 0) cache.template ask_pages<KT>(next, numbers);
+  while (any || next.count > 0) {
     wait_dma();
     lds_barrier();
-    const char* kl = lds + (j & 1) * 2 * L::kTileBytes;
-    char* vl = lds + (j & 1) * 2 * L::kTileBytes + L::kTileBytes;
-    if (j + 1 < tiles) {
-      fetch(j + 1);
-      if (j + 2 < tiles) pages = find_pages<KT>(a, key_tile<KT>(it.keys, j + 2));
+    const bool now = any;
+    const KeyTile was = cur;
+    const uint64_t was_there = there;
+    any = next.count > 0;
+    if (any) {
+      const auto at = cache.template find_rows<KT>(next, numbers, &there);
+      lds_byte* to = dst + (side ^ 1) * 2 * L::kTileBytes;
+      load_rows<T, D, N>(cache, at.k, cache.krow, to, N * wave);
+      load_rows<T, D, N>(cache, at.v, cache.vrow, to + L::kTileBytes, N * wave);
+      cur = next;
+      next_tile<KT>(keys, next);
+      if (next.count > 0) cache.template ask_pages<KT>(next, numbers);
     }
+    const char* kl = lds + side * 2 * L::kTileBytes;
+    char* vl = lds + side * 2 * L::kTileBytes + L::kTileBytes;
+    side ^= 1;
+    if (!now) continue;
     // tiles that some rows of the workgroup do not see whole
     bool odd = false;
-    if (there != kAll || (cur.own && first < cur.base + KT)) {
-      const bool found = clean_values<T, D, KT>(vl, there, threadIdx.x, kAttnThreads);
+    if (rarely(was_there != kAll || (was.own && first < was.base + KT))) {
+      const bool found = clean_values<T, D, KT>(vl, was_there, threadIdx.x, kAttnThreads);
       if (lane == 0) odds[wave] = 0;
       if (found) odds[wave] = 1;
       lds_barrier();
@@ -590,16 +680,16 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, const AttnItem& i
       for (int x = 0; x < kAttnWaves; ++x) odd |= odds[x] != 0;
       odd = __builtin_amdgcn_readfirstlane(odd);
     }
-    const bool active = !idle && !(cur.own && most <= cur.base);
-    const int limit = cur.own ? mine - cur.base : KT;
+    const bool active = !idle && !(was.own && most <= was.base);
+    const int limit = was.own ? mine - was.base : KT;
     f32x16 s[NB];
     if (active) {
       w.scores(kl, s, lane);
-      if (there != kAll || (cur.own && least < cur.base + KT)) w.mask(s, limit, there, lane);
-      w.weigh(s, a.scale2);
+      if (rarely(was_there != kAll || (was.own && least < was.base + KT))) w.mask(s, limit, was_there, lane);
+      w.weigh(s, scale2);
     }
-    if (odd) {
-      if (active) w.add_odd_values(vl, s, limit, there, lane);
+    if (rarely(odd)) {
+      if (active) w.add_odd_values(vl, s, limit, was_there, lane);
       lds_barrier();
       drop_odd_values<T, D, KT>(vl, threadIdx.x, kAttnThreads);
       lds_barrier();
@@ -608,8 +698,9 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, const AttnItem& i
   }
   if (idle) return;
   w.l = half_sum(w.l);
+  const AttnArgs e = args_again();
 #pragma unroll
-  for (int dt = 0; dt < D / 32; ++dt) put_columns<T, D>(a, it, wave, w.o[dt], dt, w.m, w.l, lane);
+  for (int dt = 0; dt < D / 32; ++dt) put_columns<T, D>(e, it, wave, w.o[dt], dt, w.m, w.l, lane);
 }
 
 // At most 32 rows: waves take keys of their own, and their results are joined.
@@ -620,72 +711,71 @@ __device__ __forceinline__ void attend_keys(const AttnArgs& a, const AttnItem& i
   constexpr int KT = 32, N = KT / Rows::kRowsPerDma;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
   const int r = min(lane % 32, it.rows - 1);
-  const RowAt at = row_at(a, it, r);
+  const RowAt mine_at = row_at(a, it, r);
   AttnWave<T, D> w;
-  w.load_q(static_cast<const T*>(a.q) + at.token * a.ldq + static_cast<int64_t>(at.head) * D, a.flip, lane / 32);
+  w.load_q(static_cast<const T*>(a.q) + mine_at.token * a.ldq + static_cast<int64_t>(mine_at.head) * D, a.flip, lane / 32);
   w.clear();
   const int mine = own_limit(it, a.groups, r), least = __builtin_amdgcn_readfirstlane(own_limit(it, a.groups, 0));
   const char* kl = lds + wave * 2 * L::kOwnBytes;
   char* vl = lds + wave * 2 * L::kOwnBytes + L::kOwnBytes;
   lds_byte* kd = (lds_byte*)lds + wave * 2 * L::kOwnBytes;
   lds_byte* vd = kd + L::kOwnBytes;
-  const int tiles = it.keys.tiles<KT>();
-  const auto present = [&](const KeyTile& t, const PageOf& p) {
-    return __ballot(lane < t.count && p.page >= 0 && p.page < a.num_pages);
-  };
+  const float scale2 = apart(a.scale2);
+  const KeyRange keys = apart_range(it.keys);
+  lds_byte* numbers = (lds_byte*)lds + L::kOffPages + 4 * kWave * wave;
   constexpr uint64_t kAll = 0xFFFFFFFFull;
   // K of the next tile is on its way while the weights are made, its V while the next
   // scores are; pages are looked up a tile further ahead, between the two
-  KeyTile cur{}, next{};
-  uint64_t there = 0, there_next = 0;
-  PageOf pages{}, ahead{};
-  if (wave < tiles) {
-    cur = key_tile<KT>(it.keys, wave);
-    pages = find_pages<KT>(a, cur);
-    there = present(cur, pages);
-    load_rows<T, D, N, true, false>(a, cache, pages, there, there == kAll, kd, vd, 0);
-    if (wave + kAttnWaves < tiles) {
-      next = key_tile<KT>(it.keys, wave + kAttnWaves);
-      ahead = find_pages<KT>(a, next);
-    }
-    load_rows<T, D, N, false, true>(a, cache, pages, there, there == kAll, kd, vd, 0);
+  KeyTile cur{}, next = first_tile(keys);
+  const auto skip = [&](int n) {
+    for (int i = 0; i < n && next.count > 0; ++i) next_tile<KT>(keys, next);
+  };
+  skip(wave);
+  uint64_t there = 0;
+  bool any = false;
+  if (next.count > 0) {
+    cache.template ask_pages<KT>(next, numbers);
+    wait_dma();
   }
-  for (int j = wave; j < tiles; j += kAttnWaves) {
-    const bool more = j + kAttnWaves < tiles;
-    wait_dma_but<N>();   // this tile's K and the next one's pages are here, V may be on its way
+  while (any || next.count > 0) {
+    const bool now = any;
+    const KeyTile was = cur;
+    const uint64_t was_there = there;
+    if (now) wait_dma_but<N>();   // its K and the next one's pages are here, V may be on its way
     f32x16 s[1];
-    w.scores(kl, s, lane);
+    if (now) w.scores(kl, s, lane);
     wait_lds();
-    KeyTile after{};
-    if (more) {
-      pages = ahead;
-      there_next = present(next, pages);
-      load_rows<T, D, N, true, false>(a, cache, pages, there_next, there_next == kAll, kd, vd, 0);
-      if (j + 2 * kAttnWaves < tiles) {
-        after = key_tile<KT>(it.keys, j + 2 * kAttnWaves);
-        ahead = find_pages<KT>(a, after);
-      }
+    any = next.count > 0;
+    typename CacheAt<T, D>::RowsAt at{};
+    bool asked = false;
+    if (any) {
+      at = cache.template find_rows<KT>(next, numbers, &there);
+      load_rows<T, D, N>(cache, at.k, cache.krow, kd, 0);
+      cur = next;
+      skip(kAttnWaves);
+      asked = next.count > 0;
+      if (asked) cache.template ask_pages<KT>(next, numbers);
     }
-    const int limit = cur.own ? mine - cur.base : KT;
-    const bool whole = there == kAll && (!cur.own || least >= cur.base + KT);
-    if (!whole) w.mask(s, limit, there, lane);
-    w.weigh(s, a.scale2);
-    if (more) wait_dma_but<N>();   // (the last of N + 1 where pages were looked up)
-    else wait_dma();
-    if (!whole) {
-      if (__any(clean_values<T, D, KT>(vl, there, lane, kWave))) {
-        w.add_odd_values(vl, s, limit, there, lane);
+    if (now) {
+      const int limit = was.own ? mine - was.base : KT;
+      const bool whole = was_there == kAll && (!was.own || least >= was.base + KT);
+      if (rarely(!whole)) w.mask(s, limit, was_there, lane);
+      w.weigh(s, scale2);
+      if (asked) wait_dma_but<N + 1>();
+      else if (any) wait_dma_but<N>();
+      else wait_dma();
+      if (rarely(!whole)) {
+        if (rarely(__any(clean_values<T, D, KT>(vl, was_there, lane, kWave)))) {
+          w.add_odd_values(vl, s, limit, was_there, lane);
+          wait_lds();
+          drop_odd_values<T, D, KT>(vl, lane, kWave);
+        }
         wait_lds();
-        drop_odd_values<T, D, KT>(vl, lane, kWave);
       }
+      w.values(vl, s, lane);
       wait_lds();
     }
-    w.values(vl, s, lane);
-    wait_lds();
-    if (more) load_rows<T, D, N, false, true>(a, cache, pages, there_next, there_next == kAll, kd, vd, 0);
-    cur = next;
-    next = after;
-    there = there_next;
+    if (any) load_rows<T, D, N>(cache, at.v, cache.vrow, vd, 0);
   }
   // the waves' results into one: every wave's maximum, then the scaled sums of 32 columns a wave
   w.l = half_sum(w.l);
@@ -724,7 +814,7 @@ __device__ __forceinline__ void attend_keys(const AttnArgs& a, const AttnItem& i
 #pragma unroll
     for (int i = 0; i < 4; ++i) o[4 * i4 + i] = sum[i];
   }
-  put_columns<T, D>(a, it, 0, o, wave, m, l, lane);
+  put_columns<T, D>(args_again(), it, 0, o, wave, m, l, lane);
 }
 
 // Largest n in [0, N) with cu[n] G / tile + n <= slot (see slot_seq).
