@@ -18,6 +18,8 @@
 // more than 8: p stays below 2^8, which neither bf16's range nor fp32 sums mind.
 #pragma once
 
+#include <type_traits>
+
 #include "gdn_varlen.h"
 
 namespace gdn {
@@ -328,11 +330,13 @@ template <typename T, int D, int N>
 __device__ __forceinline__ void load_rows(const CacheAt<T, D>& c, uint64_t rows_at, uint32_t row_off, lds_byte* to, int i0) {
   typedef KvRows<T, D> Rows;
   constexpr int RPD = Rows::kRowsPerDma;
+  uint32_t piece = c.piece;
+  asm volatile("" : "+v"(piece));   // offsets are made here, not kept in registers over the tiles
   if (!rarely(!c.dma_in_page)) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int r = (i0 + i) * RPD;
-      async_piece(uniform_at(rows_at, r), row_off + (c.piece ^ 16 * Rows::swz(r)), to + (i0 + i) * 1024);
+      async_piece(uniform_at(rows_at, r), row_off + (piece ^ 16 * Rows::swz(r)), to + (i0 + i) * 1024);
     }
   } else {
     const int lane = threadIdx.x % kWave;
@@ -340,38 +344,34 @@ __device__ __forceinline__ void load_rows(const CacheAt<T, D>& c, uint64_t rows_
     for (int i = 0; i < N; ++i) {
       const int r = (i0 + i) * RPD;
       const uint64_t at = lane_at(rows_at, r + lane / Rows::kPieces);
-      async_piece(reinterpret_cast<const void*>(at + (c.piece ^ 16 * Rows::swz(r))), to + (i0 + i) * 1024);
+      async_piece(reinterpret_cast<const void*>(at + (piece ^ 16 * Rows::swz(r))), to + (i0 + i) * 1024);
     }
   }
 }
 
-// Values of rows that are not there count as zeros.  Returns whether a row that is
-// holds an infinity or a NaN in this thread's part (of `threads` threads).
+// Values of rows that are not there count as zeros.  DROP: some rows of the item do
+// not see some keys (weight zero), so what is not finite must not enter the products
+// either; returns whether there was any in this thread's part (of `threads` threads),
+// for add_dropped.
 template <typename T, int D, int KT>
-__device__ __forceinline__ bool clean_values(char* vl, uint64_t there, int thread, int threads) {
+__device__ __forceinline__ bool clean_values(char* vl, uint64_t there, bool drop, int thread, int threads) {
   typedef KvRows<T, D> Rows;
   bool odd = false;
   asm volatile("" : "+v"(thread));
 #pragma unroll 1
   for (int p = thread; p < KT * Rows::kPieces; p += threads) {
     u32x4* at = reinterpret_cast<u32x4*>(vl + 16 * p);
-    if (there >> (p / Rows::kPieces) & 1) {
-      const u32x4 w = *at, f = finite_only<T>(w);
-      odd |= w[0] != f[0] || w[1] != f[1] || w[2] != f[2] || w[3] != f[3];
-    } else {
+    if (!(there >> (p / Rows::kPieces) & 1)) {
       *at = u32x4{0, 0, 0, 0};
+    } else if (drop) {
+      const u32x4 w = *at, f = finite_only<T>(w);
+      if (w[0] != f[0] || w[1] != f[1] || w[2] != f[2] || w[3] != f[3]) {
+        odd = true;
+        *at = f;
+      }
     }
   }
   return odd;
-}
-template <typename T, int D, int KT>
-__device__ __forceinline__ void drop_odd_values(char* vl, int thread, int threads) {
-  asm volatile("" : "+v"(thread));
-#pragma unroll 1
-  for (int p = thread; p < KT * KvRows<T, D>::kPieces; p += threads) {
-    u32x4* at = reinterpret_cast<u32x4*>(vl + 16 * p);
-    *at = finite_only<T>(*at);
-  }
 }
 
 // ---------------------------------------------------------------- a wave's rows
@@ -402,40 +402,17 @@ struct AttnWave {
       }
     }
   }
-  // S^T of the tile's NB blocks of 32 keys; operands are read a step ahead of their products
+  // The rows' maxima over NB blocks of scores; O and l follow where one moves.
   template <int NB>
-  __device__ __forceinline__ void scores(const char* kl, f32x16 (&s)[NB], int lane) const {
-    constexpr int U = D / 16;
-    int at = Rows::frag_start(lane);
-    asm volatile("" : "+v"(at));   // addresses are made here, not kept in registers over the tiles
-    R kf[2][NB];
-    const auto load = [&](int u) {
+  __device__ __forceinline__ void raise(const f32x16 (&s)[NB], float scale2) {
+    float t[4];
 #pragma unroll
-      for (int b = 0; b < NB; ++b) kf[u & 1][b] = Rows::frag_at(kl + 32 * b * Rows::kPitch, at ^ Rows::kFragStep * u);
-    };
+    for (int k = 0; k < 4; ++k) t[k] = s[0][k];
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[b][i] = 0.0f;
-    load(0);
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (u + 1 < U) load(u + 1);
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int b = 0; b < NB; ++b) s[b] = Mm<T>::mul(kf[u & 1][b], q[u], s[b]);
-      __builtin_amdgcn_sched_barrier(0);
-    }
-  }
-  // scores -> weights, for NB blocks of 32 keys
-  template <int NB>
-  __device__ __forceinline__ void weigh(f32x16 (&s)[NB], float scale2) {
-    float top = s[0][0];
-#pragma unroll
-    for (int b = 0; b < NB; ++b)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
-    top = half_max(top) * scale2;
+      for (int i = 0; i < 16; ++i) t[i % 4] = fmaxf(t[i % 4], s[b][i]);
+    const float top = half_max(fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]))) * scale2;
     // each row by itself: what one row meets does not change another's rounding
     const bool moves = top > m + 8.0f || m == -INFINITY;
     if (rarely(__any(moves))) {
@@ -448,18 +425,71 @@ struct AttnWave {
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[dt][i] *= keep;
     }
+  }
+  // Scores i0 .. i0 + 3 of the tile into weights; p[k]: operand of 16 keys.
+  template <int NB>
+  __device__ __forceinline__ void weigh4(f32x16 (&s)[NB], R (&p)[2 * NB], int i0, float scale2, float at, float (&sum)[4]) {
+    f32x16& x = s[i0 / 16];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      float& e = reinterpret_cast<float*>(&x)[i0 % 16 + k];
+      e = __builtin_amdgcn_exp2f(fmaf(e, scale2, -at));
+      sum[k] += e;
+    }
+    if (i0 % 8 == 4) {
+      float w[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) w[j] = x[i0 % 16 - 4 + j];
+      p[i0 / 8] = Mm<T>::pack(w);
+    }
+  }
+  template <int NB>
+  __device__ __forceinline__ void weigh(f32x16 (&s)[NB], R (&p)[2 * NB], float scale2) {
     const float at = m == -INFINITY ? 0.0f : m;
+    float sum[4] = {};
+#pragma unroll
+    for (int i = 0; i < 16 * NB; i += 4) weigh4(s, p, i, scale2, at, sum);
+    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+  }
+  // S^T of NB blocks of 32 keys; operands are read a step ahead of their products.
+  // With WEIGH the scores `s` become weights meanwhile: matrix and vector instructions
+  // take turns.
+  template <int NB, bool WEIGH>
+  __device__ __forceinline__ void scores(const char* kl, f32x16 (&next)[NB], f32x16 (&s)[NB], R (&p)[2 * NB], float scale2,
+                                         int lane) {
+    constexpr int U = D / 16, E = 16 * NB / U;   // scores for each step
+    int first = Rows::frag_start(lane);
+    asm volatile("" : "+v"(first));   // addresses are made here, not kept in registers over the tiles
+    R kf[2][NB];
+    const auto load = [&](int u) {
+#pragma unroll
+      for (int b = 0; b < NB; ++b) kf[u & 1][b] = Rows::frag_at(kl + 32 * b * Rows::kPitch, first ^ Rows::kFragStep * u);
+    };
+    const float at = m == -INFINITY ? 0.0f : m;
+    float sum[4] = {};
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        s[b][i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], scale2, -at));
-        l += s[b][i];
+      for (int i = 0; i < 16; ++i) next[b][i] = 0.0f;
+    load(0);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (u + 1 < U) load(u + 1);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int b = 0; b < NB; ++b) next[b] = Mm<T>::mul(kf[u & 1][b], q[u], next[b]);
+      if constexpr (WEIGH) {
+#pragma unroll
+        for (int e = 0; e < (E + 3) / 4; ++e)
+          if (E >= 4 || u % (4 / E) == 0) weigh4(s, p, E >= 4 ? E * u + 4 * e : 4 * (u / (4 / E)), scale2, at, sum);
       }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if constexpr (WEIGH) l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
   }
   // O^T += V^T P^T over the tile's NB blocks of 32 keys
   template <int NB>
-  __device__ __forceinline__ void values(const char* vl, const f32x16 (&p)[NB], int lane) {
+  __device__ __forceinline__ void values(const char* vl, const R (&p)[2 * NB], int lane) {
     constexpr int DT = D / 32, S = 2 * NB;
     int at = Rows::col_start(lane);
     asm volatile("" : "+v"(at));
@@ -473,12 +503,8 @@ struct AttnWave {
     for (int s = 0; s < S; ++s) {
       if (s + 1 < S) load(s + 1);
       __builtin_amdgcn_sched_barrier(0);
-      float w[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) w[j] = p[s / 2][8 * (s % 2) + j];
-      const R pf = Mm<T>::pack(w);
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt) o[dt] = Mm<T>::mul(vf[s & 1][dt], pf, o[dt]);
+      for (int dt = 0; dt < DT; ++dt) o[dt] = Mm<T>::mul(vf[s & 1][dt], p[s], o[dt]);
       __builtin_amdgcn_sched_barrier(0);
     }
   }
@@ -499,37 +525,6 @@ struct AttnWave {
       }
     }
   }
-  // Adds the values of a tile that are not finite to the rows that see them, element by
-  // element (they stay out of the product, where the weights of rows that do not are
-  // zero).  Rare, so small rather than fast.
-  template <int NB>
-  __device__ __forceinline__ void add_odd_values(const char* vl, const f32x16 (&p)[NB], int limit, uint64_t there, int lane) {
-    asm volatile("" : "+v"(lane));
-#pragma unroll 1
-    for (int key = 0; key < 32 * NB; ++key) {
-      bool odd = false;
-#pragma unroll
-      for (int d = 0; d < D / kWave; ++d) odd |= not_finite(Rows::elt(vl, key, kWave * d + lane));
-      if (!rarely(__any(odd))) continue;
-      // the key's weight: register 4 (key / 8) + key % 4 of half key / 4 % 2
-      const int reg = 16 * (key / 32) + 4 * (key % 32 / 8) + key % 4;
-      float pk = 0.0f;
-#pragma unroll
-      for (int b = 0; b < NB; ++b)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) pk = reg == 16 * b + i ? p[b][i] : pk;
-      pk = __shfl(pk, key / 4 % 2 * 32 + lane % 32, kWave);
-      const bool sees = key < limit && (there >> key & 1);
-#pragma unroll
-      for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const float x = Rows::elt(vl, key, 32 * dt + 8 * (i / 4) + 4 * (lane / 32) + i % 4);
-          if (sees && not_finite(x)) o[dt][i] = fmaf(pk, x, o[dt][i]);
-          if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);   // few registers, for the sake of the others
-        }
-    }
-  }
 };
 
 // Waits for this wave's LDS accesses; keeps memory accesses on their side of it.
@@ -542,11 +537,12 @@ struct AttnLds {
   static constexpr int kTileKeys = sizeof(T) == 2 ? 64 : 32;   // of a workgroup whose waves take rows of their own
   static constexpr int kTileBytes = kTileKeys * Rows::kPitch;
   static constexpr int kOwnBytes = 32 * Rows::kPitch;          // tiles of a wave that takes keys of its own
-  static constexpr int kRows = 4 * kTileBytes;                 // K and V, two of each
+  static constexpr int kOffV = 2 * kTileBytes;                 // two of K, then two of V
+  static constexpr int kRows = 4 * kTileBytes;
   static constexpr int kKeys = 2 * kAttnWaves * kOwnBytes;
   static constexpr int kMerge = kAttnWaves * D * kAttnRows * 4 + kAttnWaves * kAttnRows * 8;
   static constexpr int kMost = kRows > kKeys ? (kRows > kMerge ? kRows : kMerge) : (kKeys > kMerge ? kKeys : kMerge);
-  static constexpr int kOffOdd = kMost;                        // a word for each wave
+  static constexpr int kOffOdd = kMost;                        // a flag
   static constexpr int kOffPages = kOffOdd + 64;               // 64 page numbers for each wave
   static constexpr int kBytes = kOffPages + 4 * kAttnThreads;
 };
@@ -580,6 +576,33 @@ struct RowAt { int64_t token; int head; };
 __device__ __forceinline__ RowAt row_at(const AttnArgs& a, const AttnItem& it, int r) {
   const uint32_t row = it.row0 + r, token = row / static_cast<uint32_t>(a.groups);
   return {token, static_cast<int>(it.kvh * a.groups + (row - token * a.groups))};
+}
+
+// Adds the values that clean_values dropped to the outputs of the rows that see them:
+// a weight is positive, so what is not finite stays itself.  Own keys from the first
+// tile (of kt) that not all rows see; `limit`: the own keys that the lane's row sees;
+// o: NT column blocks from dt0 on.  Rare, so small rather than fast.
+template <typename T, int D, int NT>
+__device__ __forceinline__ void add_dropped(const AttnArgs& a, const AttnItem& it, f32x16 (&o)[NT], int dt0, int limit, int kt,
+                                            int lane) {
+  const int end = it.keys.first1 + it.keys.count1;
+  const char* head = static_cast<const char*>(a.v) + it.kvh * a.vh;
+#pragma unroll 1
+  for (int key = it.keys.first1 + max(own_limit(it, a.groups, 0) - it.keys.first1, 0) / kt * kt; key < end; ++key) {
+    asm volatile("" : "+v"(lane));   // addresses are made here, not kept in registers over the keys
+    const int page = it.keys.list1[key / a.page_size];
+    if (page < 0 || page >= a.num_pages) continue;
+    const T* row = reinterpret_cast<const T*>(
+        head + 16 * (static_cast<uint64_t>(page) * a.vp + static_cast<uint64_t>(key % a.page_size) * a.vt));
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float x = load_elt(row, 32 * (dt0 + t) + 8 * (i / 4) + 4 * (lane / 32) + i % 4);
+        if (key < limit && not_finite(x)) o[t][i] += x;
+        if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+      }
+  }
 }
 
 template <typename T, int D>
@@ -634,71 +657,77 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, const AttnItem& i
   w.clear();
   const bool idle = w0 >= it.rows;
   const int mine = own_limit(it, a.groups, r);
-  const int first = own_limit(it, a.groups, 0);   // the least of the workgroup, then the wave's least and most
-  const int least = __builtin_amdgcn_readfirstlane(own_limit(it, a.groups, min(w0, it.rows - 1))),
-            most = __builtin_amdgcn_readfirstlane(own_limit(it, a.groups, min(w0 + kAttnRows, it.rows) - 1));
+  const int first = own_limit(it, a.groups, 0);   // the least of the workgroup, then of the wave
+  const int least = __builtin_amdgcn_readfirstlane(own_limit(it, a.groups, min(w0, it.rows - 1)));
   lds_byte* dst = (lds_byte*)lds;
-  uint32_t* odds = reinterpret_cast<uint32_t*>(lds + L::kOffOdd);
+  uint32_t* odd = reinterpret_cast<uint32_t*>(lds + L::kOffOdd);   // values were dropped
+  if (threadIdx.x == 0) *odd = 0;
   const float scale2 = apart(a.scale2);
   const KeyRange keys = apart_range(it.keys);
   lds_byte* numbers = dst + L::kOffPages + 4 * kWave * wave;
   constexpr uint64_t kAll = KT == 64 ? ~0ull : (1ull << (KT % 64)) - 1;
-  // `cur` is looked at while `next` comes in, and the pages of the one after it
-  KeyTile cur{}, next = first_tile(keys);
-  uint64_t there = 0;
-  bool any = false;
-  int side = 0;   // the buffer of `cur`
-  if (next.count > 0) cache.template ask_pages<KT>(next, numbers);
-  while (any || next.count > 0) {
+  // While a tile's scores become weights and its values are added, the next one's
+  // scores are formed, the next one's V and the K of the one after that come in, and
+  // the pages of one more are looked up.  K and V of tile t lie in buffers t % 2.
+  struct State { int base; bool own, any; uint64_t there; };
+  State d0{}, d1{};   // the tile whose scores are formed, and the one whose K is here
+  uint64_t v1 = 0;    // rows of d1's V
+  KeyTile walk = first_tile(keys);
+  if (walk.count > 0) cache.template ask_pages<KT>(walk, numbers);
+  f32x16 sa[NB], sb[NB];
+  typename Mm<T>::R p[2 * NB];
+  // SIDE: the buffers of d0's V; s: its scores, then those of d1 in `next`
+  const auto step = [&](auto side, f32x16 (&s)[NB], f32x16 (&next)[NB]) {
+    constexpr int SIDE = decltype(side)::value;
     wait_dma();
     lds_barrier();
-    const bool now = any;
-    const KeyTile was = cur;
-    const uint64_t was_there = there;
-    any = next.count > 0;
-    if (any) {
-      const auto at = cache.template find_rows<KT>(next, numbers, &there);
-      lds_byte* to = dst + (side ^ 1) * 2 * L::kTileBytes;
-      load_rows<T, D, N>(cache, at.k, cache.krow, to, N * wave);
-      load_rows<T, D, N>(cache, at.v, cache.vrow, to + L::kTileBytes, N * wave);
-      cur = next;
-      next_tile<KT>(keys, next);
-      if (next.count > 0) cache.template ask_pages<KT>(next, numbers);
+    State d2{};
+    uint64_t v2 = 0;
+    if (d1.any) load_rows<T, D, N>(cache, v1, cache.vrow, dst + L::kOffV + (SIDE ^ 1) * L::kTileBytes, N * wave);
+    if (walk.count > 0) {
+      const auto at = cache.template find_rows<KT>(walk, numbers, &d2.there);
+      load_rows<T, D, N>(cache, at.k, cache.krow, dst + SIDE * L::kTileBytes, N * wave);
+      v2 = at.v;
+      d2.base = walk.base;
+      d2.own = walk.own;
+      d2.any = true;
+      next_tile<KT>(keys, walk);
+      if (walk.count > 0) cache.template ask_pages<KT>(walk, numbers);
     }
-    const char* kl = lds + side * 2 * L::kTileBytes;
-    char* vl = lds + side * 2 * L::kTileBytes + L::kTileBytes;
-    side ^= 1;
-    if (!now) continue;
+    const char* kl = lds + (SIDE ^ 1) * L::kTileBytes;
+    char* vl = lds + L::kOffV + SIDE * L::kTileBytes;
     // tiles that some rows of the workgroup do not see whole
-    bool odd = false;
-    if (rarely(was_there != kAll || (was.own && first < was.base + KT))) {
-      const bool found = clean_values<T, D, KT>(vl, was_there, threadIdx.x, kAttnThreads);
-      if (lane == 0) odds[wave] = 0;
-      if (found) odds[wave] = 1;
+    const bool partly = d0.own && first < d0.base + KT;
+    if (rarely(d0.any && (d0.there != kAll || partly))) {
+      if (clean_values<T, D, KT>(vl, d0.there, partly, threadIdx.x, kAttnThreads)) *odd = 1;
       lds_barrier();
-#pragma unroll
-      for (int x = 0; x < kAttnWaves; ++x) odd |= odds[x] != 0;
-      odd = __builtin_amdgcn_readfirstlane(odd);
+      if (d0.there != kAll || least < d0.base + KT) w.mask(s, d0.own ? mine - d0.base : KT, d0.there, lane);
     }
-    const bool active = !idle && !(was.own && most <= was.base);
-    const int limit = was.own ? mine - was.base : KT;
-    f32x16 s[NB];
-    if (active) {
-      w.scores(kl, s, lane);
-      if (rarely(was_there != kAll || (was.own && least < was.base + KT))) w.mask(s, limit, was_there, lane);
-      w.weigh(s, scale2);
+    if (!idle) {
+      if (!d0.any) {
+        if (d1.any) w.template scores<NB, false>(kl, next, s, p, scale2, lane);
+      } else {
+        w.raise(s, scale2);
+        if (d1.any) w.template scores<NB, true>(kl, next, s, p, scale2, lane);
+        else w.weigh(s, p, scale2);
+      }
     }
-    if (rarely(odd)) {
-      if (active) w.add_odd_values(vl, s, limit, was_there, lane);
-      lds_barrier();
-      drop_odd_values<T, D, KT>(vl, threadIdx.x, kAttnThreads);
-      lds_barrier();
-    }
-    if (active) w.values(vl, s, lane);
+    if (!idle && d0.any) w.template values<NB>(vl, p, lane);
+    d0 = d1;
+    d1 = d2;
+    v1 = v2;
+  };
+  while (true) {
+    step(std::integral_constant<int, 0>(), sa, sb);
+    if (!(d0.any || d1.any)) break;
+    step(std::integral_constant<int, 1>(), sb, sa);
+    if (!(d0.any || d1.any)) break;
   }
+  lds_barrier();
   if (idle) return;
   w.l = half_sum(w.l);
   const AttnArgs e = args_again();
+  if (rarely(__builtin_amdgcn_readfirstlane(*odd) != 0)) add_dropped<T, D>(e, it, w.o, 0, mine, KT, lane);
 #pragma unroll
   for (int dt = 0; dt < D / 32; ++dt) put_columns<T, D>(e, it, wave, w.o[dt], dt, w.m, w.l, lane);
 }
@@ -722,6 +751,9 @@ __device__ __forceinline__ void attend_keys(const AttnArgs& a, const AttnItem& i
   lds_byte* vd = kd + L::kOwnBytes;
   const float scale2 = apart(a.scale2);
   const KeyRange keys = apart_range(it.keys);
+  uint32_t* odd = reinterpret_cast<uint32_t*>(lds + L::kOffOdd);   // values were dropped
+  if (threadIdx.x == 0) *odd = 0;
+  lds_barrier();
   lds_byte* numbers = (lds_byte*)lds + L::kOffPages + 4 * kWave * wave;
   constexpr uint64_t kAll = 0xFFFFFFFFull;
   // K of the next tile is on its way while the weights are made, its V while the next
@@ -743,7 +775,8 @@ __device__ __forceinline__ void attend_keys(const AttnArgs& a, const AttnItem& i
     const uint64_t was_there = there;
     if (now) wait_dma_but<N>();   // its K and the next one's pages are here, V may be on its way
     f32x16 s[1];
-    if (now) w.scores(kl, s, lane);
+    typename Mm<T>::R p[2];
+    if (now) w.template scores<1, false>(kl, s, s, p, scale2, lane);
     wait_lds();
     any = next.count > 0;
     typename CacheAt<T, D>::RowsAt at{};
@@ -760,19 +793,16 @@ __device__ __forceinline__ void attend_keys(const AttnArgs& a, const AttnItem& i
       const int limit = was.own ? mine - was.base : KT;
       const bool whole = was_there == kAll && (!was.own || least >= was.base + KT);
       if (rarely(!whole)) w.mask(s, limit, was_there, lane);
-      w.weigh(s, scale2);
+      w.raise(s, scale2);
+      w.weigh(s, p, scale2);
       if (asked) wait_dma_but<N + 1>();
       else if (any) wait_dma_but<N>();
       else wait_dma();
       if (rarely(!whole)) {
-        if (rarely(__any(clean_values<T, D, KT>(vl, was_there, lane, kWave)))) {
-          w.add_odd_values(vl, s, limit, was_there, lane);
-          wait_lds();
-          drop_odd_values<T, D, KT>(vl, lane, kWave);
-        }
+        if (clean_values<T, D, KT>(vl, was_there, was.own && least < was.base + KT, lane, kWave)) *odd = 1;
         wait_lds();
       }
-      w.values(vl, s, lane);
+      w.template values<1>(vl, p, lane);
       wait_lds();
     }
     if (any) load_rows<T, D, N>(cache, at.v, cache.vrow, vd, 0);
@@ -801,7 +831,7 @@ __device__ __forceinline__ void attend_keys(const AttnArgs& a, const AttnItem& i
     f[x] = __builtin_amdgcn_exp2f(ml[0] - base);
     l = fmaf(f[x], ml[1], l);
   }
-  f32x16 o;
+  f32x16 o[1];
 #pragma unroll
   for (int i4 = 0; i4 < 4; ++i4) {
     f32x4 sum = zero4();
@@ -812,9 +842,11 @@ __device__ __forceinline__ void attend_keys(const AttnArgs& a, const AttnItem& i
       for (int i = 0; i < 4; ++i) sum[i] = fmaf(f[x], p[i], sum[i]);
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) o[4 * i4 + i] = sum[i];
+    for (int i = 0; i < 4; ++i) o[0][4 * i4 + i] = sum[i];
   }
-  put_columns<T, D>(args_again(), it, 0, o, wave, m, l, lane);
+  const AttnArgs e = args_again();
+  if (rarely(__builtin_amdgcn_readfirstlane(*odd) != 0)) add_dropped<T, D>(e, it, o, wave, mine, KT, lane);
+  put_columns<T, D>(e, it, 0, o[0], wave, m, l, lane);
 }
 
 // Largest n in [0, N) with cu[n] G / tile + n <= slot (see slot_seq).
