@@ -26,7 +26,7 @@ gdn_status launch_attn(const AttnArgs& a, const AttnPlan& p, hipStream_t stream)
   static_assert(kAttnRows == kPlanRows && kAttnTile == kPlanTile, "the plan's tiles");
   hipLaunchKernelGGL((k_attn<T, D>), dim3(static_cast<uint32_t>(p.shared_items + p.own_items)), dim3(kAttnThreads), 0, stream, a);
   if (p.joined) {
-    const int64_t tiles = (p.rows + kAttnRows - 1) / kAttnRows * a.kv_heads;
+    const int64_t tiles = (p.rows + kAttnRows - 1) / kAttnRows * a.kv_heads * (D / 8 / kAttnWaves);
     hipLaunchKernelGGL((k_attn_join<T, D>), dim3(static_cast<uint32_t>(tiles)), dim3(kAttnThreads), 0, stream, a);
   }
   const hipError_t e = hipGetLastError();

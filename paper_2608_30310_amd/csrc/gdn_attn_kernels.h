@@ -910,16 +910,17 @@ void k_attn(AttnArgs a) {
   else attend_rows<T, D>(a, it, cache, lds);
 }
 
-// The items' partial results of a row into one.  A workgroup takes 32 packed rows
-// of a K/V head, a wave D / 32 of the D / 8 groups of columns: lane (h, r) four
-// columns of row r.
+// The items' partial results of a row into one.  A wave takes 32 packed rows of a K/V
+// head and one of the D / 8 groups of columns: lane (h, r) four columns of row r.
+// kAttnAhead parts' loads are in flight at a time.
+constexpr int kAttnAhead = 8;
 template <typename T, int D>
 __global__ __launch_bounds__(kAttnThreads)
 void k_attn_join(AttnArgs a) {
-  constexpr int C = D / 8 / kAttnWaves;
+  constexpr int GROUPS = D / 8 / kAttnWaves;   // workgroups of a wave tile
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
-  const int kvh = blockIdx.x % a.kv_heads;
-  const int wt = blockIdx.x / a.kv_heads;
+  const int unit = blockIdx.x / GROUPS, col = blockIdx.x % GROUPS * kAttnWaves + wave;
+  const int kvh = unit % a.kv_heads, wt = unit / a.kv_heads;
   const bool there = wt * kAttnRows + lane % 32 < a.rows;
   const int row = there ? wt * kAttnRows + lane % 32 : a.rows - 1;
   const int token = static_cast<int>(static_cast<uint32_t>(row) / static_cast<uint32_t>(a.groups));
@@ -931,55 +932,60 @@ void k_attn_join(AttnArgs a) {
   }
   const int first = a.cu[lo] * a.groups, rs = row - first;
   const int slot = first / a.own_tile + lo + rs / a.own_tile;
-  // wave tiles of the shared items are this workgroup's rows, those of the own ones are found by sequence
-  const auto tile_of = [&](int s) {
-    if (s < a.shared_splits)
-      return ((static_cast<int64_t>(s) * a.shared_tiles + wt / kAttnWaves) * a.kv_heads + kvh) * kAttnWaves + wt % kAttnWaves;
-    return static_cast<int64_t>(a.shared_items) * kAttnWaves +
-           ((static_cast<int64_t>(slot) * a.own_splits + (s - a.shared_splits)) * a.kv_heads + kvh) * (a.own_tile / kAttnRows) +
-           rs % a.own_tile / kAttnRows;
-  };
-  const auto lane_of = [&](int s) { return s < a.shared_splits ? lane % 32 : rs % kAttnRows; };
+  // the row among the wave tiles of part s: those of the shared items are these rows,
+  // those of the own ones are found by sequence
+  const int64_t shared0 = (static_cast<int64_t>(wt / kAttnWaves) * a.kv_heads + kvh) * kAttnWaves + wt % kAttnWaves,
+                shared_step = static_cast<int64_t>(a.shared_tiles) * a.kv_heads * kAttnWaves,
+                own0 = static_cast<int64_t>(a.shared_items) * kAttnWaves +
+                       (static_cast<int64_t>(slot) * a.own_splits * a.kv_heads + kvh) * (a.own_tile / kAttnRows) +
+                       rs % a.own_tile / kAttnRows,
+                own_step = static_cast<int64_t>(a.kv_heads) * (a.own_tile / kAttnRows);
+  const auto tile_of = [&](int s) { return s < a.shared_splits ? shared0 + s * shared_step : own0 + (s - a.shared_splits) * own_step; };
+  const auto row_of = [&](int s) { return s < a.shared_splits ? lane % 32 : rs % kAttnRows; };
   const int parts = a.shared_splits + a.own_splits;
-  float m = -INFINITY;
-  for (int s = 0; s < parts; ++s) m = fmaxf(m, a.part_ml[tile_of(s) * kAttnRows + lane_of(s)][0]);
-  const float at = m == -INFINITY ? 0.0f : m;
-  float l = 0.0f;
-  f32x4 sum[C];
+  float m = -INFINITY, l = 0.0f;
+  f32x4 sum = zero4();
+  for (int s0 = 0; s0 < parts; s0 += kAttnAhead) {
+    f32x2 ml[kAttnAhead];
+    f32x4 x[kAttnAhead];
 #pragma unroll
-  for (int c = 0; c < C; ++c) sum[c] = zero4();
-  for (int s = 0; s < parts; ++s) {
-    const int64_t t = tile_of(s);
-    const int r = lane_of(s);
-    const f32x2 ml = a.part_ml[t * kAttnRows + r];
-    if (ml[1] == 0.0f) continue;   // nothing seen there (nor anything written)
-    const float f = __builtin_amdgcn_exp2f(ml[0] - at);
-    l = fmaf(f, ml[1], l);
-    const f32x4* p = a.part + (t * (D / 8) + C * wave) * kWave + lane / 32 * 32 + r;
+    for (int k = 0; k < kAttnAhead; ++k) {
+      const int s = min(s0 + k, parts - 1);
+      const int64_t t = tile_of(s);
+      ml[k] = a.part_ml[t * kAttnRows + row_of(s)];
+      x[k] = a.part[(t * (D / 8) + col) * kWave + lane / 32 * 32 + row_of(s)];
+    }
+    float top = m;
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-      const f32x4 x = p[c * kWave];
+    for (int k = 0; k < kAttnAhead; ++k) top = s0 + k < parts ? fmaxf(top, ml[k][0]) : top;
+    const float at = top == -INFINITY ? 0.0f : top, keep = __builtin_amdgcn_exp2f(m - at);
+    m = top;
+    l *= keep;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) sum[c][i] = fmaf(f, x[i], sum[c][i]);
+    for (int i = 0; i < 4; ++i) sum[i] *= keep;
+#pragma unroll
+    for (int k = 0; k < kAttnAhead; ++k) {
+      if (s0 + k >= parts || ml[k][1] == 0.0f) continue;   // nothing seen there (nor anything written)
+      const float f = __builtin_amdgcn_exp2f(ml[k][0] - at);
+      l = fmaf(f, ml[k][1], l);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sum[i] = fmaf(f, x[k][i], sum[i]);
     }
   }
   if (!there) return;
   const int head = kvh * a.groups + (row - token * a.groups);
-  T* out = static_cast<T*>(a.out) + token * a.ldo + static_cast<int64_t>(head) * D + 8 * C * wave + 4 * (lane / 32);
+  T* out = static_cast<T*>(a.out) + token * a.ldo + static_cast<int64_t>(head) * D + 8 * col + 4 * (lane / 32);
   const float inv = 1.0f / l;
+  float y[4];
 #pragma unroll
-  for (int c = 0; c < C; ++c) {
-    float x[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = l == 0.0f ? 0.0f : sum[c][i] * inv;
-    if constexpr (sizeof(T) == 2) {
-      u32x2 w;
-      w[0] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{x[0], x[1]}), bf16x2));
-      w[1] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{x[2], x[3]}), bf16x2));
-      *reinterpret_cast<u32x2*>(out + 8 * c) = w;
-    } else {
-      *reinterpret_cast<f32x4*>(out + 8 * c) = f32x4{x[0], x[1], x[2], x[3]};
-    }
+  for (int i = 0; i < 4; ++i) y[i] = l == 0.0f ? 0.0f : sum[i] * inv;
+  if constexpr (sizeof(T) == 2) {
+    u32x2 w;
+    w[0] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{y[0], y[1]}), bf16x2));
+    w[1] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{y[2], y[3]}), bf16x2));
+    *reinterpret_cast<u32x2*>(out) = w;
+  } else {
+    *reinterpret_cast<f32x4*>(out) = f32x4{y[0], y[1], y[2], y[3]};
   }
 }
 

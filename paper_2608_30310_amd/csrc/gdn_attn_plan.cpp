@@ -173,19 +173,21 @@ gdn_status make_attn_plan(const gdn_attn_shape* s, const int32_t* cu, AttnPlan* 
   int64_t tiles = 0;
   for (int64_t n = 0; n < N; ++n) tiles += ((static_cast<int64_t>(cu[n + 1]) - cu[n]) * G + p.own_tile - 1) / p.own_tile;
   p.own_slots = tile_slots(p.rows, N, p.own_tile);
-  const auto pieces = [](int64_t keys, int64_t items, int32_t* splits, int32_t* chunk) {
+  const auto pieces = [](int64_t keys, int64_t items, int64_t places, int32_t* splits, int32_t* chunk) {
     const int64_t most = std::max<int64_t>(1, (keys + kLeastChunk - 1) / kLeastChunk);
-    int64_t n = std::min(most, std::max<int64_t>(1, kAttnPlaces / std::max<int64_t>(1, items)));
+    int64_t n = std::min(most, std::max<int64_t>(1, places / std::max<int64_t>(1, items)));
     const int64_t each = std::max<int64_t>(64, ((keys + n - 1) / n + 63) / 64 * 64);
     *chunk = static_cast<int32_t>(each);
     *splits = static_cast<int32_t>(std::max<int64_t>(1, (keys + each - 1) / each));
   };
   if (P > 0 && (tiles * H < kAttnPlaces || p.rows < tiles * p.own_tile * 3 / 5)) {
     p.shared_tiles = (p.rows + kPlanTile - 1) / kPlanTile;
-    pieces(P, p.shared_tiles * H, &p.shared_splits, &p.shared_chunk);
+    // one workgroup a CU: the other place is for own items, which wait for memory while
+    // these compute
+    pieces(P, p.shared_tiles * H, kAttnPlaces / 2, &p.shared_splits, &p.shared_chunk);
     p.shared_items = p.shared_tiles * H * p.shared_splits;
   }
-  if (P == 0 || p.shared_items > 0) pieces(p.max_len, tiles * H, &p.own_splits, &p.own_chunk);
+  if (P == 0 || p.shared_items > 0) pieces(p.max_len, tiles * H, kAttnPlaces, &p.own_splits, &p.own_chunk);
   else p.own_chunk = (p.max_len + 63) / 64 * 64;
   p.own_items = p.own_slots * H * p.own_splits;
   p.joined = p.shared_items > 0 || p.own_splits > 1;
