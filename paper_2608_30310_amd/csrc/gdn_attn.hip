@@ -23,10 +23,11 @@ bool a_stride_fits(int64_t units) { return units < int64_t{1} << 24; }
 
 template <typename T, int D>
 gdn_status launch_attn(const AttnArgs& a, const AttnPlan& p, hipStream_t stream) {
-  static_assert(kAttnRows == kPlanRows && kAttnTile == kPlanTile, "the plan's tiles");
-  hipLaunchKernelGGL((k_attn<T, D>), dim3(static_cast<uint32_t>(p.shared_items + p.own_items)), dim3(kAttnThreads), 0, stream, a);
+  static_assert(kAttnRows == kPlanRows && kAttnTile == kPlanTile && kLineTile == kPlanLineTile && kStreamSeqs == kPlanLineSeqs,
+                "the plan's tiles");
+  hipLaunchKernelGGL((k_attn<T, D>), dim3(static_cast<uint32_t>(p.grid)), dim3(kAttnThreads), 0, stream, a);
   if (p.joined) {
-    const int64_t tiles = (p.rows + kAttnRows - 1) / kAttnRows * a.kv_heads * (D / 8 / kAttnWaves);
+    const int64_t tiles = (p.rows + kAttnRows - 1) / kAttnRows * a.kv_heads * (D / 8);
     hipLaunchKernelGGL((k_attn_join<T, D>), dim3(static_cast<uint32_t>(tiles)), dim3(kAttnThreads), 0, stream, a);
   }
   const hipError_t e = hipGetLastError();
@@ -104,6 +105,7 @@ gdn_status gdn_prefix_attention(const gdn_attn_shape* shape, const int32_t* cu_s
   a.shared_tiles = static_cast<int32_t>(p.shared_tiles), a.shared_items = static_cast<int32_t>(p.shared_items);
   a.own_tile = p.own_tile, a.own_splits = p.own_splits, a.own_chunk = p.own_chunk;
   a.own_slots = static_cast<int32_t>(p.own_slots), a.rows = static_cast<int32_t>(p.rows);
+  a.shared_wt = p.shared_wt, a.stream = p.stream, a.stream_first = p.stream_first, a.stream_waves = p.stream_waves;
   a.cu = cu_seqlens, a.table = table, a.lens = lens, a.prefix_pages = prefix_pages;
   a.q = q, a.k = k_cache, a.v = v_cache, a.out = out, a.ldq = s.ld_q, a.ldo = s.ld_out;
   a.kp = units(s.k_page), a.kt = units(s.k_token), a.vp = units(s.v_page), a.vt = units(s.v_token);
@@ -111,6 +113,7 @@ gdn_status gdn_prefix_attention(const gdn_attn_shape* shape, const int32_t* cu_s
   if (p.joined) {
     a.part = static_cast<f32x4*>(workspace);
     a.part_ml = reinterpret_cast<f32x2*>(static_cast<char*>(workspace) + p.off_ml);
+    a.line = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + p.off_line);
   }
   const hipStream_t hs = static_cast<hipStream_t>(stream);
   if (s.dtype == GDN_BF16) return s.head_dim == 64 ? launch_attn<uint16_t, 64>(a, p, hs) : launch_attn<uint16_t, 128>(a, p, hs);

@@ -31,6 +31,8 @@ constexpr int kAttnWaves = kAttnThreads / kWave;
 constexpr int kAttnRows = 32;                        // of a wave
 constexpr int kAttnTile = kAttnRows * kAttnWaves;    // of a workgroup whose waves take rows of their own
 
+constexpr int kStreamSeqs = 1024;                    // sequences of a line (see there)
+
 struct AttnArgs {
   int32_t n_seqs, kv_heads, groups, num_pages, page_size, width, prefix_len, max_len;
   uint32_t page_mul;      // n / page_size = mulhi(n, page_mul) >> page_shift (page_size > 1)
@@ -41,6 +43,10 @@ struct AttnArgs {
   // items: shared ones over the prefix alone, all rows packed (shared_splits 0: none), then own ones
   int32_t shared_splits, shared_chunk, shared_tiles, shared_items;
   int32_t own_tile, own_splits, own_chunk, own_slots;
+  int32_t shared_wt;      // wave tiles of a shared item: kAttnWaves, or 1 (a wave's)
+  // stream (see there): stream_waves waves from workgroup stream_first on share the own tokens out
+  int32_t stream, stream_first, stream_waves;
+  int32_t* line;          // [N + 1]
   int32_t rows;           // T G
   const int32_t* cu;
   const int32_t* table;
@@ -53,7 +59,7 @@ struct AttnArgs {
   int64_t ldq, ldo;
   uint32_t kp, kt, vp, vt;   // strides of the caches' pages and tokens, in 16 bytes
   int64_t kh, vh;            // of their heads, in bytes
-  // partial results of the items (NULL: items write out): shared ones, then own ones
+  // partial results of the items: shared ones, then own ones
   f32x4* part;            // [item][wave tile][D / 8][lane]: four columns of a row
   f32x2* part_ml;         // [item][wave tile][32]: m and l of a row
 };
@@ -251,8 +257,18 @@ __device__ __forceinline__ void async_word(const void* src, lds_byte* dst) {   /
 // every use restores a whole tuple).
 template <typename X>
 __device__ __forceinline__ X apart(X x) {
-  asm("" : "+s"(x));
-  return x;
+  static_assert(sizeof(X) == 4 || sizeof(X) == 8, "one or two registers");
+  if constexpr (sizeof(X) == 4) {
+    uint32_t u = __builtin_amdgcn_readfirstlane(__builtin_bit_cast(uint32_t, x));
+    asm("" : "+s"(u));
+    return __builtin_bit_cast(X, u);
+  } else {
+    const uint64_t u = __builtin_bit_cast(uint64_t, x);
+    uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(u)),
+             hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(u >> 32));
+    asm("" : "+s"(lo), "+s"(hi));
+    return __builtin_bit_cast(X, static_cast<uint64_t>(hi) << 32 | lo);
+  }
 }
 // Where a K/V head's rows are in the caches, and a lane's place in a DMA of
 // kRowsPerDma rows: the swizzle is linear over XOR, so piece p of row r + j (r a
@@ -542,9 +558,10 @@ struct AttnLds {
   static constexpr int kKeys = 2 * kAttnWaves * kOwnBytes;
   static constexpr int kMerge = kAttnWaves * D * kAttnRows * 4 + kAttnWaves * kAttnRows * 8;
   static constexpr int kMost = kRows > kKeys ? (kRows > kMerge ? kRows : kMerge) : (kKeys > kMerge ? kKeys : kMerge);
-  static constexpr int kOffOdd = kMost;                        // a flag
+  static constexpr int kOffOdd = kMost;                        // a flag for each wave
   static constexpr int kOffPages = kOffOdd + 64;               // 64 page numbers for each wave
-  static constexpr int kBytes = kOffPages + 4 * kAttnThreads;
+  static constexpr int kOffLine = kOffPages + 4 * kAttnThreads;
+  static constexpr int kBytes = kOffLine + 4 * (kStreamSeqs + 1);
 };
 
 // The kernel's arguments, loaded anew: what is used at the end alone is not kept in
@@ -562,7 +579,7 @@ struct AttnItem {
   int len, tail;       // own tokens; row r of the item is token (row0 + r) / G, and sees own tokens below
   int first_row;       // tail + 1 + (row0 + r - first_row) / G
   KeyRange keys;
-  int64_t part;        // its first wave tile among the partial results
+  int64_t part;        // its first wave tile among the partial results; < 0: it writes out
 };
 
 // Own tokens that row r of the item sees.
@@ -632,7 +649,7 @@ template <typename T, int D>
 __device__ __forceinline__ void put_columns(const AttnArgs& a, const AttnItem& it, int wt, const f32x16& o, int dt, float m, float l,
                                             int lane) {
   const int r = kAttnRows * wt + lane % 32;
-  if (!a.part) {
+  if (it.part < 0) {
     store_out<T, D>(a, it, o, dt, l, r, lane);
     return;
   }
@@ -732,9 +749,10 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, const AttnItem& i
   for (int dt = 0; dt < D / 32; ++dt) put_columns<T, D>(e, it, wave, w.o[dt], dt, w.m, w.l, lane);
 }
 
-// At most 32 rows: waves take keys of their own, and their results are joined.
+// At most 32 rows.  JOIN: the waves take every fourth tile of the keys each, and their
+// results are joined; else the item is this wave's alone.
 template <typename T, int D>
-__device__ __forceinline__ void attend_keys(const AttnArgs& a, const AttnItem& it, const CacheAt<T, D>& cache, char* lds) {
+__device__ __forceinline__ void attend_keys(const AttnArgs& a, const AttnItem& it, const CacheAt<T, D>& cache, bool join, char* lds) {
   typedef AttnLds<T, D> L;
   typedef typename L::Rows Rows;
   constexpr int KT = 32, N = KT / Rows::kRowsPerDma;
@@ -751,9 +769,8 @@ __device__ __forceinline__ void attend_keys(const AttnArgs& a, const AttnItem& i
   lds_byte* vd = kd + L::kOwnBytes;
   const float scale2 = apart(a.scale2);
   const KeyRange keys = apart_range(it.keys);
-  uint32_t* odd = reinterpret_cast<uint32_t*>(lds + L::kOffOdd);   // values were dropped
-  if (threadIdx.x == 0) *odd = 0;
-  lds_barrier();
+  bool odd = false;   // values were dropped
+  const int step = join ? kAttnWaves : 1;
   lds_byte* numbers = (lds_byte*)lds + L::kOffPages + 4 * kWave * wave;
   constexpr uint64_t kAll = 0xFFFFFFFFull;
   // K of the next tile is on its way while the weights are made, its V while the next
@@ -762,7 +779,7 @@ __device__ __forceinline__ void attend_keys(const AttnArgs& a, const AttnItem& i
   const auto skip = [&](int n) {
     for (int i = 0; i < n && next.count > 0; ++i) next_tile<KT>(keys, next);
   };
-  skip(wave);
+  skip(join ? wave : 0);
   uint64_t there = 0;
   bool any = false;
   if (next.count > 0) {
@@ -785,7 +802,7 @@ __device__ __forceinline__ void attend_keys(const AttnArgs& a, const AttnItem& i
       at = cache.template find_rows<KT>(next, numbers, &there);
       load_rows<T, D, N>(cache, at.k, cache.krow, kd, 0);
       cur = next;
-      skip(kAttnWaves);
+      skip(step);
       asked = next.count > 0;
       if (asked) cache.template ask_pages<KT>(next, numbers);
     }
@@ -799,7 +816,7 @@ __device__ __forceinline__ void attend_keys(const AttnArgs& a, const AttnItem& i
       else if (any) wait_dma_but<N>();
       else wait_dma();
       if (rarely(!whole)) {
-        if (clean_values<T, D, KT>(vl, was_there, was.own && least < was.base + KT, lane, kWave)) *odd = 1;
+        odd |= clean_values<T, D, KT>(vl, was_there, was.own && least < was.base + KT, lane, kWave);
         wait_lds();
       }
       w.template values<1>(vl, p, lane);
@@ -807,11 +824,21 @@ __device__ __forceinline__ void attend_keys(const AttnArgs& a, const AttnItem& i
     }
     if (any) load_rows<T, D, N>(cache, at.v, cache.vrow, vd, 0);
   }
-  // the waves' results into one: every wave's maximum, then the scaled sums of 32 columns a wave
   w.l = half_sum(w.l);
+  odd = __any(odd);
+  if (!join) {
+    const AttnArgs e = args_again();
+    if (rarely(odd)) add_dropped<T, D>(e, it, w.o, 0, mine, KT, lane);
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt) put_columns<T, D>(e, it, 0, w.o[dt], dt, w.m, w.l, lane);
+    return;
+  }
+  // the waves' results into one: every wave's maximum, then the scaled sums of 32 columns a wave
+  uint32_t* odds = reinterpret_cast<uint32_t*>(lds + L::kOffOdd);
   f32x4* os = reinterpret_cast<f32x4*>(lds);   // [wave][D / 8][lane]
   f32x2* mls = reinterpret_cast<f32x2*>(lds + kAttnWaves * D * kAttnRows * 4);
   lds_barrier();
+  if (lane == 0) odds[wave] = odd;
   if (lane < 32) mls[wave * kAttnRows + lane] = f32x2{w.m, w.l};
 #pragma unroll
   for (int dt = 0; dt < D / 32; ++dt)
@@ -844,8 +871,10 @@ __device__ __forceinline__ void attend_keys(const AttnArgs& a, const AttnItem& i
 #pragma unroll
     for (int i = 0; i < 4; ++i) o[0][4 * i4 + i] = sum[i];
   }
+#pragma unroll
+  for (int x = 0; x < kAttnWaves; ++x) odd |= odds[x] != 0;
   const AttnArgs e = args_again();
-  if (rarely(__builtin_amdgcn_readfirstlane(*odd) != 0)) add_dropped<T, D>(e, it, o, wave, mine, KT, lane);
+  if (rarely(__builtin_amdgcn_readfirstlane(odd))) add_dropped<T, D>(e, it, o, wave, mine, KT, lane);
   put_columns<T, D>(e, it, 0, o[0], wave, m, l, lane);
 }
 
@@ -864,62 +893,207 @@ __device__ __forceinline__ int row_slot_seq(const int32_t* __restrict__ cu, int 
   return __builtin_amdgcn_readfirstlane(lo);
 }
 
+// Batches of a few rows a sequence (own_tile 32: single tokens): lengths differ, and
+// the last long sequence would keep the memory waiting.  So the own tokens of all
+// sequences and K/V heads, in tiles of 32 keys, [sequence][K/V head][tile], are one
+// line, of which each wave takes an equal share: the end of one sequence's, all of some,
+// the beginning of another's.  Waves work alone, without barriers, so that the start of
+// one share (offsets, pages, first rows: one memory access after another) hides behind
+// the others' loads.  A sequence that is one wave's is done (or one part of it is, where
+// there is a prefix); of one that is shared out each wave leaves its part: the first of
+// them at 2 wave + 1, the others at 2 wave.
+constexpr int kLineTile = 32;
+
+// The line of one K/V head in LDS: line[n] tiles before sequence n (which has one where
+// it has queries but no tokens), line[N] in all.
+template <typename T, int D>
+__device__ __forceinline__ void lay_line(const AttnArgs& a, char* lds) {
+  int* line = reinterpret_cast<int*>(lds + AttnLds<T, D>::kOffLine);
+  int* sums = reinterpret_cast<int*>(lds);
+  const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+  int total = 0;
+  for (int n0 = 0; n0 < a.n_seqs; n0 += kAttnThreads) {
+    const int n = n0 + threadIdx.x;
+    int mine = 0;
+    if (n < a.n_seqs && a.cu[n + 1] > a.cu[n])
+      mine = max(1, (min(max(a.lens[n], 0), a.max_len) + kLineTile - 1) / kLineTile);
+    int up_to = mine;   // inclusive sums over the wave
+#pragma unroll
+    for (int off = 1; off < kWave; off <<= 1) {
+      const int up = __shfl_up(up_to, off, kWave);
+      up_to += lane >= off ? up : 0;
+    }
+    if (lane == kWave - 1) sums[wave] = up_to;
+    lds_barrier();
+    int before = total;
+#pragma unroll
+    for (int w = 0; w < kAttnWaves; ++w) {
+      before += w < wave ? sums[w] : 0;
+      total += sums[w];
+    }
+    if (n < a.n_seqs) line[n] = before + up_to - mine;
+    lds_barrier();
+  }
+  if (threadIdx.x == 0) line[a.n_seqs] = total;
+  lds_barrier();
+}
+// The waves that share `tiles` (of all K/V heads, of a line of `total` for each): no more
+// than leave each as many tiles as balance its walk with the joining of the parts (a tile
+// of a lonely wave takes about 1.3 us, 16 parts of a row 0.6).
+__device__ __forceinline__ int line_waves(const AttnArgs& a, int64_t tiles, int total) {
+  const int least = max(1, static_cast<int>(ceilf(sqrtf(static_cast<float>(total) / (32.0f * a.n_seqs)))));
+  return __builtin_amdgcn_readfirstlane(static_cast<int>(min((tiles + least - 1) / least, static_cast<int64_t>(a.stream_waves))));
+}
+__device__ __forceinline__ int64_t share_start(int64_t tiles, int waves, int w) { return tiles * w / waves; }
+__device__ __forceinline__ int share_of(int64_t tiles, int waves, int64_t t) {   // the wave whose share holds tile t
+  return static_cast<int>(((t + 1) * waves - 1) / tiles);
+}
+
+// The items of a wave, one after another; those of a workgroup come to all of its waves.
+struct AttnWork {
+  int shared, shared_step;   // the next shared item
+  int64_t at, end;           // what is left of the share of the line
+  int wave;                  // of the line
+  bool own_first;
+};
+enum class AttnKind { kNone, kRows, kKeys, kWave };
+
+__device__ __forceinline__ void shared_item(const AttnArgs& a, int b, AttnItem& it) {
+  // [split][row tile][K/V head]
+  it.kvh = b % a.kv_heads;
+  const int u = b / a.kv_heads, tile = u % a.shared_tiles, split = u / a.shared_tiles;
+  it.row0 = tile * kAttnTile;
+  it.rows = min(kAttnTile, a.rows - it.row0);
+  it.len = it.tail = 0;
+  it.first_row = it.row0;
+  const int first = split * a.shared_chunk;
+  it.keys = {a.prefix_pages, nullptr, first, min(a.shared_chunk, a.prefix_len - first), 0, 0};
+  it.part = ((static_cast<int64_t>(split) * a.shared_tiles + tile) * a.kv_heads + it.kvh) * a.shared_wt;
+}
+__device__ __forceinline__ bool own_item(const AttnArgs& a, int b, AttnItem& it) {
+  // [slot, the last first][split][K/V head]
+  it.kvh = b % a.kv_heads;
+  const int u = b / a.kv_heads, split = u % a.own_splits, slot = a.own_slots - 1 - u / a.own_splits;
+  const int n = row_slot_seq(a.cu, a.n_seqs, slot, a.groups, a.own_tile);
+  const int start = a.cu[n], count = a.cu[n + 1] - start;
+  it.first_row = start * a.groups;
+  const int from = (slot - (it.first_row / a.own_tile + n)) * a.own_tile;
+  const int left = count * a.groups - from;
+  if (left <= 0) return false;
+  it.row0 = it.first_row + from;
+  it.rows = min(a.own_tile, left);
+  it.len = min(max(a.lens[n], 0), a.max_len);
+  it.tail = it.len - count;
+  const int end = own_limit(it, a.groups, it.rows - 1);
+  const int64_t first = static_cast<int64_t>(split) * a.own_chunk;
+  const int64_t own = min(static_cast<int64_t>(a.own_chunk), end - first);
+  it.keys = {a.prefix_pages, a.table + static_cast<int64_t>(n) * a.width, 0, a.shared_items == 0 ? a.prefix_len : 0,
+             static_cast<int>(first), static_cast<int>(max(own, static_cast<int64_t>(0)))};
+  it.part = a.part ? static_cast<int64_t>(a.shared_items) * a.shared_wt +
+                         ((static_cast<int64_t>(slot) * a.own_splits + split) * a.kv_heads + it.kvh) * (a.own_tile / kAttnRows)
+                   : -1;
+  return true;
+}
+__device__ __forceinline__ void line_item(const AttnArgs& a, const int* line, AttnWork& w, AttnItem& it) {
+  // the last sequence that begins at the tile or before it; 64 candidates at a time
+  const int t = static_cast<int>(w.at / a.kv_heads), lane = threadIdx.x % kWave;
+  int lo = 0, hi = a.n_seqs;
+  while (hi - lo > 1) {
+    const int step = (hi - lo + kWave - 1) / kWave, at = lo + lane * step;
+    const int found = __popcll(__ballot(at < hi && line[min(at, hi)] <= t));
+    lo += (found - 1) * step;
+    hi = min(hi, lo + step);
+  }
+  const int n = __builtin_amdgcn_readfirstlane(lo);
+  const int begin = __builtin_amdgcn_readfirstlane(line[n]), tiles = __builtin_amdgcn_readfirstlane(line[n + 1]) - begin;
+  const int rest = static_cast<int>(w.at - static_cast<int64_t>(begin) * a.kv_heads), off = rest % tiles;
+  it.kvh = rest / tiles;
+  const int take = static_cast<int>(min(w.end - w.at, static_cast<int64_t>(tiles - off)));
+  const int start = a.cu[n], count = a.cu[n + 1] - start;
+  it.row0 = it.first_row = start * a.groups;
+  it.rows = count * a.groups;
+  it.len = min(max(a.lens[n], 0), a.max_len);
+  it.tail = it.len - count;
+  const int first = off * kLineTile;
+  it.keys = {nullptr, a.table + static_cast<int64_t>(n) * a.width, 0, 0, first, min(take * kLineTile, it.len - first)};
+  const int64_t base = static_cast<int64_t>(a.shared_items) * a.shared_wt;
+  if (take < tiles) it.part = base + 2 * w.wave + (off == 0);
+  else it.part = a.shared_items ? base + 2 * a.stream_waves + static_cast<int64_t>(n) * a.kv_heads + it.kvh : -1;
+  w.at += take;
+}
+__device__ __forceinline__ AttnKind next_item(const AttnArgs& a, const int* line, AttnWork& w, AttnItem& it) {
+  const bool shared = w.shared < a.shared_items, own = w.at < w.end;
+  if (shared && !(own && w.own_first)) {
+    shared_item(a, w.shared, it);
+    w.shared += w.shared_step;
+    return a.shared_wt == 1 ? AttnKind::kWave : it.rows > kAttnRows ? AttnKind::kRows : AttnKind::kKeys;
+  }
+  if (!own) return AttnKind::kNone;
+  if (a.stream) {
+    line_item(a, line, w, it);
+    return AttnKind::kWave;
+  }
+  w.at = w.end;
+  if (!own_item(a, static_cast<int>(blockIdx.x) - a.shared_items, it)) return AttnKind::kNone;
+  return it.rows > kAttnRows ? AttnKind::kRows : AttnKind::kKeys;
+}
+
 template <typename T, int D>
 __global__ __launch_bounds__(kAttnThreads, sizeof(T) == 2 ? 2 : 1)
 void k_attn(AttnArgs a) {
   __shared__ __attribute__((aligned(1024))) char lds[AttnLds<T, D>::kBytes];
-  AttnItem it;
-  int b = blockIdx.x;
-  if (b < a.shared_items) {
-    // [split][row tile][K/V head]
-    it.kvh = b % a.kv_heads;
-    const int u = b / a.kv_heads, tile = u % a.shared_tiles, split = u / a.shared_tiles;
-    it.row0 = tile * kAttnTile;
-    it.rows = min(kAttnTile, a.rows - it.row0);
-    it.len = it.tail = 0;
-    it.first_row = it.row0;
-    const int first = split * a.shared_chunk;
-    it.keys = {a.prefix_pages, nullptr, first, min(a.shared_chunk, a.prefix_len - first), 0, 0};
-    it.part = ((static_cast<int64_t>(split) * a.shared_tiles + tile) * a.kv_heads + it.kvh) * kAttnWaves;
+  const int* line = reinterpret_cast<const int*>(lds + AttnLds<T, D>::kOffLine);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), group = blockIdx.x;
+  AttnWork work{};
+  work.shared = a.shared_wt == 1 ? kAttnWaves * group + wave : group;
+  work.shared_step = a.shared_wt == 1 ? kAttnWaves * gridDim.x : gridDim.x;
+  if (!a.stream) {
+    work.end = group >= a.shared_items;   // one own item, or none
+    if (work.end) work.shared = a.shared_items;
+    else work.shared_step = a.shared_items;
   } else {
-    b -= a.shared_items;
-    // [slot, the last first][split][K/V head]
-    it.kvh = b % a.kv_heads;
-    const int u = b / a.kv_heads, split = u % a.own_splits, slot = a.own_slots - 1 - u / a.own_splits;
-    const int n = row_slot_seq(a.cu, a.n_seqs, slot, a.groups, a.own_tile);
-    const int start = a.cu[n], count = a.cu[n + 1] - start;
-    it.first_row = start * a.groups;
-    const int from = (slot - (it.first_row / a.own_tile + n)) * a.own_tile;
-    const int left = count * a.groups - from;
-    if (left <= 0) return;
-    it.row0 = it.first_row + from;
-    it.rows = min(a.own_tile, left);
-    it.len = min(max(a.lens[n], 0), a.max_len);
-    it.tail = it.len - count;
-    const int end = own_limit(it, a.groups, it.rows - 1);
-    const int64_t first = static_cast<int64_t>(split) * a.own_chunk;
-    const int64_t own = min(static_cast<int64_t>(a.own_chunk), end - first);
-    const bool both = a.shared_items == 0;
-    it.keys = {a.prefix_pages, a.table + static_cast<int64_t>(n) * a.width, 0, both ? a.prefix_len : 0, static_cast<int>(first),
-               static_cast<int>(max(own, static_cast<int64_t>(0)))};
-    it.part = static_cast<int64_t>(a.shared_items) * kAttnWaves +
-              ((static_cast<int64_t>(slot) * a.own_splits + split) * a.kv_heads + it.kvh) * (a.own_tile / kAttnRows);
+    if (group >= a.stream_first && kAttnWaves * (group - a.stream_first) < a.stream_waves) {
+      if (a.stream_first > 0) work.shared = a.shared_items;   // there are others for these
+      lay_line<T, D>(a, lds);
+      const int total = __builtin_amdgcn_readfirstlane(line[a.n_seqs]);
+      if (group == a.stream_first)   // for the joining kernel
+        for (int n = threadIdx.x; n <= a.n_seqs; n += kAttnThreads) a.line[n] = line[n];
+      const int64_t tiles = static_cast<int64_t>(total) * a.kv_heads;
+      const int waves = line_waves(a, tiles, total);
+      work.wave = kAttnWaves * (group - a.stream_first) + wave;
+      if (work.wave < waves) {
+        work.at = share_start(tiles, waves, work.wave);
+        work.end = share_start(tiles, waves, work.wave + 1);
+      }
+    }
+    // shared items compute, own ones wait for memory: half of the workgroups begin with
+    // the one, half with the other
+    work.own_first = group >= static_cast<int>(gridDim.x) / 2;
   }
-  const CacheAt<T, D> cache(a, it.kvh);
-  if (it.rows <= kAttnRows) attend_keys<T, D>(a, it, cache, lds);
-  else attend_rows<T, D>(a, it, cache, lds);
+  while (true) {
+    const AttnArgs e = args_again();
+    AttnItem it;
+    const AttnKind kind = next_item(e, line, work, it);
+    if (kind == AttnKind::kNone) break;
+    const CacheAt<T, D> cache(e, it.kvh);
+    if (kind != AttnKind::kWave) lds_barrier();   // the LDS of the item before has been read
+    if (kind == AttnKind::kRows) attend_rows<T, D>(e, it, cache, lds);
+    else attend_keys<T, D>(e, it, cache, kind == AttnKind::kKeys, lds);
+    if (kind != AttnKind::kWave) lds_barrier();
+  }
 }
 
-// The items' partial results of a row into one.  A wave takes 32 packed rows of a K/V
-// head and one of the D / 8 groups of columns: lane (h, r) four columns of row r.
-// kAttnAhead parts' loads are in flight at a time.
-constexpr int kAttnAhead = 8;
+// The items' partial results of a row into one.  A workgroup takes 32 packed rows of a
+// K/V head and one of the D / 8 groups of columns: lane (h, r) four columns of row r, a
+// wave every fourth part, kAttnAhead parts' loads in flight at a time.
+constexpr int kAttnAhead = 4;
 template <typename T, int D>
 __global__ __launch_bounds__(kAttnThreads)
 void k_attn_join(AttnArgs a) {
-  constexpr int GROUPS = D / 8 / kAttnWaves;   // workgroups of a wave tile
+  __shared__ f32x4 sums[kAttnWaves][kWave];
+  __shared__ f32x2 mls[kAttnWaves][kWave];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
-  const int unit = blockIdx.x / GROUPS, col = blockIdx.x % GROUPS * kAttnWaves + wave;
+  const int unit = blockIdx.x / (D / 8), col = blockIdx.x % (D / 8);
   const int kvh = unit % a.kv_heads, wt = unit / a.kv_heads;
   const bool there = wt * kAttnRows + lane % 32 < a.rows;
   const int row = there ? wt * kAttnRows + lane % 32 : a.rows - 1;
@@ -931,33 +1105,58 @@ void k_attn_join(AttnArgs a) {
     else lo = mid + 1;
   }
   const int first = a.cu[lo] * a.groups, rs = row - first;
-  const int slot = first / a.own_tile + lo + rs / a.own_tile;
-  // the row among the wave tiles of part s: those of the shared items are these rows,
-  // those of the own ones are found by sequence
-  const int64_t shared0 = (static_cast<int64_t>(wt / kAttnWaves) * a.kv_heads + kvh) * kAttnWaves + wt % kAttnWaves,
-                shared_step = static_cast<int64_t>(a.shared_tiles) * a.kv_heads * kAttnWaves,
-                own0 = static_cast<int64_t>(a.shared_items) * kAttnWaves +
-                       (static_cast<int64_t>(slot) * a.own_splits * a.kv_heads + kvh) * (a.own_tile / kAttnRows) +
-                       rs % a.own_tile / kAttnRows,
-                own_step = static_cast<int64_t>(a.kv_heads) * (a.own_tile / kAttnRows);
-  const auto tile_of = [&](int s) { return s < a.shared_splits ? shared0 + s * shared_step : own0 + (s - a.shared_splits) * own_step; };
-  const auto row_of = [&](int s) { return s < a.shared_splits ? lane % 32 : rs % kAttnRows; };
-  const int parts = a.shared_splits + a.own_splits;
+  // where the row is among the wave tiles of part s: those of the shared items are these
+  // rows, those of the own ones are found by sequence
+  const int64_t shared0 = (static_cast<int64_t>(wt / a.shared_wt) * a.kv_heads + kvh) * a.shared_wt + wt % a.shared_wt,
+                shared_step = static_cast<int64_t>(a.shared_tiles) * a.kv_heads * a.shared_wt,
+                base = static_cast<int64_t>(a.shared_items) * a.shared_wt;
+  int64_t own0, own_step;   // the first of the own parts (what follows: a step behind), and the steps
+  int own = a.own_splits;
+  if (a.stream) {
+    const int before = a.line[lo], mine = a.line[lo + 1] - before, total = a.line[a.n_seqs];
+    const int64_t tiles = static_cast<int64_t>(total) * a.kv_heads;
+    const int waves = line_waves(a, tiles, total);
+    const int64_t t0 = static_cast<int64_t>(before) * a.kv_heads + static_cast<int64_t>(kvh) * mine;
+    const int w0 = share_of(tiles, waves, t0);
+    own = share_of(tiles, waves, t0 + mine - 1) - w0 + 1;
+    own_step = 2;
+    own0 = own == 1 ? base + 2 * a.stream_waves + static_cast<int64_t>(lo) * a.kv_heads + kvh
+                    : base + 2 * w0;   // (its first part one behind)
+  } else {
+    const int slot = first / a.own_tile + lo + rs / a.own_tile;
+    own_step = static_cast<int64_t>(a.kv_heads) * (a.own_tile / kAttnRows);
+    own0 = base + (static_cast<int64_t>(slot) * a.own_splits * a.kv_heads + kvh) * (a.own_tile / kAttnRows) +
+           rs % a.own_tile / kAttnRows;
+  }
+  const bool split = a.stream && own > 1;
+  const bool done = a.stream && own == 1 && a.shared_splits == 0;   // its item wrote it out
+  const int parts = there && !done ? a.shared_splits + own : 0;
+  int most = parts;   // over the lanes
+#pragma unroll
+  for (int off = 1; off < kWave; off <<= 1) most = max(most, __shfl_xor(most, off, kWave));
+  most = __builtin_amdgcn_readfirstlane(most);
+  if (most == 0) return;
+  const int own_row = a.stream ? rs : rs % kAttnRows;
   float m = -INFINITY, l = 0.0f;
   f32x4 sum = zero4();
-  for (int s0 = 0; s0 < parts; s0 += kAttnAhead) {
+  for (int s0 = wave; s0 < most; s0 += kAttnWaves * kAttnAhead) {
     f32x2 ml[kAttnAhead];
     f32x4 x[kAttnAhead];
 #pragma unroll
     for (int k = 0; k < kAttnAhead; ++k) {
-      const int s = min(s0 + k, parts - 1);
-      const int64_t t = tile_of(s);
-      ml[k] = a.part_ml[t * kAttnRows + row_of(s)];
-      x[k] = a.part[(t * (D / 8) + col) * kWave + lane / 32 * 32 + row_of(s)];
+      const int s = max(min(s0 + kAttnWaves * k, parts - 1), 0), so = s - a.shared_splits;
+      const int64_t t = so < 0 ? shared0 + s * shared_step : own0 + so * own_step + (split && so == 0);
+      const int r = so < 0 ? lane % 32 : own_row;
+      ml[k] = f32x2{-INFINITY, 0.0f};
+      x[k] = zero4();
+      if (s0 + kAttnWaves * k < parts) {
+        ml[k] = a.part_ml[t * kAttnRows + r];
+        x[k] = a.part[(t * (D / 8) + col) * kWave + lane / 32 * 32 + r];
+      }
     }
     float top = m;
 #pragma unroll
-    for (int k = 0; k < kAttnAhead; ++k) top = s0 + k < parts ? fmaxf(top, ml[k][0]) : top;
+    for (int k = 0; k < kAttnAhead; ++k) top = fmaxf(top, ml[k][0]);
     const float at = top == -INFINITY ? 0.0f : top, keep = __builtin_amdgcn_exp2f(m - at);
     m = top;
     l *= keep;
@@ -965,14 +1164,31 @@ void k_attn_join(AttnArgs a) {
     for (int i = 0; i < 4; ++i) sum[i] *= keep;
 #pragma unroll
     for (int k = 0; k < kAttnAhead; ++k) {
-      if (s0 + k >= parts || ml[k][1] == 0.0f) continue;   // nothing seen there (nor anything written)
+      if (ml[k][1] == 0.0f) continue;   // nothing seen there (nor anything written)
       const float f = __builtin_amdgcn_exp2f(ml[k][0] - at);
       l = fmaf(f, ml[k][1], l);
 #pragma unroll
       for (int i = 0; i < 4; ++i) sum[i] = fmaf(f, x[k][i], sum[i]);
     }
   }
-  if (!there) return;
+  sums[wave][lane] = sum;
+  mls[wave][lane] = f32x2{m, l};
+  lds_barrier();
+  if (wave != 0 || parts == 0) return;
+#pragma unroll
+  for (int w = 1; w < kAttnWaves; ++w) m = fmaxf(m, mls[w][lane][0]);
+  const float at = m == -INFINITY ? 0.0f : m;
+  l = 0.0f;
+  sum = zero4();
+#pragma unroll
+  for (int w = 0; w < kAttnWaves; ++w) {
+    const f32x2 ml = mls[w][lane];
+    if (ml[1] == 0.0f) continue;
+    const float f = __builtin_amdgcn_exp2f(ml[0] - at);
+    l = fmaf(f, ml[1], l);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum[i] = fmaf(f, sums[w][lane][i], sum[i]);
+  }
   const int head = kvh * a.groups + (row - token * a.groups);
   T* out = static_cast<T*>(a.out) + token * a.ldo + static_cast<int64_t>(head) * D + 8 * col + 4 * (lane / 32);
   const float inv = 1.0f / l;

@@ -180,23 +180,55 @@ gdn_status make_attn_plan(const gdn_attn_shape* s, const int32_t* cu, AttnPlan* 
     *chunk = static_cast<int32_t>(each);
     *splits = static_cast<int32_t>(std::max<int64_t>(1, (keys + each - 1) / each));
   };
-  if (P > 0 && (tiles * H < kAttnPlaces || p.rows < tiles * p.own_tile * 3 / 5)) {
+  const int64_t places = s->dtype == GDN_BF16 ? kAttnPlaces : kAttnPlaces / 2;
+  constexpr int64_t waves = kPlanTile / kPlanRows;   // of a workgroup
+  const int64_t line = N * H * ((p.max_len + static_cast<int64_t>(kPlanLineTile) - 1) / kPlanLineTile);   // tiles at most
+  p.stream = p.own_tile == kPlanRows && N <= kPlanLineSeqs && line <= int64_t{1} << 30;
+  if (P > 0 && (p.stream || tiles * H < places || p.rows < tiles * p.own_tile * 3 / 5)) {
     p.shared_tiles = (p.rows + kPlanTile - 1) / kPlanTile;
-    // one workgroup a CU: the other place is for own items, which wait for memory while
-    // these compute
-    pieces(P, p.shared_tiles * H, kAttnPlaces / 2, &p.shared_splits, &p.shared_chunk);
+    if (p.stream && p.rows <= kPlanRows) {
+      // a wave's items, as many tiles each as balance their walk with the joining (see line_waves)
+      p.shared_wt = 1;
+      const int64_t keys = (P + kPlanLineTile - 1) / kPlanLineTile;
+      const int64_t least = static_cast<int64_t>(std::ceil(std::sqrt(static_cast<double>(keys) / 32)));
+      const int64_t n = std::max<int64_t>(1, std::min(places * waves / H, keys / std::max<int64_t>(1, least)));
+      const int64_t each = (keys + n - 1) / n;
+      p.shared_chunk = static_cast<int32_t>(each * kPlanLineTile);
+      p.shared_splits = static_cast<int32_t>((keys + each - 1) / each);
+    } else {
+      // one workgroup a CU: the other place is for own items, which wait for memory while
+      // these compute
+      pieces(P, p.shared_tiles * H, places / 2, &p.shared_splits, &p.shared_chunk);
+    }
     p.shared_items = p.shared_tiles * H * p.shared_splits;
   }
-  if (P == 0 || p.shared_items > 0) pieces(p.max_len, tiles * H, kAttnPlaces, &p.own_splits, &p.own_chunk);
-  else p.own_chunk = (p.max_len + 63) / 64 * 64;
-  p.own_items = p.own_slots * H * p.own_splits;
-  p.joined = p.shared_items > 0 || p.own_splits > 1;
-  if (p.shared_items + p.own_items > kMaxInt / 256) return bad(err, "too many tokens for one call", GDN_ERR_UNSUPPORTED);
+  size_t own_tiles = 0;   // wave tiles of the own items' partial results
+  if (p.stream) {
+    // workgroups of their own for the own tokens while there is room, else all take both
+    const int64_t wanted = (std::max<int64_t>(1, std::min(places * waves, line)) + waves - 1) / waves;
+    const int64_t shared = p.shared_wt == 1 ? (p.shared_items + waves - 1) / waves : p.shared_items;
+    const bool apart = shared + wanted <= places;
+    p.stream_first = apart ? static_cast<int32_t>(shared) : 0;
+    p.stream_waves = static_cast<int32_t>(wanted * waves);
+    p.grid = apart ? shared + wanted : places;
+    p.joined = true;
+    own_tiles = 2 * static_cast<size_t>(p.stream_waves) + static_cast<size_t>(N * H);
+  } else {
+    if (P == 0 || p.shared_items > 0) pieces(p.max_len, tiles * H, places, &p.own_splits, &p.own_chunk);
+    else p.own_chunk = (p.max_len + 63) / 64 * 64;
+    p.own_items = p.own_slots * H * p.own_splits;
+    p.joined = p.shared_items > 0 || p.own_splits > 1;
+    p.grid = p.shared_items + p.own_items;
+    own_tiles = static_cast<size_t>(p.own_items) * (p.own_tile / kPlanRows);
+  }
+  if (p.grid > kMaxInt / 256 || p.rows / kPlanRows * H * (s->head_dim / 8) > kMaxInt / 256)
+    return bad(err, "too many tokens for one call", GDN_ERR_UNSUPPORTED);
   if (p.joined) {
-    const size_t waves = static_cast<size_t>(p.shared_items) * (kPlanTile / kPlanRows) +
-                         static_cast<size_t>(p.own_items) * (p.own_tile / kPlanRows);
-    p.off_ml = waves * kPlanRows * s->head_dim * sizeof(float);
-    p.bytes = (p.off_ml + waves * kPlanRows * 2 * sizeof(float) + kAlign - 1) / kAlign * kAlign;
+    const size_t parts = static_cast<size_t>(p.shared_items) * p.shared_wt + own_tiles;
+    p.off_ml = parts * kPlanRows * s->head_dim * sizeof(float);
+    p.off_line = p.off_ml + parts * kPlanRows * 2 * sizeof(float);
+    p.bytes = p.off_line + (p.stream ? (static_cast<size_t>(N) + 1) * sizeof(int32_t) : 0);
+    p.bytes = (p.bytes + kAlign - 1) / kAlign * kAlign;
   }
   *plan = p;
   return GDN_OK;

@@ -29,6 +29,8 @@ gdn_status check_attn(const gdn_attn_shape* s, std::string* err);
 // Rows (one query head of one token, the heads of a K/V head next to each other)
 // of a wave, and of a workgroup whose waves take rows of their own.
 constexpr int32_t kPlanRows = 32, kPlanTile = 128;
+// Keys of a tile of the line that waves share, and sequences that it may have.
+constexpr int32_t kPlanLineTile = 32, kPlanLineSeqs = 1024;
 
 // How gdn_prefix_attention runs.  Shared items: tiles of all packed rows against
 // `shared_splits` pieces of the prefix.  Own items: tiles of a sequence's rows
@@ -43,8 +45,14 @@ struct AttnPlan {
   int64_t shared_tiles = 0, shared_items = 0;
   int32_t own_tile = kPlanTile, own_splits = 1, own_chunk = 0;
   int64_t own_slots = 0, own_items = 0;
+  int32_t shared_wt = kPlanTile / kPlanRows;   // wave tiles of a shared item; 1: it is a wave's
+  // few rows a sequence: stream_waves waves from workgroup stream_first on share all
+  // sequences' own tokens out in equal parts
+  bool stream = false;
+  int32_t stream_first = 0, stream_waves = 0;
+  int64_t grid = 0;
   bool joined = false;       // items leave partial results, which a second kernel joins
-  size_t off_ml = 0;         // workspace: partial outputs, then maxima and sums
+  size_t off_ml = 0, off_line = 0;   // workspace: partial outputs, their maxima and sums, the line
   size_t bytes = 0;
 };
 gdn_status make_attn_plan(const gdn_attn_shape* s, const int32_t* cu, AttnPlan* p, std::string* err);
