@@ -46,7 +46,7 @@ struct AttnArgs {
   int32_t shared_wt;      // wave tiles of a shared item: kAttnWaves, or 1 (a wave's)
   // stream (see there): stream_waves waves from workgroup stream_first on share the own tokens out
   int32_t stream, stream_first, stream_waves;
-  int32_t* line;          // [N + 1]
+  int32_t* line;          // [N + 1], then the sequence of each token [T], for the joining kernel
   int32_t rows;           // T G
   const int32_t* cu;
   const int32_t* table;
@@ -561,7 +561,7 @@ struct AttnLds {
   static constexpr int kOffOdd = kMost;                        // a flag for each wave
   static constexpr int kOffPages = kOffOdd + 64;               // 64 page numbers for each wave
   static constexpr int kOffLine = kOffPages + 4 * kAttnThreads;
-  static constexpr int kBytes = kOffLine + 4 * (kStreamSeqs + 1);
+  static constexpr int kBytes = kOffLine + 12 * kStreamSeqs + 8;
 };
 
 // The kernel's arguments, loaded anew: what is used at the end alone is not kept in
@@ -904,19 +904,37 @@ __device__ __forceinline__ int row_slot_seq(const int32_t* __restrict__ cu, int 
 // them at 2 wave + 1, the others at 2 wave.
 constexpr int kLineTile = 32;
 
-// The line of one K/V head in LDS: line[n] tiles before sequence n (which has one where
-// it has queries but no tokens), line[N] in all.
+// The line of one K/V head: tiles[n] before sequence n (which has one where it has
+// queries but no tokens), tiles[N] in all; and the sequences' first tokens and lengths.
+struct Line {
+  int* tiles;
+  int* cu;
+  int* lens;
+};
 template <typename T, int D>
-__device__ __forceinline__ void lay_line(const AttnArgs& a, char* lds) {
-  int* line = reinterpret_cast<int*>(lds + AttnLds<T, D>::kOffLine);
+__device__ __forceinline__ Line line_at(char* lds) {
+  int* p = reinterpret_cast<int*>(lds + AttnLds<T, D>::kOffLine);
+  return {p, p + kStreamSeqs + 1, p + 2 * kStreamSeqs + 2};
+}
+// `keep`: for the joining kernel as well.
+template <typename T, int D>
+__device__ __forceinline__ void lay_line(const AttnArgs& a, char* lds, bool keep) {
+  const Line line = line_at<T, D>(lds);
   int* sums = reinterpret_cast<int*>(lds);
   const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
   int total = 0;
   for (int n0 = 0; n0 < a.n_seqs; n0 += kAttnThreads) {
     const int n = n0 + threadIdx.x;
     int mine = 0;
-    if (n < a.n_seqs && a.cu[n + 1] > a.cu[n])
-      mine = max(1, (min(max(a.lens[n], 0), a.max_len) + kLineTile - 1) / kLineTile);
+    if (n < a.n_seqs) {
+      const int start = a.cu[n], end = a.cu[n + 1], len = min(max(a.lens[n], 0), a.max_len);
+      if (end > start) mine = max(1, (len + kLineTile - 1) / kLineTile);
+      line.cu[n] = start;
+      line.lens[n] = len;
+      if (n == a.n_seqs - 1) line.cu[n + 1] = end;
+      if (keep)
+        for (int t = start; t < end; ++t) a.line[a.n_seqs + 1 + t] = n;
+    }
     int up_to = mine;   // inclusive sums over the wave
 #pragma unroll
     for (int off = 1; off < kWave; off <<= 1) {
@@ -931,10 +949,16 @@ __device__ __forceinline__ void lay_line(const AttnArgs& a, char* lds) {
       before += w < wave ? sums[w] : 0;
       total += sums[w];
     }
-    if (n < a.n_seqs) line[n] = before + up_to - mine;
+    if (n < a.n_seqs) {
+      line.tiles[n] = before + up_to - mine;
+      if (keep) a.line[n] = before + up_to - mine;
+    }
     lds_barrier();
   }
-  if (threadIdx.x == 0) line[a.n_seqs] = total;
+  if (threadIdx.x == 0) {
+    line.tiles[a.n_seqs] = total;
+    if (keep) a.line[a.n_seqs] = total;
+  }
   lds_barrier();
 }
 // The waves that share `tiles` (of all K/V heads, of a line of `total` for each): no more
@@ -994,25 +1018,27 @@ __device__ __forceinline__ bool own_item(const AttnArgs& a, int b, AttnItem& it)
                    : -1;
   return true;
 }
-__device__ __forceinline__ void line_item(const AttnArgs& a, const int* line, AttnWork& w, AttnItem& it) {
+__device__ __forceinline__ void line_item(const AttnArgs& a, const Line& line, AttnWork& w, AttnItem& it) {
   // the last sequence that begins at the tile or before it; 64 candidates at a time
   const int t = static_cast<int>(w.at / a.kv_heads), lane = threadIdx.x % kWave;
   int lo = 0, hi = a.n_seqs;
   while (hi - lo > 1) {
     const int step = (hi - lo + kWave - 1) / kWave, at = lo + lane * step;
-    const int found = __popcll(__ballot(at < hi && line[min(at, hi)] <= t));
+    const int found = __popcll(__ballot(at < hi && line.tiles[min(at, hi)] <= t));
     lo += (found - 1) * step;
     hi = min(hi, lo + step);
   }
   const int n = __builtin_amdgcn_readfirstlane(lo);
-  const int begin = __builtin_amdgcn_readfirstlane(line[n]), tiles = __builtin_amdgcn_readfirstlane(line[n + 1]) - begin;
+  const int begin = __builtin_amdgcn_readfirstlane(line.tiles[n]),
+            tiles = __builtin_amdgcn_readfirstlane(line.tiles[n + 1]) - begin;
   const int rest = static_cast<int>(w.at - static_cast<int64_t>(begin) * a.kv_heads), off = rest % tiles;
   it.kvh = rest / tiles;
   const int take = static_cast<int>(min(w.end - w.at, static_cast<int64_t>(tiles - off)));
-  const int start = a.cu[n], count = a.cu[n + 1] - start;
+  const int start = __builtin_amdgcn_readfirstlane(line.cu[n]),
+            count = __builtin_amdgcn_readfirstlane(line.cu[n + 1]) - start;
   it.row0 = it.first_row = start * a.groups;
   it.rows = count * a.groups;
-  it.len = min(max(a.lens[n], 0), a.max_len);
+  it.len = __builtin_amdgcn_readfirstlane(line.lens[n]);
   it.tail = it.len - count;
   const int first = off * kLineTile;
   it.keys = {nullptr, a.table + static_cast<int64_t>(n) * a.width, 0, 0, first, min(take * kLineTile, it.len - first)};
@@ -1021,7 +1047,7 @@ __device__ __forceinline__ void line_item(const AttnArgs& a, const int* line, At
   else it.part = a.shared_items ? base + 2 * a.stream_waves + static_cast<int64_t>(n) * a.kv_heads + it.kvh : -1;
   w.at += take;
 }
-__device__ __forceinline__ AttnKind next_item(const AttnArgs& a, const int* line, AttnWork& w, AttnItem& it) {
+__device__ __forceinline__ AttnKind next_item(const AttnArgs& a, const Line& line, AttnWork& w, AttnItem& it) {
   const bool shared = w.shared < a.shared_items, own = w.at < w.end;
   if (shared && !(own && w.own_first)) {
     shared_item(a, w.shared, it);
@@ -1042,7 +1068,7 @@ template <typename T, int D>
 __global__ __launch_bounds__(kAttnThreads, sizeof(T) == 2 ? 2 : 1)
 void k_attn(AttnArgs a) {
   __shared__ __attribute__((aligned(1024))) char lds[AttnLds<T, D>::kBytes];
-  const int* line = reinterpret_cast<const int*>(lds + AttnLds<T, D>::kOffLine);
+  const Line line = line_at<T, D>(lds);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), group = blockIdx.x;
   AttnWork work{};
   work.shared = a.shared_wt == 1 ? kAttnWaves * group + wave : group;
@@ -1054,10 +1080,8 @@ void k_attn(AttnArgs a) {
   } else {
     if (group >= a.stream_first && kAttnWaves * (group - a.stream_first) < a.stream_waves) {
       if (a.stream_first > 0) work.shared = a.shared_items;   // there are others for these
-      lay_line<T, D>(a, lds);
-      const int total = __builtin_amdgcn_readfirstlane(line[a.n_seqs]);
-      if (group == a.stream_first)   // for the joining kernel
-        for (int n = threadIdx.x; n <= a.n_seqs; n += kAttnThreads) a.line[n] = line[n];
+      lay_line<T, D>(a, lds, group == a.stream_first);
+      const int total = __builtin_amdgcn_readfirstlane(line.tiles[a.n_seqs]);
       const int64_t tiles = static_cast<int64_t>(total) * a.kv_heads;
       const int waves = line_waves(a, tiles, total);
       work.wave = kAttnWaves * (group - a.stream_first) + wave;
@@ -1098,11 +1122,16 @@ void k_attn_join(AttnArgs a) {
   const bool there = wt * kAttnRows + lane % 32 < a.rows;
   const int row = there ? wt * kAttnRows + lane % 32 : a.rows - 1;
   const int token = static_cast<int>(static_cast<uint32_t>(row) / static_cast<uint32_t>(a.groups));
-  int lo = 0, hi = a.n_seqs - 1;   // the sequence of the token: the first whose end lies behind it
-  while (lo < hi) {
-    const int mid = (lo + hi) / 2;
-    if (a.cu[mid + 1] > token) hi = mid;
-    else lo = mid + 1;
+  int lo = 0;   // the sequence of the token: the first whose end lies behind it
+  if (a.stream) {
+    lo = a.line[a.n_seqs + 1 + token];
+  } else {
+    int hi = a.n_seqs - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi) / 2;
+      if (a.cu[mid + 1] > token) hi = mid;
+      else lo = mid + 1;
+    }
   }
   const int first = a.cu[lo] * a.groups, rs = row - first;
   // where the row is among the wave tiles of part s: those of the shared items are these

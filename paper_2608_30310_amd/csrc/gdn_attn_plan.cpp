@@ -227,7 +227,7 @@ gdn_status make_attn_plan(const gdn_attn_shape* s, const int32_t* cu, AttnPlan* 
     const size_t parts = static_cast<size_t>(p.shared_items) * p.shared_wt + own_tiles;
     p.off_ml = parts * kPlanRows * s->head_dim * sizeof(float);
     p.off_line = p.off_ml + parts * kPlanRows * 2 * sizeof(float);
-    p.bytes = p.off_line + (p.stream ? (static_cast<size_t>(N) + 1) * sizeof(int32_t) : 0);
+    p.bytes = p.off_line + (p.stream ? (static_cast<size_t>(N) + 1 + p.tokens) * sizeof(int32_t) : 0);
     p.bytes = (p.bytes + kAlign - 1) / kAlign * kAlign;
   }
   *plan = p;
