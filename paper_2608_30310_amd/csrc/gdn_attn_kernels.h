@@ -14,8 +14,8 @@
 // which registers does not matter to that product as long as V's operand has them
 // in the same order.  One pass, with the running maximum m and sum l of each row:
 //   p = 2^(s - m),  l += sum p,  O += p V,  out = O / l,
-// where m moves (and O and l are scaled) only when a row's maximum passes it by
-// more than 8: p stays below 2^8, which neither bf16's range nor fp32 sums mind.
+// where m moves (and O and l are scaled) only when weights pass 2^8 or so, which neither
+// bf16's range nor fp32 sums mind.
 #pragma once
 
 #include <type_traits>
@@ -118,6 +118,14 @@ struct Mm<float> {
 // of four pieces, transposed on the way) do because rows 0..3 differ in the high
 // bits of the piece.  (fp32: rows r and r + 4 differ in the highest, for V's
 // 4-byte reads.)
+// The lane, for what is made of it anew for each tile instead of being kept in registers
+// over the tiles.
+__device__ __forceinline__ int lane_now() {
+  int x = threadIdx.x;
+  asm volatile("" : "+v"(x));
+  return static_cast<uint32_t>(x) % kWave;
+}
+
 template <typename T, int D>
 struct KvRows {
   static constexpr int kPitch = D * static_cast<int>(sizeof(T));
@@ -278,24 +286,18 @@ struct CacheAt {
   uint64_t k, v;
   uint32_t kp, kt, vp, vt, page_mul;
   int page_shift, page_size, num_pages, dma_in_page;
-  uint32_t krow, vrow, piece;
   __device__ __forceinline__ CacheAt(const AttnArgs& a, int kvh) {
-    typedef KvRows<T, D> Rows;
-    const int lane = threadIdx.x % kWave, j = lane / Rows::kPieces;
     k = apart(reinterpret_cast<uint64_t>(a.k) + kvh * a.kh);
     v = apart(reinterpret_cast<uint64_t>(a.v) + kvh * a.vh);
     kp = apart(a.kp), kt = apart(a.kt), vp = apart(a.vp), vt = apart(a.vt), page_mul = apart(a.page_mul);
     page_shift = apart(a.page_shift), page_size = apart(a.page_size), num_pages = apart(a.num_pages);
     dma_in_page = apart(a.dma_in_page);
-    krow = 16 * j * a.kt;
-    vrow = 16 * j * a.vt;
-    piece = 16 * (lane % Rows::kPieces ^ Rows::swz(j));
   }
   // The page index of token base + lane % KT of a tile (lanes behind its end: of its
   // last token), and the token's row there.
   template <int KT>
   __device__ __forceinline__ int page_index(const KeyTile& t, int* row) const {
-    const int key = t.base + min(static_cast<int>(threadIdx.x) % KT, t.count - 1);
+    const int key = t.base + min(lane_now() % KT, t.count - 1);
     const int c = page_size == 1 ? key : static_cast<int>(__umulhi(key, page_mul) >> page_shift);
     *row = key - c * page_size;
     return c;
@@ -311,15 +313,15 @@ struct CacheAt {
   struct RowsAt { uint64_t k, v; };
   template <int KT>
   __device__ __forceinline__ RowsAt find_rows(const KeyTile& t, const lds_byte* numbers, uint64_t* there) const {
-    const int lane = threadIdx.x % kWave;
+    const int lane = lane_now();
     int row;
     page_index<KT>(t, &row);
     const int page = ((const __attribute__((address_space(3))) int32_t*)numbers)[lane];
     const bool ok = lane < min(KT, t.count) && page >= 0 && page < num_pages;
     *there = __ballot(ok);
-    const uint64_t p = ok ? page : 0;
-    const uint32_t r = ok ? row : 0;
-    return {k + 16 * (p * kp + static_cast<uint64_t>(r) * kt), v + 16 * (p * vp + static_cast<uint64_t>(r) * vt)};
+    const uint32_t p = ok ? page : 0, r = ok ? row : 0;
+    const auto far = [](uint32_t x, uint32_t y) { return static_cast<uint64_t>(x) * y; };
+    return {k + 16 * (far(p, kp) + far(r, kt)), v + 16 * (far(p, vp) + far(r, vt))};
   }
 };
 
@@ -339,15 +341,15 @@ __device__ __forceinline__ uint64_t lane_at(uint64_t x, int lane) {
   return static_cast<uint64_t>(hi) << 32 | lo;
 }
 
-// DMA of rows [i0, i0 + N) kRowsPerDma of a tile into LDS; row_off: krow or vrow.
+// DMA of rows [i0, i0 + N) kRowsPerDma of a tile into LDS; `stride`: of the rows, kt or vt.
 // Where a DMA's rows lie in one page they are read from its first row's address on:
 // rows behind the last token that way too, which are in the page and masked later.
 template <typename T, int D, int N>
-__device__ __forceinline__ void load_rows(const CacheAt<T, D>& c, uint64_t rows_at, uint32_t row_off, lds_byte* to, int i0) {
+__device__ __forceinline__ void load_rows(const CacheAt<T, D>& c, uint64_t rows_at, uint32_t stride, lds_byte* to, int i0) {
   typedef KvRows<T, D> Rows;
   constexpr int RPD = Rows::kRowsPerDma;
-  uint32_t piece = c.piece;
-  asm volatile("" : "+v"(piece));   // offsets are made here, not kept in registers over the tiles
+  const int lane = lane_now(), j = lane / Rows::kPieces;
+  const uint32_t piece = 16 * (lane % Rows::kPieces ^ Rows::swz(j)), row_off = 16 * j * stride;
   if (!rarely(!c.dma_in_page)) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
@@ -355,11 +357,10 @@ __device__ __forceinline__ void load_rows(const CacheAt<T, D>& c, uint64_t rows_
       async_piece(uniform_at(rows_at, r), row_off + (piece ^ 16 * Rows::swz(r)), to + (i0 + i) * 1024);
     }
   } else {
-    const int lane = threadIdx.x % kWave;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int r = (i0 + i) * RPD;
-      const uint64_t at = lane_at(rows_at, r + lane / Rows::kPieces);
+      const uint64_t at = lane_at(rows_at, r + j);
       async_piece(reinterpret_cast<const void*>(at + (piece ^ 16 * Rows::swz(r))), to + (i0 + i) * 1024);
     }
   }
@@ -442,72 +443,71 @@ struct AttnWave {
         for (int i = 0; i < 16; ++i) o[dt][i] *= keep;
     }
   }
-  // Scores i0 .. i0 + 3 of the tile into weights; p[k]: operand of 16 keys.
+  // Scores of 16 keys into weights, two parts of four; p[k]: operand of 16 keys.  The scores stay.
   template <int NB>
-  __device__ __forceinline__ void weigh4(f32x16 (&s)[NB], R (&p)[2 * NB], int i0, float scale2, float at, float (&sum)[4]) {
-    f32x16& x = s[i0 / 16];
+  __device__ __forceinline__ void weigh4(const f32x16 (&s)[NB], R (&p)[2 * NB], float (&w)[8], int i0, float scale2, float at,
+                                         float (&sum)[4]) const {
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      float& e = reinterpret_cast<float*>(&x)[i0 % 16 + k];
-      e = __builtin_amdgcn_exp2f(fmaf(e, scale2, -at));
+      const float e = __builtin_amdgcn_exp2f(fmaf(s[i0 / 16][i0 % 16 + k], scale2, -at));
       sum[k] += e;
+      w[i0 % 8 + k] = e;
     }
-    if (i0 % 8 == 4) {
-      float w[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) w[j] = x[i0 % 16 - 4 + j];
-      p[i0 / 8] = Mm<T>::pack(w);
-    }
+    if (i0 % 8 == 4) p[i0 / 8] = Mm<T>::pack(w);
   }
+  // All of a tile; returns the sum of the weights (of this half wave).
   template <int NB>
-  __device__ __forceinline__ void weigh(f32x16 (&s)[NB], R (&p)[2 * NB], float scale2) {
+  __device__ __forceinline__ float weigh(const f32x16 (&s)[NB], R (&p)[2 * NB], float scale2) const {
     const float at = m == -INFINITY ? 0.0f : m;
-    float sum[4] = {};
+    float sum[4] = {}, w[8];
 #pragma unroll
-    for (int i = 0; i < 16 * NB; i += 4) weigh4(s, p, i, scale2, at, sum);
-    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    for (int i = 0; i < 16 * NB; i += 4) weigh4(s, p, w, i, scale2, at, sum);
+    return (sum[0] + sum[1]) + (sum[2] + sum[3]);
   }
-  // S^T of NB blocks of 32 keys; operands are read a step ahead of their products.
-  // With WEIGH the scores `s` become weights meanwhile: matrix and vector instructions
-  // take turns.
+  // S^T of the tile's NB blocks of 32 keys; operands are read a step ahead of their
+  // products.  With WEIGH the scores `s` become weights meanwhile (returned: their sum):
+  // matrix and vector instructions take turns.
   template <int NB, bool WEIGH>
-  __device__ __forceinline__ void scores(const char* kl, f32x16 (&next)[NB], f32x16 (&s)[NB], R (&p)[2 * NB], float scale2,
-                                         int lane) {
+  __device__ __forceinline__ float scores(const char* kl, f32x16 (&next)[NB], const f32x16 (&s)[NB], R (&p)[2 * NB], float scale2,
+                                          int lane) const {
     constexpr int U = D / 16, E = 16 * NB / U;   // scores for each step
-    int first = Rows::frag_start(lane);
-    asm volatile("" : "+v"(first));   // addresses are made here, not kept in registers over the tiles
+    int first = Rows::frag_start(lane_now());
+    asm volatile("" : "+v"(first));   // one value that the steps turn, not an expression for each
     R kf[2][NB];
     const auto load = [&](int u) {
 #pragma unroll
       for (int b = 0; b < NB; ++b) kf[u & 1][b] = Rows::frag_at(kl + 32 * b * Rows::kPitch, first ^ Rows::kFragStep * u);
     };
     const float at = m == -INFINITY ? 0.0f : m;
-    float sum[4] = {};
-#pragma unroll
-    for (int b = 0; b < NB; ++b)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) next[b][i] = 0.0f;
+    float sum[4] = {}, w[8];
     load(0);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if (u + 1 < U) load(u + 1);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int b = 0; b < NB; ++b) next[b] = Mm<T>::mul(kf[u & 1][b], q[u], next[b]);
+      for (int b = 0; b < NB; ++b) {
+        f32x16 zero;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) zero[i] = 0.0f;
+        next[b] = Mm<T>::mul(kf[u & 1][b], q[u], u == 0 ? zero : next[b]);
+      }
       if constexpr (WEIGH) {
 #pragma unroll
         for (int e = 0; e < (E + 3) / 4; ++e)
-          if (E >= 4 || u % (4 / E) == 0) weigh4(s, p, E >= 4 ? E * u + 4 * e : 4 * (u / (4 / E)), scale2, at, sum);
+          if (E >= 4 || u % (4 / E) == 0) weigh4(s, p, w, E >= 4 ? E * u + 4 * e : 4 * (u / (4 / E)), scale2, at, sum);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) asm volatile("" : "+v"(sum[k]));   // made here, not where they are used first
       }
       __builtin_amdgcn_sched_barrier(0);
     }
-    if constexpr (WEIGH) l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    return (sum[0] + sum[1]) + (sum[2] + sum[3]);
   }
   // O^T += V^T P^T over the tile's NB blocks of 32 keys
   template <int NB>
   __device__ __forceinline__ void values(const char* vl, const R (&p)[2 * NB], int lane) {
     constexpr int DT = D / 32, S = 2 * NB;
-    int at = Rows::col_start(lane);
+    int at = Rows::col_start(lane_now());
     asm volatile("" : "+v"(at));
     R vf[2][DT];
     const auto load = [&](int s) {
@@ -692,6 +692,8 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, const AttnItem& i
   KeyTile walk = first_tile(keys);
   if (walk.count > 0) cache.template ask_pages<KT>(walk, numbers);
   f32x16 sa[NB], sb[NB];
+#pragma unroll
+  for (int b = 0; b < NB; ++b) sa[b] = f32x16{};
   typename Mm<T>::R p[2 * NB];
   // SIDE: the buffers of d0's V; s: its scores, then those of d1 in `next`
   const auto step = [&](auto side, f32x16 (&s)[NB], f32x16 (&next)[NB]) {
@@ -700,10 +702,10 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, const AttnItem& i
     lds_barrier();
     State d2{};
     uint64_t v2 = 0;
-    if (d1.any) load_rows<T, D, N>(cache, v1, cache.vrow, dst + L::kOffV + (SIDE ^ 1) * L::kTileBytes, N * wave);
+    if (d1.any) load_rows<T, D, N>(cache, v1, cache.vt, dst + L::kOffV + (SIDE ^ 1) * L::kTileBytes, N * wave);
     if (walk.count > 0) {
       const auto at = cache.template find_rows<KT>(walk, numbers, &d2.there);
-      load_rows<T, D, N>(cache, at.k, cache.krow, dst + SIDE * L::kTileBytes, N * wave);
+      load_rows<T, D, N>(cache, at.k, cache.kt, dst + SIDE * L::kTileBytes, N * wave);
       v2 = at.v;
       d2.base = walk.base;
       d2.own = walk.own;
@@ -721,15 +723,21 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, const AttnItem& i
       if (d0.there != kAll || least < d0.base + KT) w.mask(s, d0.own ? mine - d0.base : KT, d0.there, lane);
     }
     if (!idle) {
-      if (!d0.any) {
-        if (d1.any) w.template scores<NB, false>(kl, next, s, p, scale2, lane);
-      } else {
-        w.raise(s, scale2);
-        if (d1.any) w.template scores<NB, true>(kl, next, s, p, scale2, lane);
-        else w.weigh(s, p, scale2);
+      // The maximum is looked at only where a row has none yet, or where a weight turns out
+      // to be large (2^13 at most in a tile's half): the scores are there until then.
+      // Without a tile d0 weights are made of whatever was there, without a tile d1 scores,
+      // and not looked at.
+      if (rarely(d0.any && __any(w.m == -INFINITY))) w.raise(s, scale2);
+      float sum = w.template scores<NB, true>(kl, next, s, p, scale2, lane);
+      if (d0.any) {
+        if (rarely(__any(sum > 8192.0f))) {
+          w.raise(s, scale2);
+          sum = w.weigh(s, p, scale2);
+        }
+        w.l += sum;
+        w.template values<NB>(vl, p, lane);
       }
     }
-    if (!idle && d0.any) w.template values<NB>(vl, p, lane);
     d0 = d1;
     d1 = d2;
     v1 = v2;
@@ -793,14 +801,14 @@ __device__ __forceinline__ void attend_keys(const AttnArgs& a, const AttnItem& i
     if (now) wait_dma_but<N>();   // its K and the next one's pages are here, V may be on its way
     f32x16 s[1];
     typename Mm<T>::R p[2];
-    if (now) w.template scores<1, false>(kl, s, s, p, scale2, lane);
+    if (now) (void)w.template scores<1, false>(kl, s, s, p, scale2, lane);
     wait_lds();
     any = next.count > 0;
     typename CacheAt<T, D>::RowsAt at{};
     bool asked = false;
     if (any) {
       at = cache.template find_rows<KT>(next, numbers, &there);
-      load_rows<T, D, N>(cache, at.k, cache.krow, kd, 0);
+      load_rows<T, D, N>(cache, at.k, cache.kt, kd, 0);
       cur = next;
       skip(step);
       asked = next.count > 0;
@@ -811,7 +819,7 @@ __device__ __forceinline__ void attend_keys(const AttnArgs& a, const AttnItem& i
       const bool whole = was_there == kAll && (!was.own || least >= was.base + KT);
       if (rarely(!whole)) w.mask(s, limit, was_there, lane);
       w.raise(s, scale2);
-      w.weigh(s, p, scale2);
+      w.l += w.weigh(s, p, scale2);
       if (asked) wait_dma_but<N + 1>();
       else if (any) wait_dma_but<N>();
       else wait_dma();
@@ -822,7 +830,7 @@ __device__ __forceinline__ void attend_keys(const AttnArgs& a, const AttnItem& i
       w.template values<1>(vl, p, lane);
       wait_lds();
     }
-    if (any) load_rows<T, D, N>(cache, at.v, cache.vrow, vd, 0);
+    if (any) load_rows<T, D, N>(cache, at.v, cache.vt, vd, 0);
   }
   w.l = half_sum(w.l);
   odd = __any(odd);
