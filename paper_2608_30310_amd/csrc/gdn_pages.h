@@ -134,74 +134,102 @@ struct QkArgs {
   int64_t kp, kt, kh, vp, vt, vh;
 };
 
-// A thread takes eight elements of a head row, D / 8 neighbouring lanes a row.
-constexpr int kQkThreads = 256;
-template <typename T, int D, bool INTERLEAVED>
+// A thread takes eight elements of a head row, D / 8 neighbouring lanes a row; a wave up
+// to R rows each of one token, whose cosines and sines it keeps.  All rows are asked for
+// before the first is used.
+constexpr int kQkThreads = 256, kQkWaves = kQkThreads / kWave;
+// From here on (waves at one row for a lane) a wave takes four rows: the keys and queries
+// of 820 tokens, 32 + 4 + 4 heads of 128, take 7.0 us with one and 8.2 with four, of 8192
+// tokens 48 and 38 (with two or five as with four).
+constexpr int64_t kQkManyWaves = 16384;
+template <typename T, int D, bool INTERLEAVED, int R>
 __global__ __launch_bounds__(kQkThreads)
-void k_qk_norm_rope(QkArgs a) {
-  constexpr int LPR = D / 8, UNITS = kQkThreads / LPR;
-  const int lane = threadIdx.x % LPR, per = a.heads + (a.v ? 2 : 1) * a.kv_heads;
-  const int64_t unit = static_cast<int64_t>(blockIdx.x) * UNITS + threadIdx.x / LPR;
-  if (unit >= static_cast<int64_t>(a.tokens) * per) return;
-  const int t = static_cast<int>(unit / per), u = static_cast<int>(unit - static_cast<int64_t>(t) * per);
-  const int pos = a.positions[t];
-  if (pos < 0 || pos >= a.num_positions) return;   // whole rows of lanes leave together
-  const bool is_q = u < a.heads, is_v = u >= a.heads + a.kv_heads;
-  const int h = is_q ? u : is_v ? u - a.heads - a.kv_heads : u - a.heads;
-  const T* src = is_q ? static_cast<const T*>(a.q) + t * a.ldq
-                      : is_v ? static_cast<const T*>(a.v) + t * a.ldv : static_cast<const T*>(a.k) + t * a.ldk;
-  float x[8];
-  load_run<T, 8>(src + h * D + 8 * lane, x);
-  const float* w = is_q ? a.q_weight : is_v ? nullptr : a.k_weight;
-  if (w) {
-    float s = 0.0f;
+void k_qk_norm_rope(QkArgs a, uint32_t chunks) {
+  constexpr int LPR = D / 8, ROWS = kWave / LPR, V = sizeof(T) / 2;   // V: 16-byte pieces of eight elements
+  const uint32_t id = __builtin_amdgcn_readfirstlane(blockIdx.x * kQkWaves + threadIdx.x / kWave);
+  const int t = static_cast<int>(id / chunks), c = static_cast<int>(id % chunks);
+  if (t >= a.tokens) return;
+  const int lane = threadIdx.x % LPR, heads = a.heads + (a.v ? 2 : 1) * a.kv_heads;
+  const int pos = a.positions[t], slot = a.k_cache ? a.slots[t] : -1;
+  if (pos < 0 || pos >= a.num_positions) return;
+  const int from = c * R * ROWS + threadIdx.x % kWave / LPR;
+  u32x4 raw[R][V];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) s = fmaf(x[j], x[j], s);
+  for (int i = 0; i < R; ++i) {
+    const int u = min(from + i * ROWS, heads - 1);
+    const T* src = u < a.heads ? static_cast<const T*>(a.q) + t * a.ldq + u * D
+                   : u < a.heads + a.kv_heads ? static_cast<const T*>(a.k) + t * a.ldk + (u - a.heads) * D
+                                              : static_cast<const T*>(a.v) + t * a.ldv + (u - a.heads - a.kv_heads) * D;
 #pragma unroll
-    for (int off = 1; off < LPR; off <<= 1) s += __shfl_xor(s, off, LPR);
-    const float r = rsqrtf(s * (1.0f / D) + a.eps);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = x[j] * r * w[8 * lane + j];
+    for (int j = 0; j < V; ++j) raw[i][j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src + 8 * lane) + j);
   }
-  if (!is_v) {
-    const float* cs = a.cos_sin + static_cast<int64_t>(pos) * a.rotary;
-    const int half = a.rotary / 2;
+  const int half = a.rotary / 2;
+  const bool turned = 8 * lane < a.rotary, first = 8 * lane < half;
+  constexpr int NC = INTERLEAVED ? 4 : 8;
+  float co[NC] = {}, si[NC] = {};
+  if (turned) {
+    const float* cs = a.cos_sin + static_cast<int64_t>(pos) * a.rotary + (INTERLEAVED ? 4 * lane : 8 * lane - (first ? 0 : half));
+    load_run<float, NC>(cs, co);
+    load_run<float, NC>(cs + half, si);
+  }
+  // a pair's other element: 8 * half elements on, or back
+  const int other = INTERLEAVED || !turned ? lane : first ? lane + half / 8 : lane - half / 8;
+  const int64_t page = slot < 0 ? 0 : static_cast<uint32_t>(slot) / static_cast<uint32_t>(a.page_size);
+  const int64_t in_page = slot < 0 ? 0 : slot - page * a.page_size;
+  const bool kept = slot >= 0 && slot < a.slots_end;
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    const int u = from + i * ROWS;
+    if (u >= heads) return;   // whole rows of lanes leave together
+    const bool is_q = u < a.heads, is_v = u >= a.heads + a.kv_heads;
+    const int h = is_q ? u : is_v ? u - a.heads - a.kv_heads : u - a.heads;
+    if (is_v) {
+      if (kept) {
+        u32x4* to = reinterpret_cast<u32x4*>(static_cast<T*>(a.v_cache) + page * a.vp + in_page * a.vt + h * a.vh + 8 * lane);
+#pragma unroll
+        for (int j = 0; j < V; ++j) to[j] = raw[i][j];
+      }
+      continue;
+    }
+    float x[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = vec_elt<T>(raw[i][j / (8 / V)], j % (8 / V));
+    if (a.q_weight) {
+      float s = 0.0f, w[8];
+      load_run<float, 8>((is_q ? a.q_weight : a.k_weight) + 8 * lane, w);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) s = fmaf(x[j], x[j], s);
+#pragma unroll
+      for (int off = 1; off < LPR; off <<= 1) s += __shfl_xor(s, off, LPR);
+      const float r = rsqrtf(s * (1.0f / D) + a.eps);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] = x[j] * r * w[j];
+    }
     if constexpr (INTERLEAVED) {
-      if (8 * lane < a.rotary) {
+      if (turned) {
 #pragma unroll
         for (int p = 0; p < 4; ++p) {
-          const float c = cs[4 * lane + p], s = cs[half + 4 * lane + p], e = x[2 * p], o = x[2 * p + 1];
-          x[2 * p] = e * c - o * s;
-          x[2 * p + 1] = o * c + e * s;
+          const float e = x[2 * p], o = x[2 * p + 1];
+          x[2 * p] = e * co[p] - o * si[p];
+          x[2 * p + 1] = o * co[p] + e * si[p];
         }
       }
     } else {
-      const bool turned = 8 * lane < a.rotary, first = 8 * lane < half;
-      const int other = turned ? (first ? lane + half / 8 : lane - half / 8) : lane;
       float y[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) y[j] = __shfl(x[j], other, LPR);
       if (turned) {
-        const int p = 8 * lane - (first ? 0 : half);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const float c = cs[p + j], s = cs[half + p + j];
-          x[j] = first ? x[j] * c - y[j] * s : x[j] * c + y[j] * s;
-        }
+        for (int j = 0; j < 8; ++j) x[j] = first ? x[j] * co[j] - y[j] * si[j] : x[j] * co[j] + y[j] * si[j];
       }
     }
+    if (is_q) {
+      store8(static_cast<T*>(a.q_out) + t * a.ldqo + h * D + 8 * lane, x);
+    } else {
+      if (a.k_out) store8(static_cast<T*>(a.k_out) + t * a.ldko + h * D + 8 * lane, x);
+      if (kept) store8(static_cast<T*>(a.k_cache) + page * a.kp + in_page * a.kt + h * a.kh + 8 * lane, x);
+    }
   }
-  if (is_q) {
-    store8(static_cast<T*>(a.q_out) + t * a.ldqo + h * D + 8 * lane, x);
-    return;
-  }
-  if (!is_v && a.k_out) store8(static_cast<T*>(a.k_out) + t * a.ldko + h * D + 8 * lane, x);
-  T* cache = static_cast<T*>(is_v ? a.v_cache : a.k_cache);
-  if (!cache) return;
-  const int slot = a.slots[t];
-  if (slot < 0 || slot >= a.slots_end) return;
-  const int64_t page = slot / a.page_size, r = slot % a.page_size;
-  store8(cache + (is_v ? page * a.vp + r * a.vt + h * a.vh : page * a.kp + r * a.kt + h * a.kh) + 8 * lane, x);
 }
 
 }  // namespace gdn

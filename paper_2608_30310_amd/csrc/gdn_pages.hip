@@ -33,14 +33,22 @@ bool meet(const Region& a, const Region& b) {
   return overlap(a.p, a.bytes(), b.p, b.bytes());
 }
 
+template <typename T, int D, int R>
+gdn_status launch_qk_rows(const QkArgs& a, bool interleaved, hipStream_t stream) {
+  constexpr int rows = R * kWave / (D / 8);   // of a wave
+  const uint32_t chunks = static_cast<uint32_t>((a.heads + (a.v ? 2 : 1) * a.kv_heads + rows - 1) / rows);
+  const dim3 grid(static_cast<uint32_t>((static_cast<int64_t>(a.tokens) * chunks + kQkWaves - 1) / kQkWaves));
+  if (interleaved) hipLaunchKernelGGL((k_qk_norm_rope<T, D, true, R>), grid, dim3(kQkThreads), 0, stream, a, chunks);
+  else hipLaunchKernelGGL((k_qk_norm_rope<T, D, false, R>), grid, dim3(kQkThreads), 0, stream, a, chunks);
+  return plaunched("norm and rotation launch");
+}
+
+// With few tokens every row gets lanes of its own, with many a wave keeps a token's
+// cosines over its rows.
 template <typename T, int D>
 gdn_status launch_qk(const QkArgs& a, bool interleaved, hipStream_t stream) {
-  constexpr int units = kQkThreads / (D / 8);
-  const int64_t total = static_cast<int64_t>(a.tokens) * (a.heads + (a.v ? 2 : 1) * a.kv_heads);
-  const dim3 grid(static_cast<uint32_t>((total + units - 1) / units));
-  if (interleaved) hipLaunchKernelGGL((k_qk_norm_rope<T, D, true>), grid, dim3(kQkThreads), 0, stream, a);
-  else hipLaunchKernelGGL((k_qk_norm_rope<T, D, false>), grid, dim3(kQkThreads), 0, stream, a);
-  return plaunched("norm and rotation launch");
+  const int64_t waves = static_cast<int64_t>(a.tokens) * (a.heads + (a.v ? 2 : 1) * a.kv_heads) / (kWave / (D / 8));
+  return waves < kQkManyWaves ? launch_qk_rows<T, D, 1>(a, interleaved, stream) : launch_qk_rows<T, D, 4>(a, interleaved, stream);
 }
 
 }  // namespace
