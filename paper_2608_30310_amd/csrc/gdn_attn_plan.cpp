@@ -13,8 +13,10 @@ namespace {
 constexpr int64_t kMaxInt = std::numeric_limits<int32_t>::max();
 constexpr int64_t kMaxStride = int64_t{1} << 23;
 
-// Workgroups of the attention that the chip holds at once, and the fewest keys of
-// a piece of a split range.
+// Workgroups of the attention that the chip holds at once: two a CU, but one where a
+// workgroup's tiles (fp32, heads of 128) fill its LDS.  The fewest keys of a piece of a
+// split range: as much work as the joining of its result takes, in fp32 (a quarter of
+// the rate) from half as many keys.
 constexpr int64_t kAttnPlaces = 512, kLeastChunk = 256;
 
 gdn_status bad(std::string* err, const std::string& what, gdn_status st = GDN_ERR_BAD_SHAPE) {
@@ -173,17 +175,20 @@ gdn_status make_attn_plan(const gdn_attn_shape* s, const int32_t* cu, AttnPlan* 
   int64_t tiles = 0;
   for (int64_t n = 0; n < N; ++n) tiles += ((static_cast<int64_t>(cu[n + 1]) - cu[n]) * G + p.own_tile - 1) / p.own_tile;
   p.own_slots = tile_slots(p.rows, N, p.own_tile);
-  const auto pieces = [](int64_t keys, int64_t items, int64_t places, int32_t* splits, int32_t* chunk) {
-    const int64_t most = std::max<int64_t>(1, (keys + kLeastChunk - 1) / kLeastChunk);
+  const bool bf16 = s->dtype == GDN_BF16;
+  const int64_t least_chunk = bf16 ? kLeastChunk : kLeastChunk / 2;
+  const auto pieces = [least_chunk](int64_t keys, int64_t items, int64_t places, int32_t* splits, int32_t* chunk) {
+    const int64_t most = std::max<int64_t>(1, (keys + least_chunk - 1) / least_chunk);
     int64_t n = std::min(most, std::max<int64_t>(1, places / std::max<int64_t>(1, items)));
     const int64_t each = std::max<int64_t>(64, ((keys + n - 1) / n + 63) / 64 * 64);
     *chunk = static_cast<int32_t>(each);
     *splits = static_cast<int32_t>(std::max<int64_t>(1, (keys + each - 1) / each));
   };
-  const int64_t places = s->dtype == GDN_BF16 ? kAttnPlaces : kAttnPlaces / 2;
-  constexpr int64_t waves = kPlanTile / kPlanRows;   // of a workgroup
   const int64_t line = N * H * ((p.max_len + static_cast<int64_t>(kPlanLineTile) - 1) / kPlanLineTile);   // tiles at most
   p.stream = p.own_tile == kPlanRows && N <= kPlanLineSeqs && line <= int64_t{1} << 30;
+  // (fp32's single tokens wait for memory with half as many waves: 161 us, 175 with all)
+  const int64_t places = bf16 || (!p.stream && s->head_dim == 64) ? kAttnPlaces : kAttnPlaces / 2;
+  constexpr int64_t waves = kPlanTile / kPlanRows;   // of a workgroup
   if (P > 0 && (p.stream || tiles * H < places || p.rows < tiles * p.own_tile * 3 / 5)) {
     p.shared_tiles = (p.rows + kPlanTile - 1) / kPlanTile;
     if (p.stream && p.rows <= kPlanRows) {
