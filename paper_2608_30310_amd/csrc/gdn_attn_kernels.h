@@ -366,7 +366,7 @@ __device__ __forceinline__ void load_rows(const CacheAt<T, D>& c, uint64_t rows_
   }
 }
 
-// Values of rows that are not there count as zeros.  DROP: some rows of the item do
+// Values of rows that are not there count as zeros.  drop: some rows of the item do
 // not see some keys (weight zero), so what is not finite must not enter the products
 // either; returns whether there was any in this thread's part (of `threads` threads),
 // for add_dropped.
@@ -376,7 +376,7 @@ __device__ __forceinline__ bool clean_values(char* vl, uint64_t there, bool drop
   bool odd = false;
   asm volatile("" : "+v"(thread));
 #pragma unroll 1
-  for (int p = thread; p < KT * Rows::kPieces; p += threads) {
+  for (int p = (drop ? 0 : __builtin_ctzll(~there)) * Rows::kPieces + thread; p < KT * Rows::kPieces; p += threads) {
     u32x4* at = reinterpret_cast<u32x4*>(vl + 16 * p);
     if (!(there >> (p / Rows::kPieces) & 1)) {
       *at = u32x4{0, 0, 0, 0};
@@ -588,6 +588,12 @@ __device__ __forceinline__ int own_limit(const AttnItem& it, int groups, int r) 
   return max(min(it.tail + 1 + i, it.len), 0);
 }
 
+// The own tokens that every row of the item sees; INT_MAX if that is all there are.
+__device__ __forceinline__ int least_limit(const AttnArgs& a, const AttnItem& it) {
+  const int least = __builtin_amdgcn_readfirstlane(own_limit(it, a.groups, 0));
+  return least < it.keys.first1 + it.keys.count1 ? least : INT_MAX;
+}
+
 // The token and query head of row r of the item.
 struct RowAt { int64_t token; int head; };
 __device__ __forceinline__ RowAt row_at(const AttnArgs& a, const AttnItem& it, int r) {
@@ -674,7 +680,7 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, const AttnItem& i
   w.clear();
   const bool idle = w0 >= it.rows;
   const int mine = own_limit(it, a.groups, r);
-  const int first = own_limit(it, a.groups, 0);   // the least of the workgroup, then of the wave
+  const int first = least_limit(a, it);   // of the workgroup, then the wave's least
   const int least = __builtin_amdgcn_readfirstlane(own_limit(it, a.groups, min(w0, it.rows - 1)));
   lds_byte* dst = (lds_byte*)lds;
   uint32_t* odd = reinterpret_cast<uint32_t*>(lds + L::kOffOdd);   // values were dropped
@@ -770,7 +776,7 @@ __device__ __forceinline__ void attend_keys(const AttnArgs& a, const AttnItem& i
   AttnWave<T, D> w;
   w.load_q(static_cast<const T*>(a.q) + mine_at.token * a.ldq + static_cast<int64_t>(mine_at.head) * D, a.flip, lane / 32);
   w.clear();
-  const int mine = own_limit(it, a.groups, r), least = __builtin_amdgcn_readfirstlane(own_limit(it, a.groups, 0));
+  const int mine = own_limit(it, a.groups, r), least = least_limit(a, it);
   const char* kl = lds + wave * 2 * L::kOwnBytes;
   char* vl = lds + wave * 2 * L::kOwnBytes + L::kOwnBytes;
   lds_byte* kd = (lds_byte*)lds + wave * 2 * L::kOwnBytes;
@@ -972,19 +978,23 @@ __device__ __forceinline__ void lay_line(const AttnArgs& a, char* lds, bool keep
 // The waves that share `tiles` (of all K/V heads, of a line of `total` for each): no more
 // than leave each as many tiles as balance its walk with the joining of the parts (a tile
 // of a lonely wave takes about 1.3 us, 16 parts of a row 0.6).
-__device__ __forceinline__ int line_waves(const AttnArgs& a, int64_t tiles, int total) {
+__device__ __forceinline__ int line_waves(const AttnArgs& a, int tiles, int total) {
   const int least = max(1, static_cast<int>(ceilf(sqrtf(static_cast<float>(total) / (32.0f * a.n_seqs)))));
-  return __builtin_amdgcn_readfirstlane(static_cast<int>(min((tiles + least - 1) / least, static_cast<int64_t>(a.stream_waves))));
+  return __builtin_amdgcn_readfirstlane(min(static_cast<int>(static_cast<uint32_t>(tiles + least - 1) / static_cast<uint32_t>(least)), a.stream_waves));
 }
-__device__ __forceinline__ int64_t share_start(int64_t tiles, int waves, int w) { return tiles * w / waves; }
-__device__ __forceinline__ int share_of(int64_t tiles, int waves, int64_t t) {   // the wave whose share holds tile t
-  return static_cast<int>(((t + 1) * waves - 1) / tiles);
+// Equal shares, the first ones a tile longer where it does not come out even.
+__device__ __forceinline__ int share_start(uint32_t tiles, uint32_t waves, int w) {
+  return w * static_cast<int>(tiles / waves) + min(w, static_cast<int>(tiles % waves));
+}
+__device__ __forceinline__ int share_of(uint32_t tiles, uint32_t waves, uint32_t t) {   // the wave whose share holds tile t
+  const uint32_t each = tiles / waves, longer = tiles % waves, behind = longer * (each + 1);
+  return static_cast<int>(t < behind ? t / (each + 1) : longer + (t - behind) / each);
 }
 
 // The items of a wave, one after another; those of a workgroup come to all of its waves.
 struct AttnWork {
   int shared, shared_step;   // the next shared item
-  int64_t at, end;           // what is left of the share of the line
+  int at, end;               // what is left of the share of the line
   int wave;                  // of the line
   bool own_first;
 };
@@ -1028,7 +1038,7 @@ __device__ __forceinline__ bool own_item(const AttnArgs& a, int b, AttnItem& it)
 }
 __device__ __forceinline__ void line_item(const AttnArgs& a, const Line& line, AttnWork& w, AttnItem& it) {
   // the last sequence that begins at the tile or before it; 64 candidates at a time
-  const int t = static_cast<int>(w.at / a.kv_heads), lane = threadIdx.x % kWave;
+  const int t = static_cast<int>(static_cast<uint32_t>(w.at) / static_cast<uint32_t>(a.kv_heads)), lane = threadIdx.x % kWave;
   int lo = 0, hi = a.n_seqs;
   while (hi - lo > 1) {
     const int step = (hi - lo + kWave - 1) / kWave, at = lo + lane * step;
@@ -1039,9 +1049,9 @@ __device__ __forceinline__ void line_item(const AttnArgs& a, const Line& line, A
   const int n = __builtin_amdgcn_readfirstlane(lo);
   const int begin = __builtin_amdgcn_readfirstlane(line.tiles[n]),
             tiles = __builtin_amdgcn_readfirstlane(line.tiles[n + 1]) - begin;
-  const int rest = static_cast<int>(w.at - static_cast<int64_t>(begin) * a.kv_heads), off = rest % tiles;
-  it.kvh = rest / tiles;
-  const int take = static_cast<int>(min(w.end - w.at, static_cast<int64_t>(tiles - off)));
+  const int rest = w.at - begin * a.kv_heads;
+  it.kvh = static_cast<int>(static_cast<uint32_t>(rest) / static_cast<uint32_t>(tiles));
+  const int off = rest - it.kvh * tiles, take = min(w.end - w.at, tiles - off);
   const int start = __builtin_amdgcn_readfirstlane(line.cu[n]),
             count = __builtin_amdgcn_readfirstlane(line.cu[n + 1]) - start;
   it.row0 = it.first_row = start * a.groups;
@@ -1090,8 +1100,7 @@ void k_attn(AttnArgs a) {
       if (a.stream_first > 0) work.shared = a.shared_items;   // there are others for these
       lay_line<T, D>(a, lds, group == a.stream_first);
       const int total = __builtin_amdgcn_readfirstlane(line.tiles[a.n_seqs]);
-      const int64_t tiles = static_cast<int64_t>(total) * a.kv_heads;
-      const int waves = line_waves(a, tiles, total);
+      const int tiles = total * a.kv_heads, waves = line_waves(a, tiles, total);
       work.wave = kAttnWaves * (group - a.stream_first) + wave;
       if (work.wave < waves) {
         work.at = share_start(tiles, waves, work.wave);
@@ -1151,9 +1160,8 @@ void k_attn_join(AttnArgs a) {
   int own = a.own_splits;
   if (a.stream) {
     const int before = a.line[lo], mine = a.line[lo + 1] - before, total = a.line[a.n_seqs];
-    const int64_t tiles = static_cast<int64_t>(total) * a.kv_heads;
-    const int waves = line_waves(a, tiles, total);
-    const int64_t t0 = static_cast<int64_t>(before) * a.kv_heads + static_cast<int64_t>(kvh) * mine;
+    const int tiles = total * a.kv_heads, waves = line_waves(a, tiles, total);
+    const int t0 = before * a.kv_heads + kvh * mine;
     const int w0 = share_of(tiles, waves, t0);
     own = share_of(tiles, waves, t0 + mine - 1) - w0 + 1;
     own_step = 2;
