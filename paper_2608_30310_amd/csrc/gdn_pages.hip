@@ -111,9 +111,13 @@ gdn_status gdn_extend_pages(const gdn_pages_shape* shape, const int32_t* cu_seql
   const PagesArgs a{s.num_seqs, s.table_width, s.page_size, s.num_free, s.first, cu_seqlens, table_in, lens_in, free_pages,
                     taken_in, table_out, lens_out, taken_out, slots, positions, ws, ws + n, ws + 2 * n};
   const hipStream_t hs = static_cast<hipStream_t>(stream);
-  hipLaunchKernelGGL(k_pages_plan, dim3(1), dim3(kPagesPlanThreads), 0, hs, a);
-  if (n > 0)
-    hipLaunchKernelGGL(k_pages_fill<kPageTokens>, dim3(static_cast<uint32_t>(p.slots)), dim3(kPagesThreads), 0, hs, a);
+  const dim3 fill(static_cast<uint32_t>(p.slots));
+  if (n > 0 && n <= kPagesFew && lens_out != lens_in && taken_out != taken_in) {
+    hipLaunchKernelGGL((k_pages_fill<kPageTokens, false>), fill, dim3(kPagesThreads), 0, hs, a);
+  } else {
+    hipLaunchKernelGGL(k_pages_plan, dim3(1), dim3(kPagesPlanThreads), 0, hs, a);
+    if (n > 0) hipLaunchKernelGGL((k_pages_fill<kPageTokens, true>), fill, dim3(kPagesThreads), 0, hs, a);
+  }
   return plaunched("pages launch");
 }
 
