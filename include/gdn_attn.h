@@ -120,8 +120,9 @@ typedef struct {
   int32_t num_pages, page_size;
   int32_t table_width;   /* W >= 1                                           */
   int32_t prefix_len;    /* P >= 0: tokens that all sequences share          */
-  int32_t max_len;       /* no sequence holds more own tokens than this (the
-                            rest is not seen); at most W page_size, 0 = that */
+  int32_t max_len;       /* no sequence holds more own tokens than this: a
+                            length above it counts as max_len, one below 0 as
+                            0; at most W page_size, 0 = that                 */
   float scale;           /* finite                                           */
   int64_t ld_q, ld_out;
   int64_t k_page, k_token, k_head;  /* elements between pages, tokens of a page and heads */

@@ -185,7 +185,8 @@ def prefix_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tens
     included, which are its last: query i of q_n sees the prefix and the own
     tokens up to lens[n] - q_n + i.  A query that sees nothing gets zeros.
     ``max_len``: no sequence holds more own tokens (default: what its table row
-    has room for); a bound near the truth spares idle workgroups.  ``scale``
+    has room for), a length above it counts as it; a bound near the truth spares
+    idle workgroups.  ``scale``
     defaults to D^-1/2.  Returns out [T, Hq, D]; its rows behind the last
     sequence are left alone.
     """

@@ -37,6 +37,8 @@ gdn_status check_ld(const char* name, int64_t ld, int64_t least, int64_t vec, st
   return GDN_OK;
 }
 
+constexpr int64_t kMaxExtent = int64_t{1} << 48;   // elements between the rows of a cache: offsets in bytes fit 64 bits
+
 // Strides of a cache: its rows of `dim` elements are apart; in 16 bytes they fit 31 bits.
 gdn_status check_cache(const char* name, int32_t pages, int32_t page_size, int32_t heads, int32_t dim, int64_t page,
                        int64_t token, int64_t head, int64_t vec, std::string* err) {
@@ -55,6 +57,7 @@ gdn_status check_cache(const char* name, int32_t pages, int32_t page_size, int32
   for (const auto& x : d) {
     if (x.count == 1) continue;
     if (x.stride < extent) return bad(err, std::string("rows of ") + name + " overlap");
+    if (x.count - 1 > kMaxExtent / x.stride) return bad(err, std::string(name) + " is too large", GDN_ERR_UNSUPPORTED);
     extent += (x.count - 1) * x.stride;
   }
   return GDN_OK;

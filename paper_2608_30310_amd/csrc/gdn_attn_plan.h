@@ -21,7 +21,7 @@ struct PagesPlan {
 };
 gdn_status make_pages_plan(const gdn_pages_shape* s, const int32_t* cu, PagesPlan* p, std::string* err);
 
-// cached: a cache is given (its fields are looked at); k_out, v: k_out, v and v_cache are given
+// k_out, k_cache: given (their fields are looked at); v: v and v_cache are
 gdn_status check_qk(const gdn_qk_shape* s, bool k_out, bool k_cache, bool v, std::string* err);
 
 gdn_status check_attn(const gdn_attn_shape* s, std::string* err);
