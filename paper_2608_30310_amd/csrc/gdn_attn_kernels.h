@@ -736,9 +736,11 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, const AttnItem& i
       // Without a tile d0 weights are made of whatever was there, without a tile d1 scores,
       // and not looked at.
       if (rarely(d0.any && __any(w.m == -INFINITY))) w.raise(s, scale2);
-      float sum = w.template scores<NB, true>(kl, next, s, p, scale2, lane);
+      const bool scored = sizeof(T) == 2 || d1.any;   // (fp32's scores cost too much to be formed of nothing)
+      float sum = 0.0f;
+      if (scored) sum = w.template scores<NB, true>(kl, next, s, p, scale2, lane);
       if (d0.any) {
-        if (rarely(__any(sum > 256.0f))) {
+        if (rarely(!scored || __any(sum > 256.0f))) {
           w.raise(s, scale2);
           sum = w.weigh(s, p, scale2);
         }
