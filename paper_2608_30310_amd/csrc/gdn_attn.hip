@@ -99,7 +99,9 @@ gdn_status gdn_prefix_attention(const gdn_attn_shape* shape, const int32_t* cu_s
   a.scale2 = std::max(std::fabs(s.scale) * 1.44269504088896f, std::numeric_limits<float>::min());
   // rows of a DMA: 1 KiB of rows
   const int64_t rows = 1024 / (s.head_dim * e);
-  a.dma_in_page = s.page_size % rows == 0 && a_stride_fits(s.k_token / vec) && a_stride_fits(s.v_token / vec);
+  const bool near = a_stride_fits(s.k_token / vec) && a_stride_fits(s.v_token / vec);
+  a.dma_in_page = s.page_size % rows == 0 && near;
+  a.part_in_page = s.page_size % (s.dtype == GDN_BF16 ? kPartRows : kPartRowsF32) == 0 && near;
   a.flip = std::signbit(s.scale) ? 0x80000000u : 0u;
   a.shared_splits = p.shared_splits, a.shared_chunk = p.shared_chunk;
   a.shared_tiles = static_cast<int32_t>(p.shared_tiles), a.shared_items = static_cast<int32_t>(p.shared_items);

@@ -30,6 +30,7 @@ constexpr int kAttnThreads = 256;
 constexpr int kAttnWaves = kAttnThreads / kWave;
 constexpr int kAttnRows = 32;                        // of a wave
 constexpr int kAttnTile = kAttnRows * kAttnWaves;    // of a workgroup whose waves take rows of their own
+constexpr int kPartRows = 16, kPartRowsF32 = 8;      // rows of such a workgroup's K/V tiles that a wave loads
 
 constexpr int kStreamSeqs = 1024;                    // sequences of a line (see there)
 
@@ -40,6 +41,7 @@ struct AttnArgs {
   float scale2;           // |scale| log2 e
   uint32_t flip;          // sign bits of the queries where scale is negative
   int32_t dma_in_page;    // the rows of a DMA never lie in two pages, and their offsets fit 32 bits
+  int32_t part_in_page;   // so do those of a wave's part of a workgroup's tile
   // items: shared ones over the prefix alone, all rows packed (shared_splits 0: none), then own ones
   int32_t shared_splits, shared_chunk, shared_tiles, shared_items;
   int32_t own_tile, own_splits, own_chunk, own_slots;
@@ -79,13 +81,17 @@ struct Mm<uint16_t> {
   static __device__ __forceinline__ f32x16 mul(const R& a, const R& b, const f32x16& c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
   }
-  // p: eight weights, rounded to bf16 as the product takes them
-  static __device__ __forceinline__ R pack(const float (&p)[8]) {
+  // p: eight weights, rounded to bf16 as the product takes them, and their sums: of what
+  // enters the product, so that the rounding of a weight is one of numerator and
+  // denominator alike; two at a time
+  static __device__ __forceinline__ R pack(const float (&p)[8], float (&sum)[4]) {
     u32x4 w;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const f32x2 x = {p[2 * j], p[2 * j + 1]};
-      w[j] = __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
+      const bf16x2 y = __builtin_convertvector(x, bf16x2), one = {1.0f, 1.0f};
+      w[j] = __builtin_bit_cast(uint32_t, y);
+      sum[j] = __builtin_amdgcn_fdot2_f32_bf16(y, one, sum[j], false);
     }
     return __builtin_bit_cast(R, w);
   }
@@ -103,7 +109,11 @@ struct Mm<float> {
     for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], c, 0, 0, 0);
     return c;
   }
-  static __device__ __forceinline__ R pack(const float (&p)[8]) { return R{p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7]}; }
+  static __device__ __forceinline__ R pack(const float (&p)[8], float (&sum)[4]) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sum[j % 4] += p[j];
+    return R{p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7]};
+  }
   static __device__ __forceinline__ R flip(const R& a, uint32_t sign) {
     R r;
 #pragma unroll
@@ -285,13 +295,13 @@ template <typename T, int D>
 struct CacheAt {
   uint64_t k, v;
   uint32_t kp, kt, vp, vt, page_mul;
-  int page_shift, page_size, num_pages, dma_in_page;
+  int page_shift, page_size, num_pages, dma_in_page, part_in_page;
   __device__ __forceinline__ CacheAt(const AttnArgs& a, int kvh) {
     k = apart(reinterpret_cast<uint64_t>(a.k) + kvh * a.kh);
     v = apart(reinterpret_cast<uint64_t>(a.v) + kvh * a.vh);
     kp = apart(a.kp), kt = apart(a.kt), vp = apart(a.vp), vt = apart(a.vt), page_mul = apart(a.page_mul);
     page_shift = apart(a.page_shift), page_size = apart(a.page_size), num_pages = apart(a.num_pages);
-    dma_in_page = apart(a.dma_in_page);
+    dma_in_page = apart(a.dma_in_page), part_in_page = apart(a.part_in_page);
   }
   // The page index of token base + lane % KT of a tile (lanes behind its end: of its
   // last token), and the token's row there.
@@ -316,12 +326,28 @@ struct CacheAt {
     const int lane = lane_now();
     int row;
     page_index<KT>(t, &row);
-    const int page = ((const __attribute__((address_space(3))) int32_t*)numbers)[lane];
+    const int page = page_of(numbers);
     const bool ok = lane < min(KT, t.count) && page >= 0 && page < num_pages;
     *there = __ballot(ok);
     const uint32_t p = ok ? page : 0, r = ok ? row : 0;
     const auto far = [](uint32_t x, uint32_t y) { return static_cast<uint64_t>(x) * y; };
     return {k + 16 * (far(p, kp) + far(r, kt)), v + 16 * (far(p, vp) + far(r, vt))};
+  }
+  // Which rows of a tile are there, of the lane's page number.
+  static __device__ __forceinline__ int page_of(const lds_byte* numbers) {
+    return ((const __attribute__((address_space(3))) int32_t*)numbers)[lane_now()];
+  }
+  template <int KT>
+  __device__ __forceinline__ uint64_t rows_there(const KeyTile& t, int page) const {
+    constexpr uint64_t kAll = KT == 64 ? ~0ull : (1ull << (KT % 64)) - 1;
+    const uint64_t valid = __ballot(static_cast<uint32_t>(page) < static_cast<uint32_t>(num_pages));
+    return valid & (t.count >= KT ? kAll : (1ull << t.count) - 1);
+  }
+  // Address of row `key` of a tile, in page number `page`; of the cache's first unless ok.
+  __device__ __forceinline__ uint64_t row_at(uint64_t from, uint32_t page_step, uint32_t step, int key, int page, bool ok) const {
+    const uint32_t c = page_size == 1 ? key : __umulhi(key, page_mul) >> page_shift;
+    const uint32_t p = ok ? page : 0, r = ok ? key - c * page_size : 0;
+    return from + 16 * (static_cast<uint64_t>(p) * page_step + static_cast<uint64_t>(r) * step);
   }
 };
 
@@ -366,6 +392,37 @@ __device__ __forceinline__ void load_rows(const CacheAt<T, D>& c, uint64_t rows_
   }
 }
 
+// A wave's part of a workgroup's tile, N DMAs: rows N kRowsPerDma wave and on.  Where they
+// lie in one page their address is a scalar, and vector instructions are left for the
+// offsets of the pieces alone (the matrix unit leaves room for four a product, so each
+// counts: 16 suffixes behind 8192 tokens 2.74 ms with an address for every row, 2.58 with one).
+// `from`, `page_step`, `step`: of keys or values.
+template <typename T, int D, int N, int KT>
+__device__ __forceinline__ void load_part(const CacheAt<T, D>& c, uint64_t from, uint32_t page_step, uint32_t step, uint32_t row_off,
+                                          uint32_t piece, int base, int page, uint64_t there, lds_byte* to, int wave) {
+  typedef KvRows<T, D> Rows;
+  constexpr int RPD = Rows::kRowsPerDma, P = N * RPD;
+  to += N * wave * 1024;
+  const int turn = 16 * Rows::swz(P * wave);
+  if (!rarely(!c.part_in_page)) {
+    const bool ok = there >> (P * wave) & 1;
+    uint64_t at = c.row_at(from, page_step, step, base + P * wave, __builtin_amdgcn_readlane(page, P * wave), ok);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      async_piece(at, row_off + (piece ^ (turn ^ 16 * Rows::swz(RPD * i))), to + i * 1024);
+      at += static_cast<uint64_t>(16 * RPD) * step;
+    }
+  } else {
+    const int lane = lane_now(), r = lane % KT;
+    const uint64_t rows = c.row_at(from, page_step, step, base + r, page, there >> r & 1);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const uint64_t at = lane_at(rows, P * wave + RPD * i + lane / Rows::kPieces);
+      async_piece(reinterpret_cast<const void*>(at + (piece ^ (turn ^ 16 * Rows::swz(RPD * i)))), to + i * 1024);
+    }
+  }
+}
+
 // Values of rows that are not there count as zeros.  drop: some rows of the item do
 // not see some keys (weight zero), so what is not finite must not enter the products
 // either; returns whether there was any in this thread's part (of `threads` threads),
@@ -399,6 +456,7 @@ struct AttnWave {
   R q[D / 16];
   f32x16 o[D / 32];   // O^T: columns 32 dt + .. of row lane % 32
   float m, l;         // l: this half wave's part
+  int frag0, col0;    // where the lane's operands of a tile's K and V begin
   __device__ __forceinline__ void clear() {
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt)
@@ -406,6 +464,8 @@ struct AttnWave {
       for (int i = 0; i < 16; ++i) o[dt][i] = 0.0f;
     m = -INFINITY;
     l = 0.0f;
+    frag0 = Rows::frag_start(threadIdx.x % kWave);
+    col0 = Rows::col_start(threadIdx.x % kWave);
   }
   __device__ __forceinline__ void load_q(const T* row, uint32_t flip, int h) {
 #pragma unroll
@@ -448,12 +508,8 @@ struct AttnWave {
   __device__ __forceinline__ void weigh4(const f32x16 (&s)[NB], R (&p)[2 * NB], float (&w)[8], int i0, float scale2, float at,
                                          float (&sum)[4]) const {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const float e = __builtin_amdgcn_exp2f(fmaf(s[i0 / 16][i0 % 16 + k], scale2, -at));
-      sum[k] += e;
-      w[i0 % 8 + k] = e;
-    }
-    if (i0 % 8 == 4) p[i0 / 8] = Mm<T>::pack(w);
+    for (int k = 0; k < 4; ++k) w[i0 % 8 + k] = __builtin_amdgcn_exp2f(fmaf(s[i0 / 16][i0 % 16 + k], scale2, -at));
+    if (i0 % 8 == 4) p[i0 / 8] = Mm<T>::pack(w, sum);
   }
   // All of a tile; returns the sum of the weights (of this half wave).
   template <int NB>
@@ -471,7 +527,7 @@ struct AttnWave {
   __device__ __forceinline__ float scores(const char* kl, f32x16 (&next)[NB], const f32x16 (&s)[NB], R (&p)[2 * NB], float scale2,
                                           int lane) const {
     constexpr int U = D / 16, E = 16 * NB / U;   // scores for each step
-    int first = Rows::frag_start(lane_now());
+    int first = frag0;
     asm volatile("" : "+v"(first));   // one value that the steps turn, not an expression for each
     R kf[2][NB];
     const auto load = [&](int u) {
@@ -507,7 +563,7 @@ struct AttnWave {
   template <int NB>
   __device__ __forceinline__ void values(const char* vl, const R (&p)[2 * NB], int lane) {
     constexpr int DT = D / 32, S = 2 * NB;
-    int at = Rows::col_start(lane_now());
+    int at = col0;
     asm volatile("" : "+v"(at));
     R vf[2][DT];
     const auto load = [&](int s) {
@@ -550,7 +606,7 @@ __device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)"
 template <typename T, int D>
 struct AttnLds {
   typedef KvRows<T, D> Rows;
-  static constexpr int kTileKeys = sizeof(T) == 2 ? 64 : 32;   // of a workgroup whose waves take rows of their own
+  static constexpr int kTileKeys = kAttnWaves * (sizeof(T) == 2 ? kPartRows : kPartRowsF32);   // of a workgroup whose waves take rows of their own
   static constexpr int kTileBytes = kTileKeys * Rows::kPitch;
   static constexpr int kOwnBytes = 32 * Rows::kPitch;          // tiles of a wave that takes keys of its own
   static constexpr int kOffV = 2 * kTileBytes;                 // two of K, then two of V
@@ -688,13 +744,18 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, const AttnItem& i
   const float scale2 = apart(a.scale2);
   const KeyRange keys = apart_range(it.keys);
   lds_byte* numbers = dst + L::kOffPages + 4 * kWave * wave;
+  uint32_t piece, k_off, v_off;   // the lane's piece of a DMA, and where its row begins
+  {
+    const int j = lane / Rows::kPieces;
+    piece = 16 * (lane % Rows::kPieces ^ Rows::swz(j)), k_off = 16 * j * cache.kt, v_off = 16 * j * cache.vt;
+  }
   constexpr uint64_t kAll = KT == 64 ? ~0ull : (1ull << (KT % 64)) - 1;
   // While a tile's scores become weights and its values are added, the next one's
   // scores are formed, the next one's V and the K of the one after that come in, and
-  // the pages of one more are looked up.  K and V of tile t lie in buffers t % 2.
+  // the page numbers of one more.  K and V of tile t lie in buffers t % 2.
   struct State { int base; bool own, any; uint64_t there; };
   State d0{}, d1{};   // the tile whose scores are formed, and the one whose K is here
-  uint64_t v1 = 0;    // rows of d1's V
+  int page1 = 0;      // the lane's page number of d1
   KeyTile walk = first_tile(keys);
   if (walk.count > 0) cache.template ask_pages<KT>(walk, numbers);
   f32x16 sa[NB], sb[NB];
@@ -707,12 +768,15 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, const AttnItem& i
     wait_dma();
     lds_barrier();
     State d2{};
-    uint64_t v2 = 0;
-    if (d1.any) load_rows<T, D, N>(cache, v1, cache.vt, dst + L::kOffV + (SIDE ^ 1) * L::kTileBytes, N * wave);
+    int page2 = 0;
+    if (d1.any)
+      load_part<T, D, N, KT>(cache, cache.v, cache.vp, cache.vt, v_off, piece, d1.base, page1, d1.there,
+                             dst + L::kOffV + (SIDE ^ 1) * L::kTileBytes, wave);
     if (walk.count > 0) {
-      const auto at = cache.template find_rows<KT>(walk, numbers, &d2.there);
-      load_rows<T, D, N>(cache, at.k, cache.kt, dst + SIDE * L::kTileBytes, N * wave);
-      v2 = at.v;
+      page2 = cache.page_of(numbers);
+      d2.there = cache.template rows_there<KT>(walk, page2);
+      load_part<T, D, N, KT>(cache, cache.k, cache.kp, cache.kt, k_off, piece, walk.base, page2, d2.there,
+                             dst + SIDE * L::kTileBytes, wave);
       d2.base = walk.base;
       d2.own = walk.own;
       d2.any = true;
@@ -750,7 +814,7 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, const AttnItem& i
     }
     d0 = d1;
     d1 = d2;
-    v1 = v2;
+    page1 = page2;
   };
   while (true) {
     step(std::integral_constant<int, 0>(), sa, sb);
