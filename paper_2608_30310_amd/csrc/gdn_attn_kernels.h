@@ -722,7 +722,12 @@ __device__ __forceinline__ void put_columns(const AttnArgs& a, const AttnItem& i
   if (dt == 0 && lane < 32) a.part_ml[(it.part + wt) * kAttnRows + lane] = f32x2{m, l};
 }
 
-// Waves take rows of their own and share tiles of keys.
+// Waves take rows of their own and share tiles of keys, 64 for bf16 (two buffers each of K
+// and V are 64 KB, so two workgroups fit a CU: with one 3.59 ms instead of 2.58).  Bound by
+// the matrix cores and the vector instructions beside them, whose shares add up to most
+// of the cycles (49 % and 155 instructions a tile), at the clock that the power limit
+// leaves: 16 suffixes behind 8192 tokens 985 TFLOP/s, a prompt of 8192 tokens 956, long fp32
+// batches 115.
 template <typename T, int D>
 __device__ __forceinline__ void attend_rows(const AttnArgs& a, const AttnItem& it, const CacheAt<T, D>& cache, char* lds) {
   typedef AttnLds<T, D> L;
@@ -831,8 +836,11 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, const AttnItem& i
   for (int dt = 0; dt < D / 32; ++dt) put_columns<T, D>(e, it, wave, w.o[dt], dt, w.m, w.l, lane);
 }
 
-// At most 32 rows.  JOIN: the waves take every fourth tile of the keys each, and their
-// results are joined; else the item is this wave's alone.
+// At most 32 rows.  join: the waves take every fourth tile of the keys each, and their
+// results are joined; else the item is this wave's alone.  Nothing but loads counts: a
+// tile's K and V pass through LDS of the wave's own without a barrier, eight waves a CU keep
+// up to 128 KB on the way.  128 single tokens behind up to 2047 own and 8192 shared ones:
+// 92 us for 405 MB beside the shared items' products (72 for the DMA alone).
 template <typename T, int D>
 __device__ __forceinline__ void attend_keys(const AttnArgs& a, const AttnItem& it, const CacheAt<T, D>& cache, bool join, char* lds) {
   typedef AttnLds<T, D> L;
@@ -1194,7 +1202,8 @@ void k_attn(AttnArgs a) {
 
 // The items' partial results of a row into one.  A workgroup takes 32 packed rows of a
 // K/V head and one of the D / 8 groups of columns: lane (h, r) four columns of row r, a
-// wave every fourth part, kAttnAhead parts' loads in flight at a time.
+// wave every fourth part, kAttnAhead parts' loads in flight at a time.  11 us for 128 single
+// tokens of 32 heads with 12 parts each (32 MB), 5 for one: a chain of loads.
 constexpr int kAttnAhead = 4;
 template <typename T, int D>
 __global__ __launch_bounds__(kAttnThreads)
