@@ -840,7 +840,8 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, const AttnItem& i
 // results are joined; else the item is this wave's alone.  Nothing but loads counts: a
 // tile's K and V pass through LDS of the wave's own without a barrier, eight waves a CU keep
 // up to 128 KB on the way.  128 single tokens behind up to 2047 own and 8192 shared ones:
-// 92 us for 405 MB beside the shared items' products (72 for the DMA alone).
+// 90 us for 405 MB beside the shared items' products, 5 of them until the first tiles come
+// (72 for the DMA alone).
 template <typename T, int D>
 __device__ __forceinline__ void attend_keys(const AttnArgs& a, const AttnItem& it, const CacheAt<T, D>& cache, bool join, char* lds) {
   typedef AttnLds<T, D> L;
@@ -985,9 +986,11 @@ __device__ __forceinline__ int row_slot_seq(const int32_t* __restrict__ cu, int 
 
 // Batches of a few rows a sequence (own_tile 32: single tokens): lengths differ, and
 // the last long sequence would keep the memory waiting.  So the own tokens of all
-// sequences and K/V heads, in tiles of 32 keys, [sequence][K/V head][tile], are one
-// line, of which each wave takes an equal share: the end of one sequence's, all of some,
-// the beginning of another's.  Waves work alone, without barriers, so that the start of
+// sequences, in tiles of 32 keys, are one line, of which each wave takes an equal share for
+// one K/V head: the end of one sequence's, all of some, the beginning of another's.  The
+// waves of a workgroup take the heads of the same tokens, which lie beside each other in
+// memory (128 single tokens 104.5 us with every head's tiles after one another, 101.7 so).
+// Waves work alone, without barriers, so that the start of
 // one share (offsets, pages, first rows: one memory access after another) hides behind
 // the others' loads.  A sequence that is one wave's is done (or one part of it is, where
 // there is a prefix); of one that is shared out each wave leaves its part: the first of
@@ -1051,19 +1054,20 @@ __device__ __forceinline__ void lay_line(const AttnArgs& a, char* lds, bool keep
   }
   lds_barrier();
 }
-// The waves that share `tiles` (of all K/V heads, of a line of `total` for each): no more
-// than leave each as many tiles as balance its walk with the joining of the parts (a tile
-// of a lonely wave takes about 1.3 us, 16 parts of a row 0.6).
-__device__ __forceinline__ int line_waves(const AttnArgs& a, int tiles, int total) {
+// Shares of a line of `total` tiles, each taken by a wave for every K/V head: no more than
+// leave each as many tiles as balance its walk with the joining of the parts (a tile of a
+// lonely wave takes about 1.3 us, 16 parts of a row 0.6).
+__device__ __forceinline__ int line_shares(const AttnArgs& a, int total) {
   const int least = max(1, static_cast<int>(ceilf(sqrtf(static_cast<float>(total) / (32.0f * a.n_seqs)))));
-  return __builtin_amdgcn_readfirstlane(min(static_cast<int>(static_cast<uint32_t>(tiles + least - 1) / static_cast<uint32_t>(least)), a.stream_waves));
+  const uint32_t most = static_cast<uint32_t>(total + least - 1) / static_cast<uint32_t>(least);
+  return __builtin_amdgcn_readfirstlane(min(static_cast<int>(most), a.stream_waves / a.kv_heads));
 }
 // Equal shares, the first ones a tile longer where it does not come out even.
-__device__ __forceinline__ int share_start(uint32_t tiles, uint32_t waves, int w) {
-  return w * static_cast<int>(tiles / waves) + min(w, static_cast<int>(tiles % waves));
+__device__ __forceinline__ int share_start(uint32_t tiles, uint32_t shares, int s) {
+  return s * static_cast<int>(tiles / shares) + min(s, static_cast<int>(tiles % shares));
 }
-__device__ __forceinline__ int share_of(uint32_t tiles, uint32_t waves, uint32_t t) {   // the wave whose share holds tile t
-  const uint32_t each = tiles / waves, longer = tiles % waves, behind = longer * (each + 1);
+__device__ __forceinline__ int share_of(uint32_t tiles, uint32_t shares, uint32_t t) {   // the share that holds tile t
+  const uint32_t each = tiles / shares, longer = tiles % shares, behind = longer * (each + 1);
   return static_cast<int>(t < behind ? t / (each + 1) : longer + (t - behind) / each);
 }
 
@@ -1071,7 +1075,7 @@ __device__ __forceinline__ int share_of(uint32_t tiles, uint32_t waves, uint32_t
 struct AttnWork {
   int shared, shared_step;   // the next shared item
   int at, end;               // what is left of the share of the line
-  int wave;                  // of the line
+  int wave, kvh;             // of the line
   bool own_first;
 };
 enum class AttnKind { kNone, kRows, kKeys, kWave };
@@ -1114,7 +1118,7 @@ __device__ __forceinline__ bool own_item(const AttnArgs& a, int b, AttnItem& it)
 }
 __device__ __forceinline__ void line_item(const AttnArgs& a, const Line& line, AttnWork& w, AttnItem& it) {
   // the last sequence that begins at the tile or before it; 64 candidates at a time
-  const int t = static_cast<int>(static_cast<uint32_t>(w.at) / static_cast<uint32_t>(a.kv_heads)), lane = threadIdx.x % kWave;
+  const int t = w.at, lane = threadIdx.x % kWave;
   int lo = 0, hi = a.n_seqs;
   while (hi - lo > 1) {
     const int step = (hi - lo + kWave - 1) / kWave, at = lo + lane * step;
@@ -1125,9 +1129,8 @@ __device__ __forceinline__ void line_item(const AttnArgs& a, const Line& line, A
   const int n = __builtin_amdgcn_readfirstlane(lo);
   const int begin = __builtin_amdgcn_readfirstlane(line.tiles[n]),
             tiles = __builtin_amdgcn_readfirstlane(line.tiles[n + 1]) - begin;
-  const int rest = w.at - begin * a.kv_heads;
-  it.kvh = static_cast<int>(static_cast<uint32_t>(rest) / static_cast<uint32_t>(tiles));
-  const int off = rest - it.kvh * tiles, take = min(w.end - w.at, tiles - off);
+  const int off = t - begin, take = min(w.end - t, tiles - off);
+  it.kvh = w.kvh;
   const int start = __builtin_amdgcn_readfirstlane(line.cu[n]),
             count = __builtin_amdgcn_readfirstlane(line.cu[n + 1]) - start;
   it.row0 = it.first_row = start * a.groups;
@@ -1176,11 +1179,14 @@ void k_attn(AttnArgs a) {
       if (a.stream_first > 0) work.shared = a.shared_items;   // there are others for these
       lay_line<T, D>(a, lds, group == a.stream_first);
       const int total = __builtin_amdgcn_readfirstlane(line.tiles[a.n_seqs]);
-      const int tiles = total * a.kv_heads, waves = line_waves(a, tiles, total);
+      // the waves of a workgroup walk the same tokens' K/V heads, which lie beside each other
+      const int shares = line_shares(a, total);
       work.wave = kAttnWaves * (group - a.stream_first) + wave;
-      if (work.wave < waves) {
-        work.at = share_start(tiles, waves, work.wave);
-        work.end = share_start(tiles, waves, work.wave + 1);
+      const int share = static_cast<int>(static_cast<uint32_t>(work.wave) / static_cast<uint32_t>(a.kv_heads));
+      work.kvh = work.wave - share * a.kv_heads;
+      if (share < shares) {
+        work.at = share_start(total, shares, share);
+        work.end = share_start(total, shares, share + 1);
       }
     }
     // shared items compute, own ones wait for memory: half of the workgroups begin with
@@ -1237,13 +1243,11 @@ void k_attn_join(AttnArgs a) {
   int own = a.own_splits;
   if (a.stream) {
     const int before = a.line[lo], mine = a.line[lo + 1] - before, total = a.line[a.n_seqs];
-    const int tiles = total * a.kv_heads, waves = line_waves(a, tiles, total);
-    const int t0 = before * a.kv_heads + kvh * mine;
-    const int w0 = share_of(tiles, waves, t0);
-    own = share_of(tiles, waves, t0 + mine - 1) - w0 + 1;
-    own_step = 2;
+    const int shares = line_shares(a, total), w0 = share_of(total, shares, before);
+    own = share_of(total, shares, before + mine - 1) - w0 + 1;
+    own_step = 2 * a.kv_heads;
     own0 = own == 1 ? base + 2 * a.stream_waves + static_cast<int64_t>(lo) * a.kv_heads + kvh
-                    : base + 2 * w0;   // (its first part one behind)
+                    : base + 2 * (static_cast<int64_t>(w0) * a.kv_heads + kvh);   // (its first part one behind)
   } else {
     const int slot = first / a.own_tile + lo + rs / a.own_tile;
     own_step = static_cast<int64_t>(a.kv_heads) * (a.own_tile / kAttnRows);

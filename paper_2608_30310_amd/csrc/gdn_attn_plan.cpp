@@ -188,14 +188,14 @@ gdn_status make_attn_plan(const gdn_attn_shape* s, const int32_t* cu, AttnPlan* 
     *splits = static_cast<int32_t>(std::max<int64_t>(1, (keys + each - 1) / each));
   };
   const int64_t line = N * H * ((p.max_len + static_cast<int64_t>(kPlanLineTile) - 1) / kPlanLineTile);   // tiles at most
-  p.stream = p.own_tile == kPlanRows && N <= kPlanLineSeqs && line <= int64_t{1} << 30;
+  p.stream = p.own_tile == kPlanRows && N <= kPlanLineSeqs && H <= kPlanLineHeads && line <= int64_t{1} << 30;
   // (fp32's single tokens wait for memory with half as many waves: 161 us, 175 with all)
   const int64_t places = bf16 || (!p.stream && s->head_dim == 64) ? kAttnPlaces : kAttnPlaces / 2;
   constexpr int64_t waves = kPlanTile / kPlanRows;   // of a workgroup
   if (P > 0 && (p.stream || tiles * H < places || p.rows < tiles * p.own_tile * 3 / 5)) {
     p.shared_tiles = (p.rows + kPlanTile - 1) / kPlanTile;
     if (p.stream && p.rows <= kPlanRows) {
-      // a wave's items, as many tiles each as balance their walk with the joining (see line_waves)
+      // a wave's items, as many tiles each as balance their walk with the joining (see line_shares)
       p.shared_wt = 1;
       const int64_t keys = (P + kPlanLineTile - 1) / kPlanLineTile;
       const int64_t least = static_cast<int64_t>(std::ceil(std::sqrt(static_cast<double>(keys) / 32)));

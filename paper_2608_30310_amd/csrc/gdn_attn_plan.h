@@ -29,8 +29,9 @@ gdn_status check_attn(const gdn_attn_shape* s, std::string* err);
 // Rows (one query head of one token, the heads of a K/V head next to each other)
 // of a wave, and of a workgroup whose waves take rows of their own.
 constexpr int32_t kPlanRows = 32, kPlanTile = 128;
-// Keys of a tile of the line that waves share, and sequences that it may have.
-constexpr int32_t kPlanLineTile = 32, kPlanLineSeqs = 1024;
+// Keys of a tile of the line that waves share, sequences that it may have, and K/V heads (a
+// wave for each at least).
+constexpr int32_t kPlanLineTile = 32, kPlanLineSeqs = 1024, kPlanLineHeads = 1024;
 
 // How gdn_prefix_attention runs.  Shared items: tiles of all packed rows against
 // `shared_splits` pieces of the prefix.  Own items: tiles of a sequence's rows

@@ -309,7 +309,7 @@ def test_plan_covers_every_key_of_every_row(lib, seed):
     parts = p["shared_items"] * p["shared_wt"]
     if p["stream"]:
         # at most 32 rows a sequence: one wave's; every workgroup of the line is in the grid
-        assert max(lens) * G <= 32 and n <= 1024 and p["joined"] and p["stream_waves"] >= 1
+        assert max(lens) * G <= 32 and n <= 1024 and p["joined"] and p["stream_waves"] >= Hk
         assert p["grid"] >= p["stream_first"] + -(-p["stream_waves"] // 4)
         if p["stream_first"]:
             assert p["stream_first"] * (4 if p["shared_wt"] == 1 else 1) >= p["shared_items"]
