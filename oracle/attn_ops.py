@@ -73,7 +73,7 @@ def attention(q, k_cache, v_cache, table, lens, cu, prefix_pages=None, prefix_le
         own = torch.arange(len(at), device=dev) - prefix_len
         for i in range(L):
             t = cu[s] + i
-            see = there & (own <= m - L + i)
+            see = there & (own <= max(m - L + i, -1))   # (the prefix is below 0: seen by all)
             r = at[see]
             count[t] = len(r)
             if len(r) == 0:

@@ -47,6 +47,14 @@ def test_attention_of_pages_that_are_none_and_of_nothing():
     assert (out[0] == 5.0).all() and (out[1:] == 0).all() and count.tolist() == [2, 0, 0]
 
 
+def test_queries_before_the_own_tokens_see_the_prefix_alone():
+    kc = torch.ones(4, 2, 1, 4, dtype=F64)
+    vc = torch.arange(4, dtype=F64)[:, None, None, None].expand(4, 2, 1, 4)
+    out, _, _, _, count = ref.attention(torch.ones(3, 1, 4), kc, vc, torch.tensor([[3]], dtype=torch.int32), torch.tensor([1]),
+                                        [0, 3], torch.tensor([1, 2], dtype=torch.int32), 4)
+    assert count.tolist() == [4, 4, 5] and (out[:2] == 1.5).all() and torch.allclose(out[2], torch.tensor(9 / 5, dtype=F64))
+
+
 @pytest.mark.parametrize("interleaved", [False, True])
 def test_rotation_is_complex_multiplication(interleaved):
     torch.manual_seed(1)

@@ -2,6 +2,8 @@
 sequences, batches of both kinds, outputs that are an input in part, caches whose rows lie
 far apart, values near the largest (bounds as in the tests of each operator).
 """
+import random
+
 import pytest
 import torch
 
@@ -131,3 +133,28 @@ def test_rows_of_a_page_far_apart(new):
     far(0).copy_(c["k_cache"])
     far(1).copy_(c["v_cache"])
     assert torch.equal(attn.call(dict(c, k_cache=far(0), v_cache=far(1))), attn.call(c))
+
+
+@pytest.mark.parametrize("seed", range(40))
+def test_whatever_the_workspace_held(seed):
+    """Batches drawn over the ranges, on a workspace full of NaN; some entries of the tables are no pages."""
+    rng = random.Random(seed)
+    Hk = rng.choice([1, 2, 3, 4, 8])
+    H, D = Hk * rng.choice([1, 2, 5, 8]), rng.choice([64, 128])
+    n = rng.choice([1, 2, 5, 30])
+    new = [rng.choice([0, 1, 1, 2, rng.randrange(1, 150)]) for _ in range(n)] if rng.random() < 0.6 else [1] * n
+    before = [rng.choice([0, 1, 31, 64, rng.randrange(600)]) for _ in range(n)]
+    dtype, ps = rng.choice(["bf16", "f32"]), rng.choice([1, 5, 16, 24, 64, 128])
+    c = attn.case(new, before, rng.choice([0, 0, 1, 100, 640]), H=H, Hk=Hk, D=D, ps=ps, dtype=dtype, seed=seed,
+                  layout=rng.choice(["pages", "heads", "both", "rows"]), pad=rng.choice([0, 8]), spare=rng.choice([0, 3]))
+    if rng.random() < 0.4:
+        for _ in range(3):
+            c["table"][rng.randrange(n), rng.randrange(c["table"].shape[1])] = rng.choice([-1, 2 ** 31 - 1])
+    kw = dict(scale=rng.choice([None, 0.05, -0.3]))
+    if rng.random() < 0.3:
+        kw["max_len"] = rng.randrange(1, c["table"].shape[1] * ps + 1)
+        c["lens"].clamp_(max=kw["max_len"])   # (a bound that holds)
+    ws = torch.full((64 << 20,), 0xFF, dtype=torch.uint8, device=DEV)
+    out = torch.full_like(c["q"], 7.0).contiguous()
+    attn.check(c, attn.call(c, workspace=ws, out=out, **kw), **kw)
+    assert (out[sum(new):] == 7).all()
