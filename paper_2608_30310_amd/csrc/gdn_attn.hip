@@ -27,8 +27,9 @@ gdn_status launch_attn(const AttnArgs& a, const AttnPlan& p, hipStream_t stream)
                 "the plan's tiles");
   hipLaunchKernelGGL((k_attn<T, D>), dim3(static_cast<uint32_t>(p.grid)), dim3(kAttnThreads), 0, stream, a);
   if (p.joined) {
-    const int64_t tiles = (p.rows + kAttnRows - 1) / kAttnRows * a.kv_heads * (D / 8);
-    hipLaunchKernelGGL((k_attn_join<T, D>), dim3(static_cast<uint32_t>(tiles)), dim3(kAttnThreads), 0, stream, a);
+    const uint32_t tiles = static_cast<uint32_t>((p.rows + kAttnRows - 1) / kAttnRows * a.kv_heads);
+    if (p.spread) hipLaunchKernelGGL((k_attn_join<T, D, true>), dim3(tiles * (D / 8)), dim3(kAttnThreads), 0, stream, a);
+    else hipLaunchKernelGGL((k_attn_join<T, D, false>), dim3(tiles), dim3(kAttnThreads), 0, stream, a);
   }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return afail(GDN_ERR_HIP, std::string("attention launch: ") + hipGetErrorString(e));

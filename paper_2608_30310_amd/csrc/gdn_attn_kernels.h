@@ -1207,17 +1207,18 @@ void k_attn(AttnArgs a) {
 }
 
 // The items' partial results of a row into one.  A workgroup takes 32 packed rows of a
-// K/V head and one of the D / 8 groups of columns: lane (h, r) four columns of row r, a
-// wave every fourth part, kAttnAhead parts' loads in flight at a time.  11 us for 128 single
-// tokens of 32 heads with 12 parts each (32 MB), 5 for one: a chain of loads.
+// K/V head, lane (h, r) four columns of row r at a time.  SPREAD, for many parts: one of the
+// D / 8 groups of columns a workgroup, a wave every fourth part (11 us for 128 single tokens of
+// 32 heads with 12 parts each, 32 MB; 5 for one: a chain of loads).  Else a wave takes a quarter
+// of the columns and all parts (two parts of 512 tokens, 17 MB: 5.9 us, 15 the other way).
+// kAttnAhead parts' loads are in flight at a time.
 constexpr int kAttnAhead = 4;
-template <typename T, int D>
+template <typename T, int D, bool SPREAD>
 __global__ __launch_bounds__(kAttnThreads)
 void k_attn_join(AttnArgs a) {
-  __shared__ f32x4 sums[kAttnWaves][kWave];
-  __shared__ f32x2 mls[kAttnWaves][kWave];
+  constexpr int COLS = SPREAD ? 1 : D / 8 / kAttnWaves, AHEAD = SPREAD ? kAttnAhead : kAttnAhead / 2;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
-  const int unit = blockIdx.x / (D / 8), col = blockIdx.x % (D / 8);
+  const int unit = SPREAD ? blockIdx.x / (D / 8) : blockIdx.x, col = SPREAD ? blockIdx.x % (D / 8) : COLS * wave;
   const int kvh = unit % a.kv_heads, wt = unit / a.kv_heads;
   const bool there = wt * kAttnRows + lane % 32 < a.rows;
   const int row = there ? wt * kAttnRows + lane % 32 : a.rows - 1;
@@ -1264,70 +1265,87 @@ void k_attn_join(AttnArgs a) {
   if (most == 0) return;
   const int own_row = a.stream ? rs : rs % kAttnRows;
   float m = -INFINITY, l = 0.0f;
-  f32x4 sum = zero4();
-  for (int s0 = wave; s0 < most; s0 += kAttnWaves * kAttnAhead) {
-    f32x2 ml[kAttnAhead];
-    f32x4 x[kAttnAhead];
+  f32x4 sum[COLS];
 #pragma unroll
-    for (int k = 0; k < kAttnAhead; ++k) {
-      const int s = max(min(s0 + kAttnWaves * k, parts - 1), 0), so = s - a.shared_splits;
+  for (int c = 0; c < COLS; ++c) sum[c] = zero4();
+  constexpr int STEP = SPREAD ? kAttnWaves : 1;
+  for (int s0 = SPREAD ? wave : 0; s0 < most; s0 += STEP * AHEAD) {
+    f32x2 ml[AHEAD];
+    f32x4 x[AHEAD][COLS];
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+      const int s = max(min(s0 + STEP * k, parts - 1), 0), so = s - a.shared_splits;
       const int64_t t = so < 0 ? shared0 + s * shared_step : own0 + so * own_step + (split && so == 0);
       const int r = so < 0 ? lane % 32 : own_row;
       ml[k] = f32x2{-INFINITY, 0.0f};
-      x[k] = zero4();
-      if (s0 + kAttnWaves * k < parts) {
+#pragma unroll
+      for (int c = 0; c < COLS; ++c) x[k][c] = zero4();
+      if (s0 + STEP * k < parts) {
         ml[k] = a.part_ml[t * kAttnRows + r];
-        x[k] = a.part[(t * (D / 8) + col) * kWave + lane / 32 * 32 + r];
+#pragma unroll
+        for (int c = 0; c < COLS; ++c) x[k][c] = a.part[(t * (D / 8) + col + c) * kWave + lane / 32 * 32 + r];
       }
     }
     float top = m;
 #pragma unroll
-    for (int k = 0; k < kAttnAhead; ++k) top = fmaxf(top, ml[k][0]);
+    for (int k = 0; k < AHEAD; ++k) top = fmaxf(top, ml[k][0]);
     const float at = top == -INFINITY ? 0.0f : top, keep = __builtin_amdgcn_exp2f(m - at);
     m = top;
     l *= keep;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) sum[i] *= keep;
+    for (int c = 0; c < COLS; ++c)
 #pragma unroll
-    for (int k = 0; k < kAttnAhead; ++k) {
+      for (int i = 0; i < 4; ++i) sum[c][i] *= keep;
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
       if (ml[k][1] == 0.0f) continue;   // nothing seen there (nor anything written)
       const float f = __builtin_amdgcn_exp2f(ml[k][0] - at);
       l = fmaf(f, ml[k][1], l);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) sum[i] = fmaf(f, x[k][i], sum[i]);
+      for (int c = 0; c < COLS; ++c)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[c][i] = fmaf(f, x[k][c][i], sum[c][i]);
     }
   }
-  sums[wave][lane] = sum;
-  mls[wave][lane] = f32x2{m, l};
-  lds_barrier();
-  if (wave != 0 || parts == 0) return;
+  if constexpr (SPREAD) {
+    __shared__ f32x4 sums[kAttnWaves][kWave];
+    __shared__ f32x2 mls[kAttnWaves][kWave];
+    sums[wave][lane] = sum[0];
+    mls[wave][lane] = f32x2{m, l};
+    lds_barrier();
+    if (wave != 0) return;
 #pragma unroll
-  for (int w = 1; w < kAttnWaves; ++w) m = fmaxf(m, mls[w][lane][0]);
-  const float at = m == -INFINITY ? 0.0f : m;
-  l = 0.0f;
-  sum = zero4();
+    for (int w = 1; w < kAttnWaves; ++w) m = fmaxf(m, mls[w][lane][0]);
+    const float at = m == -INFINITY ? 0.0f : m;
+    l = 0.0f;
+    sum[0] = zero4();
 #pragma unroll
-  for (int w = 0; w < kAttnWaves; ++w) {
-    const f32x2 ml = mls[w][lane];
-    if (ml[1] == 0.0f) continue;
-    const float f = __builtin_amdgcn_exp2f(ml[0] - at);
-    l = fmaf(f, ml[1], l);
+    for (int w = 0; w < kAttnWaves; ++w) {
+      const f32x2 ml = mls[w][lane];
+      if (ml[1] == 0.0f) continue;
+      const float f = __builtin_amdgcn_exp2f(ml[0] - at);
+      l = fmaf(f, ml[1], l);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) sum[i] = fmaf(f, sums[w][lane][i], sum[i]);
+      for (int i = 0; i < 4; ++i) sum[0][i] = fmaf(f, sums[w][lane][i], sum[0][i]);
+    }
   }
+  if (parts == 0) return;
   const int head = kvh * a.groups + (row - token * a.groups);
   T* out = static_cast<T*>(a.out) + token * a.ldo + static_cast<int64_t>(head) * D + 8 * col + 4 * (lane / 32);
   const float inv = 1.0f / l;
-  float y[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) y[i] = l == 0.0f ? 0.0f : sum[i] * inv;
-  if constexpr (sizeof(T) == 2) {
-    u32x2 w;
-    w[0] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{y[0], y[1]}), bf16x2));
-    w[1] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{y[2], y[3]}), bf16x2));
-    *reinterpret_cast<u32x2*>(out) = w;
-  } else {
-    *reinterpret_cast<f32x4*>(out) = f32x4{y[0], y[1], y[2], y[3]};
+  for (int c = 0; c < COLS; ++c) {
+    float y[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = l == 0.0f ? 0.0f : sum[c][i] * inv;
+    if constexpr (sizeof(T) == 2) {
+      u32x2 w;
+      w[0] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{y[0], y[1]}), bf16x2));
+      w[1] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{y[2], y[3]}), bf16x2));
+      *reinterpret_cast<u32x2*>(out + 8 * c) = w;
+    } else {
+      *reinterpret_cast<f32x4*>(out + 8 * c) = f32x4{y[0], y[1], y[2], y[3]};
+    }
   }
 }
 

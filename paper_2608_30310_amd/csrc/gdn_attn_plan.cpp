@@ -15,8 +15,7 @@ constexpr int64_t kMaxStride = int64_t{1} << 23;
 
 // Workgroups of the attention that the chip holds at once: two a CU, but one where a
 // workgroup's tiles (fp32, heads of 128) fill its LDS.  The fewest keys of a piece of a
-// split range: as much work as the joining of its result takes, in fp32 (a quarter of
-// the rate) from half as many keys.
+// split range, in fp32 (a quarter of the rate) half as many.
 constexpr int64_t kAttnPlaces = 512, kLeastChunk = 256;
 
 gdn_status bad(std::string* err, const std::string& what, gdn_status st = GDN_ERR_BAD_SHAPE) {
@@ -180,12 +179,26 @@ gdn_status make_attn_plan(const gdn_attn_shape* s, const int32_t* cu, AttnPlan* 
   p.own_slots = tile_slots(p.rows, N, p.own_tile);
   const bool bf16 = s->dtype == GDN_BF16;
   const int64_t least_chunk = bf16 ? kLeastChunk : kLeastChunk / 2;
-  const auto pieces = [least_chunk](int64_t keys, int64_t items, int64_t places, int32_t* splits, int32_t* chunk) {
-    const int64_t most = std::max<int64_t>(1, (keys + least_chunk - 1) / least_chunk);
-    int64_t n = std::min(most, std::max<int64_t>(1, places / std::max<int64_t>(1, items)));
-    const int64_t each = std::max<int64_t>(64, ((keys + n - 1) / n + 63) / 64 * 64);
-    *chunk = static_cast<int32_t>(each);
-    *splits = static_cast<int32_t>(std::max<int64_t>(1, (keys + each - 1) / each));
+  // A range of keys in as many pieces as are expected to end soonest, in us: a workgroup's
+  // tiles of 64 keys one after the other, with one workgroup a CU or two; the joining's
+  // launch, and each piece's partial results written and read.  Measured, 32 / 4 bf16 heads
+  // of 128: prompts of 512 and 1024 tokens 23 and 39 us in two pieces, 20 and 31 in one; three
+  // suffixes of up to 300 tokens behind 2000 shared ones 56 with two pieces of the prefix, 60
+  // with one; fp32, 8 heads of 64, 20 suffixes of up to 200 tokens behind 1001: 99 and 115.
+  const double scale = s->head_dim / 128.0, alone = scale * (bf16 ? 1.5 : 11.6), beside = scale * (bf16 ? 2.2 : 19.2);
+  const double part = static_cast<double>(p.rows) * H * s->head_dim * 8 / 4.5e6;
+  const auto pieces = [=](int64_t keys, int64_t items, int64_t most, bool joined, int32_t* splits, int32_t* chunk) {
+    most = std::max<int64_t>(1, std::min((keys + least_chunk - 1) / least_chunk, most));
+    double best = 0.0;
+    for (int64_t n = 1; n <= most; ++n) {
+      const int64_t each = std::max<int64_t>(64, ((keys + n - 1) / n + 63) / 64 * 64), got = std::max<int64_t>(1, (keys + each - 1) / each);
+      const double cost = (items * got > kAttnPlaces / 2 ? beside : alone) * static_cast<double>(each / 64) +
+                          (got > 1 && !joined ? 5.0 : 0.0) + part * static_cast<double>(got);
+      if (n > 1 && cost >= best) continue;
+      best = cost;
+      *chunk = static_cast<int32_t>(each);
+      *splits = static_cast<int32_t>(got);
+    }
   };
   const int64_t line = N * H * ((p.max_len + static_cast<int64_t>(kPlanLineTile) - 1) / kPlanLineTile);   // tiles at most
   p.stream = p.own_tile == kPlanRows && N <= kPlanLineSeqs && H <= kPlanLineHeads && line <= int64_t{1} << 30;
@@ -204,9 +217,16 @@ gdn_status make_attn_plan(const gdn_attn_shape* s, const int32_t* cu, AttnPlan* 
       p.shared_chunk = static_cast<int32_t>(each * kPlanLineTile);
       p.shared_splits = static_cast<int32_t>((keys + each - 1) / each);
     } else {
-      // one workgroup a CU: the other place is for own items, which wait for memory while
-      // these compute
-      pieces(P, p.shared_tiles * H, places / 2, &p.shared_splits, &p.shared_chunk);
+      if (p.stream) {
+        // one workgroup a CU: the other place is for own items, which wait for memory while
+        // these compute
+        const int64_t n = std::max<int64_t>(1, std::min((P + least_chunk - 1) / least_chunk, places / 2 / (p.shared_tiles * H)));
+        p.shared_chunk = static_cast<int32_t>(std::max<int64_t>(64, ((P + n - 1) / n + 63) / 64 * 64));
+        p.shared_splits = static_cast<int32_t>((P + p.shared_chunk - 1) / p.shared_chunk);
+      } else {
+        // with room for the own items beside them, unless that leaves the prefix whole
+        pieces(P, p.shared_tiles * H, std::max<int64_t>(2, places / 2 / (p.shared_tiles * H)), true, &p.shared_splits, &p.shared_chunk);
+      }
     }
     p.shared_items = p.shared_tiles * H * p.shared_splits;
   }
@@ -222,7 +242,7 @@ gdn_status make_attn_plan(const gdn_attn_shape* s, const int32_t* cu, AttnPlan* 
     p.joined = true;
     own_tiles = 2 * static_cast<size_t>(p.stream_waves) + static_cast<size_t>(N * H);
   } else {
-    if (P == 0 || p.shared_items > 0) pieces(p.max_len, tiles * H, places, &p.own_splits, &p.own_chunk);
+    if (P == 0 || p.shared_items > 0) pieces(p.max_len, tiles * H, places / std::max<int64_t>(1, tiles * H), p.shared_items > 0, &p.own_splits, &p.own_chunk);
     else p.own_chunk = (p.max_len + 63) / 64 * 64;
     p.own_items = p.own_slots * H * p.own_splits;
     p.joined = p.shared_items > 0 || p.own_splits > 1;
@@ -231,6 +251,7 @@ gdn_status make_attn_plan(const gdn_attn_shape* s, const int32_t* cu, AttnPlan* 
   }
   if (p.grid > kMaxInt / 256 || p.rows / kPlanRows * H * (s->head_dim / 8) > kMaxInt / 256)
     return bad(err, "too many tokens for one call", GDN_ERR_UNSUPPORTED);
+  p.spread = p.stream || p.shared_splits + p.own_splits > kPlanFewParts;
   if (p.joined) {
     const size_t parts = static_cast<size_t>(p.shared_items) * p.shared_wt + own_tiles;
     p.off_ml = parts * kPlanRows * s->head_dim * sizeof(float);

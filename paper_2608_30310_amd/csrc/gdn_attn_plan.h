@@ -33,6 +33,9 @@ constexpr int32_t kPlanRows = 32, kPlanTile = 128;
 // wave for each at least).
 constexpr int32_t kPlanLineTile = 32, kPlanLineSeqs = 1024, kPlanLineHeads = 1024;
 
+// Up to so many partial results of a row a wave joins them by itself.
+constexpr int32_t kPlanFewParts = 8;
+
 // How gdn_prefix_attention runs.  Shared items: tiles of all packed rows against
 // `shared_splits` pieces of the prefix.  Own items: tiles of a sequence's rows
 // against `own_splits` pieces of its own tokens, and against the whole prefix
@@ -53,6 +56,7 @@ struct AttnPlan {
   int32_t stream_first = 0, stream_waves = 0;
   int64_t grid = 0;
   bool joined = false;       // items leave partial results, which a second kernel joins
+  bool spread = false;       // many of them: its waves share out the parts
   size_t off_ml = 0, off_line = 0;   // workspace: partial outputs, their maxima and sums, the line
   size_t bytes = 0;
 };
