@@ -725,9 +725,9 @@ __device__ __forceinline__ void put_columns(const AttnArgs& a, const AttnItem& i
 // Waves take rows of their own and share tiles of keys, 64 for bf16 (two buffers each of K
 // and V are 64 KB, so two workgroups fit a CU: with one 3.59 ms instead of 2.58).  Bound by
 // the matrix cores and the vector instructions beside them, whose shares add up to most
-// of the cycles (49 % and 155 instructions a tile), at the clock that the power limit
-// leaves: 16 suffixes behind 8192 tokens 985 TFLOP/s, a prompt of 8192 tokens 956, long fp32
-// batches 115.
+// of the cycles (50 % and 155 instructions a tile), at the clock that the power limit
+// leaves: 16 suffixes behind 8192 tokens 985 to 1068 TFLOP/s from card to card, a prompt of
+// 8192 tokens 956 to 1033, long fp32 batches 115.
 template <typename T, int D>
 __device__ __forceinline__ void attend_rows(const AttnArgs& a, const AttnItem& it, const CacheAt<T, D>& cache, char* lds) {
   typedef AttnLds<T, D> L;
