@@ -14,8 +14,8 @@
 // which registers does not matter to that product as long as V's operand has them
 // in the same order.  One pass, with the running maximum m and sum l of each row:
 //   p = 2^(s - m),  l += sum p,  O += p V,  out = O / l,
-// where m moves (and O and l are scaled) only when weights pass 2^8 or so, which neither
-// bf16's range nor fp32 sums mind.
+// where m moves (and O and l are scaled) only when weights or a tile's sum of them pass 2^8,
+// which neither bf16's range nor fp32 sums mind.
 #pragma once
 
 #include <type_traits>
@@ -449,6 +449,7 @@ __device__ __forceinline__ bool clean_values(char* vl, uint64_t there, bool drop
 }
 
 // ---------------------------------------------------------------- a wave's rows
+constexpr float kSlack = 8.0f;   // weights up to 2^8 are let pass
 template <typename T, int D>
 struct AttnWave {
   typedef KvRows<T, D> Rows;
@@ -479,9 +480,10 @@ struct AttnWave {
       }
     }
   }
-  // The rows' maxima over NB blocks of scores; O and l follow where one moves.
+  // The rows' maxima over NB blocks of scores; O and l follow where one moves, by more than
+  // `slack` (the same in both halves of a row).
   template <int NB>
-  __device__ __forceinline__ void raise(const f32x16 (&s)[NB], float scale2) {
+  __device__ __forceinline__ void raise(const f32x16 (&s)[NB], float scale2, float slack) {
     float t[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) t[k] = s[0][k];
@@ -491,7 +493,7 @@ struct AttnWave {
       for (int i = 0; i < 16; ++i) t[i % 4] = fmaxf(t[i % 4], s[b][i]);
     const float top = half_max(fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]))) * scale2;
     // each row by itself: what one row meets does not change another's rounding
-    const bool moves = top > m + 8.0f || m == -INFINITY;
+    const bool moves = top > m + slack || m == -INFINITY;
     if (rarely(__any(moves))) {
       const float next = moves ? fmaxf(m, top) : m;
       const float keep = moves ? __builtin_amdgcn_exp2f(m - (next == -INFINITY ? 0.0f : next)) : 1.0f;
@@ -799,18 +801,19 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, const AttnItem& i
     }
     if (!idle) {
       // The maximum is looked at only where a row has none yet, or where weights turn out to
-      // be large (the sum over a tile's half above 2^8): the scores are there until then.
+      // be large (a row's sum over a tile's half above 2^8, whose maximum becomes the largest
+      // score then): the scores are there until then.
       // 35 vector instructions a tile less, and the moves that kept the scores (16 suffixes
       // behind 8192 tokens 2.64 -> 2.55 ms).
       // Without a tile d0 weights are made of whatever was there, without a tile d1 scores,
       // and not looked at.
-      if (rarely(d0.any && __any(w.m == -INFINITY))) w.raise(s, scale2);
+      if (rarely(d0.any && __any(w.m == -INFINITY))) w.raise(s, scale2, kSlack);
       const bool scored = sizeof(T) == 2 || d1.any;   // (fp32's scores cost too much to be formed of nothing)
       float sum = 0.0f;
       if (scored) sum = w.template scores<NB, true>(kl, next, s, p, scale2, lane);
       if (d0.any) {
         if (rarely(!scored || __any(sum > 256.0f))) {
-          w.raise(s, scale2);
+          w.raise(s, scale2, !scored ? kSlack : half_max(sum) > 256.0f ? 0.0f : INFINITY);
           sum = w.weigh(s, p, scale2);
         }
         w.l += sum;
@@ -901,7 +904,7 @@ __device__ __forceinline__ void attend_keys(const AttnArgs& a, const AttnItem& i
       const int limit = was.own ? mine - was.base : KT;
       const bool whole = was_there == kAll && (!was.own || least >= was.base + KT);
       if (rarely(!whole)) w.mask(s, limit, was_there, lane);
-      w.raise(s, scale2);
+      w.raise(s, scale2, kSlack);
       w.l += w.weigh(s, p, scale2);
       if (asked) wait_dma_but<N + 1>();
       else if (any) wait_dma_but<N>();

@@ -112,8 +112,23 @@ def test_scores_that_rise_all_the_way(dtype):
 
 
 @DT
+@pytest.mark.parametrize("low", [3.0, 5.4, 7.0, 40.0])
+def test_a_first_tile_far_below_the_rest(dtype, low):
+    """All other scores lie `low` above the first tile's (5.5: 2^8 of its weights), in some rows alone."""
+    c = attn.case([100, 1, 1], [700, 900, 3], 200, dtype=dtype, seed=8)
+    c["q"].mul_(0.02)
+    c["q"][..., 0] = torch.where(torch.arange(102, device=DEV) % 3 > 0, 8.0, 0.0)[:, None].to(c["q"].dtype)   # scale 2^-3
+    rows = torch.arange(64, device=DEV)
+    flat = c["k_cache"].reshape(-1, 2, 64)
+    flat[..., 0] = low
+    flat[c["prefix_pages"].long()[rows // 16] * 16 + rows % 16, :, 0] = 0.0
+    c["k_cache"].copy_(flat.view_as(c["k_cache"]))
+    attn.check(c, attn.call(c))
+
+
+@DT
 def test_values_near_the_largest(dtype):
-    """Sums of weights stay below 2^8 a tile's half, so values of 2^100 do not leave the range."""
+    """Weights stay below 2^8, so values of 2^100 do not leave the range."""
     for new, before in (([100], 900), ([1, 1], 900)):
         c = attn.case(new, before, 300, dtype=dtype, seed=6, size=3.0)
         c["v_cache"].mul_(2.0 ** 100)
