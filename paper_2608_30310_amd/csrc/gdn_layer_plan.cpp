@@ -125,7 +125,8 @@ gdn_status check_ssm(const gdn_ssm_shape* s, std::string* err, bool outputs) {
   return GDN_OK;
 }
 
-gdn_status make_ssm_plan(const gdn_ssm_shape* s, const int32_t* cu, SsmPlan* plan, std::string* err, bool outputs) {
+gdn_status make_ssm_plan(const gdn_ssm_shape* s, const int32_t* cu, SsmPlan* plan, std::string* err, bool outputs,
+                         int64_t least_segment) {
   gdn_status st = check_ssm(s, err, outputs);
   SsmPlan p;
   if (st == GDN_OK) st = check_seqlens(s->num_seqs, cu, &p.tokens, &p.longest, err);
@@ -177,7 +178,7 @@ gdn_status make_ssm_plan(const gdn_ssm_shape* s, const int32_t* cu, SsmPlan* pla
   int64_t seg = 0;
   const bool joinable = N * H * s->d_state * s->head_dim / 4 <= kMaxGrid;   // a thread of the join takes four elements
   for (int64_t more = 0; joinable && more <= 4 && least + more * ((least + 3) / 4) < longest; ++more) {
-    const int64_t try_seg = least + more * ((least + 3) / 4);
+    const int64_t try_seg = std::max(least_segment, least + more * ((least + 3) / 4));
     int64_t segs = 0;
     for (int64_t n = 0; n < N; ++n) segs += std::max<int64_t>(1, (chunks_of(cu, n) + try_seg - 1) / try_seg);
     const int64_t rounds = (segs * groups + kSsmPlaces - 1) / kSsmPlaces;

@@ -45,7 +45,8 @@ struct SsmPlan {
   size_t off_decay = 0;          // workspace: states [slots, H, d_state, head_dim], then decays [slots, H]
   size_t bytes = 0;
 };
-gdn_status make_ssm_plan(const gdn_ssm_shape* s, const int32_t* cu, SsmPlan* p, std::string* err, bool outputs = true);
+gdn_status make_ssm_plan(const gdn_ssm_shape* s, const int32_t* cu, SsmPlan* p, std::string* err, bool outputs = true,
+                         int64_t least_segment = 1);   // chunks of a segment at least
 
 gdn_status check_lora(const gdn_lora_shape* s, std::string* err);
 

@@ -368,3 +368,16 @@ def test_caches_apart_never_share_a_byte(lib, seed):
             assert not rows & {r + off for r in rows}, off
         else:
             assert off < 2 * at
+
+
+def test_states_alone_need_no_more_workspace():
+    """They are walked in other segments than with outputs, for which the size is given."""
+    for lens in ((500,), (819,), (2048,), (1200, 64), (8192,), (819,) * 4, (64,) * 3):
+        for H in (4, 32):
+            need = ctypes.c_size_t(0)
+            s = linear_shape(len(lens), num_v_heads=H, num_k_heads=H // 2, ld_q=64 * H // 2, ld_k=64 * H // 2, ld_v=128 * H, ld_o=128 * H)
+            assert gdn.load_library().gdn_linear_attention_workspace_size(ctypes.byref(s), host_of(lens, "lens"), ctypes.byref(need)) == 0
+            call = lambda wsb: gdn.load_library().gdn_linear_attention(
+                ctypes.byref(s), host_of(lens, "lens"), P(0x1000), None, P(0x200000), P(0x300000), None, None, None, P(0x500000),
+                P(0x1000000) if wsb else None, wsb, None)
+            assert call(need.value) == NULL   # for g, which is looked at behind the workspace
