@@ -38,6 +38,8 @@ def build(verbose: bool = False) -> str:
              # MFMA results in ordinary VGPRs: the scan feeds them to VALU work
              # every step, and accumulator-register copies would serialise it
              "-mllvm", "-amdgpu-mfma-vgpr-form",
+             # (a clobber of M0, which the loads into LDS set, is reported for each of them)
+             "-Wno-inline-asm",
              "-Wall", "-I", INCLUDE, "-I", CSRC]
     noise = "is not a recognized feature for this target"
 

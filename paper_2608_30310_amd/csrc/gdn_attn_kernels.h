@@ -260,14 +260,21 @@ __device__ __forceinline__ void next_tile(const KeyRange& k, KeyTile& t) {
 __device__ __forceinline__ uint32_t lds_address(lds_byte* p) {
   return __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(reinterpret_cast<uintptr_t>(p)));
 }
+// Two waits that the compiler does not add inside a string: one instruction between the
+// write of M0 and the load that takes its place in LDS from it; and five between a vector
+// instruction's write of a scalar register (a lane read) and a load that takes its address
+// from it, but none where a scalar move lies between.  (16 suffixes and the single tokens
+// take as long with them as without.)
 __device__ __forceinline__ void async_piece(const void* src, lds_byte* dst) {   // 16 bytes a lane
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_address(dst)), "v"(src) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_address(dst)), "v"(src) : "memory", "m0");
 }
 __device__ __forceinline__ void async_piece(uint64_t base, uint32_t off, lds_byte* dst) {   // from a uniform base
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds_address(dst)), "v"(off), "s"(base) : "memory");
+  uint64_t at;
+  asm volatile("s_mov_b32 m0, %1\n\ts_mov_b64 %0, %3\n\tglobal_load_lds_dwordx4 %2, %0"
+               : "=&s"(at) : "s"(lds_address(dst)), "v"(off), "s"(base) : "memory", "m0");
 }
 __device__ __forceinline__ void async_word(const void* src, lds_byte* dst) {   // 4 bytes a lane
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, off" ::"s"(lds_address(dst)), "v"(src) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds_address(dst)), "v"(src) : "memory", "m0");
 }
 
 // What the loop over tiles needs of the arguments: each value a register of its own
