@@ -205,7 +205,8 @@ gdn_status make_attn_plan(const gdn_attn_shape* s, const int32_t* cu, AttnPlan* 
   // (fp32's single tokens wait for memory with half as many waves: 161 us, 175 with all)
   const int64_t places = bf16 || (!p.stream && s->head_dim == 64) ? kAttnPlaces : kAttnPlaces / 2;
   constexpr int64_t waves = kPlanTile / kPlanRows;   // of a workgroup
-  if (P > 0 && (p.stream || tiles * H < places || p.rows < tiles * p.own_tile * 3 / 5)) {
+  // (without rows there are no tiles to share places out to)
+  if (P > 0 && p.rows > 0 && (p.stream || tiles * H < places || p.rows < tiles * p.own_tile * 3 / 5)) {
     p.shared_tiles = (p.rows + kPlanTile - 1) / kPlanTile;
     if (p.stream && p.rows <= kPlanRows) {
       // a wave's items, as many tiles each as balance their walk with the joining (see line_shares)

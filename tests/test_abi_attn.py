@@ -334,6 +334,23 @@ def test_plan_covers_every_key_of_every_row(lib, seed):
     assert need.value == p["bytes"]
 
 
+@pytest.mark.parametrize("dtype", [GDN_BF16, GDN_F32])
+@pytest.mark.parametrize("n,heads,kw", [(1025, 4, {}), (4, 1025, {}), (64, 4, dict(table_width=1 << 24)), (1, 1, {}), (1024, 4, {}), (0, 4, {})],
+                         ids=lambda x: str(x))
+@pytest.mark.parametrize("prefix", [0, 1, 100, 200000])
+def test_batches_without_queries_are_planned(lib, prefix, n, heads, kw, dtype):
+    """Sequences without new tokens behind a prefix, also too many (or too many heads, or too wide a table) for a line:
+    nothing to run, and no error."""
+    strides = dict(k_page=16 * heads * 64, k_token=heads * 64, k_head=64, v_page=16 * heads * 64, v_token=heads * 64, v_head=64)
+    kw = dict(num_heads=heads, num_kv_heads=heads, ld_q=heads * 64, ld_out=heads * 64, prefix_len=prefix, dtype=dtype, **strides, **kw)
+    st, p, s = plan_of(lib, (0,) * n, **kw)
+    assert st == 0 and p["rows"] == p["shared_items"] == 0
+    need = ctypes.c_size_t(7)
+    assert gdn.load_library().gdn_prefix_attention_workspace_size(ctypes.byref(s), host_of((0,) * n, "lens"), ctypes.byref(need)) == 0
+    assert need.value == p["bytes"]
+    assert attn(lens=(0,) * n, cu=None, q=None, out=None, prefix=None, ws=None, **kw) == 0
+
+
 def test_caches_that_share_an_allocation(lib):
     """Two caches of the same strides: keys and values by turns, at each of the strides; and such that do meet."""
     ap = lib.apart
