@@ -139,7 +139,8 @@ gdn_status gdn_prefix_attention_workspace_size(const gdn_attn_shape* shape, cons
  * over the P tokens of the shared prefix and the sequence's own tokens
  * j <= lens[n] - q_n + i: its queries are its last tokens, whose keys and values
  * are in the cache already.  With P = 0 this is plain causal attention over
- * pages.  A query that sees no token gets zeros.
+ * pages.  A query that sees no token gets zeros; one all of whose scores are -inf
+ * has no output, 0 / 0, and gets NaN.
  *   q, out [T, Hq, D]; k_cache, v_cache as in gdn_qk_norm_rope; table [N, W]
  *   int32; lens [N] int32; prefix_pages [ceil(P / page_size)] int32.
  * Scores and sums are fp32; for bf16 the weights w enter the second product

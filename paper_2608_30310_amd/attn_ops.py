@@ -183,7 +183,8 @@ def prefix_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tens
     page_size)] int32, what sequence n has behind them in those of block_table
     [N, W] int32; lens [N] int32 counts the latter, the queries' own tokens
     included, which are its last: query i of q_n sees the prefix and the own
-    tokens up to lens[n] - q_n + i.  A query that sees nothing gets zeros.
+    tokens up to lens[n] - q_n + i.  A query that sees nothing gets zeros,
+    one all of whose scores are -inf NaN.
     ``max_len``: no sequence holds more own tokens (default: what its table row
     has room for), a length above it counts as it; a bound near the truth spares
     idle workgroups.  ``scale``

@@ -693,6 +693,20 @@ __device__ __forceinline__ void add_dropped(const AttnArgs& a, const AttnItem& i
   }
 }
 
+// The sum of a row's weights is zero where it sees no token, whose output is zero, and
+// where all of its scores are -inf, which has none: 0 / 0.  The latter's sum becomes a NaN.
+// Rare: whether any of the `tokens` first tokens of a list of pages lies in a page that is there.
+__device__ __forceinline__ bool any_there(const AttnArgs& a, const int32_t* list, int tokens) {
+#pragma unroll 1
+  for (int c = 0; c * static_cast<int64_t>(a.page_size) < tokens; ++c)
+    if (static_cast<uint32_t>(list[c]) < static_cast<uint32_t>(a.num_pages)) return true;
+  return false;
+}
+__device__ __forceinline__ float sum_or_none(const AttnArgs& a, const int32_t* prefix, int count, const int32_t* own, int limit, float l) {
+  if (l != 0.0f) return l;
+  return any_there(a, prefix, count) || any_there(a, own, limit) ? __builtin_nanf("") : 0.0f;
+}
+
 template <typename T, int D>
 __device__ __forceinline__ void store_out(const AttnArgs& a, const AttnItem& it, const f32x16& o, int dt, float l, int r, int lane) {
   if (r >= it.rows) return;
@@ -842,6 +856,7 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, const AttnItem& i
   w.l = half_sum(w.l);
   const AttnArgs e = args_again();
   if (rarely(__builtin_amdgcn_readfirstlane(*odd) != 0)) add_dropped<T, D>(e, it, w.o, 0, mine, KT, lane);
+  if (rarely(it.part < 0 && __any(w.l == 0.0f))) w.l = sum_or_none(e, it.keys.list0, it.keys.count0, it.keys.list1, mine, w.l);
 #pragma unroll
   for (int dt = 0; dt < D / 32; ++dt) put_columns<T, D>(e, it, wave, w.o[dt], dt, w.m, w.l, lane);
 }
@@ -930,6 +945,7 @@ __device__ __forceinline__ void attend_keys(const AttnArgs& a, const AttnItem& i
   if (!join) {
     const AttnArgs e = args_again();
     if (rarely(odd)) add_dropped<T, D>(e, it, w.o, 0, mine, KT, lane);
+    if (rarely(it.part < 0 && __any(w.l == 0.0f))) w.l = sum_or_none(e, it.keys.list0, it.keys.count0, it.keys.list1, mine, w.l);
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt) put_columns<T, D>(e, it, 0, w.o[dt], dt, w.m, w.l, lane);
     return;
@@ -976,6 +992,7 @@ __device__ __forceinline__ void attend_keys(const AttnArgs& a, const AttnItem& i
   for (int x = 0; x < kAttnWaves; ++x) odd |= odds[x] != 0;
   const AttnArgs e = args_again();
   if (rarely(__builtin_amdgcn_readfirstlane(odd))) add_dropped<T, D>(e, it, o, wave, mine, KT, lane);
+  if (rarely(it.part < 0 && __any(l == 0.0f))) l = sum_or_none(e, it.keys.list0, it.keys.count0, it.keys.list1, mine, l);
   put_columns<T, D>(e, it, 0, o[0], wave, m, l, lane);
 }
 
@@ -1308,7 +1325,7 @@ void k_attn_join(AttnArgs a) {
       for (int i = 0; i < 4; ++i) sum[c][i] *= keep;
 #pragma unroll
     for (int k = 0; k < AHEAD; ++k) {
-      if (ml[k][1] == 0.0f) continue;   // nothing seen there (nor anything written)
+      // (a part without weights too: a value that is not finite counts at a weight of nothing)
       const float f = __builtin_amdgcn_exp2f(ml[k][0] - at);
       l = fmaf(f, ml[k][1], l);
 #pragma unroll
@@ -1332,7 +1349,6 @@ void k_attn_join(AttnArgs a) {
 #pragma unroll
     for (int w = 0; w < kAttnWaves; ++w) {
       const f32x2 ml = mls[w][lane];
-      if (ml[1] == 0.0f) continue;
       const float f = __builtin_amdgcn_exp2f(ml[0] - at);
       l = fmaf(f, ml[1], l);
 #pragma unroll
@@ -1340,6 +1356,11 @@ void k_attn_join(AttnArgs a) {
     }
   }
   if (parts == 0) return;
+  if (rarely(__any(l == 0.0f))) {
+    const int count = a.cu[lo + 1] - a.cu[lo], len = min(max(a.lens[lo], 0), a.max_len);
+    l = sum_or_none(a, a.prefix_pages, a.prefix_len, a.table + static_cast<int64_t>(lo) * a.width,
+                    max(min(len - count + 1 + (token - a.cu[lo]), len), 0), l);
+  }
   const int head = kvh * a.groups + (row - token * a.groups);
   T* out = static_cast<T*>(a.out) + token * a.ldo + static_cast<int64_t>(head) * D + 8 * col + 4 * (lane / 32);
   const float inv = 1.0f / l;

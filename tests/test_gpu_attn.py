@@ -204,6 +204,69 @@ def test_values_that_are_not_finite_reach_those_who_see_them(dtype, value, which
         assert torch.isnan(out[37:90, 2:].float()).all()
 
 
+# Sequences of such batches take each of the ways: rows of their own, with and without a prefix that all rows share
+# out, single tokens of one line with and without a prefix, few rows of too many sequences for a line.
+WAYS = pytest.mark.parametrize("new,before,prefix", [([70, 1], 0, 0), ([150, 40], [30, 7], 70), ([1, 1, 1], [0, 40, 300], 0), ([1, 2], [3, 90], 130),
+                                                     ([1, 2] + [1] * 1030, 3, 0), ([3], 0, 0)], ids=["rows", "shared", "line", "behind", "many", "few"])
+
+
+def formula(c, out_head, t, n, i):
+    """The formula for query i of sequence n (packed row t) and a head, its pieces in fp64: the output, the weighted
+    magnitudes, and S, R and the keys seen over the scores that are finite."""
+    ps, Hk = c["k_cache"].shape[1:3]
+    q = c["q"][t, out_head].double()
+    kvh = out_head // (c["q"].shape[1] // Hk)
+    m = int(c["lens"][n])
+    own = torch.arange(max(0, m - (int(c["cu_host"][n + 1]) - int(c["cu_host"][n])) + i + 1), device=DEV)
+    at = torch.arange(c["prefix_len"], device=DEV)
+    rows = c["table"][n].long()[own // ps] * ps + own % ps
+    if c["prefix_len"]:
+        rows = torch.cat([c["prefix_pages"].long()[at // ps] * ps + at % ps, rows])
+    k, v = (c[x].reshape(-1, *c[x].shape[2:])[rows, kvh].double() for x in ("k_cache", "v_cache"))
+    x = (q * k).sum(1) * len(q) ** -0.5
+    w = torch.exp(x - x.max())
+    w = w / w.sum()
+    fin = torch.isfinite(x)
+    S = float((q * k)[fin].abs().sum(1).max()) * len(q) ** -0.5 if fin.any() else 0.0
+    R = float(x[fin].max() - x[fin].min()) if fin.any() else 0.0
+    return (w[:, None] * v).sum(0), (w[:, None] * v.abs()).sum(0), S, R, len(rows)
+
+
+@DT
+@WAYS
+@pytest.mark.parametrize("value", [1.0, float("nan")])
+def test_scores_of_minus_infinity(dtype, new, before, prefix, value):
+    """Keys whose score is -inf weigh nothing beside others, and a query that sees no other has no output: 0 / 0.  The
+    first 37 tokens, and the prefix, have such keys for head 2, whose scores for head 3 are +inf.  A value of theirs
+    that is not finite reaches those who see it at a weight of nothing too."""
+    c = case(new, before, prefix, dtype=dtype, seed=19)
+    c["q"][:, 2, 5], c["q"][:, 3, 5] = c["q"][:, 2, 5].abs() + 0.1, -c["q"][:, 3, 5].abs() - 0.1
+    ps = 16
+    first = min(37, int(c["lens"][0]))
+    slots = [int(c["table"][0, j // ps]) * ps + j % ps for j in range(first)]
+    slots += [int(c["prefix_pages"][j // ps]) * ps + j % ps for j in range(prefix)]
+    for s in slots:
+        c["k_cache"][s // ps, s % ps, 1, 5] = float("-inf")
+    c["v_cache"][slots[-1] // ps, slots[-1] % ps, 1, 9] = value
+    out = call(c)
+    D, bf, nans, worst = 64, dtype == "bf16", 0, 0.0
+    for n in range(min(len(new), 3)):
+        for i in range(new[n]):
+            t = int(c["cu_host"][n]) + i
+            for h in range(4):
+                want, mag, S, R, keys = formula(c, h, t, n, i)
+                got, none = out[t, h].double(), torch.isnan(want)
+                assert torch.equal(torch.isnan(got), none), (n, i, h)
+                nans += int(none.all())
+                e = (D + 2) * 2.0 ** -24 * S + 2.0 ** -23 * R + 2.0 ** -22
+                bound = 2 * e + keys * 2.0 ** -23 + (2.0 ** -8 if bf else 0.0)
+                allowed = bound * mag + (2.0 ** -8 * want.abs() * (1 + bound) if bf else 0.0) + 1e-37
+                if not none.all():
+                    worst = max(worst, float(((got - want).abs() / allowed)[~none].max()))
+    print(f"[attn] worst {worst:.3f} of the bound, {nans} rows without an output", flush=True)
+    assert nans > 0 and worst <= 1.0
+
+
 @DT
 def test_rows_left_alone_and_out(dtype):
     c = case([20, 5], [0, 30], 20, dtype=dtype, seed=10, spare=6, pad=8)
