@@ -14,8 +14,9 @@
 // which registers does not matter to that product as long as V's operand has them
 // in the same order.  One pass, with the running maximum m and sum l of each row:
 //   p = 2^(s - m),  l += sum p,  O += p V,  out = O / l,
-// where m moves (and O and l are scaled) only when weights or a tile's sum of them pass 2^8,
-// which neither bf16's range nor fp32 sums mind.
+// where m is 8 above a maximum and moves (and O and l are scaled) only when weights or a
+// tile's sum of them pass 1: weights are 2^-8 at first and never above 1, so that no sum of
+// values grows beyond that of the values themselves.
 #pragma once
 
 #include <type_traits>
@@ -456,7 +457,7 @@ __device__ __forceinline__ bool clean_values(char* vl, uint64_t there, bool drop
 }
 
 // ---------------------------------------------------------------- a wave's rows
-constexpr float kSlack = 8.0f;   // weights up to 2^8 are let pass
+constexpr float kSlack = 8.0f;   // m is so far above the maximum that it was taken at
 template <typename T, int D>
 struct AttnWave {
   typedef KvRows<T, D> Rows;
@@ -498,7 +499,7 @@ struct AttnWave {
     for (int b = 0; b < NB; ++b)
 #pragma unroll
       for (int i = 0; i < 16; ++i) t[i % 4] = fmaxf(t[i % 4], s[b][i]);
-    const float top = half_max(fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]))) * scale2;
+    const float top = fmaf(half_max(fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]))), scale2, kSlack);
     // each row by itself: what one row meets does not change another's rounding
     const bool moves = top > m + slack || m == -INFINITY;
     if (rarely(__any(moves))) {
@@ -822,7 +823,7 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, const AttnItem& i
     }
     if (!idle) {
       // The maximum is looked at only where a row has none yet, or where weights turn out to
-      // be large (a row's sum over a tile's half above 2^8, whose maximum becomes the largest
+      // be large (a row's sum over a tile's half above 1, whose maximum becomes the largest
       // score then): the scores are there until then.
       // 35 vector instructions a tile less, and the moves that kept the scores (16 suffixes
       // behind 8192 tokens 2.64 -> 2.55 ms).
@@ -833,8 +834,8 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, const AttnItem& i
       float sum = 0.0f;
       if (scored) sum = w.template scores<NB, true>(kl, next, s, p, scale2, lane);
       if (d0.any) {
-        if (rarely(!scored || __any(sum > 256.0f))) {
-          w.raise(s, scale2, !scored ? kSlack : half_max(sum) > 256.0f ? 0.0f : INFINITY);
+        if (rarely(!scored || __any(sum > 1.0f))) {
+          w.raise(s, scale2, !scored ? kSlack : half_max(sum) > 1.0f ? 0.0f : INFINITY);
           sum = w.weigh(s, p, scale2);
         }
         w.l += sum;

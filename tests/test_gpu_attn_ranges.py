@@ -173,3 +173,24 @@ def test_whatever_the_workspace_held(seed):
     out = torch.full_like(c["q"], 7.0).contiguous()
     attn.check(c, attn.call(c, workspace=ws, out=out, **kw), **kw)
     assert (out[sum(new):] == 7).all()
+
+
+@DT
+@pytest.mark.parametrize("new,before,prefix,H,Hk", [([200, 20], [300, 480], 0, 4, 2), ([150, 3], [120, 30], 230, 4, 2),
+                                                    ([1] * 300, 499, 0, 8, 8), ([1] * 300, 249, 250, 8, 8)],
+                         ids=["rows", "shared", "line", "behind"])
+@pytest.mark.parametrize("rise", [2.0, 5.0])
+def test_sums_of_large_values_stay_finite(dtype, rise, new, before, prefix, H, Hk):
+    """All scores but the first 48 tokens' are higher by less than moves the running maximum at once (weights of e^2 and
+    e^5).  Values below 2^118 of 500 tokens at most: sums of values below 2^127, as they are of weights up to one."""
+    c = attn.case(new, before, prefix, H=H, Hk=Hk, dtype=dtype, seed=5)
+    assert int(c["lens"].max()) + prefix <= 500
+    c["q"].zero_()
+    c["q"][..., 0] = 1.0
+    c["k_cache"].copy_(torch.where(torch.isnan(c["k_cache"]), c["k_cache"], 0.0))   # (unused rows stay NaN)
+    c["k_cache"][..., 0] += rise
+    low = (c["prefix_pages"][:3] if prefix else c["table"][:, :3].reshape(-1)).long()
+    c["k_cache"][low, :, :, 0] -= rise
+    c["v_cache"].copy_((c["v_cache"].float().abs().clamp(0.5, 0.99) * 2.0 ** 118).to(c["v_cache"].dtype))
+    out = attn.call(c, scale=1.0)
+    attn.check(c, out, scale=1.0)
