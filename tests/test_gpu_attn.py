@@ -8,6 +8,7 @@ bf16 the weights enter the second product rounded, by 2^-8 each.  So outputs are
 within 2 e + n 2^-23 (+ 2^-8) of sum w |v| / sum w, and a bf16 output is rounded once
 more, by 2^-8 of itself.
 """
+import ctypes
 import threading
 
 import pytest
@@ -482,3 +483,22 @@ def test_refusals():
         call(big, workspace=need)
     except gdn.GDNError as e:
         assert e.status == 5
+
+
+@pytest.mark.parametrize("new,before,prefix", [([1], 3000, 5000), ([300], 0, 2000)], ids=["line", "shared"])
+def test_a_workspace_that_is_too_small_is_refused(new, before, prefix):
+    """Before anything runs; one of the size that is asked for is enough."""
+    c = case(new, before, prefix, H=2, Hk=1, seed=18)
+    want = call(c)
+    shape = gdn.binding.AttnShape(len(new), 2, 1, 64, 1, *c["k_cache"].shape[:2], c["table"].shape[1], prefix, 0, 0.125, 128, 128,
+                                  *c["k_cache"].stride()[:3], *c["v_cache"].stride()[:3])
+    size = ctypes.c_size_t(0)
+    lib = gdn.load_library()
+    assert lib.gdn_prefix_attention_workspace_size(ctypes.byref(shape), c["cu_host"].data_ptr(), ctypes.byref(size)) == 0
+    assert size.value > 256
+    for few in (1, 255, size.value - 256, size.value - 1):
+        out = torch.full_like(want, 7.0)
+        with pytest.raises(gdn.GDNError) as e:
+            call(c, out=out, workspace=torch.empty(few, dtype=torch.uint8, device=DEV))
+        assert e.value.status == 5 and (out == 7).all()
+    assert torch.equal(call(c, workspace=torch.empty(size.value, dtype=torch.uint8, device=DEV)), want)
