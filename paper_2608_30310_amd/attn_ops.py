@@ -27,6 +27,14 @@ def _ints(t, name, shape, device):
         raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
 
 
+def _int32(x, name):
+    """A number that a field of a shape holds as it is."""
+    x = int(x)
+    if not -2 ** 31 <= x < 2 ** 31:
+        raise ValueError(f"{name} must fit 32 bits, got {x}")
+    return x
+
+
 def _cache(t, name, dtype, device, heads, dim):
     """Checks a cache of pages [pages, page_size, heads, dim] with dense elements; its strides."""
     if not isinstance(t, torch.Tensor):
@@ -91,7 +99,7 @@ def extend_pages(block_table: torch.Tensor, lens: torch.Tensor, cu_seqlens, free
     _ints(table_out, "table_out", (N, W), device)
     _ints(lens_out, "lens_out", (N,), device)
     _ints(taken_out, "taken_out", (1,), device)
-    shp = PagesShape(N, W, int(page_size), free_pages.numel(), int(first))
+    shp = PagesShape(N, W, _int32(page_size, "page_size"), free_pages.numel(), _int32(first, "first"))
     stream = _stream(device)
     h = host.data_ptr()
     args = (ctypes.byref(shp), h, cu.data_ptr(), block_table.data_ptr(), lens.data_ptr(), free_pages.data_ptr(), _ptr(taken),
@@ -221,8 +229,8 @@ def prefix_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tens
             raise ValueError("out must hold the same tokens as q")
     if max_len is not None and max_len < 1:
         raise ValueError("max_len must be at least 1")
-    shp = AttnShape(n, H, Hk, D, _dtype_code(q), pages, page_size, block_table.shape[1], int(prefix_len),
-                    0 if max_len is None else int(max_len), float(D ** -0.5 if scale is None else scale), ldq, ldo, *ks, *vs)
+    shp = AttnShape(n, H, Hk, D, _dtype_code(q), pages, page_size, block_table.shape[1], _int32(prefix_len, "prefix_len"),
+                    0 if max_len is None else _int32(max_len, "max_len"), float(D ** -0.5 if scale is None else scale), ldq, ldo, *ks, *vs)
     stream = _stream(device)
     h = host.data_ptr()
     args = (ctypes.byref(shp), h, cu.data_ptr(), q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),

@@ -236,6 +236,16 @@ def test_calls_refuse_host_tensors():
             call()
 
 
+@pytest.mark.parametrize("x", [2 ** 31, 2 ** 32, 2 ** 32 + 40, -2 ** 31 - 1, -2 ** 32 + 40, 2 ** 63])
+def test_numbers_are_not_cut_to_32_bits(x):
+    """A field of a shape would keep the low bits of them."""
+    from paper_2608_30310_amd.attn_ops import _int32
+    assert AttnShape(max_len=x).max_len != x
+    with pytest.raises(ValueError, match="max_len must fit 32 bits"):
+        _int32(x, "max_len")
+    assert [_int32(y, "max_len") for y in (-2 ** 31, 0, 2 ** 31 - 1)] == [-2 ** 31, 0, 2 ** 31 - 1]
+
+
 # ---------------------------------------------------------------- the plan, built here with the host compiler
 SHIM = r"""
 #include "gdn_attn_plan.h"

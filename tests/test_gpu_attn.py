@@ -502,3 +502,17 @@ def test_a_workspace_that_is_too_small_is_refused(new, before, prefix):
             call(c, out=out, workspace=torch.empty(few, dtype=torch.uint8, device=DEV))
         assert e.value.status == 5 and (out == 7).all()
     assert torch.equal(call(c, workspace=torch.empty(size.value, dtype=torch.uint8, device=DEV)), want)
+
+
+@pytest.mark.parametrize("x", [2 ** 31, 2 ** 32, 2 ** 32 + 40, -2 ** 32 + 40, 2 ** 63])
+def test_numbers_past_32_bits_are_refused(x):
+    """Not taken for what their low bits are (40 tokens, pages of 40)."""
+    c = case([20, 5], [0, 30], 40, seed=17)
+    with pytest.raises(ValueError):
+        call(c, max_len=x)
+    with pytest.raises(ValueError):
+        call(c, prefix_len=x)
+    free = torch.arange(8, dtype=torch.int32, device=DEV)
+    for kw in (dict(page_size=x), dict(page_size=16, first=x)):
+        with pytest.raises(ValueError, match="32 bits"):
+            gdn.extend_pages(c["table"], c["lens"], c["cu"], free, cu_seqlens_host=c["cu_host"], **kw)
