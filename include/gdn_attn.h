@@ -145,9 +145,10 @@ gdn_status gdn_prefix_attention_workspace_size(const gdn_attn_shape* shape, cons
  *   int32; lens [N] int32; prefix_pages [ceil(P / page_size)] int32.
  * Scores and sums are fp32 (so the values that a query sees must not add up to
  * 2^128 or more: the sums are formed at weights up to 1 and divided at the end);
- * for bf16 the weights w enter the second product rounded to bf16.  What lies in a cache where no query looks (behind a
- * sequence's last token, in other pages) has no effect, whatever its bits; a key
- * or value that is not finite reaches the queries that see it, and no others.
+ * for bf16 the weights w enter the second product rounded to bf16.  What lies in
+ * a cache where no query looks (behind a sequence's last token, in other pages)
+ * has no effect, whatever its bits; a key or value that is not finite reaches the
+ * queries that see it, and no others.
  * out must not overlap q or the caches.  q, out and the caches must be 16-byte
  * aligned, strides multiples of 16 bytes (GDN_ERR_UNSUPPORTED otherwise).
  * workspace: at least gdn_prefix_attention_workspace_size bytes, 256-byte aligned.

@@ -123,12 +123,6 @@ struct Mm<float> {
   }
 };
 
-// Rows of D elements in LDS as they lie in memory, 16-byte piece p of row r at
-// p ^ swz(r).  The swizzle is a permutation of the low row bits, so the operand
-// reads of K (32 rows of one piece) meet every bank once; those of V (four rows
-// of four pieces, transposed on the way) do because rows 0..3 differ in the high
-// bits of the piece.  (fp32: rows r and r + 4 differ in the highest, for V's
-// 4-byte reads.)
 // The lane, for what is made of it anew for each tile instead of being kept in registers
 // over the tiles.
 __device__ __forceinline__ int lane_now() {
@@ -137,6 +131,12 @@ __device__ __forceinline__ int lane_now() {
   return static_cast<uint32_t>(x) % kWave;
 }
 
+// Rows of D elements in LDS as they lie in memory, 16-byte piece p of row r at
+// p ^ swz(r).  The swizzle is a permutation of the low row bits, so the operand
+// reads of K (32 rows of one piece) meet every bank once; those of V (four rows
+// of four pieces, transposed on the way) do because rows 0..3 differ in the high
+// bits of the piece.  (fp32: rows r and r + 4 differ in the highest, for V's
+// 4-byte reads.)
 template <typename T, int D>
 struct KvRows {
   static constexpr int kPitch = D * static_cast<int>(sizeof(T));
@@ -183,12 +183,6 @@ struct KvRows {
       }
       return x;
     }
-  }
-  static __device__ __forceinline__ float elt(const char* base, int r, int col) {
-    const int b = col * static_cast<int>(sizeof(T));
-    const char* p = base + at(r, b / 16) + b % 16;
-    if constexpr (sizeof(T) == 2) return bf2f(*reinterpret_cast<const uint16_t*>(p));
-    else return *reinterpret_cast<const float*>(p);
   }
 };
 
