@@ -122,7 +122,8 @@ typedef struct {
   int32_t prefix_len;    /* P >= 0: tokens that all sequences share          */
   int32_t max_len;       /* no sequence holds more own tokens than this: a
                             length above it counts as max_len, one below 0 as
-                            0; at most W page_size, 0 = that                 */
+                            0; at most W page_size, 0 = that.  Work is cut by
+                            it: to be given where tables are much wider      */
   float scale;           /* finite                                           */
   int64_t ld_q, ld_out;
   int64_t k_page, k_token, k_head;  /* elements between pages, tokens of a page and heads */

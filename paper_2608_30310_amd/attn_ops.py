@@ -194,9 +194,10 @@ def prefix_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tens
     tokens up to lens[n] - q_n + i.  A query that sees nothing gets zeros,
     one all of whose scores are -inf NaN.
     ``max_len``: no sequence holds more own tokens (default: what its table row
-    has room for), a length above it counts as it; a bound near the truth spares
-    idle workgroups.  ``scale``
-    defaults to D^-1/2.  Returns out [T, Hq, D]; its rows behind the last
+    has room for), a length above it counts as it.  The work is cut by it, so it
+    should be given where tables are much wider than the sequences are long (64
+    tokens behind 4000: 26 us, 119 without it from a table of 131072 tokens).
+    ``scale`` defaults to D^-1/2.  Returns out [T, Hq, D]; its rows behind the last
     sequence are left alone.
     """
     lib = load_library()

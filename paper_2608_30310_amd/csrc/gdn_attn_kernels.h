@@ -745,7 +745,8 @@ __device__ __forceinline__ void put_columns(const AttnArgs& a, const AttnItem& i
 // the matrix cores and the vector instructions beside them, whose shares add up to most
 // of the cycles (50 % and 155 instructions a tile), at the clock that the power limit
 // leaves: 16 suffixes behind 8192 tokens 985 to 1068 TFLOP/s from card to card, a prompt of
-// 8192 tokens 956 to 1033, long fp32 batches 115.
+// 8192 tokens 956 to 1033 (916 in the first 25 ms, until the clock has settled), 16 fp32
+// suffixes of 1024 behind 4096 115.
 template <typename T, int D>
 __device__ __forceinline__ void attend_rows(const AttnArgs& a, const AttnItem& it, const CacheAt<T, D>& cache, char* lds) {
   typedef AttnLds<T, D> L;

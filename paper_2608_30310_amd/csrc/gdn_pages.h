@@ -87,7 +87,7 @@ void k_pages_plan(PagesArgs a) {
 // and those from it on only written.  PLANNED: behind k_pages_plan; else a workgroup
 // sums up by itself what the sequences before its own take, which needs the old lengths
 // and the old `taken` to stay, and spares a launch where there are few sequences (256
-// single tokens: 12.5 -> 10.8 us a call, the kernels 5.8 -> 4.3).
+// single tokens: 12.9 -> 10.4 us a call, the kernels 5.5 -> 4.3).
 constexpr int kPagesThreads = 256, kPagesFew = 1024;
 template <int TILE, bool PLANNED>
 __global__ __launch_bounds__(kPagesThreads)
