@@ -84,7 +84,9 @@ struct Mm<uint16_t> {
   }
   // p: eight weights, rounded to bf16 as the product takes them, and their sums: of what
   // enters the product, so that the rounding of a weight is one of numerator and
-  // denominator alike; two at a time
+  // denominator alike; two at a time.  Outputs are within 2.0e-3 to 2.4e-3 of 64 bits that
+  // way, 1.5e-3 to 1.7e-3 of which are the output's own rounding; weights in two parts would
+  // take half as many products again.
   static __device__ __forceinline__ R pack(const float (&p)[8], float (&sum)[4]) {
     u32x4 w;
 #pragma unroll
